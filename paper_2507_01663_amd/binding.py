@@ -1,4 +1,4 @@
-"""ctypes binding of the rollout_attn C ABI (include/rollout_attn.h).  Argument marshalling only: every
+"""ctypes binding of the rollout_attn C ABI (include/rollout_attn.h, include/rollout_attn_chunk.h).  Argument marshalling only: every
 step of the decode path runs in the library's kernels.  There is no fallback: if the shared library is
 missing the import of a symbol raises."""
 import ctypes
@@ -51,6 +51,44 @@ class ra_prefill(ctypes.Structure):
         ("kv_dtype", ctypes.c_int32),
         ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
         ("page_offsets", ctypes.c_void_p), ("pages", ctypes.c_void_p),
+    ]
+
+
+class ra_rotate(ctypes.Structure):
+    _fields_ = [
+        ("num_tokens", ctypes.c_int32), ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("q", ctypes.c_void_p), ("k", ctypes.c_void_p), ("q_out", ctypes.c_void_p), ("k_out", ctypes.c_void_p),
+        ("q_stride_token", ctypes.c_int64), ("k_stride_token", ctypes.c_int64),
+        ("q_out_stride_token", ctypes.c_int64), ("k_out_stride_token", ctypes.c_int64),
+        ("q_weight", ctypes.c_void_p), ("k_weight", ctypes.c_void_p), ("eps", ctypes.c_float),
+        ("positions", ctypes.c_void_p), ("rope", ctypes.c_void_p),
+        ("rope_len", ctypes.c_int32), ("rot_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32),
+    ]
+
+
+class ra_append_chunk(ctypes.Structure):
+    _fields_ = [
+        ("rot", ra_rotate), ("v", ctypes.c_void_p), ("v_stride_token", ctypes.c_int64),
+        ("num_seqs", ctypes.c_int32), ("max_chunk_len", ctypes.c_int32),
+        ("cu_seqlens", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+        ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("block_table", ctypes.c_void_p), ("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p),
+        ("kv_stride_page", ctypes.c_int64), ("kv_stride_head", ctypes.c_int64), ("kv_stride_token", ctypes.c_int64),
+        ("kv_dtype", ctypes.c_int32), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+    ]
+
+
+class ra_extend(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("total_tokens", ctypes.c_int32), ("max_chunk_len", ctypes.c_int32),
+        ("Hq", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+        ("q", ctypes.c_void_p), ("q_stride_token", ctypes.c_int64),
+        ("cu_seqlens", ctypes.c_void_p), ("seq_lens", ctypes.c_void_p),
+        ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("block_table", ctypes.c_void_p), ("k_pool", ctypes.c_void_p), ("v_pool", ctypes.c_void_p),
+        ("kv_stride_page", ctypes.c_int64), ("kv_stride_head", ctypes.c_int64), ("kv_stride_token", ctypes.c_int64),
+        ("kv_dtype", ctypes.c_int32), ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+        ("softmax_scale", ctypes.c_float), ("out", ctypes.c_void_p), ("lse", ctypes.c_void_p),
     ]
 
 
@@ -112,6 +150,14 @@ def load_library():
     lib.rollout_attn_set_timing.argtypes = [ctypes.c_void_p, ctypes.c_int]
     lib.rollout_attn_get_timing.restype = ctypes.c_int
     lib.rollout_attn_get_timing.argtypes = [ctypes.c_void_p, P(ctypes.c_float)]
+    for name, kind in (("rotate", ra_rotate), ("append_chunk", ra_append_chunk), ("extend", ra_extend)):
+        check = getattr(lib, "rollout_attn_check_" + name)
+        check.restype, check.argtypes = ctypes.c_int, [P(kind), ctypes.c_char_p, ctypes.c_size_t]
+        call = getattr(lib, "rollout_attn_" + name)
+        call.restype, call.argtypes = ctypes.c_int, [ctypes.c_void_p, P(kind), ctypes.c_void_p]
+    lib.rollout_attn_extend.argtypes = [ctypes.c_void_p, P(ra_extend), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+    lib.rollout_attn_extend_workspace_size.restype = ctypes.c_int
+    lib.rollout_attn_extend_workspace_size.argtypes = [ctypes.c_void_p, P(ra_extend), P(ctypes.c_size_t)]
     _lib = lib
     return lib
 
@@ -188,6 +234,45 @@ def rollout_attn_check_prefill(prefill):
 
 def rollout_attn_prefill(ctx, prefill, hip_stream=None):
     _check(load_library().rollout_attn_prefill(ctx, ctypes.byref(prefill), hip_stream), ctx)
+
+
+def _check_only(name, desc):
+    buf = ctypes.create_string_buffer(512)
+    st = getattr(load_library(), name)(ctypes.byref(desc) if desc is not None else None, buf, 512)
+    return int(st), buf.value.decode()
+
+
+def rollout_attn_check_rotate(rotate):
+    """Returns (status, message) of the host-side argument check of a norm and rotation."""
+    return _check_only("rollout_attn_check_rotate", rotate)
+
+
+def rollout_attn_check_append_chunk(append):
+    """Returns (status, message) of the host-side argument check of an append of chunks."""
+    return _check_only("rollout_attn_check_append_chunk", append)
+
+
+def rollout_attn_check_extend(extend):
+    """Returns (status, message) of the host-side argument check of an attention of chunks."""
+    return _check_only("rollout_attn_check_extend", extend)
+
+
+def rollout_attn_rotate(ctx, rotate, hip_stream=None):
+    _check(load_library().rollout_attn_rotate(ctx, ctypes.byref(rotate), hip_stream), ctx)
+
+
+def rollout_attn_append_chunk(ctx, append, hip_stream=None):
+    _check(load_library().rollout_attn_append_chunk(ctx, ctypes.byref(append), hip_stream), ctx)
+
+
+def rollout_attn_extend_workspace_size(ctx, extend):
+    n = ctypes.c_size_t()
+    _check(load_library().rollout_attn_extend_workspace_size(ctx, ctypes.byref(extend), ctypes.byref(n)), ctx)
+    return int(n.value)
+
+
+def rollout_attn_extend(ctx, extend, workspace_ptr, workspace_bytes, hip_stream=None):
+    _check(load_library().rollout_attn_extend(ctx, ctypes.byref(extend), workspace_ptr, workspace_bytes, hip_stream), ctx)
 
 
 def rollout_attn_balance(weights, k, equal_count=False):
@@ -305,6 +390,108 @@ def prefill_from_tensors(q, k, v, cu_seqlens, max_prompt_len, out, lse, softmax_
     return p
 
 
+def _rows(t, name):
+    """(address, token stride) of a bf16 tensor [T, heads, D] whose tokens' heads lie one after the other."""
+    import torch
+    assert t.dtype == torch.bfloat16 and t.dim() == 3, name
+    assert t.shape[0] == 0 or (t.stride(2) == 1 and (t.shape[1] == 1 or t.stride(1) == t.shape[2])), name
+    # (a single token's stride means nothing; torch may have any there)
+    return _ptr(t), t.stride(0) if t.shape[0] > 1 else t.shape[1] * t.shape[2]
+
+
+def _fill_rotation(r, q, k, q_out, k_out, positions, rope, q_weight, k_weight, eps, interleaved):
+    import torch
+    some = q if q is not None else k
+    r.num_tokens, _, r.D = some.shape
+    if q is not None:
+        assert q.shape == q_out.shape
+        r.Hq = q.shape[1]
+        r.q, r.q_stride_token = _rows(q, "q")
+        r.q_out, r.q_out_stride_token = _rows(q_out, "q_out")
+    if k is not None:
+        assert k.shape[0] == r.num_tokens and k.shape[2] == r.D
+        r.Hkv = k.shape[1]
+        r.k, r.k_stride_token = _rows(k, "k")
+        if k_out is not None:
+            assert k.shape == k_out.shape
+            r.k_out, r.k_out_stride_token = _rows(k_out, "k_out")
+    for w in (q_weight, k_weight):
+        assert w is None or (w.dtype == torch.float32 and w.is_contiguous() and w.numel() == r.D)
+    r.q_weight, r.k_weight, r.eps, r.interleaved = _ptr(q_weight), _ptr(k_weight), float(eps), int(bool(interleaved))
+    if rope is not None:
+        assert rope.dtype == torch.float32 and rope.is_contiguous() and rope.dim() == 2
+        r.rope, r.rope_len, r.rot_dim = _ptr(rope), rope.shape[0], rope.shape[1]
+    if positions is not None:
+        assert positions.dtype == torch.int32 and positions.is_contiguous() and positions.numel() == r.num_tokens
+        r.positions = _ptr(positions)
+
+
+def rope_table(length, rot_dim, theta=1e4, device="cuda:0"):
+    """The table of a plain rotation: float32 [length, rot_dim], position p's cosines of p * theta^(-2 j / rot_dim), j <
+    rot_dim / 2, then their sines.  (A scaled rotation is another table.)"""
+    import torch
+    j = torch.arange(0, rot_dim, 2, dtype=torch.float64)
+    angle = torch.arange(length, dtype=torch.float64)[:, None] * theta ** (-j / rot_dim)
+    return torch.cat([angle.cos(), angle.sin()], dim=1).float().to(device)
+
+
+def rotate_from_tensors(q, k, q_out, k_out, positions=None, rope=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+    """Fills a ra_rotate from device tensors: q/q_out bf16 [T,Hq,D], k/k_out bf16 [T,Hkv,D] (the heads of a token
+    contiguous, tokens any 16-byte stride apart; q or k may be None); positions int32 [T]; rope float32 [length,rot_dim]
+    (rope_table; None: no rotation); q_weight, k_weight float32 [D] (None: no norm)."""
+    r = ra_rotate()
+    _fill_rotation(r, q, k, q_out, k_out, positions, rope, q_weight, k_weight, eps, interleaved)
+    return r
+
+
+def _fill_cache(p, cu_seqlens, max_chunk_len, block_table, seq_lens, k_pool, v_pool, k_scale, v_scale):
+    import torch
+    for t in (cu_seqlens, seq_lens, block_table):
+        assert t.dtype == torch.int32 and t.is_contiguous()
+    assert k_pool.shape == v_pool.shape and k_pool.stride() == v_pool.stride() and k_pool.stride(3) == 1
+    p.num_seqs, p.max_chunk_len = cu_seqlens.numel() - 1, int(max_chunk_len)
+    assert seq_lens.numel() == p.num_seqs and block_table.shape[0] == p.num_seqs
+    p.cu_seqlens, p.seq_lens, p.block_table = _ptr(cu_seqlens), _ptr(seq_lens), _ptr(block_table)
+    p.max_pages_per_seq = block_table.shape[1]
+    p.num_pages, _, p.page_size, _ = k_pool.shape
+    p.k_pool, p.v_pool = _ptr(k_pool), _ptr(v_pool)
+    p.kv_stride_page, p.kv_stride_head, p.kv_stride_token = k_pool.stride(0), k_pool.stride(1), k_pool.stride(2)
+    p.kv_dtype = RA_KV_FP8_E4M3 if k_pool.element_size() == 1 else RA_KV_BF16
+    for s in (k_scale, v_scale):
+        assert s is None or (s.dtype == torch.float32 and s.is_contiguous())
+    p.k_scale, p.v_scale = _ptr(k_scale), _ptr(v_scale)
+
+
+def append_chunk_from_tensors(k, v, cu_seqlens, max_chunk_len, block_table, seq_lens, k_pool, v_pool, k_scale=None, v_scale=None, q=None,
+                              q_out=None, positions=None, rope=None, q_weight=None, k_weight=None, eps=1e-6, interleaved=False):
+    """Fills a ra_append_chunk from device tensors: k, v bf16 [T,Hkv,D] and q, q_out bf16 [T,Hq,D] as for
+    rotate_from_tensors; cu_seqlens int32 [n+1]; seq_lens int32 [n], the lengths before the append; block_table and pools
+    as for problem_from_tensors; positions None: a token's place in its sequence."""
+    p = ra_append_chunk()
+    assert k.shape == v.shape and k.shape[1] == k_pool.shape[1] and k.shape[2] == k_pool.shape[3]
+    _fill_rotation(p.rot, q, k, q_out, None, positions, rope, q_weight, k_weight, eps, interleaved)
+    p.v, p.v_stride_token = _rows(v, "v")
+    _fill_cache(p, cu_seqlens, max_chunk_len, block_table, seq_lens, k_pool, v_pool, k_scale, v_scale)
+    return p
+
+
+def extend_from_tensors(q, k_pool, v_pool, cu_seqlens, max_chunk_len, block_table, seq_lens, out, lse, softmax_scale, k_scale=None,
+                        v_scale=None):
+    """Fills a ra_extend from device tensors: q bf16 [T,Hq,D] (tokens any 16-byte stride apart); out bf16 [T,Hq,D] and
+    lse float32 [T,Hq] contiguous; seq_lens int32 [n], the lengths with the chunk; the rest as for append_chunk_from_tensors."""
+    import torch
+    assert out.is_contiguous() and lse.is_contiguous() and out.dtype == torch.bfloat16 and lse.dtype == torch.float32
+    assert q.shape == out.shape and lse.shape == q.shape[:2] and q.shape[2] == k_pool.shape[3]
+    p = ra_extend()
+    p.total_tokens, p.Hq, p.D = q.shape
+    p.Hkv = k_pool.shape[1]
+    p.q, p.q_stride_token = _rows(q, "q")
+    _fill_cache(p, cu_seqlens, max_chunk_len, block_table, seq_lens, k_pool, v_pool, k_scale, v_scale)
+    p.softmax_scale = float(softmax_scale)
+    p.out, p.lse = _ptr(out), _ptr(lse)
+    return p
+
+
 class ra_schedule_info(ctypes.Structure):
     _fields_ = [("header_offset", ctypes.c_int64), ("work_list_offset", ctypes.c_int64), ("merge_desc_offset", ctypes.c_int64),
                 ("waves", ctypes.c_int32), ("segments_per_chunk", ctypes.c_int32)]
@@ -321,6 +508,8 @@ class Decoder:
         self.ctx = rollout_attn_create(device_ordinal)
         self._ws = None
         self._ws_at = None           # its address and size, always those of one tensor
+        self._chunk_ws = None        # extend's (a schedule that decode keeps in the other one outlives it)
+        self._chunk_ws_at = None
         self._retired = []
         self._raw_stream = None
 
@@ -330,7 +519,7 @@ class Decoder:
             torch.cuda.synchronize(self.device_ordinal)      # nothing enqueued may outlive the buffers
             rollout_attn_destroy(self.ctx)
             self.ctx = None
-            self._ws = self._ws_at = None
+            self._ws = self._ws_at = self._chunk_ws = self._chunk_ws_at = None
             self._retired = []
 
     def __del__(self):
@@ -396,6 +585,33 @@ class Decoder:
     def prefill(self, prefill, stream=None):
         """Enqueues the prompts' causal attention (and the cache write, if the ra_prefill names pools)."""
         _check(load_library().rollout_attn_prefill(self.ctx, prefill, self._hip_stream(stream)), self.ctx)
+
+    def rotate(self, rotate, stream=None):
+        """Enqueues the norm and rotation of query and key rows."""
+        _check(load_library().rollout_attn_rotate(self.ctx, rotate, self._hip_stream(stream)), self.ctx)
+
+    def append_chunk(self, append, stream=None):
+        """Enqueues the append of a chunk of new tokens per sequence, with the norm and rotation on the way."""
+        _check(load_library().rollout_attn_append_chunk(self.ctx, append, self._hip_stream(stream)), self.ctx)
+
+    def extend(self, extend, stream=None):
+        """Enqueues the attention of every sequence's chunk over its pages.  Its workspace grows as decode's does, and calls
+        of one Decoder that overlap in time share it: put them on one stream, or take a Decoder for each."""
+        s = self._hip_stream(stream)
+        at = self._chunk_ws_at       # (read once: another thread's call may put a larger one there)
+        if at is not None:
+            status = load_library().rollout_attn_extend(self.ctx, extend, at[0], at[1], s)
+            if status == RA_OK:
+                return
+            if status != RA_ERR_WORKSPACE_TOO_SMALL:
+                _check(status, self.ctx)
+        import torch
+        need = max(256, rollout_attn_extend_workspace_size(self.ctx, extend))
+        if self._chunk_ws is not None:
+            self._retired.append(self._chunk_ws)
+        self._chunk_ws = torch.empty(need, dtype=torch.uint8, device="cuda:%d" % self.device_ordinal)
+        self._chunk_ws_at = (self._chunk_ws.data_ptr(), need)
+        rollout_attn_extend(self.ctx, extend, ctypes.c_void_p(self._chunk_ws.data_ptr()), need, ctypes.c_void_p(s))
 
     def debug_gather(self, problem, b, kv_head, k_out, v_out, stream=None):
         import torch

@@ -5,7 +5,7 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librollout_attn.so")
-SOURCES = ["ra_kernels.hip", "ra_prefill.hip", "ra_prefill_four.hip", "ra_api.cpp", "ra_balance.cpp"]
+SOURCES = ["ra_kernels.hip", "ra_prefill.hip", "ra_prefill_four.hip", "ra_rotate.hip", "ra_extend.hip", "ra_api.cpp", "ra_chunk_api.cpp", "ra_balance.cpp"]
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-Wall", "-Wno-inline-asm", "-Wno-int-to-pointer-cast", "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option"]
@@ -49,7 +49,7 @@ def is_stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in os.listdir(CSRC)] + [os.path.join(HERE, "..", "include", "rollout_attn.h")]
+    deps = [os.path.join(d, f) for d in (CSRC, os.path.join(HERE, "..", "include")) for f in os.listdir(d)]
     return any(os.path.getmtime(d) > t for d in deps)
 
 

@@ -1,6 +1,7 @@
 // C-ABI of rollout_attn (see include/rollout_attn.h): argument checks, workspace carving, kernel sequencing.
 #include "../../include/rollout_attn.h"
-#include "ra_internal.h"
+#include "ra_chunk.h"
+#include "ra_context.h"
 
 #include <cmath>
 #include <cstdarg>
@@ -14,32 +15,9 @@
 constexpr size_t kScratchBytes = (size_t)64 << 20;
 static __device__ __align__(256) unsigned char scratch[kScratchBytes];
 
-struct ra_ctx {
-    int device;
-    void *scratch_ptr; // device address of `scratch` on this context's device
-    int num_cus;
-    int waves[2][2];  // resident attention waves, [e4m3 KV][D == 128]
-    int stages[2][2]; // LDS ring depth, same indices
-    int cost_prefix[2]; // scheduling weight of a shared-prefix page, [e4m3 KV]
-    int cost_item;   // ... of a segment, on top of its pages
-    int cost_item_pfx[2]; // ... of a shared-prefix row's segment (bf16, e4m3 pools)
-    int xcd_w[8];              // default share of the page stream per accelerator die, per mille of the mean
-    int32_t *wave_cum[2][2];   // device: running sums of the workgroups' shares, [e4m3 KV][D == 128], kMaxWaves + 1 each
-    uint32_t *tickets;         // device: the streaming probe's ticket counter (cleared by every launch that uses it)
-    int prefill_stay;          // -1: the prefill launch chooses by the batch; else ROLLOUT_ATTN_PREFILL_WGS_PER_DIE
-    void *zeros;  // 256 bytes of zeros on the device
-    int self_plan; // attention waves may plan their spans themselves (no schedule kernel)
-    int direct;    // batches that direct_plan says so may go without a schedule
-    int32_t *host_flags; // pinned, for RA_FLAG_VALIDATE
-    int timing;          // record events around the phases
-    int timed;           // a decode call has recorded them (2: with a schedule launch between the first two)
-    hipEvent_t ev[4];
-    char err[512];
-};
+static thread_local char g_err[512] = "";
 
-namespace {
-
-thread_local char g_err[512] = "";
+namespace ra {
 
 void set_err(ra_ctx *ctx, const char *fmt, ...)
 {
@@ -49,6 +27,12 @@ void set_err(ra_ctx *ctx, const char *fmt, ...)
     vsnprintf(dst, 512, fmt, ap);
     va_end(ap);
 }
+
+} // namespace ra
+
+using ra::set_err;
+
+namespace {
 
 ra_status check(const ra_problem *p, char *msg, size_t n)
 {
@@ -232,6 +216,7 @@ ra_status rollout_attn_create(ra_ctx **out, int device)
             if (e == hipSuccess) e = ra::attention_config(d ? 128 : 64, f, c->num_cus, &c->stages[f][d], &c->waves[f][d]);
     if (e == hipSuccess) e = ra::direct_config();
     if (e == hipSuccess) e = ra::prefill_config();
+    if (e == hipSuccess) e = ra::extend_config();
     for (int f = 0; f < 2; f++)
         for (int d = 0; d < 2; d++) {
             if (e == hipSuccess) e = hipMalloc((void **)&c->wave_cum[f][d], ((size_t)ra::kMaxWaves + 1) * 4);

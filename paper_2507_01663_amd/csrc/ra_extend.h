@@ -1,0 +1,958 @@
+// gfx950 kernels of the attention of chunks of new tokens over the paged cache.
+//
+// A sequence's n new tokens and the G query heads of a kv head are n * G rows that read the same keys: row r is token r / G,
+// head r % G, and sees the keys up to L - n + r / G.  Packed that way 32 rows are a few tokens, so under the causal mask
+// they need the same keys but for the last one or two stages of 32.
+//
+// Many rows are bound by the matrix cores: extend_tile_kernel, whose workgroup takes a block of 128 rows, 32 to a wave, all
+// waves multiplying every stage of 32 keys that streams through one LDS ring:
+//   S^T[key, row] = K . Q^T,   O^T[d, row] += V^T . P^T     (32x32x16 MFMA, binary32 sums, softmax running per row)
+// Few rows are bound by the stream of pages: extend_few_kernel, whose four waves stream stages of their own (every fourth
+// one) through rings of their own and multiply them with all of the up to 64 rows; what they have is added up in LDS.
+//
+// The work is a line of items, one per (sequence, kv head, block), each as long as it has stages, and the line is cut into
+// as many spans of one length as workgroups are resident, so that ragged lengths load them alike.  Every workgroup finds its
+// span by itself, from sums over the lengths.  An item that a cut goes through leaves its parts in the workspace, and a
+// second kernel adds them up; items so short that cutting them would not pay are not cut: the cut moves to their nearer
+// end.
+#pragma once
+#include "ra_chunk.h"
+#include "ra_prefill.h"
+
+namespace ra {
+
+constexpr int kExWaves = 4;
+constexpr int kExTileRows = kPfRows * kExWaves; // rows of a block of the tile kernel
+constexpr int kExFewRows = 64;                  // rows of a sequence and kv head up to which the other one takes them
+
+// ---- the line of items and its spans ------------------------------------------------------------------
+
+struct ExSeq {
+    int t0, n, L;  // first packed token, new tokens, tokens in all
+    int blocks, cost; // blocks of a kv head; the length of each on the line (stages, the mean of the sequence's blocks)
+};
+
+__device__ __forceinline__ int ex_div_g(const ExtendLaunch &a, int r) { return pf_div(r, a.G, a.magic_g); }
+
+// Stages that block j of a sequence needs: up to the one with its last row's last key.
+template <int ROWS> __device__ __forceinline__ int ex_stages(const ExtendLaunch &a, const ExSeq &s, int j)
+{
+    int last = ex_div_g(a, ROWS * (j + 1) - 1);
+    last = s.L - s.n + (last < s.n - 1 ? last : s.n - 1);
+    return (last + 32) >> 5; // (last >= -n: no key at all gives a number of zero or less)
+}
+
+template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
+{
+    ExSeq s = {0, 0, 0, 0, 0};
+    if (b >= a.B) return s;
+    const int t0 = a.cu[b], n = a.cu[b + 1] - t0, L = a.seq_lens[b], most = a.max_pages * kPage;
+    if (t0 < 0 || t0 > a.T || n <= 0 || n > a.T - t0) return s;
+    s.t0 = t0;
+    s.n = n < a.max_chunk ? n : a.max_chunk;
+    s.L = L < 0 ? 0 : (L < most ? L : most);
+    s.blocks = (s.n * a.G + ROWS - 1) / ROWS;
+    const int first = ex_stages<ROWS>(a, s, 0), last = ex_stages<ROWS>(a, s, s.blocks - 1);
+    s.cost = ((first > 0 ? first : 0) + (last > 0 ? last : 0) + 1) >> 1;
+    s.cost = s.cost < 1 ? 1 : s.cost;
+    return s;
+}
+
+// The line: lane c has chunk c of the sequences (64 of them, or a multiple of that in a very large batch).
+template <int ROWS> struct ExLine {
+    int lane, sub, before, total; // sub: sixty-fours of sequences in a chunk; before: start of this lane's chunk
+    int q, r, spans, cut;         // span k starts at q k + min(k, r), before cuts are moved; items up to `cut` are not cut
+
+    __device__ __forceinline__ void measure(const ExtendLaunch &a)
+    {
+        lane = threadIdx.x & 63;
+        sub = (a.B + 4095) >> 12;
+        const int chunks = (a.B + 64 * sub - 1) / (64 * sub);
+        int mine = 0;
+        for (int c = 0; c < chunks; c++) {
+            int n = 0;
+            for (int i = 0; i < sub; i++) {
+                const ExSeq s = ex_sequence<ROWS>(a, (c * sub + i) * 64 + lane);
+                int t;
+                (void)wave_scan(a.Hkv * s.blocks * s.cost, lane, t);
+                n += t;
+            }
+            if (lane == c) mine = n;
+        }
+        before = wave_scan(mine, lane, total);
+        spans = total / a.least;
+        spans = spans < 1 ? 1 : (spans < a.spans ? spans : a.spans);
+        q = total / spans;
+        r = total - q * spans;
+        cut = q >> 3 > a.least ? q >> 3 : a.least;
+    }
+    __device__ __forceinline__ int raw(int k) const { return q * k + (k < r ? k : r); }
+    // The last span that starts before x (x > 0).
+    __device__ __forceinline__ int span_before(int x) const
+    {
+        const int y = x - 1, big = r * (q + 1);
+        return y < big ? y / (q + 1) : r + (y - big) / q;
+    }
+};
+
+// A place on the line: an item, and how far into it.
+struct ExPlace {
+    int b, item, x0; // the sequence, its item (kv head * blocks + number), the item's start
+    ExSeq s;
+    int next;        // the next sequence of the same sixty-four that has items, or -1
+};
+
+// The item that x lies in (0 <= x < total).
+template <int ROWS> __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<ROWS> &line, int x, ExPlace &p)
+{
+    const unsigned long long m = __ballot(line.before <= x);
+    int c = 63 - __builtin_clzll(m);
+    const int chunks = (a.B + 64 * line.sub - 1) / (64 * line.sub);
+    c = c < chunks ? c : chunks - 1;
+    int start = __builtin_amdgcn_readlane(line.before, c);
+    for (int i = 0; i < line.sub; i++) {
+        const int base = (c * line.sub + i) * 64;
+        const ExSeq s = ex_sequence<ROWS>(a, base + line.lane);
+        const int own = a.Hkv * s.blocks * s.cost;
+        int t;
+        const int before = start + wave_scan(own, line.lane, t);
+        if (x >= start + t && i + 1 < line.sub) {
+            start += t;
+            continue;
+        }
+        const int l = 63 - __builtin_clzll(__ballot(own > 0 && before <= x));
+        p.b = base + l;
+        p.s.t0 = __builtin_amdgcn_readlane(s.t0, l), p.s.n = __builtin_amdgcn_readlane(s.n, l), p.s.L = __builtin_amdgcn_readlane(s.L, l);
+        p.s.blocks = __builtin_amdgcn_readlane(s.blocks, l), p.s.cost = __builtin_amdgcn_readlane(s.cost, l);
+        const int at = __builtin_amdgcn_readlane(before, l);
+        p.item = (x - at) / p.s.cost;
+        p.x0 = at + p.item * p.s.cost;
+        return;
+    }
+}
+
+// Where span k starts once short items are left whole.
+template <int ROWS> __device__ __forceinline__ int ex_start(const ExtendLaunch &a, const ExLine<ROWS> &line, int k, ExPlace &p)
+{
+    if (k >= line.spans) return line.total;
+    const int x = line.raw(k);
+    ex_find<ROWS>(a, line, x, p);
+    if (p.s.cost > line.cut || x == p.x0) return x;
+    return 2 * (x - p.x0) < p.s.cost ? p.x0 : p.x0 + p.s.cost;
+}
+
+// The workgroup's span: workgroups are dealt to the eight dies round-robin, and a die gets neighbouring spans, so that blocks
+// that read the same keys find them in its L2.
+__device__ __forceinline__ int ex_span_of(int spans)
+{
+    const int per = (spans + 7) >> 3, at = (int)blockIdx.x >> 3;
+    return at < per ? ((int)blockIdx.x & 7) * per + at : spans;
+}
+
+// A part of an item that a workgroup works on.
+struct ExPart {
+    int kvh, row0, rows; // rows of the sequence and kv head in all
+    int lo, hi;          // stages
+    int64_t slot;        // -1: the item is whole; else where its part goes
+};
+
+// The blocks of a (sequence, kv head) come from both ends in turn: their mean cost is the line's.
+template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch &a, const ExPlace &p, int y0, int y1, int span)
+{
+    ExPart t;
+    t.kvh = p.item / p.s.blocks;
+    const int jj = p.item - t.kvh * p.s.blocks, j = jj & 1 ? p.s.blocks - 1 - (jj >> 1) : jj >> 1;
+    t.row0 = ROWS * j;
+    t.rows = p.s.n * a.G;
+    int stages = ex_stages<ROWS>(a, p.s, j);
+    stages = stages < 0 ? 0 : stages;
+    t.lo = y0 == 0 ? 0 : (int)((int64_t)stages * y0 / p.s.cost);
+    t.hi = y1 == p.s.cost ? stages : (int)((int64_t)stages * y1 / p.s.cost);
+    t.slot = y0 == 0 ? (y1 == p.s.cost ? -1 : 2 * (int64_t)span + 1) : 2 * (int64_t)span;
+    return t;
+}
+
+// Goes through the parts of the workgroup's span; `work` is called with each.  Also tells the merge which items begin here and
+// end elsewhere: desc[2 k], desc[2 k + 1] = {first packed token, first row, rows, kv head}, {last span, -, -, -}.
+template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, F &&work)
+{
+    ExLine<ROWS> line;
+    line.measure(a);
+    int span = -1, last = 0;
+    ExPlace p;
+    int4 begun = {0, 0, 0, 0};
+    const int k = ex_span_of(line.spans);
+    if (line.total > 0 && k < line.spans) {
+        span = k;
+        ExPlace e;
+        const int end = ex_start<ROWS>(a, line, k + 1, e);
+        int x = ex_start<ROWS>(a, line, k, p);
+        if (x < end && x >= p.x0 + p.s.cost) ex_find<ROWS>(a, line, x, p);
+        while (x < end) {
+            const int x1 = p.x0 + p.s.cost, stop = x1 < end ? x1 : end;
+            const ExPart part = ex_part<ROWS>(a, p, x - p.x0, stop - p.x0, span);
+            if (x == p.x0 && stop < x1) {
+                begun = make_int4(p.s.t0, part.row0, part.rows, part.kvh);
+                last = line.span_before(x1);
+            }
+            work(p, part);
+            x = stop;
+            if (x >= end) break;
+            if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x1;
+            else ex_find<ROWS>(a, line, x, p);
+        }
+    }
+    // (every workgroup answers for one span, also for one that does not exist)
+    const int per = (line.spans + 7) >> 3, at = (int)blockIdx.x >> 3, answers = at < per ? ((int)blockIdx.x & 7) * per + at : (int)blockIdx.x;
+    if (threadIdx.x == 0) {
+        a.desc[2 * answers] = begun;
+        a.desc[2 * answers + 1] = make_int4(last, 0, 0, 0);
+    }
+}
+
+// ---- values that a row does not see ---------------------------------------------------------------------
+//
+// In the stages that the causal mask cuts, a row's weight of a later token is zero, and zero times an infinite or NaN value
+// is NaN.  Where a V operand of such a stage holds one, its product is made key by key, each added only to rows that see it.
+
+__device__ __forceinline__ bool ex_odd(bf16x8 v)
+{
+    const u32x4 w = __builtin_bit_cast(u32x4, v);
+    bool odd = false;
+#pragma unroll
+    for (int i = 0; i < 4; i++) odd = odd || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
+    return odd;
+}
+// The operand with only element e of its eight kept.
+__device__ __forceinline__ bf16x8 ex_only(bf16x8 v, bool lanes, int e)
+{
+    u32x4 w = __builtin_bit_cast(u32x4, v);
+#pragma unroll
+    for (int i = 0; i < 4; i++) w[i] &= lanes && (e >> 1) == i ? 0xffffu << (16 * (e & 1)) : 0u;
+    return __builtin_bit_cast(bf16x8, w);
+}
+
+// ---- many rows ------------------------------------------------------------------------------------------
+
+// Scale of a stage's first and second page for the scores (softmax scale and binary logarithm included), and for V.
+struct ExScale {
+    float k0, k1, v0, v1;
+};
+
+// One step of a wave's software pipeline: the weights of a stage (whose scores are st.s) and the scores of the next
+// (NEXT; MASK: the causal mask cuts one of the two), then O += P V of the first and the maxima of the new scores.
+// key, key_next: first keys of the two stages; lim: the last key that the lane's row sees.
+// As pf_step, but for the scales of e4m3 pages (their codes lie in the ring as bf16, exactly) and what MASK does with V.
+template <int D, bool FP8, bool MASK, bool NEXT>
+__device__ __forceinline__ void ex_step(PfState<D> &st, uint32_t k_next, uint32_t v_addr, const PfLane<D> &pl, const ExScale &sc, const ExScale &sn_,
+                                        int key, int key_next, int lim)
+{
+    using G = Geo<D, 2>;
+    typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
+    typedef bf16x8 __attribute__((address_space(3))) * lds_bf16x8;
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    const int hh = (threadIdx.x & 63) >> 5;
+    constexpr int KS = D / 16, DT = D / 32;
+#define EX_FENCE() __builtin_amdgcn_sched_barrier(0)
+    EX_FENCE();
+    constexpr int KA = KS < 4 ? KS : 4; // K operands are read four products ahead of their use
+    bf16x8 kf[KS];
+    uint32_t ka = k_next + (uint32_t)pl.k_base;
+    asm volatile("" : "+v"(ka));
+    if (NEXT) {
+#pragma unroll
+        for (int i = 0; i < KA; i++) kf[i] = *(lds_bf16x8)(ka ^ (uint32_t)(32 * i));
+    }
+    uint32_t vb = v_addr + (uint32_t)pl.v_base;
+    asm volatile("" : "+v"(vb));
+    s16x4 vr[DT][2][2];
+    auto v_read = [&](int dt, int kk) {
+#pragma unroll
+        for (int rd = 0; rd < 2; rd++)
+            vr[dt][kk][rd] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb ^ (uint32_t)pf_v_xor<D>(dt, rd)) + kk * G::kTile / 8);
+    };
+    EX_FENCE();
+    u32x4 pw[2];
+    float pprev = 0.f, acc0 = 0.f, acc1 = 0.f;
+    auto w_item = [&](int k) {
+        if (k < 16) {
+            float pk = __builtin_amdgcn_exp2f(__builtin_fmaf(st.s[k], k < 8 ? sc.k0 : sc.k1, -st.m));
+            if (k & 1) acc1 = k == 1 ? pk : acc1 + pk;
+            else acc0 = k == 0 ? pk : acc0 + pk;
+            if (FP8) pk *= k < 8 ? sc.v0 : sc.v1;
+            if (k & 1) pw[k >> 3][(k >> 1) & 3] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{pprev, pk}), bf16x2));
+            else pprev = pk;
+        } else {
+            st.lsum += acc0 + acc1;
+        }
+    };
+    constexpr int NW = 17;
+    f32x16 sn;
+    if (NEXT) {
+#pragma unroll
+        for (int k = 0; k < 3; k++) w_item(k);
+        EX_FENCE();
+#pragma unroll
+        for (int i = 0; i < KS; i++) {
+            if (i == 0) {
+#pragma unroll
+                for (int e = 0; e < 16; e++) sn[e] = 0.f;
+            }
+            sn = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[i], st.qf[i], sn, 0, 0, 0);
+            if (i + KA < KS) kf[i + KA] = *(lds_bf16x8)(ka ^ (uint32_t)(32 * (i + KA)));
+#pragma unroll
+            for (int w = 3 + i * (NW - 3) / KS; w < 3 + (i + 1) * (NW - 3) / KS; w++) w_item(w);
+            if (i >= KS - DT) v_read((i - (KS - DT)) / 2, (i - (KS - DT)) % 2);
+            EX_FENCE();
+        }
+    } else {
+#pragma unroll
+        for (int n = 0; n < DT; n++) v_read(n / 2, n % 2);
+#pragma unroll
+        for (int w = 0; w < NW; w++) w_item(w);
+        EX_FENCE();
+    }
+    // item k: 0..3 the causal mask, 4..11 partial maxima, 12 the exchange, 13 the end
+    float mx = 0.f, mx0 = 0.f, mn = 0.f;
+    bool grew = false;
+    auto m_item = [&](int k) {
+        if (k < 4) {
+            if (MASK) {
+                const int kk = key_next + 8 * k + 4 * hh; // element e = 4 k + x is key 8 k + 4 hh + x of the stage
+#pragma unroll
+                for (int x = 0; x < 4; x++) {
+                    if (kk + x > lim) sn[4 * k + x] = -INFINITY;
+                }
+            }
+        } else if (k == 4) {
+            mx = max3(first_max(sn[0], sn[1]), sn[2], sn[2]);
+        } else if (k < 8) {
+            mx = max3(mx, sn[2 * k - 7], sn[2 * k - 6]); // k = 5..7: elements 3..8
+        } else if (k < 11) {
+            mx = max3(mx, sn[2 * k - 7], sn[2 * k - 6]); // k = 8..10: elements 9..14
+        } else if (k == 11) {
+            mx = max3(mx, sn[15], sn[15]);
+        } else if (k == 12) {
+            const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+            mx = max3(__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[1]));
+        } else {
+            mn = FP8 ? mx : mx * sn_.k0;
+            grew = mn > st.m + kPfSlack;
+            st.s = sn;
+        }
+    };
+    // (two pages of unlike scales: their maxima apart, each scaled, then the larger)
+    auto m_item8 = [&](int k) {
+        if (k < 4) m_item(k);
+        else if (k == 4) mx0 = max3(first_max(sn[0], sn[1]), sn[2], sn[3]);
+        else if (k == 5) mx0 = max3(mx0, sn[4], sn[5]);
+        else if (k == 6) mx0 = max3(mx0, sn[6], sn[7]);
+        else if (k == 7) mx = max3(first_max(sn[8], sn[9]), sn[10], sn[11]);
+        else if (k == 8) mx = max3(mx, sn[12], sn[13]);
+        else if (k == 9) mx = max3(mx, sn[14], sn[15]);
+        else if (k == 10) mx = fmaxf(mx0 * sn_.k0, mx * sn_.k1);
+        else if (k >= 12) m_item(k);
+    };
+    constexpr int NMI = NEXT ? 14 : 0, NPV = 2 * DT;
+#pragma unroll
+    for (int n = 0; n < NPV; n++) {
+        const int dt = n / 2, kk = n % 2;
+        if (n + DT < NPV) v_read((n + DT) / 2, (n + DT) % 2);
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(vr[dt][kk][0], vr[dt][kk][1], 0, 1, 2, 3, 4, 5, 6, 7));
+        const bf16x8 pf = __builtin_bit_cast(bf16x8, pw[kk]);
+        if ((MASK || !NEXT) && __builtin_expect(__any(ex_odd(vf)), 0)) {
+#pragma unroll 1
+            for (int i = 0; i < 16; i++) { // key 8 (e / 4) + 4 h + e % 4 of the sixteen: element e of the lanes of half h
+                const int e = i & 7, h = i >> 3;
+                f32x16 t;
+#pragma unroll
+                for (int x = 0; x < 16; x++) t[x] = 0.f;
+                t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ex_only(vf, hh == h, e), pf, t, 0, 0, 0);
+                const bool sees = key + 16 * kk + 8 * (e >> 2) + 4 * h + (e & 3) <= lim;
+#pragma unroll
+                for (int x = 0; x < 16; x++) st.o[dt][x] += sees ? t[x] : 0.f;
+            }
+        } else {
+            st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, st.o[dt], 0, 0, 0);
+        }
+#pragma unroll
+        for (int w = n * NMI / NPV; w < (n + 1) * NMI / NPV; w++) {
+            if (FP8) m_item8(w);
+            else m_item(w);
+        }
+        EX_FENCE();
+    }
+    if (NEXT) {
+        if (__any(grew)) {
+            mn = grew ? mn : st.m; // (row by row: a row's result is the same whatever the wave's other rows hold)
+            const float alpha = __builtin_amdgcn_exp2f(st.m - mn);
+            st.m = mn;
+            st.lsum *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) st.o[dt] *= alpha;
+        }
+    }
+#undef EX_FENCE
+}
+
+constexpr int kExSlots = 4; // ring slots of one stage each
+
+template <int D> struct ExTileLds {
+    static constexpr int kStage = kExSlots * Geo<D, 2>::kStage; // the waves' staging areas follow the ring
+    static constexpr int kBytes = kStage + kPfStageBytes * kExWaves;
+};
+
+template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_tile_kernel(ExtendLaunch a)
+{
+    using G = Geo<D, 2>;
+    using X = ExTileLds<D>;
+    constexpr int NSL = kExSlots, DPW = G::kDmaPerTile;
+    extern __shared__ __attribute__((aligned(16384))) uint8_t lds[]; // the step forms LDS addresses by XOR
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)lds;
+    const int lane = threadIdx.x & 63, n = lane & 31, hh = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    LaneConst<D, 2> lc;
+    if (!FP8) lane_setup<D, 2>(lc, lane, a.stride_token_b);
+    PfLane<D> pl;
+    pf_lane_setup<D>(pl, lane);
+    uint8_t *const staging = lds + X::kStage + kPfStageBytes * wave;
+    int done = 0; // stages of the parts before this one: stage s of it lives in ring slot (done + s) % NSL
+
+    ex_walk<kExTileRows>(a, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
+        const int nst = t.hi - t.lo, row = t.row0 + kPfRows * wave + n; // this lane's row
+        const bool exists = row < t.rows;
+        const int token = ex_div_g(a, exists ? row : t.rows - 1), head = t.kvh * a.G + ((exists ? row : t.rows - 1) - token * a.G);
+        const int shift = p.s.L - p.s.n, lim = shift + token;
+        // the wave's first and last row: stages below `whole` are seen by all of its rows, those from `mine` on by none
+        const int row_lo = t.row0 + kPfRows * wave, row_hi = row_lo + kPfRows < t.rows ? row_lo + kPfRows - 1 : t.rows - 1;
+        const int whole = row_lo < t.rows ? (shift + ex_div_g(a, row_lo) + 1) >> 5 : 0;
+        int mine = row_lo < t.rows ? (shift + ex_div_g(a, row_hi) + 32) >> 5 : 0;
+        mine = (mine < t.hi ? mine : t.hi) - t.lo; // of the part's stages
+
+        // Wave w brings tile w of every stage (K of its two pages, V of its two pages).
+        const int32_t *const pages = a.table + (int64_t)p.b * a.max_pages;
+        const int count = (p.s.L + kPage - 1) / kPage; // pages that exist
+        const int of = wave & 1; // the wave's page of a stage's two
+        const uint8_t *const pool = (wave < 2 ? a.k_pool : a.v_pool) + (int64_t)t.kvh * a.stride_head_b;
+        auto page_id = [&](int s, int h) __attribute__((always_inline)) { // of page h of stage s of the part
+            const int i = 2 * (t.lo + s) + h;
+            const int id = s < nst && i < count ? uniform_load(pages, i) : -1;
+            return id < a.num_pages ? id : -1;
+        };
+        int issued = 0, id = page_id(0, of), other = FP8 ? page_id(0, 1 - of) : 0;
+        auto issue = [&]() __attribute__((always_inline)) { // bf16 pools: the next stage's tile
+            if (issued < nst) {
+                const int valid = id < 0 ? 0 : p.s.L - kPage * (2 * (t.lo + issued) + of);
+                issue_tile<D, 2>(lc, pool + (int64_t)(id < 0 ? 0 : id) * a.stride_page_b, valid, lds_addr + ((done + issued) & (NSL - 1)) * G::kStage + wave * G::kTile, a.zeros);
+                issued++;
+                id = page_id(issued, of);
+            }
+        };
+        // e4m3 pools: a tile goes through registers, and its codes into the ring as bf16
+        constexpr int NB = D / 64; // 16-byte pieces of a tile that a lane has
+        uint4 raw[NB];
+        float scales_next = 1.f; // lanes 0..3: K and V scale of the first page, of the second
+        auto fetch = [&]() __attribute__((always_inline)) {
+            const int i0 = 2 * (t.lo + issued);
+            const int valid = id < 0 ? 0 : p.s.L - kPage * (i0 + of);
+            const uint8_t *const tile = pool + (int64_t)(id < 0 ? 0 : id) * a.stride_page_b;
+#pragma unroll
+            for (int x = 0; x < NB; x++) {
+                const int u = 64 * x + lane, r = u / (D / 16), c = u % (D / 16);
+                raw[x] = make_uint4(0, 0, 0, 0);
+                if (issued < nst && r < valid) raw[x] = *(const uint4 *)(tile + (int64_t)r * a.stride_token_b + 16 * c);
+            }
+            scales_next = 1.f;
+            const int pid = ((lane >> 1) & 1) == of ? id : other;
+            if (lane < 4 && pid >= 0) {
+                scales_next = ((lane & 1) ? a.v_scale : a.k_scale)[(int64_t)pid * a.Hkv + t.kvh];
+            }
+            issued++;
+            id = page_id(issued, of), other = page_id(issued, 1 - of);
+        };
+        auto put = [&](int s) __attribute__((always_inline)) { // what was fetched, as stage s
+            uint8_t *const tile = lds + ((done + s) & (NSL - 1)) * G::kStage + wave * G::kTile;
+#pragma unroll
+            for (int x = 0; x < NB; x++) {
+                const int u = 64 * x + lane, r = u / (D / 16), c = u % (D / 16), z = swz(r) & (G::kUnits - 1);
+                *(bf16x8 *)(tile + 16 * (r * G::kUnits + ((2 * c) ^ z))) = fp8x8_to_bf16((int)raw[x].x, (int)raw[x].y);
+                *(bf16x8 *)(tile + 16 * (r * G::kUnits + ((2 * c + 1) ^ z))) = fp8x8_to_bf16((int)raw[x].z, (int)raw[x].w);
+            }
+        };
+        ExScale sc = {a.scale_log2, a.scale_log2, 1.f, 1.f}, sc_next = sc, sc_put = sc;
+        auto scales_of = [&](float x) __attribute__((always_inline)) {
+            x = x == 0.f ? 1e-30f : x; // (zero times the mask's -inf would be NaN)
+            auto lane_of = [&](int l) __attribute__((always_inline)) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)); };
+            return ExScale{lane_of(0) * a.scale_log2, lane_of(2) * a.scale_log2, lane_of(1), lane_of(3)};
+        };
+        // Before the first step that reads stage s: it has landed, for every wave, and every wave has left the step that read
+        // stage s - 2, whose slot the next load takes.
+        auto open = [&](int s) __attribute__((always_inline)) {
+            if (!FP8) WaitTail<NSL - 1, DPW>::run(issued - 1 - s);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_s_barrier();
+            asm volatile("" ::: "memory");
+            if (FP8) {
+                sc = sc_next, sc_next = sc_put;
+                if (s + 1 < nst) {
+                    put(s + 1);
+                    sc_put = scales_of(scales_next);
+                    fetch();
+                }
+            } else {
+                issue();
+            }
+        };
+
+        PfState<D> st;
+        {
+            const uint16_t *const q = a.q + (int64_t)(p.s.t0 + token) * a.q_stride + head * D + 8 * hh;
+#pragma unroll
+            for (int i = 0; i < D / 16; i++) st.qf[i] = *(const bf16x8 *)(q + 16 * i);
+        }
+        if (FP8) {
+            fetch();
+            put(0); // (the barriers of the part before have passed its slot)
+            sc_put = scales_of(scales_next);
+            fetch();
+        } else {
+            issue();
+            issue();
+        }
+        st.m = kPfLowest, st.lsum = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < D / 32; dt++) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) st.o[dt][e] = 0.f;
+        }
+        // Stage s is opened before step s - 1, which makes its scores; the first one before the scores alone.
+        if (nst > 0) {
+            open(0);
+            if (FP8) sc = sc_next; // (stage 0; sc_next: stage 1 once that has been opened)
+            if (mine > 0) {
+                pf_scores<D>(lds_addr + (done & (NSL - 1)) * G::kStage, pl, st.qf, st.s);
+                if (t.lo >= whole) {
+#pragma unroll
+                    for (int e = 0; e < 16; e++) {
+                        if (32 * t.lo + 8 * (e / 4) + 4 * hh + (e % 4) > lim) st.s[e] = -INFINITY;
+                    }
+                }
+                float m0 = first_max(st.s[0], st.s[1]), m1 = first_max(st.s[8], st.s[9]);
+#pragma unroll
+                for (int e = 2; e < 8; e += 2) m0 = max3(m0, st.s[e], st.s[e + 1]), m1 = max3(m1, st.s[8 + e], st.s[9 + e]);
+                float mx = fmaxf(m0 * sc.k0, m1 * sc.k1);
+                const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
+                st.m = fmaxf(max3(__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[1])), kPfLowest);
+            }
+            auto at = [&](int s) __attribute__((always_inline)) { return lds_addr + ((done + s) & (NSL - 1)) * G::kStage; };
+#define EX_STEP(MASK, NEXT) ex_step<D, FP8, MASK, NEXT>(st, at(s + 1), at(s) + 2 * G::kTile, pl, sc, sc_next, 32 * (t.lo + s), 32 * (t.lo + s + 1), lim)
+            int s = 0;
+            auto advance = [&]() __attribute__((always_inline)) {
+                if (s + 1 < nst) open(s + 1);
+                else if (FP8) sc = sc_next;
+            };
+            if (mine > 0) {
+                const int free = whole - t.lo < mine ? whole - t.lo : mine; // stages without a mask
+#pragma unroll 1
+                for (; s + 1 < free; s++) {
+                    open(s + 1);
+                    EX_STEP(false, true);
+                }
+#pragma unroll 1
+                for (; s + 1 < mine; s++) {
+                    open(s + 1);
+                    EX_STEP(true, true);
+                }
+                advance();
+                EX_STEP(false, false);
+                s++;
+            }
+            for (; s < nst; s++) advance();
+#undef EX_STEP
+        }
+        done = (done + nst) & (NSL - 1);
+
+        // a row's sum is spread over its two lanes
+        float l;
+        {
+            const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(st.lsum), __float_as_uint(st.lsum), false, false);
+            l = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        }
+        if (row_lo >= t.rows) return;
+        if (t.slot >= 0) {
+            // a part: as the accumulators lie, which is whole lines
+            float *const o = a.part_o + t.slot * (kExTileRows * D) + wave * (kPfRows * D) + 4 * lane;
+#pragma unroll
+            for (int dt = 0; dt < D / 32; dt++) {
+#pragma unroll
+                for (int j = 0; j < 4; j++)
+                    *(f32x4 *)(o + 256 * (4 * dt + j)) = f32x4{st.o[dt][4 * j], st.o[dt][4 * j + 1], st.o[dt][4 * j + 2], st.o[dt][4 * j + 3]};
+            }
+            if (hh == 0) *(float2 *)(a.part_lse + 2 * (t.slot * kExTileRows + kPfRows * wave + n)) = make_float2(st.m, l);
+            return;
+        }
+        const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l; // (no key: zeros; NaN stays)
+#pragma unroll
+        for (int pc = 0; pc < D / 64; pc++) {
+#pragma unroll
+            for (int dtl = 0; dtl < 2; dtl++) {
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    f32x4 v;
+#pragma unroll
+                    for (int x = 0; x < 4; x++) v[x] = st.o[2 * pc + dtl][4 * j + x] * inv;
+                    *(bf16x4 *)(staging + kPfStageRow * n + 16 * ((4 * dtl + j) ^ pf_stage_swz(n)) + 8 * hh) = __builtin_convertvector(v, bf16x4);
+                }
+            }
+#pragma unroll
+            for (int m = 0; m < 4; m++) {
+                const int r = 8 * m + (lane >> 3), c = lane & 7, orow = row_lo + r;
+                const u32x4 v = *(const u32x4 *)(staging + kPfStageRow * r + 16 * (c ^ pf_stage_swz(r)));
+                if (orow < t.rows) {
+                    const int i = ex_div_g(a, orow);
+                    *(u32x4 *)(a.out + ((int64_t)(p.s.t0 + i) * a.Hq + t.kvh * a.G + (orow - i * a.G)) * D + 64 * pc + 8 * c) = v;
+                }
+            }
+        }
+        if (exists && hh == 0) a.lse[(int64_t)(p.s.t0 + token) * a.Hq + head] = (st.m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+    });
+    wait_vmcnt<0>(); // nothing may land in LDS after the workgroup has left
+}
+
+// ---- few rows -------------------------------------------------------------------------------------------
+
+template <int D, int KVB> struct ExFewLds {
+    using G = Geo<D, KVB>;
+    static constexpr int kSlots = KVB == 2 ? 2 : 4;        // a wave's ring, in stages
+    static constexpr int kRing = kSlots * G::kStage;
+    static constexpr int kStats = kExWaves * kRing;         // what the waves' rows have as maximum and sum
+    static constexpr int kBytes = kStats + kExWaves * kExFewRows * 8;
+    static_assert(kRing >= kExFewRows * D * 4, "a wave's sums take the place of its ring");
+    static_assert((kSlots - 1) * G::kDmaPerStage < 64, "the vector-memory counter holds 6 bits");
+};
+
+// NQT: tiles of sixteen rows that a sequence and kv head has at most.
+template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1) void extend_few_kernel(ExtendLaunch a)
+{
+    using G = Geo<D, KVB>;
+    using X = ExFewLds<D, KVB>;
+    constexpr int NST = X::kSlots, DPS = G::kDmaPerStage, W = kExWaves;
+    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int rn = lane & 15, j = lane >> 4;
+    uint8_t *const ring = lds + wave * X::kRing;
+    const uint32_t ring_addr = (uint32_t)(uintptr_t)ring;
+    LaneConst<D, KVB> lc;
+    lane_setup<D, KVB>(lc, lane, a.stride_token_b);
+
+    ex_walk<kExFewRows>(a, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
+        const int ntiles = (t.rows + 15) >> 4, shift = p.s.L - p.s.n;
+        // the wave's stages of the part: wave, wave + 4, ...
+        const int left = t.hi - t.lo - wave, mine = left > 0 ? (left + W - 1) / W : 0;
+        const int32_t *const pages = a.table + (int64_t)p.b * a.max_pages;
+        const int count = (p.s.L + kPage - 1) / kPage;
+        const int64_t head_b = (int64_t)t.kvh * a.stride_head_b;
+        auto page_id = [&](int i, int h) __attribute__((always_inline)) {
+            const int g = 2 * (t.lo + wave + W * i) + h;
+            const int id = i < mine && g < count ? uniform_load(pages, g) : -1;
+            return id < a.num_pages ? id : -1;
+        };
+        int issued = 0, id0 = page_id(0, 0), id1 = page_id(0, 1);
+        auto issue = [&]() __attribute__((always_inline)) {
+            if (issued >= mine) return;
+            const int nv = p.s.L - 2 * kPage * (t.lo + wave + W * issued);
+            const int nv0 = id0 < 0 ? 0 : nv, nv1 = id1 < 0 ? 0 : nv - kPage;
+            const int64_t off0 = (int64_t)(id0 < 0 ? 0 : id0) * a.stride_page_b + head_b, off1 = (int64_t)(id1 < 0 ? 0 : id1) * a.stride_page_b + head_b;
+            const uint32_t sb = ring_addr + (issued % NST) * G::kStage;
+            issue_tile<D, KVB, true>(lc, a.k_pool + off0, nv0, sb, a.zeros);
+            issue_tile<D, KVB, true>(lc, a.k_pool + off1, nv1, sb + G::kTile, a.zeros);
+            issue_tile<D, KVB, true>(lc, a.v_pool + off0, nv0, sb + 2 * G::kTile, a.zeros);
+            issue_tile<D, KVB, true>(lc, a.v_pool + off1, nv1, sb + 3 * G::kTile, a.zeros);
+            if (KVB == 1) { // the pages' scales land behind the tiles: lanes 0..3 bring k0, v0, k1, v1
+                const int pid = (lane & 2) ? id1 : id0;
+                const void *src = a.zeros;
+                if (lane < 4 && pid >= 0) src = ((lane & 1) ? a.v_scale : a.k_scale) + (int64_t)pid * a.Hkv + t.kvh;
+                dma4(src, sb + 4 * G::kTile);
+            }
+            issued++;
+            id0 = page_id(issued, 0), id1 = page_id(issued, 1);
+        };
+        // Query rows as the second operand of K . Q^T wants them: lane (row, j) holds the d values that its K operand holds.
+        bf16x8 qf[NQT][G::kKSteps];
+        int lim[NQT];
+#pragma unroll
+        for (int q = 0; q < NQT; q++) {
+            int r = 16 * q + rn;
+            r = r < t.rows ? r : t.rows - 1;
+            const int token = ex_div_g(a, r);
+            lim[q] = shift + token;
+            const uint16_t *const src = a.q + (int64_t)(p.s.t0 + token) * a.q_stride + (t.kvh * a.G + r - token * a.G) * D;
+#pragma unroll
+            for (int i = 0; i < G::kKSteps; i++) {
+                const int d0 = KVB == 2 ? 32 * i + 8 * j : 16 * (4 * (i / 2) + j) + 8 * (i % 2);
+                if (q < ntiles) qf[q][i] = *(const bf16x8 *)(src + d0);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < NST - 1; i++) issue();
+
+        f32x4 o[NQT][G::kDTiles];
+        float m[NQT], lsum[NQT];
+#pragma unroll
+        for (int q = 0; q < NQT; q++) {
+            m[q] = kPfLowest, lsum[q] = 0.f;
+#pragma unroll
+            for (int dt = 0; dt < G::kDTiles; dt++) o[q][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+#pragma unroll 1
+        for (int it = 0; it < mine; it++) {
+            issue();
+            WaitTail<NST - 1, DPS>::run(issued - 1 - it);
+            const uint8_t *const st = ring + (it % NST) * G::kStage;
+            const int key = 32 * (t.lo + wave + W * it);
+            f32x4 s[NQT][2];
+#pragma unroll
+            for (int pg = 0; pg < 2; pg++) {
+#pragma unroll
+                for (int q = 0; q < NQT; q++) s[q][pg] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int i = 0; i < G::kKReads; i++) {
+                    if (KVB == 2) {
+                        const bf16x8 kf = *(const bf16x8 *)(st + pg * G::kTile + lc.k_off[i]);
+#pragma unroll
+                        for (int q = 0; q < NQT; q++)
+                            if (q < ntiles) s[q][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[q][i], s[q][pg], 0, 0, 0);
+                    } else {
+                        const int4 kc = *(const int4 *)(st + pg * G::kTile + lc.k_off[i]); // 16 codes: two k-steps
+                        const bf16x8 k0 = fp8x8_to_bf16(kc.x, kc.y), k1 = fp8x8_to_bf16(kc.z, kc.w);
+#pragma unroll
+                        for (int q = 0; q < NQT; q++)
+                            if (q < ntiles) {
+                                s[q][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[q][2 * i], s[q][pg], 0, 0, 0);
+                                s[q][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[q][2 * i + 1], s[q][pg], 0, 0, 0);
+                            }
+                    }
+                }
+            }
+            // e4m3: the K scale folds into the score's, the V scale into the weights before they are rounded to bf16 (the
+            // row sum keeps them unscaled)
+            float ks0 = a.scale_log2, ks1 = a.scale_log2, vs0 = 1.0f, vs1 = 1.0f;
+            if (KVB == 1) {
+                const f32x4 sc = *(const f32x4 *)(st + 4 * G::kTile);
+                ks0 *= sc[0], vs0 = sc[1], ks1 *= sc[2], vs1 = sc[3];
+            }
+            const bool masked = key + 31 > shift; // (the first row sees the least)
+            bf16x8 pf[NQT];
+#pragma unroll
+            for (int q = 0; q < NQT; q++) {
+                if (q >= ntiles) continue;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 4; e++) v[e] = s[q][0][e] * ks0, v[4 + e] = s[q][1][e] * ks1;
+                if (masked) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) {
+                        if (key + 4 * j + e > lim[q]) v[e] = -INFINITY;
+                        if (key + kPage + 4 * j + e > lim[q]) v[4 + e] = -INFINITY;
+                    }
+                }
+                const float mx = row_max3(max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[7])));
+                const float mn = max3(m[q], mx, mx);
+                f32x8 w;
+#pragma unroll
+                for (int e = 0; e < 8; e++) w[e] = __builtin_amdgcn_exp2f(v[e] - mn);
+                const float ws = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
+                if (KVB == 1) {
+#pragma unroll
+                    for (int e = 0; e < 4; e++) w[e] *= vs0, w[4 + e] *= vs1;
+                }
+                pf[q] = __builtin_convertvector(w, bf16x8);
+                if (__any(mn != m[q])) {
+                    const float alpha = __builtin_amdgcn_exp2f(m[q] - mn);
+                    m[q] = mn;
+                    lsum[q] *= alpha;
+#pragma unroll
+                    for (int dt = 0; dt < G::kDTiles; dt++) o[q][dt] *= alpha;
+                }
+                lsum[q] += ws;
+            }
+            typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
+            typedef int __attribute__((ext_vector_type(2))) i32x2;
+            typedef i32x2 __attribute__((address_space(3))) * lds_i32x2;
+            typedef short s16x8 __attribute__((ext_vector_type(8)));
+            const uint32_t vb = ring_addr + (it % NST) * G::kStage + 2 * G::kTile;
+#pragma unroll
+            for (int dt = 0; dt < G::kDTiles; dt++) {
+                bf16x8 vf;
+                if (KVB == 2) {
+                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + lc.v_off[dt]));
+                    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + G::kTile + lc.v_off[dt]));
+                    vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
+                } else {
+                    const i32x2 vc = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)((vb + lc.v_off[0]) ^ (uint32_t)(16 * dt)));
+                    vf = fp8x8_to_bf16(vc[0], vc[1]);
+                }
+                if (masked && __builtin_expect(__any(ex_odd(vf)), 0)) {
+#pragma unroll 1
+                    for (int i = 0; i < 32; i++) { // element e of lane group h: key 4 h + e of the first page, or 4 h + e - 4 of the second
+                        const int e = i & 7, h = i >> 3, at = key + 4 * h + (e & 3) + (e & 4 ? kPage : 0);
+                        const bf16x8 one = ex_only(vf, j == h, e);
+#pragma unroll
+                        for (int q = 0; q < NQT; q++) {
+                            if (q >= ntiles) continue;
+                            const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pf[q], (f32x4{0.f, 0.f, 0.f, 0.f}), 0, 0, 0);
+#pragma unroll
+                            for (int c = 0; c < 4; c++) o[q][dt][c] += at <= lim[q] ? x[c] : 0.f;
+                        }
+                    }
+                    continue;
+                }
+#pragma unroll
+                for (int q = 0; q < NQT; q++)
+                    if (q < ntiles) o[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[q], o[q][dt], 0, 0, 0);
+            }
+            // every LDS read of this stage has returned before a later load may overwrite it
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        }
+
+        // The four waves' sums: a row's 16-byte pieces lie XOR-swizzled by the row, in the wave's ring.
+        float *const mine_o = (float *)ring;
+        float2 *const stats = (float2 *)(lds + X::kStats);
+        constexpr int PIECES = D / 4;
+#pragma unroll
+        for (int q = 0; q < NQT; q++) {
+            if (q >= ntiles) continue;
+            const int r = 16 * q + rn;
+            const float l = row_sum(lsum[q]);
+#pragma unroll
+            for (int dt = 0; dt < G::kDTiles; dt++) *(f32x4 *)(mine_o + r * D + 4 * ((4 * dt + j) ^ rn)) = o[q][dt];
+            if (j == 0) stats[wave * kExFewRows + r] = make_float2(m[q], l);
+        }
+        __syncthreads();
+        for (int x = threadIdx.x; x < t.rows * PIECES; x += 64 * W) {
+            const int r = x / PIECES, c = x % PIECES;
+            float mm = kPfLowest, l = 0.f;
+            float2 ml[W];
+            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < W; w++) ml[w] = stats[w * kExFewRows + r], mm = fmaxf(mm, ml[w].x);
+#pragma unroll
+            for (int w = 0; w < W; w++) {
+                const float f = __builtin_amdgcn_exp2f(ml[w].x - mm);
+                l += f * ml[w].y;
+                acc += f * *(const f32x4 *)((const float *)(lds + w * X::kRing) + r * D + 4 * (c ^ (r & 15)));
+            }
+            if (t.slot >= 0) {
+                *(f32x4 *)(a.part_o + (t.slot * kExFewRows + r) * D + 4 * c) = acc;
+                if (c == 0) *(float2 *)(a.part_lse + 2 * (t.slot * kExFewRows + r)) = make_float2(mm, l);
+            } else {
+                const int token = ex_div_g(a, r);
+                const int64_t rh = (int64_t)(p.s.t0 + token) * a.Hq + t.kvh * a.G + (r - token * a.G);
+                const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l; // (no key: zeros; NaN stays)
+                *(bf16x4 *)(a.out + rh * D + 4 * c) = __builtin_convertvector(acc * inv, bf16x4);
+                if (c == 0) a.lse[rh] = (mm + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
+            }
+        }
+        __syncthreads(); // (the rings take the next part's stages)
+    });
+    wait_vmcnt<0>();
+}
+
+// ---- what spans share -----------------------------------------------------------------------------------
+
+constexpr int kExMergeWgs = 1024, kExMaxSpans = 2048;
+
+// Adds up the parts of the items that a cut goes through: a workgroup takes 256 consecutive values of an item at a time, its
+// waves every fourth part each.  ROWS: those of the kernel that left them, with its layout.
+template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(ExtendLaunch a)
+{
+    constexpr int W = kExWaves, CHUNKS = ROWS * D / 256;
+    __shared__ int list[kExMaxSpans];
+    __shared__ int counts[W];
+    __shared__ f32x4 sums[W][64];
+    __shared__ float2 stats[W][64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    // the spans in which such an item begins, in order
+    int items = 0;
+    for (int base = 0; base < a.spans; base += 64 * W) {
+        const int k = base + (int)threadIdx.x;
+        const bool is = k < a.spans && a.desc[2 * k + 1].x > k;
+        const unsigned long long m = __ballot(is);
+        if (lane == 0) counts[wave] = __popcll(m);
+        __syncthreads();
+        int at = items;
+#pragma unroll
+        for (int w = 0; w < W; w++) {
+            if (w < wave) at += counts[w];
+            items += counts[w];
+        }
+        if (is) list[at + __popcll(m & ((1ull << lane) - 1ull))] = k;
+        __syncthreads();
+    }
+    for (int u = blockIdx.x; u < items * CHUNKS; u += gridDim.x) {
+        const int k = list[u / CHUNKS], chunk = u % CHUNKS;
+        const int4 item = a.desc[2 * k]; // {first packed token, first row, rows, kv head}
+        const int last = a.desc[2 * k + 1].x;
+        int r, d; // this lane's row of the block, and the first of its four values
+        if (ROWS == kExTileRows) {
+            const int wv = chunk / (D / 8), c = chunk % (D / 8);
+            r = kPfRows * wv + (lane & 31), d = 32 * (c >> 2) + 8 * (c & 3) + 4 * (lane >> 5);
+        } else {
+            r = chunk * (256 / D) + lane / (D / 4), d = 4 * (lane % (D / 4));
+        }
+        const int row = item.y + r;
+        const bool exists = row < item.z;
+        float mm = kPfLowest, l = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        if (exists) {
+            constexpr int AT = 4;
+            for (int p0 = k + wave; p0 <= last; p0 += AT * W) {
+                float2 ml[AT];
+                f32x4 o[AT];
+#pragma unroll
+                for (int i = 0; i < AT; i++) {
+                    const int p = p0 + W * i;
+                    const int64_t slot = p == k ? 2 * (int64_t)k + 1 : 2 * (int64_t)p;
+                    ml[i] = make_float2(kPfLowest, 0.f), o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+                    if (p <= last) {
+                        ml[i] = *(const float2 *)(a.part_lse + 2 * (slot * ROWS + r));
+                        o[i] = *(const f32x4 *)(a.part_o + slot * (ROWS * D) + 256 * chunk + 4 * lane);
+                    }
+                }
+                float top = mm;
+#pragma unroll
+                for (int i = 0; i < AT; i++) top = fmaxf(top, ml[i].x);
+                const float f0 = __builtin_amdgcn_exp2f(mm - top);
+                l *= f0, acc *= f0, mm = top;
+#pragma unroll
+                for (int i = 0; i < AT; i++) {
+                    const float f = __builtin_amdgcn_exp2f(ml[i].x - top);
+                    l += f * ml[i].y, acc += f * o[i];
+                }
+            }
+        }
+        sums[wave][lane] = acc, stats[wave][lane] = make_float2(mm, l);
+        __syncthreads();
+        if (wave == 0 && exists) {
+            float top = kPfLowest, all = 0.f;
+            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int w = 0; w < W; w++) top = fmaxf(top, stats[w][lane].x);
+#pragma unroll
+            for (int w = 0; w < W; w++) {
+                const float f = __builtin_amdgcn_exp2f(stats[w][lane].x - top);
+                all += f * stats[w][lane].y, v += f * sums[w][lane];
+            }
+            const int token = ex_div_g(a, row);
+            const int64_t rh = (int64_t)(item.x + token) * a.Hq + item.w * a.G + (row - token * a.G);
+            const float inv = all > 0.f ? 1.0f / all : all == 0.f ? 0.f : all;
+            *(bf16x4 *)(a.out + rh * D + d) = __builtin_convertvector(v * inv, bf16x4);
+            if (d == 0) a.lse[rh] = (top + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+        }
+        __syncthreads();
+    }
+}
+
+} // namespace ra

@@ -1,0 +1,83 @@
+// The launches of the attention of chunks over the paged cache (the kernels: ra_extend.h).
+#include "ra_extend.h"
+
+namespace ra {
+
+constexpr int kExLeast = 8; // stages of a span at least
+
+// Which kernel a call takes, its workgroups, and how finely the work is cut.
+static void extend_shape(ExtendLaunch &a)
+{
+    a.few = (int64_t)a.max_chunk * a.G <= kExFewRows;
+    const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExTileRows + a.B;
+    const int64_t line = blocks * a.Hkv * (a.max_pages / 2 + 1); // its length at most
+    a.least = kExLeast;
+    const int64_t resident = (int64_t)(a.num_cus < 8 ? 8 : a.num_cus & ~7) * (a.few ? (a.D == 64 ? 2 : 1) : (a.D == 64 ? 3 : 2));
+    int64_t spans = (line / a.least + 7) & ~(int64_t)7;
+    spans = spans < 8 ? 8 : spans < resident ? spans : resident;
+    a.spans = (int)(spans < kExMaxSpans ? spans : kExMaxSpans);
+}
+
+size_t carve_extend(ExtendLaunch &a, void *base)
+{
+    extend_shape(a);
+    const int64_t slots = 2 * (int64_t)a.spans, rows = a.few ? kExFewRows : kExTileRows;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        void *const p = base ? (char *)base + at : nullptr;
+        at += (bytes + 255) & ~(size_t)255;
+        return p;
+    };
+    a.desc = (int4 *)take(sizeof(int4) * 2 * a.spans);
+    a.part_lse = (float *)take((size_t)(slots * rows * 8));
+    a.part_o = (float *)take((size_t)(slots * rows * a.D * 4));
+    return at;
+}
+
+#define RA_EX_TILES(X) X(64, false) X(64, true) X(128, false) X(128, true)
+#define RA_EX_FEWS(X) X(64, 2, 1) X(64, 2, 2) X(64, 2, 4) X(64, 1, 1) X(64, 1, 2) X(64, 1, 4) X(128, 2, 1) X(128, 2, 2) X(128, 2, 4) X(128, 1, 1) X(128, 1, 2) X(128, 1, 4)
+
+hipError_t extend_config()
+{
+    hipError_t e = hipSuccess;
+#define RA_EX_CONFIG(DD, F) \
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)extend_tile_kernel<DD, F>, hipFuncAttributeMaxDynamicSharedMemorySize, ExTileLds<DD>::kBytes);
+    RA_EX_TILES(RA_EX_CONFIG)
+#undef RA_EX_CONFIG
+#define RA_EX_CONFIG(DD, KVB, Q) \
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)extend_few_kernel<DD, KVB, Q>, hipFuncAttributeMaxDynamicSharedMemorySize, ExFewLds<DD, KVB>::kBytes);
+    RA_EX_FEWS(RA_EX_CONFIG)
+#undef RA_EX_CONFIG
+    return e;
+}
+
+hipError_t launch_extend(const ExtendLaunch &a, hipStream_t s)
+{
+    const dim3 grid((unsigned)a.spans), block(64 * kExWaves);
+    if (!a.few) {
+#define RA_EX_LAUNCH(DD, F) \
+    if (a.D == DD && (a.kv_fp8 != 0) == F) hipLaunchKernelGGL((extend_tile_kernel<DD, F>), grid, block, (ExTileLds<DD>::kBytes), s, a);
+        RA_EX_TILES(RA_EX_LAUNCH)
+#undef RA_EX_LAUNCH
+    } else {
+        const int rows = a.max_chunk * a.G, tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+#define RA_EX_LAUNCH(DD, KVB, Q) \
+    if (a.D == DD && (a.kv_fp8 ? 1 : 2) == KVB && tiles == Q) hipLaunchKernelGGL((extend_few_kernel<DD, KVB, Q>), grid, block, (ExFewLds<DD, KVB>::kBytes), s, a);
+        RA_EX_FEWS(RA_EX_LAUNCH)
+#undef RA_EX_LAUNCH
+    }
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || a.max_pages / 2 + 1 <= a.least) return e; // (no item is long enough to be cut)
+#define RA_EX_MERGE(DD) \
+    if (a.few) hipLaunchKernelGGL((extend_merge_kernel<DD, kExFewRows>), dim3(kExMergeWgs), block, 0, s, a); \
+    else hipLaunchKernelGGL((extend_merge_kernel<DD, kExTileRows>), dim3(kExMergeWgs), block, 0, s, a)
+    if (a.D == 128) {
+        RA_EX_MERGE(128);
+    } else {
+        RA_EX_MERGE(64);
+    }
+#undef RA_EX_MERGE
+    return hipGetLastError();
+}
+
+} // namespace ra
