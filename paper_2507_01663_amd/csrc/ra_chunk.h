@@ -45,7 +45,8 @@ struct ExtendLaunch {
     const void *zeros;
     float *part_o, *part_lse;    // partial results, two slots per span
     int4 *desc;                  // [spans][2] what the merge adds up
-    int32_t spans, least, few;   // workgroups, stages of a span at least, and whether every sequence has few rows (set by carve_extend)
+    int32_t spans, grid, least;  // workgroups that share the work, workgroups launched, stages of a span at least,
+    int32_t few;                 // and whether every sequence has few rows (set by carve_extend)
 };
 // How a call is launched (from B, T, max_chunk, Hkv, G, D, max_pages and num_cus), and its workspace: the bytes; places the pointers
 // when base is not null.

@@ -132,7 +132,7 @@ ra_status check_extend(const ra_extend *p, char *msg, size_t n)
     // 32-bit row numbers inside a sequence, and a stream of work (32 keys of a block of rows to a unit) below 2^30 units
     const int64_t rows = (int64_t)p->max_chunk_len * (p->Hq / p->Hkv);
     const int64_t blocks = (int64_t)p->total_tokens * (p->Hq / p->Hkv) / 128 + p->num_seqs;
-    if (rows >= (int64_t)1 << 30 || blocks * p->Hkv >= (int64_t)1 << 30 || blocks * p->Hkv * ((int64_t)p->max_pages_per_seq / 2 + 1) >= (int64_t)1 << 30)
+    if (rows >= (int64_t)1 << 30 || blocks * p->Hkv >= (int64_t)1 << 23 || blocks * p->Hkv * ((int64_t)p->max_pages_per_seq / 2 + 16) >= (int64_t)1 << 30)
         return fail(RA_ERR_UNSUPPORTED, "batch too large");
     if (p->num_seqs == 0 || p->total_tokens == 0 || p->max_chunk_len == 0) return RA_OK;
     if (!p->q || !p->out || !p->lse) return fail(RA_ERR_INVALID_ARG, "a required pointer (q, out, lse) is NULL");

@@ -8,7 +8,7 @@
 // waves multiplying every stage of 32 keys that streams through one LDS ring:
 //   S^T[key, row] = K . Q^T,   O^T[d, row] += V^T . P^T     (32x32x16 MFMA, binary32 sums, softmax running per row)
 // Few rows are bound by the stream of pages: extend_few_kernel, whose four waves stream stages of their own (every fourth
-// one) through rings of their own and multiply them with all of the up to 64 rows; what they have is added up in LDS.
+// one) through rings of their own and multiply them with all of the up to 32 rows; what they have is added up in LDS.
 //
 // The work is a line of items, one per (sequence, kv head, block), each as long as it has stages, and the line is cut into
 // as many spans of one length as workgroups are resident, so that ragged lengths load them alike.  Every workgroup finds its
@@ -23,14 +23,30 @@ namespace ra {
 
 constexpr int kExWaves = 4;
 constexpr int kExTileRows = kPfRows * kExWaves; // rows of a block of the tile kernel
-constexpr int kExFewRows = 64;                  // rows of a sequence and kv head up to which the other one takes them
+constexpr int kExFewRows = 32;                  // rows of a sequence and kv head up to which the other one takes them
 
 // ---- the line of items and its spans ------------------------------------------------------------------
 
 struct ExSeq {
     int t0, n, L;  // first packed token, new tokens, tokens in all
-    int blocks, cost; // blocks of a kv head; the length of each on the line (stages, the mean of the sequence's blocks)
+    int blocks, cost; // blocks of a kv head; the length of each on the line (stages, the mean of the sequence's blocks, and kFixed)
 };
+
+// What an item costs beside its stages, in stages: finding it, its query rows, the first trip to memory, its results.
+template <int ROWS> constexpr int kExFixed = ROWS == kExTileRows ? 4 : 8;
+constexpr int kExEdge = 2; // no part of an item has fewer stages than this (about; a span is longer than kExFixed + 2 kExEdge)
+
+__device__ __forceinline__ int ex_uni(int x) { return __builtin_amdgcn_readfirstlane(x); } // (a quotient comes from the vector unit)
+// x / y for 0 <= x < 2^30, y > 0, both the wave's: the quotient by the reciprocal in binary32 is off by x / y 2^-22 at most, the
+// remainder's by less than one, and a last comparison settles that.  (A quarter of the instructions of the compiler's.)
+__device__ __forceinline__ int ex_div(int x, int y)
+{
+    const float inv = __builtin_amdgcn_rcpf((float)y);
+    int q = (int)((float)x * inv);
+    q += (int)((float)(x - q * y) * inv);
+    const int r = x - q * y;
+    return ex_uni(q + (r >= y) - (r < 0));
+}
 
 __device__ __forceinline__ int ex_div_g(const ExtendLaunch &a, int r) { return pf_div(r, a.G, a.magic_g); }
 
@@ -53,160 +69,185 @@ template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLau
     s.L = L < 0 ? 0 : (L < most ? L : most);
     s.blocks = (s.n * a.G + ROWS - 1) / ROWS;
     const int first = ex_stages<ROWS>(a, s, 0), last = ex_stages<ROWS>(a, s, s.blocks - 1);
-    s.cost = ((first > 0 ? first : 0) + (last > 0 ? last : 0) + 1) >> 1;
-    s.cost = s.cost < 1 ? 1 : s.cost;
+    s.cost = kExFixed<ROWS> + 1 + (((first > 0 ? first : 0) + (last > 0 ? last : 0)) >> 1);
     return s;
 }
 
+
 // The line: lane c has chunk c of the sequences (64 of them, or a multiple of that in a very large batch).
 template <int ROWS> struct ExLine {
-    int lane, sub, before, total; // sub: sixty-fours of sequences in a chunk; before: start of this lane's chunk
-    int q, r, spans, cut;         // span k starts at q k + min(k, r), before cuts are moved; items up to `cut` are not cut
+    int lane, sub, chunks; // sixty-fours of sequences in a chunk
+    int unit;              // items are left whole, each of length one
+    int before, total;     // start of this lane's chunk
+    int q, r, spans, cut;  // span k starts at q k + min(k, r), before cuts are moved; items up to `cut` are not cut
 
-    __device__ __forceinline__ void measure(const ExtendLaunch &a)
+    __device__ __forceinline__ int length(const ExtendLaunch &a, const ExSeq &s) const { return a.Hkv * s.blocks * (unit ? 1 : s.cost); }
+
+    // first: the first sixty-four sequences.
+    __device__ __forceinline__ void measure(const ExtendLaunch &a, ExSeq &first)
     {
         lane = threadIdx.x & 63;
         sub = (a.B + 4095) >> 12;
-        const int chunks = (a.B + 64 * sub - 1) / (64 * sub);
-        int mine = 0;
+        chunks = sub == 1 ? (a.B + 63) >> 6 : ex_div(a.B + 64 * sub - 1, 64 * sub);
+        first = ex_sequence<ROWS>(a, lane);
+        int cost = 0, items = 0, longest = first.cost; // this lane's chunk, lane by lane first
         for (int c = 0; c < chunks; c++) {
-            int n = 0;
+            int l = 0, n = 0;
             for (int i = 0; i < sub; i++) {
-                const ExSeq s = ex_sequence<ROWS>(a, (c * sub + i) * 64 + lane);
-                int t;
-                (void)wave_scan(a.Hkv * s.blocks * s.cost, lane, t);
-                n += t;
+                const ExSeq s = c + i ? ex_sequence<ROWS>(a, (c * sub + i) * 64 + lane) : first;
+                l += a.Hkv * s.blocks * s.cost, n += a.Hkv * s.blocks;
+                longest = longest > s.cost ? longest : s.cost;
             }
-            if (lane == c) mine = n;
+            int tl, tn;
+            (void)wave_scan(l, lane, tl), (void)wave_scan(n, lane, tn);
+            if (lane == c) cost = tl, items = tn;
         }
-        before = wave_scan(mine, lane, total);
-        spans = total / a.least;
-        spans = spans < 1 ? 1 : (spans < a.spans ? spans : a.spans);
-        q = total / spans;
+        int all_cost, all_items;
+        const int before_cost = wave_scan(cost, lane, all_cost), before_items = wave_scan(items, lane, all_items);
+        // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each, in
+        // order, so that blocks that read the same keys run side by side.
+        const int mean = ex_div(all_cost, a.spans);
+        unit = all_items >= 2 * a.spans && !__any(longest > mean);
+        before = unit ? before_items : before_cost;
+        total = unit ? all_items : all_cost;
+        const int most = ex_div(all_cost, a.least);
+        spans = unit ? all_items : most < 1 ? 1 : (most < a.spans ? most : a.spans);
+        q = unit ? 1 : ex_div(total, spans);
         r = total - q * spans;
         cut = q >> 3 > a.least ? q >> 3 : a.least;
     }
     __device__ __forceinline__ int raw(int k) const { return q * k + (k < r ? k : r); }
-    // The last span that starts before x (x > 0).
-    __device__ __forceinline__ int span_before(int x) const
+    // The last span that an item which ends at x1 has a part in, if it is cut.
+    __device__ __forceinline__ int last_of(int x1) const
     {
-        const int y = x - 1, big = r * (q + 1);
-        return y < big ? y / (q + 1) : r + (y - big) / q;
+        const int y = x1 - 1, big = r * (q + 1);
+        const int k = y < big ? ex_div(y, q + 1) : r + ex_div(y - big, q); // the last one that starts before x1
+        return x1 - raw(k) < kExEdge ? k - 1 : k;                          // (but for a cut that moves there)
     }
 };
 
-// A place on the line: an item, and how far into it.
+// A place on the line: an item of a sequence.
 struct ExPlace {
     int b, item, x0; // the sequence, its item (kv head * blocks + number), the item's start
-    ExSeq s;
-    int next;        // the next sequence of the same sixty-four that has items, or -1
+    ExSeq s;         // (cost: the item's length on the line)
 };
 
-// The item that x lies in (0 <= x < total).
-template <int ROWS> __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<ROWS> &line, int x, ExPlace &p)
+// Where x lies among the sixty-four sequences from `base` on, whose items start at `start`.
+template <int ROWS> __device__ __forceinline__ void ex_pick(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExSeq &s, int base, int before, int x, ExPlace &p)
 {
-    const unsigned long long m = __ballot(line.before <= x);
-    int c = 63 - __builtin_clzll(m);
-    const int chunks = (a.B + 64 * line.sub - 1) / (64 * line.sub);
-    c = c < chunks ? c : chunks - 1;
+    const int l = 63 - __builtin_clzll(__ballot(s.blocks > 0 && before <= x));
+    p.b = base + l;
+    p.s.t0 = __builtin_amdgcn_readlane(s.t0, l), p.s.n = __builtin_amdgcn_readlane(s.n, l), p.s.L = __builtin_amdgcn_readlane(s.L, l);
+    p.s.blocks = __builtin_amdgcn_readlane(s.blocks, l), p.s.cost = line.unit ? 1 : __builtin_amdgcn_readlane(s.cost, l);
+    const int at = __builtin_amdgcn_readlane(before, l);
+    p.item = ex_div(x - at, p.s.cost);
+    p.x0 = at + p.item * p.s.cost;
+}
+
+// The item that x lies in (0 <= x < total).
+template <int ROWS> __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExSeq *first, int x, ExPlace &p)
+{
+    int t;
+    if (first && line.chunks == 1 && line.sub == 1) {
+        const int before = wave_scan(line.length(a, *first), line.lane, t);
+        ex_pick<ROWS>(a, line, *first, 0, before, x, p);
+        return;
+    }
+    int c = 63 - __builtin_clzll(__ballot(line.before <= x));
+    c = c < line.chunks ? c : line.chunks - 1;
     int start = __builtin_amdgcn_readlane(line.before, c);
     for (int i = 0; i < line.sub; i++) {
         const int base = (c * line.sub + i) * 64;
         const ExSeq s = ex_sequence<ROWS>(a, base + line.lane);
-        const int own = a.Hkv * s.blocks * s.cost;
-        int t;
-        const int before = start + wave_scan(own, line.lane, t);
+        const int before = start + wave_scan(line.length(a, s), line.lane, t);
         if (x >= start + t && i + 1 < line.sub) {
             start += t;
             continue;
         }
-        const int l = 63 - __builtin_clzll(__ballot(own > 0 && before <= x));
-        p.b = base + l;
-        p.s.t0 = __builtin_amdgcn_readlane(s.t0, l), p.s.n = __builtin_amdgcn_readlane(s.n, l), p.s.L = __builtin_amdgcn_readlane(s.L, l);
-        p.s.blocks = __builtin_amdgcn_readlane(s.blocks, l), p.s.cost = __builtin_amdgcn_readlane(s.cost, l);
-        const int at = __builtin_amdgcn_readlane(before, l);
-        p.item = (x - at) / p.s.cost;
-        p.x0 = at + p.item * p.s.cost;
+        ex_pick<ROWS>(a, line, s, base, before, x, p);
         return;
     }
 }
 
-// Where span k starts once short items are left whole.
-template <int ROWS> __device__ __forceinline__ int ex_start(const ExtendLaunch &a, const ExLine<ROWS> &line, int k, ExPlace &p)
+// Where span k starts once short items are left whole, and no part of an item is next to nothing.
+template <int ROWS> __device__ __forceinline__ int ex_start(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExSeq *first, int k, ExPlace &p)
 {
     if (k >= line.spans) return line.total;
     const int x = line.raw(k);
-    ex_find<ROWS>(a, line, x, p);
-    if (p.s.cost > line.cut || x == p.x0) return x;
-    return 2 * (x - p.x0) < p.s.cost ? p.x0 : p.x0 + p.s.cost;
-}
-
-// The workgroup's span: workgroups are dealt to the eight dies round-robin, and a die gets neighbouring spans, so that blocks
-// that read the same keys find them in its L2.
-__device__ __forceinline__ int ex_span_of(int spans)
-{
-    const int per = (spans + 7) >> 3, at = (int)blockIdx.x >> 3;
-    return at < per ? ((int)blockIdx.x & 7) * per + at : spans;
+    ex_find<ROWS>(a, line, first, x, p);
+    const int y = x - p.x0;
+    if (p.s.cost > line.cut) return y < kExFixed<ROWS> + kExEdge ? p.x0 : p.s.cost - y < kExEdge ? p.x0 + p.s.cost : x;
+    return 2 * y < p.s.cost ? p.x0 : p.x0 + p.s.cost;
 }
 
 // A part of an item that a workgroup works on.
 struct ExPart {
     int kvh, row0, rows; // rows of the sequence and kv head in all
     int lo, hi;          // stages
-    int64_t slot;        // -1: the item is whole; else where its part goes
+    int slot;            // -1: the item is whole; else where its part goes
 };
 
 // The blocks of a (sequence, kv head) come from both ends in turn: their mean cost is the line's.
 template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch &a, const ExPlace &p, int y0, int y1, int span)
 {
     ExPart t;
-    t.kvh = p.item / p.s.blocks;
+    t.kvh = ex_div(p.item, p.s.blocks);
     const int jj = p.item - t.kvh * p.s.blocks, j = jj & 1 ? p.s.blocks - 1 - (jj >> 1) : jj >> 1;
     t.row0 = ROWS * j;
     t.rows = p.s.n * a.G;
-    int stages = ex_stages<ROWS>(a, p.s, j);
+    int stages = ex_uni(ex_stages<ROWS>(a, p.s, j));
     stages = stages < 0 ? 0 : stages;
-    t.lo = y0 == 0 ? 0 : (int)((int64_t)stages * y0 / p.s.cost);
-    t.hi = y1 == p.s.cost ? stages : (int)((int64_t)stages * y1 / p.s.cost);
-    t.slot = y0 == 0 ? (y1 == p.s.cost ? -1 : 2 * (int64_t)span + 1) : 2 * (int64_t)span;
+    // (a place inside the item, in proportion: the same for the two parts that it divides)
+    auto stage_at = [&](int y) __attribute__((always_inline)) {
+        return ex_uni((int)((float)stages * ((float)(y - kExFixed<ROWS>) / (float)(p.s.cost - kExFixed<ROWS>))));
+    };
+    t.lo = y0 == 0 ? 0 : stage_at(y0);
+    t.hi = y1 == p.s.cost ? stages : stage_at(y1);
+    t.slot = y0 == 0 ? (y1 == p.s.cost ? -1 : 2 * span + 1) : 2 * span;
     return t;
 }
 
-// Goes through the parts of the workgroup's span; `work` is called with each.  Also tells the merge which items begin here and
-// end elsewhere: desc[2 k], desc[2 k + 1] = {first packed token, first row, rows, kv head}, {last span, -, -, -}.
+// Goes through the parts of the workgroup's span; `work` is called with each.  Workgroups are dealt to the eight dies
+// round-robin, and a die gets neighbouring spans, so that blocks that read the same keys find them in its L2.
+// Also tells the merge which items begin here and end elsewhere: desc[2 k], desc[2 k + 1] = {first packed token, first row,
+// rows, kv head}, {last span, -, -, -}.
 template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, F &&work)
 {
     ExLine<ROWS> line;
-    line.measure(a);
-    int span = -1, last = 0;
-    ExPlace p;
+    ExSeq first;
+    line.measure(a, first);
+    const int per = (line.spans + 7) >> 3, at = (int)blockIdx.x >> 3;
+    const int k = at < per ? ((int)blockIdx.x & 7) * per + at : (int)blockIdx.x; // (past the spans: one that does not exist)
+    int last = 0;
     int4 begun = {0, 0, 0, 0};
-    const int k = ex_span_of(line.spans);
-    if (line.total > 0 && k < line.spans) {
-        span = k;
-        ExPlace e;
-        const int end = ex_start<ROWS>(a, line, k + 1, e);
-        int x = ex_start<ROWS>(a, line, k, p);
-        if (x < end && x >= p.x0 + p.s.cost) ex_find<ROWS>(a, line, x, p);
+    if (line.total > 0 && at < per && k < line.spans) {
+        ExPlace p;
+        int x, end;
+        if (line.unit) {
+            ex_find<ROWS>(a, line, &first, k, p);
+            x = k, end = k + 1;
+        } else {
+            end = ex_start<ROWS>(a, line, &first, k + 1, p);
+            x = ex_start<ROWS>(a, line, &first, k, p);
+            if (x < end && x >= p.x0 + p.s.cost) ex_find<ROWS>(a, line, &first, x, p);
+        }
         while (x < end) {
             const int x1 = p.x0 + p.s.cost, stop = x1 < end ? x1 : end;
-            const ExPart part = ex_part<ROWS>(a, p, x - p.x0, stop - p.x0, span);
+            const ExPart part = ex_part<ROWS>(a, p, x - p.x0, stop - p.x0, k);
             if (x == p.x0 && stop < x1) {
                 begun = make_int4(p.s.t0, part.row0, part.rows, part.kvh);
-                last = line.span_before(x1);
+                last = line.last_of(x1);
             }
             work(p, part);
             x = stop;
             if (x >= end) break;
             if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x1;
-            else ex_find<ROWS>(a, line, x, p);
+            else ex_find<ROWS>(a, line, nullptr, x, p);
         }
     }
-    // (every workgroup answers for one span, also for one that does not exist)
-    const int per = (line.spans + 7) >> 3, at = (int)blockIdx.x >> 3, answers = at < per ? ((int)blockIdx.x & 7) * per + at : (int)blockIdx.x;
-    if (threadIdx.x == 0) {
-        a.desc[2 * answers] = begun;
-        a.desc[2 * answers + 1] = make_int4(last, 0, 0, 0);
+    if (threadIdx.x == 0 && k < a.spans) { // (every span is answered for, also one that does not exist)
+        a.desc[2 * k] = begun;
+        a.desc[2 * k + 1] = make_int4(last, 0, 0, 0);
     }
 }
 
@@ -397,28 +438,33 @@ __device__ __forceinline__ void ex_step(PfState<D> &st, uint32_t k_next, uint32_
 #undef EX_FENCE
 }
 
-constexpr int kExSlots = 4; // ring slots of one stage each
-
-template <int D> struct ExTileLds {
-    static constexpr int kStage = kExSlots * Geo<D, 2>::kStage; // the waves' staging areas follow the ring
-    static constexpr int kBytes = kStage + kPfStageBytes * kExWaves;
+// The LDS of a workgroup: a ring of stages in bf16, and for each wave an area of its own, where e4m3 tiles land as they are
+// stored (a ring of its own loads) and results are put in order on their way out.
+template <int D, bool FP8> struct ExTileLds {
+    static constexpr int kSlots = FP8 ? 3 : 4, kRaw = 3;
+    static constexpr int kRawSlot = Geo<D, 1>::kTile + 256; // a tile, and the stage's scales
+    static constexpr int kArea = FP8 && kRaw * kRawSlot > kPfStageBytes ? kRaw * kRawSlot : kPfStageBytes;
+    static constexpr int kAreas = kSlots * Geo<D, 2>::kStage; // the areas follow the ring
+    static constexpr int kBytes = kAreas + kArea * kExWaves;
 };
 
 template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_tile_kernel(ExtendLaunch a)
 {
     using G = Geo<D, 2>;
-    using X = ExTileLds<D>;
-    constexpr int NSL = kExSlots, DPW = G::kDmaPerTile;
+    using P = Geo<D, FP8 ? 1 : 2>; // as the pools have it
+    using X = ExTileLds<D, FP8>;
     extern __shared__ __attribute__((aligned(16384))) uint8_t lds[]; // the step forms LDS addresses by XOR
     const uint32_t lds_addr = (uint32_t)(uintptr_t)lds;
     const int lane = threadIdx.x & 63, n = lane & 31, hh = lane >> 5;
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    LaneConst<D, 2> lc;
-    if (!FP8) lane_setup<D, 2>(lc, lane, a.stride_token_b);
+    const int wave = ex_uni((int)threadIdx.x >> 6);
+    LaneConst<D, FP8 ? 1 : 2> lc;
+    lane_setup<D, FP8 ? 1 : 2>(lc, lane, a.stride_token_b);
     PfLane<D> pl;
     pf_lane_setup<D>(pl, lane);
-    uint8_t *const staging = lds + X::kStage + kPfStageBytes * wave;
-    int done = 0; // stages of the parts before this one: stage s of it lives in ring slot (done + s) % NSL
+    uint8_t *const area = lds + X::kAreas + X::kArea * wave;
+    const uint32_t area_addr = lds_addr + X::kAreas + X::kArea * wave;
+    auto after = [](int slot) __attribute__((always_inline)) { return slot + 1 == X::kSlots ? 0 : slot + 1; };
+    int slot0 = 0; // ring slot of the part's first stage; the others follow
 
     ex_walk<kExTileRows>(a, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
         const int nst = t.hi - t.lo, row = t.row0 + kPfRows * wave + n; // this lane's row
@@ -427,8 +473,8 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
         const int shift = p.s.L - p.s.n, lim = shift + token;
         // the wave's first and last row: stages below `whole` are seen by all of its rows, those from `mine` on by none
         const int row_lo = t.row0 + kPfRows * wave, row_hi = row_lo + kPfRows < t.rows ? row_lo + kPfRows - 1 : t.rows - 1;
-        const int whole = row_lo < t.rows ? (shift + ex_div_g(a, row_lo) + 1) >> 5 : 0;
-        int mine = row_lo < t.rows ? (shift + ex_div_g(a, row_hi) + 32) >> 5 : 0;
+        const int whole = row_lo < t.rows ? ex_uni((shift + ex_div_g(a, row_lo) + 1) >> 5) : 0;
+        int mine = row_lo < t.rows ? ex_uni((shift + ex_div_g(a, row_hi) + 32) >> 5) : 0;
         mine = (mine < t.hi ? mine : t.hi) - t.lo; // of the part's stages
 
         // Wave w brings tile w of every stage (K of its two pages, V of its two pages).
@@ -436,74 +482,75 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
         const int count = (p.s.L + kPage - 1) / kPage; // pages that exist
         const int of = wave & 1; // the wave's page of a stage's two
         const uint8_t *const pool = (wave < 2 ? a.k_pool : a.v_pool) + (int64_t)t.kvh * a.stride_head_b;
+        // (An id is asked for a stage ahead of its use, and looked at only there: until then the load may be on its way.  A page
+        // that does not exist takes another's place in the row, or the first, and none of its rows are read.)
+        const int last_page = count > 0 ? count - 1 : 0;
         auto page_id = [&](int s, int h) __attribute__((always_inline)) { // of page h of stage s of the part
             const int i = 2 * (t.lo + s) + h;
-            const int id = s < nst && i < count ? uniform_load(pages, i) : -1;
-            return id < a.num_pages ? id : -1;
+            return uniform_load(pages, i < last_page ? i : last_page);
         };
-        int issued = 0, id = page_id(0, of), other = FP8 ? page_id(0, 1 - of) : 0;
-        auto issue = [&]() __attribute__((always_inline)) { // bf16 pools: the next stage's tile
-            if (issued < nst) {
-                const int valid = id < 0 ? 0 : p.s.L - kPage * (2 * (t.lo + issued) + of);
-                issue_tile<D, 2>(lc, pool + (int64_t)(id < 0 ? 0 : id) * a.stride_page_b, valid, lds_addr + ((done + issued) & (NSL - 1)) * G::kStage + wave * G::kTile, a.zeros);
-                issued++;
-                id = page_id(issued, of);
-            }
-        };
-        // e4m3 pools: a tile goes through registers, and its codes into the ring as bf16
-        constexpr int NB = D / 64; // 16-byte pieces of a tile that a lane has
-        uint4 raw[NB];
-        float scales_next = 1.f; // lanes 0..3: K and V scale of the first page, of the second
-        auto fetch = [&]() __attribute__((always_inline)) {
-            const int i0 = 2 * (t.lo + issued);
-            const int valid = id < 0 ? 0 : p.s.L - kPage * (i0 + of);
-            const uint8_t *const tile = pool + (int64_t)(id < 0 ? 0 : id) * a.stride_page_b;
-#pragma unroll
-            for (int x = 0; x < NB; x++) {
-                const int u = 64 * x + lane, r = u / (D / 16), c = u % (D / 16);
-                raw[x] = make_uint4(0, 0, 0, 0);
-                if (issued < nst && r < valid) raw[x] = *(const uint4 *)(tile + (int64_t)r * a.stride_token_b + 16 * c);
-            }
-            scales_next = 1.f;
-            const int pid = ((lane >> 1) & 1) == of ? id : other;
-            if (lane < 4 && pid >= 0) {
-                scales_next = ((lane & 1) ? a.v_scale : a.k_scale)[(int64_t)pid * a.Hkv + t.kvh];
+        int issued = 0, id = 0, other = 0;
+        if (count > 0) {
+            id = page_id(0, of);
+            if (FP8) other = page_id(0, 1 - of);
+        }
+        int load_slot = FP8 ? 0 : slot0; // where the next tile goes (e4m3: in the wave's own ring)
+        constexpr int DPW = P::kDmaPerTile + (FP8 ? 1 : 0); // a wave's loads per stage
+        auto issue = [&]() __attribute__((always_inline)) { // the next stage's tile
+            if (issued >= nst) return;
+            const int valid = p.s.L - kPage * (2 * (t.lo + issued) + of);
+            const uint32_t to = FP8 ? area_addr + load_slot * X::kRawSlot : lds_addr + load_slot * G::kStage + wave * G::kTile;
+            issue_tile<D, FP8 ? 1 : 2>(lc, pool + (int64_t)id * a.stride_page_b, valid, to, a.zeros);
+            if (FP8) { // lanes 0..3 bring K and V scale of the first page, K and V scale of the second
+                const int h = (lane >> 1) & 1, pid = h == of ? id : other;
+                const void *src = a.zeros;
+                if (lane < 4 && (h == of ? valid : p.s.L - kPage * (2 * (t.lo + issued) + 1 - of)) > 0)
+                    src = ((lane & 1) ? a.v_scale : a.k_scale) + (int64_t)pid * a.Hkv + t.kvh;
+                dma4(src, to + P::kTile);
             }
             issued++;
-            id = page_id(issued, of), other = page_id(issued, 1 - of);
+            load_slot = FP8 ? (load_slot + 1 == X::kRaw ? 0 : load_slot + 1) : after(load_slot);
+            id = page_id(issued, of);
+            if (FP8) other = page_id(issued, 1 - of);
         };
-        auto put = [&](int s) __attribute__((always_inline)) { // what was fetched, as stage s
-            uint8_t *const tile = lds + ((done + s) & (NSL - 1)) * G::kStage + wave * G::kTile;
+        ExScale sc = {a.scale_log2, a.scale_log2, 1.f, 1.f}, sc_next = sc, sc_put = sc;
+        int raw_slot = 0, put_slot = slot0;
+        // e4m3 pools: the wave's tile of stage s, once landed, goes into the ring as bf16 (exactly; its scales stay apart)
+        auto put = [&](int s) __attribute__((always_inline)) {
+            WaitTail<X::kRaw - 1, DPW>::run(issued - 1 - s);
+            asm volatile("" ::: "memory");
+            const uint8_t *const from = area + raw_slot * X::kRawSlot;
+            uint8_t *const tile = lds + put_slot * G::kStage + wave * G::kTile;
+            const f32x4 w = *(const f32x4 *)(from + P::kTile);
+            uint4 raw[P::kDmaPerTile];
 #pragma unroll
-            for (int x = 0; x < NB; x++) {
-                const int u = 64 * x + lane, r = u / (D / 16), c = u % (D / 16), z = swz(r) & (G::kUnits - 1);
+            for (int x = 0; x < P::kDmaPerTile; x++) raw[x] = *(const uint4 *)(from + 1024 * x + 16 * lane);
+#pragma unroll
+            for (int x = 0; x < P::kDmaPerTile; x++) {
+                const int u = 64 * x + lane, r = u / P::kUnits, c = (u % P::kUnits) ^ (swz(r) & (P::kUnits - 1)), z = swz(r) & (G::kUnits - 1);
                 *(bf16x8 *)(tile + 16 * (r * G::kUnits + ((2 * c) ^ z))) = fp8x8_to_bf16((int)raw[x].x, (int)raw[x].y);
                 *(bf16x8 *)(tile + 16 * (r * G::kUnits + ((2 * c + 1) ^ z))) = fp8x8_to_bf16((int)raw[x].z, (int)raw[x].w);
             }
-        };
-        ExScale sc = {a.scale_log2, a.scale_log2, 1.f, 1.f}, sc_next = sc, sc_put = sc;
-        auto scales_of = [&](float x) __attribute__((always_inline)) {
-            x = x == 0.f ? 1e-30f : x; // (zero times the mask's -inf would be NaN)
-            auto lane_of = [&](int l) __attribute__((always_inline)) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(x), l)); };
-            return ExScale{lane_of(0) * a.scale_log2, lane_of(2) * a.scale_log2, lane_of(1), lane_of(3)};
+            auto scale = [&](float f, bool k) __attribute__((always_inline)) {
+                const int bits = ex_uni(__float_as_int(f));
+                return __int_as_float(k && (bits & 0x7fffffff) == 0 ? 0x0da24260 : bits); // (1e-30: zero times the mask's -inf would be NaN)
+            };
+            sc_put = {scale(w[0], true) * a.scale_log2, scale(w[2], true) * a.scale_log2, scale(w[1], false), scale(w[3], false)};
+            raw_slot = raw_slot + 1 == X::kRaw ? 0 : raw_slot + 1;
+            put_slot = after(put_slot);
         };
         // Before the first step that reads stage s: it has landed, for every wave, and every wave has left the step that read
-        // stage s - 2, whose slot the next load takes.
+        // stage s - 2, whose slot the next load (e4m3: stage s + 1) may take.
         auto open = [&](int s) __attribute__((always_inline)) {
-            if (!FP8) WaitTail<NSL - 1, DPW>::run(issued - 1 - s);
+            if (!FP8) WaitTail<X::kSlots - 1, DPW>::run(issued - 1 - s);
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_s_barrier();
             asm volatile("" ::: "memory");
             if (FP8) {
                 sc = sc_next, sc_next = sc_put;
-                if (s + 1 < nst) {
-                    put(s + 1);
-                    sc_put = scales_of(scales_next);
-                    fetch();
-                }
-            } else {
-                issue();
+                if (s + 1 < nst) put(s + 1);
             }
+            issue();
         };
 
         PfState<D> st;
@@ -512,14 +559,12 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
 #pragma unroll
             for (int i = 0; i < D / 16; i++) st.qf[i] = *(const bf16x8 *)(q + 16 * i);
         }
+        // (the barriers of the part before have passed the slots that are filled now)
+        issue();
+        issue();
         if (FP8) {
-            fetch();
-            put(0); // (the barriers of the part before have passed its slot)
-            sc_put = scales_of(scales_next);
-            fetch();
-        } else {
             issue();
-            issue();
+            if (nst > 0) put(0);
         }
         st.m = kPfLowest, st.lsum = 0.f;
 #pragma unroll
@@ -532,7 +577,7 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
             open(0);
             if (FP8) sc = sc_next; // (stage 0; sc_next: stage 1 once that has been opened)
             if (mine > 0) {
-                pf_scores<D>(lds_addr + (done & (NSL - 1)) * G::kStage, pl, st.qf, st.s);
+                pf_scores<D>(lds_addr + slot0 * G::kStage, pl, st.qf, st.s);
                 if (t.lo >= whole) {
 #pragma unroll
                     for (int e = 0; e < 16; e++) {
@@ -546,8 +591,11 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
                 const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mx), __float_as_uint(mx), false, false);
                 st.m = fmaxf(max3(__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[1])), kPfLowest);
             }
-            auto at = [&](int s) __attribute__((always_inline)) { return lds_addr + ((done + s) & (NSL - 1)) * G::kStage; };
-#define EX_STEP(MASK, NEXT) ex_step<D, FP8, MASK, NEXT>(st, at(s + 1), at(s) + 2 * G::kTile, pl, sc, sc_next, 32 * (t.lo + s), 32 * (t.lo + s + 1), lim)
+            int cur = slot0, nxt = after(slot0); // of stages s and s + 1
+#define EX_STEP(MASK, NEXT)                                                                                                          \
+    ex_step<D, FP8, MASK, NEXT>(st, lds_addr + nxt * G::kStage, lds_addr + cur * G::kStage + 2 * G::kTile, pl, sc, sc_next, 32 * (t.lo + s), \
+                                32 * (t.lo + s + 1), lim);                                                                            \
+    cur = nxt, nxt = after(nxt)
             int s = 0;
             auto advance = [&]() __attribute__((always_inline)) {
                 if (s + 1 < nst) open(s + 1);
@@ -571,8 +619,8 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
             }
             for (; s < nst; s++) advance();
 #undef EX_STEP
+            slot0 = ex_uni((slot0 + nst) % X::kSlots);
         }
-        done = (done + nst) & (NSL - 1);
 
         // a row's sum is spread over its two lanes
         float l;
@@ -583,14 +631,14 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
         if (row_lo >= t.rows) return;
         if (t.slot >= 0) {
             // a part: as the accumulators lie, which is whole lines
-            float *const o = a.part_o + t.slot * (kExTileRows * D) + wave * (kPfRows * D) + 4 * lane;
+            float *const o = a.part_o + (int64_t)t.slot * (kExTileRows * D) + wave * (kPfRows * D) + 4 * lane;
 #pragma unroll
             for (int dt = 0; dt < D / 32; dt++) {
 #pragma unroll
                 for (int j = 0; j < 4; j++)
-                    *(f32x4 *)(o + 256 * (4 * dt + j)) = f32x4{st.o[dt][4 * j], st.o[dt][4 * j + 1], st.o[dt][4 * j + 2], st.o[dt][4 * j + 3]};
+                    if (exists) *(f32x4 *)(o + 256 * (4 * dt + j)) = f32x4{st.o[dt][4 * j], st.o[dt][4 * j + 1], st.o[dt][4 * j + 2], st.o[dt][4 * j + 3]};
             }
-            if (hh == 0) *(float2 *)(a.part_lse + 2 * (t.slot * kExTileRows + kPfRows * wave + n)) = make_float2(st.m, l);
+            if (exists && hh == 0) *(float2 *)(a.part_lse + 2 * ((int64_t)t.slot * kExTileRows + kPfRows * wave + n)) = make_float2(st.m, l);
             return;
         }
         const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l; // (no key: zeros; NaN stays)
@@ -603,13 +651,13 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
                     f32x4 v;
 #pragma unroll
                     for (int x = 0; x < 4; x++) v[x] = st.o[2 * pc + dtl][4 * j + x] * inv;
-                    *(bf16x4 *)(staging + kPfStageRow * n + 16 * ((4 * dtl + j) ^ pf_stage_swz(n)) + 8 * hh) = __builtin_convertvector(v, bf16x4);
+                    *(bf16x4 *)(area + kPfStageRow * n + 16 * ((4 * dtl + j) ^ pf_stage_swz(n)) + 8 * hh) = __builtin_convertvector(v, bf16x4);
                 }
             }
 #pragma unroll
             for (int m = 0; m < 4; m++) {
                 const int r = 8 * m + (lane >> 3), c = lane & 7, orow = row_lo + r;
-                const u32x4 v = *(const u32x4 *)(staging + kPfStageRow * r + 16 * (c ^ pf_stage_swz(r)));
+                const u32x4 v = *(const u32x4 *)(area + kPfStageRow * r + 16 * (c ^ pf_stage_swz(r)));
                 if (orow < t.rows) {
                     const int i = ex_div_g(a, orow);
                     *(u32x4 *)(a.out + ((int64_t)(p.s.t0 + i) * a.Hq + t.kvh * a.G + (orow - i * a.G)) * D + 64 * pc + 8 * c) = v;
@@ -654,17 +702,17 @@ template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1
         const int32_t *const pages = a.table + (int64_t)p.b * a.max_pages;
         const int count = (p.s.L + kPage - 1) / kPage;
         const int64_t head_b = (int64_t)t.kvh * a.stride_head_b;
+        const int last_page = count > 0 ? count - 1 : 0; // (a page that does not exist takes its place, and none of its rows are read)
         auto page_id = [&](int i, int h) __attribute__((always_inline)) {
             const int g = 2 * (t.lo + wave + W * i) + h;
-            const int id = i < mine && g < count ? uniform_load(pages, g) : -1;
-            return id < a.num_pages ? id : -1;
+            return uniform_load(pages, g < last_page ? g : last_page);
         };
-        int issued = 0, id0 = page_id(0, 0), id1 = page_id(0, 1);
+        int issued = 0, id0 = 0, id1 = 0;
+        if (mine > 0) id0 = page_id(0, 0), id1 = page_id(0, 1);
         auto issue = [&]() __attribute__((always_inline)) {
             if (issued >= mine) return;
-            const int nv = p.s.L - 2 * kPage * (t.lo + wave + W * issued);
-            const int nv0 = id0 < 0 ? 0 : nv, nv1 = id1 < 0 ? 0 : nv - kPage;
-            const int64_t off0 = (int64_t)(id0 < 0 ? 0 : id0) * a.stride_page_b + head_b, off1 = (int64_t)(id1 < 0 ? 0 : id1) * a.stride_page_b + head_b;
+            const int nv0 = p.s.L - 2 * kPage * (t.lo + wave + W * issued), nv1 = nv0 - kPage;
+            const int64_t off0 = (int64_t)id0 * a.stride_page_b + head_b, off1 = (int64_t)id1 * a.stride_page_b + head_b;
             const uint32_t sb = ring_addr + (issued % NST) * G::kStage;
             issue_tile<D, KVB, true>(lc, a.k_pool + off0, nv0, sb, a.zeros);
             issue_tile<D, KVB, true>(lc, a.k_pool + off1, nv1, sb + G::kTile, a.zeros);
@@ -673,7 +721,7 @@ template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1
             if (KVB == 1) { // the pages' scales land behind the tiles: lanes 0..3 bring k0, v0, k1, v1
                 const int pid = (lane & 2) ? id1 : id0;
                 const void *src = a.zeros;
-                if (lane < 4 && pid >= 0) src = ((lane & 1) ? a.v_scale : a.k_scale) + (int64_t)pid * a.Hkv + t.kvh;
+                if (lane < 4 && ((lane & 2) ? nv1 : nv0) > 0) src = ((lane & 1) ? a.v_scale : a.k_scale) + (int64_t)pid * a.Hkv + t.kvh;
                 dma4(src, sb + 4 * G::kTile);
             }
             issued++;
@@ -845,8 +893,8 @@ template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1
                 acc += f * *(const f32x4 *)((const float *)(lds + w * X::kRing) + r * D + 4 * (c ^ (r & 15)));
             }
             if (t.slot >= 0) {
-                *(f32x4 *)(a.part_o + (t.slot * kExFewRows + r) * D + 4 * c) = acc;
-                if (c == 0) *(float2 *)(a.part_lse + 2 * (t.slot * kExFewRows + r)) = make_float2(mm, l);
+                *(f32x4 *)(a.part_o + ((int64_t)t.slot * kExFewRows + r) * D + 4 * c) = acc;
+                if (c == 0) *(float2 *)(a.part_lse + 2 * ((int64_t)t.slot * kExFewRows + r)) = make_float2(mm, l);
             } else {
                 const int token = ex_div_g(a, r);
                 const int64_t rh = (int64_t)(p.s.t0 + token) * a.Hq + t.kvh * a.G + (r - token * a.G);
@@ -862,37 +910,58 @@ template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1
 
 // ---- what spans share -----------------------------------------------------------------------------------
 
-constexpr int kExMergeWgs = 1024, kExMaxSpans = 2048;
+constexpr int kExMergeWgs = 1024, kExMaxSpans = 1024;
+constexpr int kExMergeFew = 12; // parts of an item that one wave adds up
 
-// Adds up the parts of the items that a cut goes through: a workgroup takes 256 consecutive values of an item at a time, its
-// waves every fourth part each.  ROWS: those of the kernel that left them, with its layout.
+// Adds up the parts of the items that a cut goes through, 256 consecutive values of an item's parts at a time: a wave alone
+// where every item has few parts, else a workgroup's waves every fourth part each.  ROWS: those of the kernel that left them,
+// with its layout.
 template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(ExtendLaunch a)
 {
-    constexpr int W = kExWaves, CHUNKS = ROWS * D / 256;
+    constexpr int W = kExWaves, CHUNKS = ROWS * D / 256, N = kExMaxSpans / (64 * W);
     __shared__ int list[kExMaxSpans];
-    __shared__ int counts[W];
+    __shared__ int counts[W][N], longest[W];
     __shared__ f32x4 sums[W][64];
     __shared__ float2 stats[W][64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = ex_uni((int)threadIdx.x >> 6);
     // the spans in which such an item begins, in order
-    int items = 0;
-    for (int base = 0; base < a.spans; base += 64 * W) {
-        const int k = base + (int)threadIdx.x;
-        const bool is = k < a.spans && a.desc[2 * k + 1].x > k;
-        const unsigned long long m = __ballot(is);
-        if (lane == 0) counts[wave] = __popcll(m);
-        __syncthreads();
+    int ends[N], most = 0, items = 0;
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const int k = 64 * W * i + (int)threadIdx.x;
+        ends[i] = k < a.spans ? a.desc[2 * k + 1].x : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const int k = 64 * W * i + (int)threadIdx.x;
+        most = most > ends[i] - k ? most : ends[i] - k;
+        const int n = __popcll(__ballot(ends[i] > k));
+        if (lane == 0) counts[wave][i] = n;
+    }
+    const bool long_ones = __any(most >= kExMergeFew);
+    if (lane == 0) longest[wave] = long_ones;
+    __syncthreads();
+    bool split = false;
+#pragma unroll
+    for (int w = 0; w < W; w++) split = split || longest[w];
+#pragma unroll
+    for (int i = 0; i < N; i++) {
+        const int k = 64 * W * i + (int)threadIdx.x;
         int at = items;
 #pragma unroll
         for (int w = 0; w < W; w++) {
-            if (w < wave) at += counts[w];
-            items += counts[w];
+            if (w < wave) at += counts[w][i];
+            items += counts[w][i];
         }
-        if (is) list[at + __popcll(m & ((1ull << lane) - 1ull))] = k;
-        __syncthreads();
+        const unsigned long long m = __ballot(ends[i] > k);
+        if (ends[i] > k) list[at + __popcll(m & ((1ull << lane) - 1ull))] = k;
     }
-    for (int u = blockIdx.x; u < items * CHUNKS; u += gridDim.x) {
-        const int k = list[u / CHUNKS], chunk = u % CHUNKS;
+    __syncthreads();
+    const int each = split ? 1 : W; // units of work that a workgroup takes at a time
+    for (int u0 = blockIdx.x * each; u0 < items * CHUNKS; u0 += gridDim.x * each) {
+        const int u = split ? u0 : u0 + wave, chunk = u % CHUNKS;
+        const bool have = u < items * CHUNKS;
+        const int k = list[have ? u / CHUNKS : 0];
         const int4 item = a.desc[2 * k]; // {first packed token, first row, rows, kv head}
         const int last = a.desc[2 * k + 1].x;
         int r, d; // this lane's row of the block, and the first of its four values
@@ -903,17 +972,18 @@ template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void exte
             r = chunk * (256 / D) + lane / (D / 4), d = 4 * (lane % (D / 4));
         }
         const int row = item.y + r;
-        const bool exists = row < item.z;
+        const bool exists = have && row < item.z;
         float mm = kPfLowest, l = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
         if (exists) {
             constexpr int AT = 4;
-            for (int p0 = k + wave; p0 <= last; p0 += AT * W) {
+            const int step = split ? W : 1;
+            for (int p0 = split ? k + wave : k; p0 <= last; p0 += AT * step) {
                 float2 ml[AT];
                 f32x4 o[AT];
 #pragma unroll
                 for (int i = 0; i < AT; i++) {
-                    const int p = p0 + W * i;
+                    const int p = p0 + step * i;
                     const int64_t slot = p == k ? 2 * (int64_t)k + 1 : 2 * (int64_t)p;
                     ml[i] = make_float2(kPfLowest, 0.f), o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
                     if (p <= last) {
@@ -933,25 +1003,26 @@ template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void exte
                 }
             }
         }
-        sums[wave][lane] = acc, stats[wave][lane] = make_float2(mm, l);
-        __syncthreads();
-        if (wave == 0 && exists) {
-            float top = kPfLowest, all = 0.f;
-            f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (split) {
+            sums[wave][lane] = acc, stats[wave][lane] = make_float2(mm, l);
+            __syncthreads();
+            mm = kPfLowest, l = 0.f, acc = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int w = 0; w < W; w++) top = fmaxf(top, stats[w][lane].x);
+            for (int w = 0; w < W; w++) mm = fmaxf(mm, stats[w][lane].x);
 #pragma unroll
             for (int w = 0; w < W; w++) {
-                const float f = __builtin_amdgcn_exp2f(stats[w][lane].x - top);
-                all += f * stats[w][lane].y, v += f * sums[w][lane];
+                const float f = __builtin_amdgcn_exp2f(stats[w][lane].x - mm);
+                l += f * stats[w][lane].y, acc += f * sums[w][lane];
             }
+            __syncthreads();
+        }
+        if (exists && (wave == 0 || !split)) {
             const int token = ex_div_g(a, row);
             const int64_t rh = (int64_t)(item.x + token) * a.Hq + item.w * a.G + (row - token * a.G);
-            const float inv = all > 0.f ? 1.0f / all : all == 0.f ? 0.f : all;
-            *(bf16x4 *)(a.out + rh * D + d) = __builtin_convertvector(v * inv, bf16x4);
-            if (d == 0) a.lse[rh] = (top + __builtin_amdgcn_logf(all)) * 0.6931471805599453f;
+            const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l;
+            *(bf16x4 *)(a.out + rh * D + d) = __builtin_convertvector(acc * inv, bf16x4);
+            if (d == 0) a.lse[rh] = (mm + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
         }
-        __syncthreads();
     }
 }
 

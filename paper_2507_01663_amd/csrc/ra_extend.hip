@@ -3,19 +3,22 @@
 
 namespace ra {
 
-constexpr int kExLeast = 8; // stages of a span at least
+constexpr int kExLeast = 10, kExLeastFew = 16; // length of a span on the line at least
 
 // Which kernel a call takes, its workgroups, and how finely the work is cut.
 static void extend_shape(ExtendLaunch &a)
 {
     a.few = (int64_t)a.max_chunk * a.G <= kExFewRows;
     const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExTileRows + a.B;
-    const int64_t line = blocks * a.Hkv * (a.max_pages / 2 + 1); // its length at most
-    a.least = kExLeast;
+    const int64_t line = blocks * a.Hkv * (a.max_pages / 2 + 1 + (a.few ? kExFixed<kExFewRows> : kExFixed<kExTileRows>) + 1); // its length at most
+    a.least = a.few ? kExLeastFew : kExLeast;
     const int64_t resident = (int64_t)(a.num_cus < 8 ? 8 : a.num_cus & ~7) * (a.few ? (a.D == 64 ? 2 : 1) : (a.D == 64 ? 3 : 2));
     int64_t spans = (line / a.least + 7) & ~(int64_t)7;
     spans = spans < 8 ? 8 : spans < resident ? spans : resident;
     a.spans = (int)(spans < kExMaxSpans ? spans : kExMaxSpans);
+    // (a workgroup for every item where there may be so many that they are left whole: see ExLine::measure)
+    const int64_t items = blocks * a.Hkv;
+    a.grid = (int)(items >= 2 * a.spans ? (items + 7) & ~(int64_t)7 : a.spans);
 }
 
 size_t carve_extend(ExtendLaunch &a, void *base)
@@ -35,13 +38,13 @@ size_t carve_extend(ExtendLaunch &a, void *base)
 }
 
 #define RA_EX_TILES(X) X(64, false) X(64, true) X(128, false) X(128, true)
-#define RA_EX_FEWS(X) X(64, 2, 1) X(64, 2, 2) X(64, 2, 4) X(64, 1, 1) X(64, 1, 2) X(64, 1, 4) X(128, 2, 1) X(128, 2, 2) X(128, 2, 4) X(128, 1, 1) X(128, 1, 2) X(128, 1, 4)
+#define RA_EX_FEWS(X) X(64, 2, 1) X(64, 2, 2) X(64, 1, 1) X(64, 1, 2) X(128, 2, 1) X(128, 2, 2) X(128, 1, 1) X(128, 1, 2)
 
 hipError_t extend_config()
 {
     hipError_t e = hipSuccess;
 #define RA_EX_CONFIG(DD, F) \
-    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)extend_tile_kernel<DD, F>, hipFuncAttributeMaxDynamicSharedMemorySize, ExTileLds<DD>::kBytes);
+    if (e == hipSuccess) e = hipFuncSetAttribute((const void *)extend_tile_kernel<DD, F>, hipFuncAttributeMaxDynamicSharedMemorySize, (ExTileLds<DD, F>::kBytes));
     RA_EX_TILES(RA_EX_CONFIG)
 #undef RA_EX_CONFIG
 #define RA_EX_CONFIG(DD, KVB, Q) \
@@ -53,21 +56,21 @@ hipError_t extend_config()
 
 hipError_t launch_extend(const ExtendLaunch &a, hipStream_t s)
 {
-    const dim3 grid((unsigned)a.spans), block(64 * kExWaves);
+    const dim3 grid((unsigned)a.grid), block(64 * kExWaves);
     if (!a.few) {
 #define RA_EX_LAUNCH(DD, F) \
-    if (a.D == DD && (a.kv_fp8 != 0) == F) hipLaunchKernelGGL((extend_tile_kernel<DD, F>), grid, block, (ExTileLds<DD>::kBytes), s, a);
+    if (a.D == DD && (a.kv_fp8 != 0) == F) hipLaunchKernelGGL((extend_tile_kernel<DD, F>), grid, block, (ExTileLds<DD, F>::kBytes), s, a);
         RA_EX_TILES(RA_EX_LAUNCH)
 #undef RA_EX_LAUNCH
     } else {
-        const int rows = a.max_chunk * a.G, tiles = rows <= 16 ? 1 : rows <= 32 ? 2 : 4;
+        const int rows = a.max_chunk * a.G, tiles = rows <= 16 ? 1 : 2;
 #define RA_EX_LAUNCH(DD, KVB, Q) \
     if (a.D == DD && (a.kv_fp8 ? 1 : 2) == KVB && tiles == Q) hipLaunchKernelGGL((extend_few_kernel<DD, KVB, Q>), grid, block, (ExFewLds<DD, KVB>::kBytes), s, a);
         RA_EX_FEWS(RA_EX_LAUNCH)
 #undef RA_EX_LAUNCH
     }
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.max_pages / 2 + 1 <= a.least) return e; // (no item is long enough to be cut)
+    if (e != hipSuccess || a.max_pages / 2 + 2 + (a.few ? kExFixed<kExFewRows> : kExFixed<kExTileRows>) <= a.least) return e; // (no item is long enough to be cut)
 #define RA_EX_MERGE(DD) \
     if (a.few) hipLaunchKernelGGL((extend_merge_kernel<DD, kExFewRows>), dim3(kExMergeWgs), block, 0, s, a); \
     else hipLaunchKernelGGL((extend_merge_kernel<DD, kExTileRows>), dim3(kExMergeWgs), block, 0, s, a)
