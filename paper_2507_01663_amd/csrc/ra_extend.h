@@ -58,11 +58,11 @@ template <int ROWS> __device__ __forceinline__ int ex_stages(const ExtendLaunch 
     return (last + 32) >> 5; // (last >= -n: no key at all gives a number of zero or less)
 }
 
-template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
+// What the sequence of t0, t1 (where its chunk starts and ends) and length L is.
+template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int t1, int L)
 {
     ExSeq s = {0, 0, 0, 0, 0};
-    if (b >= a.B) return s;
-    const int t0 = a.cu[b], n = a.cu[b + 1] - t0, L = a.seq_lens[b], most = a.max_pages * kPage;
+    const int n = t1 - t0, most = a.max_pages * kPage;
     if (t0 < 0 || t0 > a.T || n <= 0 || n > a.T - t0) return s;
     s.t0 = t0;
     s.n = n < a.max_chunk ? n : a.max_chunk;
@@ -72,47 +72,77 @@ template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLau
     s.cost = kExFixed<ROWS> + 1 + (((first > 0 ? first : 0) + (last > 0 ? last : 0)) >> 1);
     return s;
 }
+template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
+{
+    return b < a.B ? ex_sequence<ROWS>(a, a.cu[b], a.cu[b + 1], a.seq_lens[b]) : ExSeq{0, 0, 0, 0, 0};
+}
 
+// The line: lane c has chunk c of the sequences (64 of them, or a multiple of that in a very large batch).  Of a batch of up to
+// 512, `known` keeps in LDS what the first search for a place needs; the waves write the same there.
+constexpr int kExKnown = 512;
+struct ExKnown {
+    int4 rec[kExKnown]; // {start on the line, blocks before, first packed token, new tokens}
+    int len[kExKnown];
+};
 
-// The line: lane c has chunk c of the sequences (64 of them, or a multiple of that in a very large batch).
 template <int ROWS> struct ExLine {
-    int lane, sub, chunks; // sixty-fours of sequences in a chunk
-    int unit;              // items are left whole, each of length one
-    int before, total;     // start of this lane's chunk
-    int q, r, spans, cut;  // span k starts at q k + min(k, r), before cuts are moved; items up to `cut` are not cut
+    int lane, sub, chunks;   // sixty-fours of sequences in a chunk
+    int unit;                // items are left whole (see measure)
+    int before, total;       // start of this lane's chunk
+    int before_blocks, blocks; // ... counted in blocks of one kv head
+    int q, r, spans, cut;    // span k starts at q k + min(k, r), before cuts are moved; items up to `cut` are not cut
 
-    __device__ __forceinline__ int length(const ExtendLaunch &a, const ExSeq &s) const { return a.Hkv * s.blocks * (unit ? 1 : s.cost); }
-
-    // first: the first sixty-four sequences.
-    __device__ __forceinline__ void measure(const ExtendLaunch &a, ExSeq &first)
+    __device__ __forceinline__ void measure(const ExtendLaunch &a, ExKnown *known)
     {
         lane = threadIdx.x & 63;
-        sub = (a.B + 4095) >> 12;
-        chunks = sub == 1 ? (a.B + 63) >> 6 : ex_div(a.B + 64 * sub - 1, 64 * sub);
-        first = ex_sequence<ROWS>(a, lane);
-        int cost = 0, items = 0, longest = first.cost; // this lane's chunk, lane by lane first
-        for (int c = 0; c < chunks; c++) {
-            int l = 0, n = 0;
-            for (int i = 0; i < sub; i++) {
-                const ExSeq s = c + i ? ex_sequence<ROWS>(a, (c * sub + i) * 64 + lane) : first;
-                l += a.Hkv * s.blocks * s.cost, n += a.Hkv * s.blocks;
-                longest = longest > s.cost ? longest : s.cost;
+        before = before_blocks = total = blocks = 0;
+        int longest = 0;
+        sub = 1;
+        if (a.B <= kExKnown) {
+            chunks = (a.B + 63) >> 6;
+            constexpr int AT = 4;
+            for (int c0 = 0; c0 < chunks; c0 += AT) {
+                int t0[AT], t1[AT], len[AT];
+#pragma unroll
+                for (int i = 0; i < AT; i++) {
+                    const int b = 64 * (c0 + i) + lane;
+                    t0[i] = t1[i] = len[i] = 0;
+                    if (b < a.B) t0[i] = a.cu[b], t1[i] = a.cu[b + 1], len[i] = a.seq_lens[b];
+                }
+#pragma unroll
+                for (int i = 0; i < AT; i++) {
+                    if (c0 + i >= chunks) break;
+                    const ExSeq s = ex_sequence<ROWS>(a, t0[i], t1[i], len[i]);
+                    int tc, tb;
+                    const int at = wave_scan(a.Hkv * s.blocks * s.cost, lane, tc), at_blocks = wave_scan(s.blocks, lane, tb);
+                    const int b = 64 * (c0 + i) + lane;
+                    known->rec[b] = make_int4(total + at, blocks + at_blocks, s.t0, s.n);
+                    known->len[b] = s.L;
+                    if (lane == c0 + i) before = total, before_blocks = blocks;
+                    total += tc, blocks += tb;
+                    longest = longest > s.cost ? longest : s.cost;
+                }
             }
-            int tl, tn;
-            (void)wave_scan(l, lane, tl), (void)wave_scan(n, lane, tn);
-            if (lane == c) cost = tl, items = tn;
+        } else {
+            sub = (a.B + 4095) >> 12;
+            chunks = ex_div(a.B + 64 * sub - 1, 64 * sub);
+            for (int c = 0; c < chunks; c++) {
+                if (lane == c) before = total, before_blocks = blocks;
+                for (int i = 0; i < sub; i++) {
+                    const ExSeq s = ex_sequence<ROWS>(a, (c * sub + i) * 64 + lane);
+                    int tc, tb;
+                    (void)wave_scan(a.Hkv * s.blocks * s.cost, lane, tc), (void)wave_scan(s.blocks, lane, tb);
+                    total += tc, blocks += tb;
+                    longest = longest > s.cost ? longest : s.cost;
+                }
+            }
         }
-        int all_cost, all_items;
-        const int before_cost = wave_scan(cost, lane, all_cost), before_items = wave_scan(items, lane, all_items);
-        // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each, in
-        // order, so that blocks that read the same keys run side by side.
-        const int mean = ex_div(all_cost, a.spans);
-        unit = all_items >= 2 * a.spans && !__any(longest > mean);
-        before = unit ? before_items : before_cost;
-        total = unit ? all_items : all_cost;
-        const int most = ex_div(all_cost, a.least);
-        spans = unit ? all_items : most < 1 ? 1 : (most < a.spans ? most : a.spans);
-        q = unit ? 1 : ex_div(total, spans);
+        if (lane >= chunks) before = before_blocks = INT32_MAX;
+        // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.
+        unit = blocks * a.Hkv >= 2 * a.spans && !__any(longest > ex_div(total, a.spans));
+        const int most = ex_div(total, a.least);
+        spans = most < 1 ? 1 : (most < a.spans ? most : a.spans);
+        q = ex_div(total, spans);
         r = total - q * spans;
         cut = q >> 3 > a.least ? q >> 3 : a.least;
     }
@@ -132,49 +162,53 @@ struct ExPlace {
     ExSeq s;         // (cost: the item's length on the line)
 };
 
-// Where x lies among the sixty-four sequences from `base` on, whose items start at `start`.
-template <int ROWS> __device__ __forceinline__ void ex_pick(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExSeq &s, int base, int before, int x, ExPlace &p)
+// The sequence that x lies in (0 <= x < total), x counted as the line is or (BLOCKS) in blocks of one kv head; returns x's
+// distance from its start.
+template <int ROWS, bool BLOCKS> __device__ __forceinline__ int ex_sequence_at(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExKnown *known, int x, ExPlace &p)
 {
-    const int l = 63 - __builtin_clzll(__ballot(s.blocks > 0 && before <= x));
-    p.b = base + l;
-    p.s.t0 = __builtin_amdgcn_readlane(s.t0, l), p.s.n = __builtin_amdgcn_readlane(s.n, l), p.s.L = __builtin_amdgcn_readlane(s.L, l);
-    p.s.blocks = __builtin_amdgcn_readlane(s.blocks, l), p.s.cost = line.unit ? 1 : __builtin_amdgcn_readlane(s.cost, l);
-    const int at = __builtin_amdgcn_readlane(before, l);
-    p.item = ex_div(x - at, p.s.cost);
-    p.x0 = at + p.item * p.s.cost;
-}
-
-// The item that x lies in (0 <= x < total).
-template <int ROWS> __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExSeq *first, int x, ExPlace &p)
-{
-    int t;
-    if (first && line.chunks == 1 && line.sub == 1) {
-        const int before = wave_scan(line.length(a, *first), line.lane, t);
-        ex_pick<ROWS>(a, line, *first, 0, before, x, p);
-        return;
+    const int chunk_before = BLOCKS ? line.before_blocks : line.before;
+    const int c = 63 - __builtin_clzll(__ballot(chunk_before <= x));
+    auto take = [&](int base, const ExSeq &s, int before) __attribute__((always_inline)) {
+        const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && before <= x));
+        p.b = base + l;
+        p.s.t0 = __builtin_amdgcn_readlane(s.t0, l), p.s.n = __builtin_amdgcn_readlane(s.n, l), p.s.L = __builtin_amdgcn_readlane(s.L, l);
+        p.s = ex_sequence<ROWS>(a, p.s.t0, p.s.t0 + p.s.n, p.s.L);
+        p.s.blocks = ex_uni(p.s.blocks), p.s.cost = ex_uni(p.s.cost);
+        return x - __builtin_amdgcn_readlane(before, l);
+    };
+    if (known) {
+        const int4 rec = known->rec[64 * c + line.lane];
+        const ExSeq s = {rec.z, rec.w, known->len[64 * c + line.lane], 0, 0};
+        return take(64 * c, s, BLOCKS ? rec.y : rec.x);
     }
-    int c = 63 - __builtin_clzll(__ballot(line.before <= x));
-    c = c < line.chunks ? c : line.chunks - 1;
-    int start = __builtin_amdgcn_readlane(line.before, c);
-    for (int i = 0; i < line.sub; i++) {
+    int start = __builtin_amdgcn_readlane(chunk_before, c);
+    for (int i = 0;; i++) {
         const int base = (c * line.sub + i) * 64;
         const ExSeq s = ex_sequence<ROWS>(a, base + line.lane);
-        const int before = start + wave_scan(line.length(a, s), line.lane, t);
+        int t;
+        const int before = start + wave_scan(BLOCKS ? s.blocks : a.Hkv * s.blocks * s.cost, line.lane, t);
         if (x >= start + t && i + 1 < line.sub) {
             start += t;
             continue;
         }
-        ex_pick<ROWS>(a, line, s, base, before, x, p);
-        return;
+        return take(base, s, before);
     }
 }
 
+// The item that x lies in.
+template <int ROWS> __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExKnown *known, int x, ExPlace &p)
+{
+    const int y = ex_sequence_at<ROWS, false>(a, line, known, x, p);
+    p.item = ex_div(y, p.s.cost);
+    p.x0 = x - y + p.item * p.s.cost;
+}
+
 // Where span k starts once short items are left whole, and no part of an item is next to nothing.
-template <int ROWS> __device__ __forceinline__ int ex_start(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExSeq *first, int k, ExPlace &p)
+template <int ROWS> __device__ __forceinline__ int ex_start(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExKnown *known, int k, ExPlace &p)
 {
     if (k >= line.spans) return line.total;
     const int x = line.raw(k);
-    ex_find<ROWS>(a, line, first, x, p);
+    ex_find<ROWS>(a, line, known, x, p);
     const int y = x - p.x0;
     if (p.s.cost > line.cut) return y < kExFixed<ROWS> + kExEdge ? p.x0 : p.s.cost - y < kExEdge ? p.x0 + p.s.cost : x;
     return 2 * y < p.s.cost ? p.x0 : p.x0 + p.s.cost;
@@ -207,43 +241,61 @@ template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch
     return t;
 }
 
-// Goes through the parts of the workgroup's span; `work` is called with each.  Workgroups are dealt to the eight dies
-// round-robin, and a die gets neighbouring spans, so that blocks that read the same keys find them in its L2.
-// Also tells the merge which items begin here and end elsewhere: desc[2 k], desc[2 k + 1] = {first packed token, first row,
-// rows, kv head}, {last span, -, -, -}.
-template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, F &&work)
+// Goes through the parts that the workgroup works on; `work` is called with each.  Workgroups are dealt to the eight dies
+// round-robin, each with an L2 of its own.
+// Items that are left whole: with gg = gcd(Hkv, 8), a die takes the kv heads congruent to it mod gg, and the 8 / gg dies that
+// take the same heads take their items in turn, so that every die has its share of every sequence, and blocks that read the
+// same keys run side by side on few of them.
+// Else: a die takes neighbouring spans.  Also tells the merge which items begin in a span and end in another: desc[2 k],
+// desc[2 k + 1] = {first packed token, first row, rows, kv head}, {last span, -, -, -}.
+template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, uint8_t *lds, F &&work)
 {
+    ExKnown *known = a.B <= kExKnown ? (ExKnown *)lds : nullptr;
     ExLine<ROWS> line;
-    ExSeq first;
-    line.measure(a, first);
-    const int per = (line.spans + 7) >> 3, at = (int)blockIdx.x >> 3;
-    const int k = at < per ? ((int)blockIdx.x & 7) * per + at : (int)blockIdx.x; // (past the spans: one that does not exist)
-    int last = 0;
+    line.measure(a, (ExKnown *)lds);
+    const int die = (int)blockIdx.x & 7, at = (int)blockIdx.x >> 3;
+    const int per = (line.spans + 7) >> 3, k = at < per ? die * per + at : (int)blockIdx.x; // (past the spans: one that does not exist)
+    int last = 0, x = 0, end = 0, step = 1, span = k;
     int4 begun = {0, 0, 0, 0};
-    if (line.total > 0 && at < per && k < line.spans) {
-        ExPlace p;
-        int x, end;
+    ExPlace p;
+    p.item = 0, p.x0 = 0;
+    const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift;
+    if (line.unit) {
+        x = (at << s_shift) + (die >> gg_shift), end = line.blocks * (a.Hkv >> gg_shift);
+        step = (int)gridDim.x >> 3 << s_shift; // (there are as many workgroups as items, if the call's sizes are what they say)
+    } else if (line.total > 0 && at < per && k < line.spans) {
+        end = ex_start<ROWS>(a, line, known, k + 1, p);
+        x = ex_start<ROWS>(a, line, known, k, p);
+        if (x < end && x >= p.x0 + p.s.cost) ex_find<ROWS>(a, line, known, x, p);
+    }
+    bool first = true;
+    while (x < end) {
+        ExPart part;
+        int next;
         if (line.unit) {
-            ex_find<ROWS>(a, line, &first, k, p);
-            x = k, end = k + 1;
+            const int heads = a.Hkv >> gg_shift;
+            const int y = ex_sequence_at<ROWS, true>(a, line, first ? known : nullptr, ex_div(x, heads), p); // (a sequence's items: its blocks times heads)
+            const int block0 = ex_div(x, heads) - y, i = x - block0 * heads;
+            const int h = ex_div(i, p.s.blocks);
+            p.item = i + ((h << gg_shift) + (die & ((1 << gg_shift) - 1)) - h) * p.s.blocks;
+            part = ex_part<ROWS>(a, p, 0, p.s.cost, 0);
+            next = x + step;
         } else {
-            end = ex_start<ROWS>(a, line, &first, k + 1, p);
-            x = ex_start<ROWS>(a, line, &first, k, p);
-            if (x < end && x >= p.x0 + p.s.cost) ex_find<ROWS>(a, line, &first, x, p);
-        }
-        while (x < end) {
-            const int x1 = p.x0 + p.s.cost, stop = x1 < end ? x1 : end;
-            const ExPart part = ex_part<ROWS>(a, p, x - p.x0, stop - p.x0, k);
-            if (x == p.x0 && stop < x1) {
+            const int x1 = p.x0 + p.s.cost;
+            next = x1 < end ? x1 : end;
+            part = ex_part<ROWS>(a, p, x - p.x0, next - p.x0, span);
+            if (x == p.x0 && next < x1) {
                 begun = make_int4(p.s.t0, part.row0, part.rows, part.kvh);
                 last = line.last_of(x1);
             }
-            work(p, part);
-            x = stop;
-            if (x >= end) break;
-            if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x1;
-            else ex_find<ROWS>(a, line, nullptr, x, p);
         }
+        if (first) __syncthreads(); // (what the waves know of the line makes room for the ring)
+        first = false;
+        work(p, part);
+        x = next;
+        if (x >= end || line.unit) continue;
+        if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
+        else ex_find<ROWS>(a, line, nullptr, x, p);
     }
     if (threadIdx.x == 0 && k < a.spans) { // (every span is answered for, also one that does not exist)
         a.desc[2 * k] = begun;
@@ -466,7 +518,7 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
     auto after = [](int slot) __attribute__((always_inline)) { return slot + 1 == X::kSlots ? 0 : slot + 1; };
     int slot0 = 0; // ring slot of the part's first stage; the others follow
 
-    ex_walk<kExTileRows>(a, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
+    ex_walk<kExTileRows>(a, lds, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
         const int nst = t.hi - t.lo, row = t.row0 + kPfRows * wave + n; // this lane's row
         const bool exists = row < t.rows;
         const int token = ex_div_g(a, exists ? row : t.rows - 1), head = t.kvh * a.G + ((exists ? row : t.rows - 1) - token * a.G);
@@ -695,7 +747,7 @@ template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1
     LaneConst<D, KVB> lc;
     lane_setup<D, KVB>(lc, lane, a.stride_token_b);
 
-    ex_walk<kExFewRows>(a, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
+    ex_walk<kExFewRows>(a, lds, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
         const int ntiles = (t.rows + 15) >> 4, shift = p.s.L - p.s.n;
         // the wave's stages of the part: wave, wave + 4, ...
         const int left = t.hi - t.lo - wave, mine = left > 0 ? (left + W - 1) / W : 0;
@@ -910,7 +962,7 @@ template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1
 
 // ---- what spans share -----------------------------------------------------------------------------------
 
-constexpr int kExMergeWgs = 1024, kExMaxSpans = 1024;
+constexpr int kExMergeWgs = 2048, kExMaxSpans = 1024;
 constexpr int kExMergeFew = 12; // parts of an item that one wave adds up
 
 // Adds up the parts of the items that a cut goes through, 256 consecutive values of an item's parts at a time: a wave alone
