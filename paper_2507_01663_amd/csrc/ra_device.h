@@ -30,6 +30,18 @@ template <int DPS> struct WaitTail<0, DPS> {
     static __device__ __forceinline__ void run(int) { wait_vmcnt<0>(); }
 };
 
+// Kernel arguments live in memory that takes a microsecond or two to reach the first time, and the compiler fetches a field
+// where it is first used.  One word of every cache line of them, asked for up front, makes those trips one.
+template <typename T> __device__ __forceinline__ void touch_lines(const T &args)
+{
+    const int32_t *p = reinterpret_cast<const int32_t *>(&args);
+    int32_t s = 0;
+#pragma unroll
+    for (unsigned i = 0; i < sizeof(T) / 4; i += 16) s |= p[i];
+    s |= p[sizeof(T) / 4 - 1];
+    asm volatile("" ::"s"(s));
+}
+
 // 16 bytes per lane from global memory straight into LDS at lds_addr + lane*16 (no registers in between).
 // The compiler does not see these as loads, so their completion is tracked by hand with wait_vmcnt().
 // Two address forms: a full 64-bit address per lane, or a wave-uniform base plus a 32-bit lane offset.

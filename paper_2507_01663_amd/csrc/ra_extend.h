@@ -22,6 +22,18 @@
 namespace ra {
 
 constexpr int kExWaves = 4;
+
+// The kernels' arguments: what the search for a workgroup's work needs first is in registers when a wave starts, the rest is
+// asked for at once.
+#define EX_PARAMS                                                                                                               \
+    const int32_t *__restrict__ cu, const int32_t *__restrict__ seq_lens, int B, int T, int max_chunk, int max_pages, int group, int Hkv, \
+        uint32_t magic_g, int spans, ExtendLaunch given
+#define EX_TAKE(a)                                                                                                             \
+    ExtendLaunch a = given;                                                                                                     \
+    a.cu = cu, a.seq_lens = seq_lens, a.B = B, a.T = T, a.max_chunk = max_chunk, a.max_pages = max_pages, a.G = group, a.Hkv = Hkv; \
+    a.magic_g = magic_g, a.spans = spans;                                                                                       \
+    touch_lines(given)
+#define EX_GIVE(a) (a).cu, (a).seq_lens, (a).B, (a).T, (a).max_chunk, (a).max_pages, (a).G, (a).Hkv, (a).magic_g, (a).spans, (a)
 constexpr int kExTileRows = kPfRows * kExWaves; // rows of a block of the tile kernel
 constexpr int kExFewRows = 32;                  // rows of a sequence and kv head up to which the other one takes them
 
@@ -58,7 +70,8 @@ template <int ROWS> __device__ __forceinline__ int ex_stages(const ExtendLaunch 
     return (last + 32) >> 5; // (last >= -n: no key at all gives a number of zero or less)
 }
 
-// What the sequence of t0, t1 (where its chunk starts and ends) and length L is.
+// What the sequence of t0, t1 (where its chunk starts and ends) and length L is.  (A workgroup comes past everything up to its
+// first keys once and alone, an instruction after the other: they are few.)
 template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int t1, int L)
 {
     ExSeq s = {0, 0, 0, 0, 0};
@@ -68,8 +81,8 @@ template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLau
     s.n = n < a.max_chunk ? n : a.max_chunk;
     s.L = L < 0 ? 0 : (L < most ? L : most);
     s.blocks = (s.n * a.G + ROWS - 1) / ROWS;
-    const int first = ex_stages<ROWS>(a, s, 0), last = ex_stages<ROWS>(a, s, s.blocks - 1);
-    s.cost = kExFixed<ROWS> + 1 + (((first > 0 ? first : 0) + (last > 0 ? last : 0)) >> 1);
+    const int mean = (s.L - (s.n >> 1) + 48) >> 5; // keys that a row sees, in stages
+    s.cost = kExFixed<ROWS> + (mean > 1 ? mean : 1);
     return s;
 }
 template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
@@ -78,12 +91,14 @@ template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLau
 }
 
 // The line: lane c has chunk c of the sequences (64 of them, or a multiple of that in a very large batch).  Of a batch of up to
-// 512, `known` keeps in LDS what the first search for a place needs; the waves write the same there.
+// 512, `known` keeps in LDS what the first search for a place needs; every wave writes all of it, the same values to the same
+// place.
 constexpr int kExKnown = 512;
 struct ExKnown {
     int4 rec[kExKnown]; // {start on the line, blocks before, first packed token, new tokens}
     int len[kExKnown];
 };
+static_assert(sizeof(ExKnown) <= 3 * Geo<64, 2>::kStage, "it fits the smallest ring");
 
 template <int ROWS> struct ExLine {
     int lane, sub, chunks;   // sixty-fours of sequences in a chunk
@@ -98,9 +113,16 @@ template <int ROWS> struct ExLine {
         before = before_blocks = total = blocks = 0;
         int longest = 0;
         sub = 1;
+        auto add = [&](const ExSeq &s, int &at, int &at_blocks) __attribute__((always_inline)) {
+            int tc, tb;
+            at = total + wave_scan(a.Hkv * s.blocks * s.cost, lane, tc), at_blocks = blocks + wave_scan(s.blocks, lane, tb);
+            total += tc, blocks += tb;
+            longest = longest > s.cost ? longest : s.cost;
+        };
         if (a.B <= kExKnown) {
             chunks = (a.B + 63) >> 6;
-            constexpr int AT = 4;
+            constexpr int AT = 2;
+#pragma unroll 1
             for (int c0 = 0; c0 < chunks; c0 += AT) {
                 int t0[AT], t1[AT], len[AT];
 #pragma unroll
@@ -113,38 +135,34 @@ template <int ROWS> struct ExLine {
                 for (int i = 0; i < AT; i++) {
                     if (c0 + i >= chunks) break;
                     const ExSeq s = ex_sequence<ROWS>(a, t0[i], t1[i], len[i]);
-                    int tc, tb;
-                    const int at = wave_scan(a.Hkv * s.blocks * s.cost, lane, tc), at_blocks = wave_scan(s.blocks, lane, tb);
-                    const int b = 64 * (c0 + i) + lane;
-                    known->rec[b] = make_int4(total + at, blocks + at_blocks, s.t0, s.n);
-                    known->len[b] = s.L;
                     if (lane == c0 + i) before = total, before_blocks = blocks;
-                    total += tc, blocks += tb;
-                    longest = longest > s.cost ? longest : s.cost;
+                    int at, at_blocks;
+                    add(s, at, at_blocks);
+                    known->rec[64 * (c0 + i) + lane] = make_int4(at, at_blocks, s.t0, s.n);
+                    known->len[64 * (c0 + i) + lane] = s.L;
                 }
             }
         } else {
             sub = (a.B + 4095) >> 12;
             chunks = ex_div(a.B + 64 * sub - 1, 64 * sub);
-            for (int c = 0; c < chunks; c++) {
-                if (lane == c) before = total, before_blocks = blocks;
-                for (int i = 0; i < sub; i++) {
-                    const ExSeq s = ex_sequence<ROWS>(a, (c * sub + i) * 64 + lane);
-                    int tc, tb;
-                    (void)wave_scan(a.Hkv * s.blocks * s.cost, lane, tc), (void)wave_scan(s.blocks, lane, tb);
-                    total += tc, blocks += tb;
-                    longest = longest > s.cost ? longest : s.cost;
-                }
+#pragma unroll 1
+            for (int c = 0; c < chunks * sub; c++) {
+                if (lane * sub == c) before = total, before_blocks = blocks;
+                int at, at_blocks;
+                add(ex_sequence<ROWS>(a, 64 * c + lane), at, at_blocks);
             }
         }
         if (lane >= chunks) before = before_blocks = INT32_MAX;
-        // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.
-        unit = blocks * a.Hkv >= 2 * a.spans && !__any(longest > ex_div(total, a.spans));
-        const int most = ex_div(total, a.least);
-        spans = most < 1 ? 1 : (most < a.spans ? most : a.spans);
+        spans = a.spans;
+        if (total < a.least * a.spans) {
+            spans = ex_div(total, a.least);
+            spans = spans < 1 ? 1 : spans;
+        }
         q = ex_div(total, spans);
         r = total - q * spans;
         cut = q >> 3 > a.least ? q >> 3 : a.least;
+        // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.
+        unit = blocks * a.Hkv >= 2 * a.spans && !__any(longest > q);
     }
     __device__ __forceinline__ int raw(int k) const { return q * k + (k < r ? k : r); }
     // The last span that an item which ends at x1 has a part in, if it is cut.
@@ -153,6 +171,14 @@ template <int ROWS> struct ExLine {
         const int y = x1 - 1, big = r * (q + 1);
         const int k = y < big ? ex_div(y, q + 1) : r + ex_div(y - big, q); // the last one that starts before x1
         return x1 - raw(k) < kExEdge ? k - 1 : k;                          // (but for a cut that moves there)
+    }
+    // Where a cut at x goes in the item of that length that starts at x0: nowhere into short items, and not so near an end of
+    // others that a part would be next to nothing.
+    __device__ __forceinline__ int moved(int x, int x0, int cost) const
+    {
+        const int y = x - x0, left = cost - y;
+        const bool down = cost > cut ? y < kExFixed<ROWS> + kExEdge : y < left, up = cost > cut ? left < kExEdge : true;
+        return down ? x0 : up ? x0 + cost : x;
     }
 };
 
@@ -168,31 +194,28 @@ template <int ROWS, bool BLOCKS> __device__ __forceinline__ int ex_sequence_at(c
 {
     const int chunk_before = BLOCKS ? line.before_blocks : line.before;
     const int c = 63 - __builtin_clzll(__ballot(chunk_before <= x));
-    auto take = [&](int base, const ExSeq &s, int before) __attribute__((always_inline)) {
-        const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && before <= x));
-        p.b = base + l;
-        p.s.t0 = __builtin_amdgcn_readlane(s.t0, l), p.s.n = __builtin_amdgcn_readlane(s.n, l), p.s.L = __builtin_amdgcn_readlane(s.L, l);
-        p.s = ex_sequence<ROWS>(a, p.s.t0, p.s.t0 + p.s.n, p.s.L);
-        p.s.blocks = ex_uni(p.s.blocks), p.s.cost = ex_uni(p.s.cost);
-        return x - __builtin_amdgcn_readlane(before, l);
-    };
+    int base = 64 * c, before;
+    ExSeq s = {0, 0, 0, 0, 0};
     if (known) {
-        const int4 rec = known->rec[64 * c + line.lane];
-        const ExSeq s = {rec.z, rec.w, known->len[64 * c + line.lane], 0, 0};
-        return take(64 * c, s, BLOCKS ? rec.y : rec.x);
-    }
-    int start = __builtin_amdgcn_readlane(chunk_before, c);
-    for (int i = 0;; i++) {
-        const int base = (c * line.sub + i) * 64;
-        const ExSeq s = ex_sequence<ROWS>(a, base + line.lane);
-        int t;
-        const int before = start + wave_scan(BLOCKS ? s.blocks : a.Hkv * s.blocks * s.cost, line.lane, t);
-        if (x >= start + t && i + 1 < line.sub) {
+        const int4 rec = known->rec[base + line.lane];
+        s.t0 = rec.z, s.n = rec.w, s.L = known->len[base + line.lane], before = BLOCKS ? rec.y : rec.x;
+    } else {
+        int start = __builtin_amdgcn_readlane(chunk_before, c);
+#pragma unroll 1
+        for (int i = 0;; i++) {
+            base = (c * line.sub + i) * 64;
+            s = ex_sequence<ROWS>(a, base + line.lane);
+            int t;
+            before = start + wave_scan(BLOCKS ? s.blocks : a.Hkv * s.blocks * s.cost, line.lane, t);
+            if (x < start + t || i + 1 == line.sub) break;
             start += t;
-            continue;
         }
-        return take(base, s, before);
     }
+    const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && before <= x));
+    p.b = base + l;
+    const int t0 = __builtin_amdgcn_readlane(s.t0, l);
+    p.s = ex_sequence<ROWS>(a, t0, t0 + __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.L, l));
+    return x - __builtin_amdgcn_readlane(before, l);
 }
 
 // The item that x lies in.
@@ -201,17 +224,6 @@ template <int ROWS> __device__ __forceinline__ void ex_find(const ExtendLaunch &
     const int y = ex_sequence_at<ROWS, false>(a, line, known, x, p);
     p.item = ex_div(y, p.s.cost);
     p.x0 = x - y + p.item * p.s.cost;
-}
-
-// Where span k starts once short items are left whole, and no part of an item is next to nothing.
-template <int ROWS> __device__ __forceinline__ int ex_start(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExKnown *known, int k, ExPlace &p)
-{
-    if (k >= line.spans) return line.total;
-    const int x = line.raw(k);
-    ex_find<ROWS>(a, line, known, x, p);
-    const int y = x - p.x0;
-    if (p.s.cost > line.cut) return y < kExFixed<ROWS> + kExEdge ? p.x0 : p.s.cost - y < kExEdge ? p.x0 + p.s.cost : x;
-    return 2 * y < p.s.cost ? p.x0 : p.x0 + p.s.cost;
 }
 
 // A part of an item that a workgroup works on.
@@ -233,7 +245,7 @@ template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch
     stages = stages < 0 ? 0 : stages;
     // (a place inside the item, in proportion: the same for the two parts that it divides)
     auto stage_at = [&](int y) __attribute__((always_inline)) {
-        return ex_uni((int)((float)stages * ((float)(y - kExFixed<ROWS>) / (float)(p.s.cost - kExFixed<ROWS>))));
+        return ex_uni((int)((float)stages * ((float)(y - kExFixed<ROWS>) * __builtin_amdgcn_rcpf((float)(p.s.cost - kExFixed<ROWS>)))));
     };
     t.lo = y0 == 0 ? 0 : stage_at(y0);
     t.hi = y1 == p.s.cost ? stages : stage_at(y1);
@@ -250,40 +262,46 @@ template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch
 // desc[2 k + 1] = {first packed token, first row, rows, kv head}, {last span, -, -, -}.
 template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, uint8_t *lds, F &&work)
 {
-    ExKnown *known = a.B <= kExKnown ? (ExKnown *)lds : nullptr;
+    const ExKnown *known = a.B <= kExKnown ? (ExKnown *)lds : nullptr;
     ExLine<ROWS> line;
     line.measure(a, (ExKnown *)lds);
     const int die = (int)blockIdx.x & 7, at = (int)blockIdx.x >> 3;
     const int per = (line.spans + 7) >> 3, k = at < per ? die * per + at : (int)blockIdx.x; // (past the spans: one that does not exist)
-    int last = 0, x = 0, end = 0, step = 1, span = k;
+    int last = 0, x = 0, end = 0, step = 0;
     int4 begun = {0, 0, 0, 0};
     ExPlace p;
     p.item = 0, p.x0 = 0;
-    const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift;
+    const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift, heads = a.Hkv >> gg_shift;
     if (line.unit) {
-        x = (at << s_shift) + (die >> gg_shift), end = line.blocks * (a.Hkv >> gg_shift);
+        x = (at << s_shift) + (die >> gg_shift), end = line.blocks * heads;
         step = (int)gridDim.x >> 3 << s_shift; // (there are as many workgroups as items, if the call's sizes are what they say)
     } else if (line.total > 0 && at < per && k < line.spans) {
-        end = ex_start<ROWS>(a, line, known, k + 1, p);
-        x = ex_start<ROWS>(a, line, known, k, p);
-        if (x < end && x >= p.x0 + p.s.cost) ex_find<ROWS>(a, line, known, x, p);
+        // `end` is moved where the span gets to it
+        end = k + 1 < line.spans ? line.raw(k + 1) : line.total, x = line.raw(k);
+        ex_find<ROWS>(a, line, known, x, p);
+        x = line.moved(x, p.x0, p.s.cost);
+        if (x == p.x0 + p.s.cost) {
+            if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
+            else if (x < end) ex_find<ROWS>(a, line, known, x, p);
+        }
     }
     bool first = true;
     while (x < end) {
         ExPart part;
         int next;
         if (line.unit) {
-            const int heads = a.Hkv >> gg_shift;
-            const int y = ex_sequence_at<ROWS, true>(a, line, first ? known : nullptr, ex_div(x, heads), p); // (a sequence's items: its blocks times heads)
-            const int block0 = ex_div(x, heads) - y, i = x - block0 * heads;
-            const int h = ex_div(i, p.s.blocks);
+            const int at_block = ex_div(x, heads);
+            const int i = x - (at_block - ex_sequence_at<ROWS, true>(a, line, first ? known : nullptr, at_block, p)) * heads;
+            const int h = ex_div(i, p.s.blocks); // (a sequence's items: its blocks times heads)
             p.item = i + ((h << gg_shift) + (die & ((1 << gg_shift) - 1)) - h) * p.s.blocks;
             part = ex_part<ROWS>(a, p, 0, p.s.cost, 0);
             next = x + step;
         } else {
             const int x1 = p.x0 + p.s.cost;
+            if (end < x1) end = line.moved(end, p.x0, p.s.cost);
+            if (x >= end) break;
             next = x1 < end ? x1 : end;
-            part = ex_part<ROWS>(a, p, x - p.x0, next - p.x0, span);
+            part = ex_part<ROWS>(a, p, x - p.x0, next - p.x0, k);
             if (x == p.x0 && next < x1) {
                 begun = make_int4(p.s.t0, part.row0, part.rows, part.kvh);
                 last = line.last_of(x1);
@@ -500,8 +518,9 @@ template <int D, bool FP8> struct ExTileLds {
     static constexpr int kBytes = kAreas + kArea * kExWaves;
 };
 
-template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_tile_kernel(ExtendLaunch a)
+template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_tile_kernel(EX_PARAMS)
 {
+    EX_TAKE(a);
     using G = Geo<D, 2>;
     using P = Geo<D, FP8 ? 1 : 2>; // as the pools have it
     using X = ExTileLds<D, FP8>;
@@ -734,8 +753,9 @@ template <int D, int KVB> struct ExFewLds {
 };
 
 // NQT: tiles of sixteen rows that a sequence and kv head has at most.
-template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1) void extend_few_kernel(ExtendLaunch a)
+template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1) void extend_few_kernel(EX_PARAMS)
 {
+    EX_TAKE(a);
     using G = Geo<D, KVB>;
     using X = ExFewLds<D, KVB>;
     constexpr int NST = X::kSlots, DPS = G::kDmaPerStage, W = kExWaves;
@@ -968,8 +988,11 @@ constexpr int kExMergeFew = 12; // parts of an item that one wave adds up
 // Adds up the parts of the items that a cut goes through, 256 consecutive values of an item's parts at a time: a wave alone
 // where every item has few parts, else a workgroup's waves every fourth part each.  ROWS: those of the kernel that left them,
 // with its layout.
-template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(ExtendLaunch a)
+template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(const int4 *__restrict__ desc, int spans, ExtendLaunch given)
 {
+    ExtendLaunch a = given;
+    a.desc = (int4 *)desc, a.spans = spans;
+    touch_lines(given);
     constexpr int W = kExWaves, CHUNKS = ROWS * D / 256, N = kExMaxSpans / (64 * W);
     __shared__ int list[kExMaxSpans];
     __shared__ int counts[W][N], longest[W];

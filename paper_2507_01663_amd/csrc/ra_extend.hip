@@ -59,21 +59,21 @@ hipError_t launch_extend(const ExtendLaunch &a, hipStream_t s)
     const dim3 grid((unsigned)a.grid), block(64 * kExWaves);
     if (!a.few) {
 #define RA_EX_LAUNCH(DD, F) \
-    if (a.D == DD && (a.kv_fp8 != 0) == F) hipLaunchKernelGGL((extend_tile_kernel<DD, F>), grid, block, (ExTileLds<DD, F>::kBytes), s, a);
+    if (a.D == DD && (a.kv_fp8 != 0) == F) hipLaunchKernelGGL((extend_tile_kernel<DD, F>), grid, block, (ExTileLds<DD, F>::kBytes), s, EX_GIVE(a));
         RA_EX_TILES(RA_EX_LAUNCH)
 #undef RA_EX_LAUNCH
     } else {
         const int rows = a.max_chunk * a.G, tiles = rows <= 16 ? 1 : 2;
 #define RA_EX_LAUNCH(DD, KVB, Q) \
-    if (a.D == DD && (a.kv_fp8 ? 1 : 2) == KVB && tiles == Q) hipLaunchKernelGGL((extend_few_kernel<DD, KVB, Q>), grid, block, (ExFewLds<DD, KVB>::kBytes), s, a);
+    if (a.D == DD && (a.kv_fp8 ? 1 : 2) == KVB && tiles == Q) hipLaunchKernelGGL((extend_few_kernel<DD, KVB, Q>), grid, block, (ExFewLds<DD, KVB>::kBytes), s, EX_GIVE(a));
         RA_EX_FEWS(RA_EX_LAUNCH)
 #undef RA_EX_LAUNCH
     }
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.max_pages / 2 + 2 + (a.few ? kExFixed<kExFewRows> : kExFixed<kExTileRows>) <= a.least) return e; // (no item is long enough to be cut)
 #define RA_EX_MERGE(DD) \
-    if (a.few) hipLaunchKernelGGL((extend_merge_kernel<DD, kExFewRows>), dim3(kExMergeWgs), block, 0, s, a); \
-    else hipLaunchKernelGGL((extend_merge_kernel<DD, kExTileRows>), dim3(kExMergeWgs), block, 0, s, a)
+    if (a.few) hipLaunchKernelGGL((extend_merge_kernel<DD, kExFewRows>), dim3(kExMergeWgs), block, 0, s, a.desc, a.spans, a); \
+    else hipLaunchKernelGGL((extend_merge_kernel<DD, kExTileRows>), dim3(kExMergeWgs), block, 0, s, a.desc, a.spans, a)
     if (a.D == 128) {
         RA_EX_MERGE(128);
     } else {

@@ -215,8 +215,12 @@ template <int D, RowsTo TO, int N> __device__ __forceinline__ void rows_of_wave(
     }
 }
 
-template <int D, RowsTo TO, int N> __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(RowsLaunch a)
+template <int D, RowsTo TO, int N> __global__ __launch_bounds__(64 * kRowWaves) void rows_kernel(const uint16_t *__restrict__ q, const uint16_t *__restrict__ k, int64_t q_stride, int64_t k_stride, int T,
+                                                                                    int Hq, int Hkv, int slots_shift, RowsLaunch given)
 {
+    RowsLaunch a = given; // (what the first loads need is in registers when a wave starts)
+    a.q = q, a.k = k, a.q_stride = q_stride, a.k_stride = k_stride, a.T = T, a.Hq = Hq, a.Hkv = Hkv, a.slots_shift = slots_shift;
+    touch_lines(given);
     rows_of_wave<D, TO, N>(a, blockIdx.x * kRowWaves + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), threadIdx.x & 63);
 }
 
@@ -241,8 +245,10 @@ template <int D, RowsTo TO> static hipError_t launch_rows(RowsLaunch &a, int num
     if (many) units = rows_units<D>(a, rows, 4);
     const int64_t groups = (units + kRowWaves - 1) / kRowWaves;
     if (groups > INT32_MAX) return hipErrorInvalidValue;
-    if (many) hipLaunchKernelGGL((rows_kernel<D, TO, 4>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, a);
-    else hipLaunchKernelGGL((rows_kernel<D, TO, 1>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, a);
+#define RA_ROWS(a) a.q, a.k, a.q_stride, a.k_stride, a.T, a.Hq, a.Hkv, a.slots_shift, a
+    if (many) hipLaunchKernelGGL((rows_kernel<D, TO, 4>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, RA_ROWS(a));
+    else hipLaunchKernelGGL((rows_kernel<D, TO, 1>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, RA_ROWS(a));
+#undef RA_ROWS
     return hipGetLastError();
 }
 
@@ -397,8 +403,11 @@ template <int D> __device__ __forceinline__ void page_of_wave(const RowsLaunch &
     if (lane == 0) *scale_ptr = s;
 }
 
-template <int D, int N> __global__ __launch_bounds__(64 * kRowWaves) void append_pages_kernel(RowsLaunch a, int page_groups, int page_units)
+template <int D, int N> __global__ __launch_bounds__(64 * kRowWaves) void append_pages_kernel(const int32_t *__restrict__ cu, int B, int Hkv, int page_groups, int page_units, RowsLaunch given)
 {
+    RowsLaunch a = given;
+    a.cu = cu, a.B = B, a.Hkv = Hkv;
+    touch_lines(given);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
     if ((int)blockIdx.x < page_groups) {
         const int unit = blockIdx.x * kRowWaves + wave;
@@ -424,7 +433,7 @@ hipError_t launch_append_chunk(const RowsLaunch &given, int kv_fp8, int num_cus,
     const int64_t groups = page_groups + (row_units + kRowWaves - 1) / kRowWaves;
     if (groups > INT32_MAX || page_units > INT32_MAX) return hipErrorInvalidValue;
 #define RA_APPEND(DD, N) \
-    hipLaunchKernelGGL((append_pages_kernel<DD, N>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, a, (int)page_groups, (int)page_units)
+    hipLaunchKernelGGL((append_pages_kernel<DD, N>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, a.cu, a.B, a.Hkv, (int)page_groups, (int)page_units, a)
     if (a.D == 128) {
         if (many) RA_APPEND(128, 4);
         else RA_APPEND(128, 1);
