@@ -156,8 +156,8 @@ typedef struct {
 ra_status rollout_attn_check_extend(const ra_extend *extend, char *msg, size_t msg_len);
 
 /* Bytes of device workspace rollout_attn_extend needs for this shape (only the dimensions, the
- * page counts and kv_dtype are read).  ctx may
- * be NULL: the size for a 256-compute-unit device is returned. */
+ * page counts and kv_dtype are read).  ctx may be NULL: the
+ * size for a 256-compute-unit device is returned.  0 (a batch of short sequences): none, and it may be NULL. */
 ra_status rollout_attn_extend_workspace_size(const ra_ctx *ctx, const ra_extend *shape_only, size_t *bytes);
 
 /* Enqueues the attention on hip_stream: at most three kernels.  workspace as for rollout_attn_decode: dev memory of at

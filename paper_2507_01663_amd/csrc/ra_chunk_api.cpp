@@ -257,7 +257,7 @@ ra_status rollout_attn_extend(ra_ctx *c, const ra_extend *p, void *workspace, si
     size_t need = 0;
     const ra_status sized = rollout_attn_extend_workspace_size(c, p, &need);
     if (sized != RA_OK) return sized;
-    if (!workspace || ((uintptr_t)workspace & 255)) { set_err(c, "workspace is NULL or not 256-byte aligned"); return RA_ERR_INVALID_ARG; }
+    if (need && (!workspace || ((uintptr_t)workspace & 255))) { set_err(c, "workspace is NULL or not 256-byte aligned"); return RA_ERR_INVALID_ARG; }
     if (workspace_bytes < need) {
         set_err(c, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
         return RA_ERR_WORKSPACE_TOO_SMALL;

@@ -69,6 +69,12 @@ template <int ROWS> __device__ __forceinline__ int ex_stages(const ExtendLaunch 
     last = s.L - s.n + (last < s.n - 1 ? last : s.n - 1);
     return (last + 32) >> 5; // (last >= -n: no key at all gives a number of zero or less)
 }
+// ... where x is often below 64 y: the multiples of y up to x are counted.
+__device__ __forceinline__ int ex_div_short(int x, int y)
+{
+    if (x >= 64 * y) return ex_div(x, y);
+    return __popcll(__ballot((int)(threadIdx.x & 63) * y <= x)) - 1;
+}
 
 // What the sequence of t0, t1 (where its chunk starts and ends) and length L is.  (A workgroup comes past everything up to its
 // first keys once and alone, an instruction after the other: they are few.)
@@ -160,7 +166,7 @@ template <int ROWS> struct ExLine {
         }
         q = ex_div(total, spans);
         r = total - q * spans;
-        cut = q >> 3 > a.least ? q >> 3 : a.least;
+        cut = q >> 3 > a.cut ? q >> 3 : a.cut;
         // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.
         unit = blocks * a.Hkv >= 2 * a.spans && !__any(longest > q);
     }
@@ -169,7 +175,8 @@ template <int ROWS> struct ExLine {
     __device__ __forceinline__ int last_of(int x1) const
     {
         const int y = x1 - 1, big = r * (q + 1);
-        const int k = y < big ? ex_div(y, q + 1) : r + ex_div(y - big, q); // the last one that starts before x1
+        const bool in_big = y < big;
+        const int k = (in_big ? 0 : r) + ex_div(in_big ? y : y - big, in_big ? q + 1 : q); // the last one that starts before x1
         return x1 - raw(k) < kExEdge ? k - 1 : k;                          // (but for a cut that moves there)
     }
     // Where a cut at x goes in the item of that length that starts at x0: nowhere into short items, and not so near an end of
@@ -222,7 +229,7 @@ template <int ROWS, bool BLOCKS> __device__ __forceinline__ int ex_sequence_at(c
 template <int ROWS> __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExKnown *known, int x, ExPlace &p)
 {
     const int y = ex_sequence_at<ROWS, false>(a, line, known, x, p);
-    p.item = ex_div(y, p.s.cost);
+    p.item = ex_div_short(y, p.s.cost);
     p.x0 = x - y + p.item * p.s.cost;
 }
 
@@ -237,7 +244,7 @@ struct ExPart {
 template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch &a, const ExPlace &p, int y0, int y1, int span)
 {
     ExPart t;
-    t.kvh = ex_div(p.item, p.s.blocks);
+    t.kvh = ex_div_short(p.item, p.s.blocks);
     const int jj = p.item - t.kvh * p.s.blocks, j = jj & 1 ? p.s.blocks - 1 - (jj >> 1) : jj >> 1;
     t.row0 = ROWS * j;
     t.rows = p.s.n * a.G;
@@ -262,38 +269,69 @@ template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch
 // desc[2 k + 1] = {first packed token, first row, rows, kv head}, {last span, -, -, -}.
 template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, uint8_t *lds, F &&work)
 {
+    const int die = (int)blockIdx.x & 7, at = (int)blockIdx.x >> 3;
+    const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift, heads = a.Hkv >> gg_shift;
+    const int first_head = die & ((1 << gg_shift) - 1), share = (at << s_shift) + (die >> gg_shift);
     const ExKnown *known = a.B <= kExKnown ? (ExKnown *)lds : nullptr;
     ExLine<ROWS> line;
-    line.measure(a, (ExKnown *)lds);
-    const int die = (int)blockIdx.x & 7, at = (int)blockIdx.x >> 3;
-    const int per = (line.spans + 7) >> 3, k = at < per ? die * per + at : (int)blockIdx.x; // (past the spans: one that does not exist)
-    int last = 0, x = 0, end = 0, step = 0;
-    int4 begun = {0, 0, 0, 0};
     ExPlace p;
+    ExPart part;
     p.item = 0, p.x0 = 0;
-    const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift, heads = a.Hkv >> gg_shift;
-    if (line.unit) {
-        x = (at << s_shift) + (die >> gg_shift), end = line.blocks * heads;
-        step = (int)gridDim.x >> 3 << s_shift; // (there are as many workgroups as items, if the call's sizes are what they say)
-    } else if (line.total > 0 && at < per && k < line.spans) {
-        // `end` is moved where the span gets to it
-        end = k + 1 < line.spans ? line.raw(k + 1) : line.total, x = line.raw(k);
-        ex_find<ROWS>(a, line, known, x, p);
-        x = line.moved(x, p.x0, p.s.cost);
-        if (x == p.x0 + p.s.cost) {
-            if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
-            else if (x < end) ex_find<ROWS>(a, line, known, x, p);
+    int last = 0, x = 0, end = 0, step = 0, k = 0;
+    int4 begun = {0, 0, 0, 0};
+    if (a.direct) {
+        // Every item is short: a workgroup for each, and no line.  Blocks are numbered without counting them: sequence b's
+        // are given the numbers from cu[b] G / ROWS + b on, which leaves it as many as it can have.
+        const int number = ex_div_short(share, heads), lane = threadIdx.x & 63;
+        int j = 0;
+        p.b = number;
+        if (ROWS != kExFewRows) { // (few rows are one block)
+            p.b = -1;
+#pragma unroll 1
+            for (int base = 0; base < a.B; base += 64) {
+                const int start = base + lane < a.B ? (int)((int64_t)a.cu[base + lane] * a.G / ROWS) + base + lane : INT32_MAX;
+                const unsigned long long m = __ballot(start <= number);
+                if (!m) break;
+                const int l = 63 - __builtin_clzll(m);
+                p.b = base + l, j = number - __builtin_amdgcn_readlane(start, l);
+                if (l < 63) break;
+            }
+        }
+        if (p.b < 0 || p.b >= a.B) return;
+        p.s = ex_sequence<ROWS>(a, uniform_load(a.cu, p.b), uniform_load(a.cu, p.b + 1), uniform_load(a.seq_lens, p.b));
+        if (j < 0 || j >= p.s.blocks) return;
+        part.kvh = ((share - number * heads) << gg_shift) + first_head;
+        part.row0 = ROWS * j, part.rows = p.s.n * a.G;
+        part.lo = 0, part.hi = ex_stages<ROWS>(a, p.s, j), part.slot = -1;
+        part.hi = part.hi < 0 ? 0 : part.hi;
+        end = 1;
+    } else {
+        line.measure(a, (ExKnown *)lds);
+        const int per = (line.spans + 7) >> 3;
+        k = at < per ? die * per + at : (int)blockIdx.x; // (past the spans: one that does not exist)
+        if (line.unit) {
+            x = share, end = line.blocks * heads;
+            step = (int)gridDim.x >> 3 << s_shift; // (there are as many workgroups as items, if the call's sizes are what they say)
+        } else if (line.total > 0 && at < per && k < line.spans) {
+            // `end` is moved where the span gets to it
+            end = k + 1 < line.spans ? line.raw(k + 1) : line.total, x = line.raw(k);
+            ex_find<ROWS>(a, line, known, x, p);
+            x = line.moved(x, p.x0, p.s.cost);
+            if (x == p.x0 + p.s.cost) {
+                if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
+                else if (x < end) ex_find<ROWS>(a, line, known, x, p);
+            }
         }
     }
-    bool first = true;
+    bool first = !a.direct;
     while (x < end) {
-        ExPart part;
-        int next;
-        if (line.unit) {
+        int next = 1;
+        if (a.direct) {
+        } else if (line.unit) {
             const int at_block = ex_div(x, heads);
             const int i = x - (at_block - ex_sequence_at<ROWS, true>(a, line, first ? known : nullptr, at_block, p)) * heads;
-            const int h = ex_div(i, p.s.blocks); // (a sequence's items: its blocks times heads)
-            p.item = i + ((h << gg_shift) + (die & ((1 << gg_shift) - 1)) - h) * p.s.blocks;
+            const int h = ex_div_short(i, p.s.blocks); // (a sequence's items: its blocks times heads)
+            p.item = i + ((h << gg_shift) + first_head - h) * p.s.blocks;
             part = ex_part<ROWS>(a, p, 0, p.s.cost, 0);
             next = x + step;
         } else {
@@ -315,7 +353,7 @@ template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const Ex
         if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
         else ex_find<ROWS>(a, line, nullptr, x, p);
     }
-    if (threadIdx.x == 0 && k < a.spans) { // (every span is answered for, also one that does not exist)
+    if (threadIdx.x == 0 && !a.direct && k < a.spans) { // (every span is answered for, also one that does not exist)
         a.desc[2 * k] = begun;
         a.desc[2 * k + 1] = make_int4(last, 0, 0, 0);
     }

@@ -3,27 +3,32 @@
 
 namespace ra {
 
-constexpr int kExLeast = 10, kExLeastFew = 16; // length of a span on the line at least
-
 // Which kernel a call takes, its workgroups, and how finely the work is cut.
+// An item of S stages that is cut in two saves half of them, and pays for a second workgroup's fixed part and the merge, a
+// kernel of its own: kExCut.
+constexpr int kExLeast = 10, kExLeastFew = 16, kExCut = 20, kExCutFew = 32;
 static void extend_shape(ExtendLaunch &a)
 {
     a.few = (int64_t)a.max_chunk * a.G <= kExFewRows;
-    const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExTileRows + a.B;
-    const int64_t line = blocks * a.Hkv * (a.max_pages / 2 + 1 + (a.few ? kExFixed<kExFewRows> : kExFixed<kExTileRows>) + 1); // its length at most
+    const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExTileRows + a.B, items = blocks * a.Hkv;
+    const int longest = a.max_pages / 2 + 1 + (a.few ? kExFixed<kExFewRows> : kExFixed<kExTileRows>); // an item at most
     a.least = a.few ? kExLeastFew : kExLeast;
+    a.cut = a.few ? kExCutFew : kExCut;
+    a.direct = longest <= a.cut;
     const int64_t resident = (int64_t)(a.num_cus < 8 ? 8 : a.num_cus & ~7) * (a.few ? (a.D == 64 ? 2 : 1) : (a.D == 64 ? 3 : 2));
-    int64_t spans = (line / a.least + 7) & ~(int64_t)7;
+    int64_t spans = (items * longest / a.least + 7) & ~(int64_t)7;
     spans = spans < 8 ? 8 : spans < resident ? spans : resident;
     a.spans = (int)(spans < kExMaxSpans ? spans : kExMaxSpans);
-    // (a workgroup for every item where there may be so many that they are left whole: see ExLine::measure)
-    const int64_t items = blocks * a.Hkv;
-    a.grid = (int)(items >= 2 * a.spans ? (items + 7) & ~(int64_t)7 : a.spans);
+    // (a workgroup for every item where items are left whole, or may be: see ex_walk, and ExLine::measure)
+    const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift;
+    const int64_t each = 8 * ((blocks * (a.Hkv >> gg_shift) + (1 << s_shift) - 1) >> s_shift);
+    a.grid = (int)(a.direct || items >= 2 * a.spans ? each : a.spans);
 }
 
 size_t carve_extend(ExtendLaunch &a, void *base)
 {
     extend_shape(a);
+    if (a.direct) return 0;
     const int64_t slots = 2 * (int64_t)a.spans, rows = a.few ? kExFewRows : kExTileRows;
     size_t at = 0;
     auto take = [&](size_t bytes) {
@@ -70,7 +75,7 @@ hipError_t launch_extend(const ExtendLaunch &a, hipStream_t s)
 #undef RA_EX_LAUNCH
     }
     hipError_t e = hipGetLastError();
-    if (e != hipSuccess || a.max_pages / 2 + 2 + (a.few ? kExFixed<kExFewRows> : kExFixed<kExTileRows>) <= a.least) return e; // (no item is long enough to be cut)
+    if (e != hipSuccess || a.direct) return e;
 #define RA_EX_MERGE(DD) \
     if (a.few) hipLaunchKernelGGL((extend_merge_kernel<DD, kExFewRows>), dim3(kExMergeWgs), block, 0, s, a.desc, a.spans, a); \
     else hipLaunchKernelGGL((extend_merge_kernel<DD, kExTileRows>), dim3(kExMergeWgs), block, 0, s, a.desc, a.spans, a)

@@ -131,6 +131,8 @@ def test_check_extend():
 
 def test_extend_workspace_size():
     p = extend()
+    assert ra.rollout_attn_extend_workspace_size(None, p) % 256 == 0
+    p.max_pages_per_seq = 200                                          # long enough to be shared by workgroups
     n = ra.rollout_attn_extend_workspace_size(None, p)
     assert n > 0 and n % 256 == 0
     p.D = 100
