@@ -45,9 +45,9 @@ struct ExtendLaunch {
     const void *zeros;
     float *part_o, *part_lse;    // partial results, two slots per span
     int4 *desc;                  // [spans][2] what the merge adds up
-    // (set by carve_extend) workgroups that share the work, workgroups launched, length of a span and of an item that is cut at
-    // least, whether every sequence has few rows, and whether no item can be cut
-    int32_t spans, grid, least, cut, few, direct;
+    // (set by carve_extend) workgroups that share the work, workgroups launched, length of a span at least, whether every
+    // sequence is one block, and whether no item is long enough to be cut
+    int32_t spans, grid, least, few, direct;
 };
 // How a call is launched (from B, T, max_chunk, Hkv, G, D, max_pages and num_cus), and its workspace: the bytes; places the pointers
 // when base is not null.

@@ -4,11 +4,11 @@
 // head r % G, and sees the keys up to L - n + r / G.  Packed that way 32 rows are a few tokens, so under the causal mask
 // they need the same keys but for the last one or two stages of 32.
 //
-// Many rows are bound by the matrix cores: extend_tile_kernel, whose workgroup takes a block of 128 rows, 32 to a wave, all
-// waves multiplying every stage of 32 keys that streams through one LDS ring:
+// A workgroup of four waves takes a block of up to 128 rows.  Many are bound by the matrix cores and the vector work between:
+// 32 to a wave, all waves multiplying every stage of 32 keys that streams through one LDS ring:
 //   S^T[key, row] = K . Q^T,   O^T[d, row] += V^T . P^T     (32x32x16 MFMA, binary32 sums, softmax running per row)
-// Few rows are bound by the stream of pages: extend_few_kernel, whose four waves stream stages of their own (every fourth
-// one) through rings of their own and multiply them with all of the up to 32 rows; what they have is added up in LDS.
+// Where no sequence has more than 64, they are bound by the stream of pages: every wave multiplies stages of its own with all
+// the rows, and what the waves have is added up in LDS (ex_narrow).
 //
 // The work is a line of items, one per (sequence, kv head, block), each as long as it has stages, and the line is cut into
 // as many spans of one length as workgroups are resident, so that ragged lengths load them alike.  Every workgroup finds its
@@ -34,8 +34,7 @@ constexpr int kExWaves = 4;
     a.magic_g = magic_g, a.spans = spans;                                                                                       \
     touch_lines(given)
 #define EX_GIVE(a) (a).cu, (a).seq_lens, (a).B, (a).T, (a).max_chunk, (a).max_pages, (a).G, (a).Hkv, (a).magic_g, (a).spans, (a)
-constexpr int kExTileRows = kPfRows * kExWaves; // rows of a block of the tile kernel
-constexpr int kExFewRows = 32;                  // rows of a sequence and kv head up to which the other one takes them
+constexpr int kExRows = kPfRows * kExWaves; // rows of a block
 
 // ---- the line of items and its spans ------------------------------------------------------------------
 
@@ -45,8 +44,8 @@ struct ExSeq {
 };
 
 // What an item costs beside its stages, in stages: finding it, its query rows, the first trip to memory, its results.
-template <int ROWS> constexpr int kExFixed = ROWS == kExTileRows ? 4 : 8;
-constexpr int kExEdge = 2; // no part of an item has fewer stages than this (about; a span is longer than kExFixed + 2 kExEdge)
+constexpr int kExFixed = 4;
+constexpr int kExEdge = 2; // no part of an item is shorter than this (a span is longer than kExFixed + 2 kExEdge)
 
 __device__ __forceinline__ int ex_uni(int x) { return __builtin_amdgcn_readfirstlane(x); } // (a quotient comes from the vector unit)
 // x / y for 0 <= x < 2^30, y > 0, both the wave's: the quotient by the reciprocal in binary32 is off by x / y 2^-22 at most, the
@@ -63,9 +62,9 @@ __device__ __forceinline__ int ex_div(int x, int y)
 __device__ __forceinline__ int ex_div_g(const ExtendLaunch &a, int r) { return pf_div(r, a.G, a.magic_g); }
 
 // Stages that block j of a sequence needs: up to the one with its last row's last key.
-template <int ROWS> __device__ __forceinline__ int ex_stages(const ExtendLaunch &a, const ExSeq &s, int j)
+__device__ __forceinline__ int ex_stages(const ExtendLaunch &a, const ExSeq &s, int j)
 {
-    int last = ex_div_g(a, ROWS * (j + 1) - 1);
+    int last = ex_div_g(a, kExRows * (j + 1) - 1);
     last = s.L - s.n + (last < s.n - 1 ? last : s.n - 1);
     return (last + 32) >> 5; // (last >= -n: no key at all gives a number of zero or less)
 }
@@ -76,9 +75,12 @@ __device__ __forceinline__ int ex_div_short(int x, int y)
     return __popcll(__ballot((int)(threadIdx.x & 63) * y <= x)) - 1;
 }
 
+// The length on the line of a number of stages, where sequences have up to so many rows: few rows take four at a time.
+__host__ __device__ __forceinline__ int ex_weight(int stages, int most) { return most > 64 ? stages : stages * (most > 32 ? 14 : 9) >> 5; }
+
 // What the sequence of t0, t1 (where its chunk starts and ends) and length L is.  (A workgroup comes past everything up to its
 // first keys once and alone, an instruction after the other: they are few.)
-template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int t1, int L)
+__device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int t1, int L)
 {
     ExSeq s = {0, 0, 0, 0, 0};
     const int n = t1 - t0, most = a.max_pages * kPage;
@@ -86,14 +88,14 @@ template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLau
     s.t0 = t0;
     s.n = n < a.max_chunk ? n : a.max_chunk;
     s.L = L < 0 ? 0 : (L < most ? L : most);
-    s.blocks = (s.n * a.G + ROWS - 1) / ROWS;
+    s.blocks = (s.n * a.G + kExRows - 1) / kExRows;
     const int mean = (s.L - (s.n >> 1) + 48) >> 5; // keys that a row sees, in stages
-    s.cost = kExFixed<ROWS> + (mean > 1 ? mean : 1);
+    s.cost = kExFixed + 1 + (mean > 0 ? ex_weight(mean, a.max_chunk * a.G) : 0);
     return s;
 }
-template <int ROWS> __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
+__device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
 {
-    return b < a.B ? ex_sequence<ROWS>(a, a.cu[b], a.cu[b + 1], a.seq_lens[b]) : ExSeq{0, 0, 0, 0, 0};
+    return b < a.B ? ex_sequence(a, a.cu[b], a.cu[b + 1], a.seq_lens[b]) : ExSeq{0, 0, 0, 0, 0};
 }
 
 // The line: lane c has chunk c of the sequences (64 of them, or a multiple of that in a very large batch).  Of a batch of up to
@@ -106,7 +108,7 @@ struct ExKnown {
 };
 static_assert(sizeof(ExKnown) <= 3 * Geo<64, 2>::kStage, "it fits the smallest ring");
 
-template <int ROWS> struct ExLine {
+struct ExLine {
     int lane, sub, chunks;   // sixty-fours of sequences in a chunk
     int unit;                // items are left whole (see measure)
     int before, total;       // start of this lane's chunk
@@ -140,7 +142,7 @@ template <int ROWS> struct ExLine {
 #pragma unroll
                 for (int i = 0; i < AT; i++) {
                     if (c0 + i >= chunks) break;
-                    const ExSeq s = ex_sequence<ROWS>(a, t0[i], t1[i], len[i]);
+                    const ExSeq s = ex_sequence(a, t0[i], t1[i], len[i]);
                     if (lane == c0 + i) before = total, before_blocks = blocks;
                     int at, at_blocks;
                     add(s, at, at_blocks);
@@ -155,7 +157,7 @@ template <int ROWS> struct ExLine {
             for (int c = 0; c < chunks * sub; c++) {
                 if (lane * sub == c) before = total, before_blocks = blocks;
                 int at, at_blocks;
-                add(ex_sequence<ROWS>(a, 64 * c + lane), at, at_blocks);
+                add(ex_sequence(a, 64 * c + lane), at, at_blocks);
             }
         }
         if (lane >= chunks) before = before_blocks = INT32_MAX;
@@ -166,7 +168,7 @@ template <int ROWS> struct ExLine {
         }
         q = ex_div(total, spans);
         r = total - q * spans;
-        cut = q >> 3 > a.cut ? q >> 3 : a.cut;
+        cut = q >> 3 > a.least ? q >> 3 : a.least;
         // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.
         unit = blocks * a.Hkv >= 2 * a.spans && !__any(longest > q);
     }
@@ -184,7 +186,7 @@ template <int ROWS> struct ExLine {
     __device__ __forceinline__ int moved(int x, int x0, int cost) const
     {
         const int y = x - x0, left = cost - y;
-        const bool down = cost > cut ? y < kExFixed<ROWS> + kExEdge : y < left, up = cost > cut ? left < kExEdge : true;
+        const bool down = cost > cut ? y < kExFixed + kExEdge : y < left, up = cost > cut ? left < kExEdge : true;
         return down ? x0 : up ? x0 + cost : x;
     }
 };
@@ -197,7 +199,7 @@ struct ExPlace {
 
 // The sequence that x lies in (0 <= x < total), x counted as the line is or (BLOCKS) in blocks of one kv head; returns x's
 // distance from its start.
-template <int ROWS, bool BLOCKS> __device__ __forceinline__ int ex_sequence_at(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExKnown *known, int x, ExPlace &p)
+template <bool BLOCKS> __device__ __forceinline__ int ex_sequence_at(const ExtendLaunch &a, const ExLine &line, const ExKnown *known, int x, ExPlace &p)
 {
     const int chunk_before = BLOCKS ? line.before_blocks : line.before;
     const int c = 63 - __builtin_clzll(__ballot(chunk_before <= x));
@@ -211,7 +213,7 @@ template <int ROWS, bool BLOCKS> __device__ __forceinline__ int ex_sequence_at(c
 #pragma unroll 1
         for (int i = 0;; i++) {
             base = (c * line.sub + i) * 64;
-            s = ex_sequence<ROWS>(a, base + line.lane);
+            s = ex_sequence(a, base + line.lane);
             int t;
             before = start + wave_scan(BLOCKS ? s.blocks : a.Hkv * s.blocks * s.cost, line.lane, t);
             if (x < start + t || i + 1 == line.sub) break;
@@ -221,14 +223,14 @@ template <int ROWS, bool BLOCKS> __device__ __forceinline__ int ex_sequence_at(c
     const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && before <= x));
     p.b = base + l;
     const int t0 = __builtin_amdgcn_readlane(s.t0, l);
-    p.s = ex_sequence<ROWS>(a, t0, t0 + __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.L, l));
+    p.s = ex_sequence(a, t0, t0 + __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.L, l));
     return x - __builtin_amdgcn_readlane(before, l);
 }
 
 // The item that x lies in.
-template <int ROWS> __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<ROWS> &line, const ExKnown *known, int x, ExPlace &p)
+__device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine &line, const ExKnown *known, int x, ExPlace &p)
 {
-    const int y = ex_sequence_at<ROWS, false>(a, line, known, x, p);
+    const int y = ex_sequence_at<false>(a, line, known, x, p);
     p.item = ex_div_short(y, p.s.cost);
     p.x0 = x - y + p.item * p.s.cost;
 }
@@ -241,18 +243,18 @@ struct ExPart {
 };
 
 // The blocks of a (sequence, kv head) come from both ends in turn: their mean cost is the line's.
-template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch &a, const ExPlace &p, int y0, int y1, int span)
+__device__ __forceinline__ ExPart ex_part(const ExtendLaunch &a, const ExPlace &p, int y0, int y1, int span)
 {
     ExPart t;
     t.kvh = ex_div_short(p.item, p.s.blocks);
     const int jj = p.item - t.kvh * p.s.blocks, j = jj & 1 ? p.s.blocks - 1 - (jj >> 1) : jj >> 1;
-    t.row0 = ROWS * j;
+    t.row0 = kExRows * j;
     t.rows = p.s.n * a.G;
-    int stages = ex_uni(ex_stages<ROWS>(a, p.s, j));
+    int stages = ex_uni(ex_stages(a, p.s, j));
     stages = stages < 0 ? 0 : stages;
     // (a place inside the item, in proportion: the same for the two parts that it divides)
     auto stage_at = [&](int y) __attribute__((always_inline)) {
-        return ex_uni((int)((float)stages * ((float)(y - kExFixed<ROWS>) * __builtin_amdgcn_rcpf((float)(p.s.cost - kExFixed<ROWS>)))));
+        return ex_uni((int)((float)stages * ((float)(y - kExFixed) * __builtin_amdgcn_rcpf((float)(p.s.cost - kExFixed)))));
     };
     t.lo = y0 == 0 ? 0 : stage_at(y0);
     t.hi = y1 == p.s.cost ? stages : stage_at(y1);
@@ -267,13 +269,13 @@ template <int ROWS> __device__ __forceinline__ ExPart ex_part(const ExtendLaunch
 // same keys run side by side on few of them.
 // Else: a die takes neighbouring spans.  Also tells the merge which items begin in a span and end in another: desc[2 k],
 // desc[2 k + 1] = {first packed token, first row, rows, kv head}, {last span, -, -, -}.
-template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, uint8_t *lds, F &&work)
+template <typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, uint8_t *lds, F &&work)
 {
     const int die = (int)blockIdx.x & 7, at = (int)blockIdx.x >> 3;
     const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift, heads = a.Hkv >> gg_shift;
     const int first_head = die & ((1 << gg_shift) - 1), share = (at << s_shift) + (die >> gg_shift);
     const ExKnown *known = a.B <= kExKnown ? (ExKnown *)lds : nullptr;
-    ExLine<ROWS> line;
+    ExLine line;
     ExPlace p;
     ExPart part;
     p.item = 0, p.x0 = 0;
@@ -281,15 +283,15 @@ template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const Ex
     int4 begun = {0, 0, 0, 0};
     if (a.direct) {
         // Every item is short: a workgroup for each, and no line.  Blocks are numbered without counting them: sequence b's
-        // are given the numbers from cu[b] G / ROWS + b on, which leaves it as many as it can have.
+        // are given the numbers from cu[b] G / kExRows + b on, which leaves it as many as it can have.
         const int number = ex_div_short(share, heads), lane = threadIdx.x & 63;
         int j = 0;
         p.b = number;
-        if (ROWS != kExFewRows) { // (few rows are one block)
+        if (!a.few) {
             p.b = -1;
 #pragma unroll 1
             for (int base = 0; base < a.B; base += 64) {
-                const int start = base + lane < a.B ? (int)((int64_t)a.cu[base + lane] * a.G / ROWS) + base + lane : INT32_MAX;
+                const int start = base + lane < a.B ? (int)((int64_t)a.cu[base + lane] * a.G / kExRows) + base + lane : INT32_MAX;
                 const unsigned long long m = __ballot(start <= number);
                 if (!m) break;
                 const int l = 63 - __builtin_clzll(m);
@@ -298,11 +300,11 @@ template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const Ex
             }
         }
         if (p.b < 0 || p.b >= a.B) return;
-        p.s = ex_sequence<ROWS>(a, uniform_load(a.cu, p.b), uniform_load(a.cu, p.b + 1), uniform_load(a.seq_lens, p.b));
+        p.s = ex_sequence(a, uniform_load(a.cu, p.b), uniform_load(a.cu, p.b + 1), uniform_load(a.seq_lens, p.b));
         if (j < 0 || j >= p.s.blocks) return;
         part.kvh = ((share - number * heads) << gg_shift) + first_head;
-        part.row0 = ROWS * j, part.rows = p.s.n * a.G;
-        part.lo = 0, part.hi = ex_stages<ROWS>(a, p.s, j), part.slot = -1;
+        part.row0 = kExRows * j, part.rows = p.s.n * a.G;
+        part.lo = 0, part.hi = ex_stages(a, p.s, j), part.slot = -1;
         part.hi = part.hi < 0 ? 0 : part.hi;
         end = 1;
     } else {
@@ -315,11 +317,11 @@ template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const Ex
         } else if (line.total > 0 && at < per && k < line.spans) {
             // `end` is moved where the span gets to it
             end = k + 1 < line.spans ? line.raw(k + 1) : line.total, x = line.raw(k);
-            ex_find<ROWS>(a, line, known, x, p);
+            ex_find(a, line, known, x, p);
             x = line.moved(x, p.x0, p.s.cost);
             if (x == p.x0 + p.s.cost) {
                 if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
-                else if (x < end) ex_find<ROWS>(a, line, known, x, p);
+                else if (x < end) ex_find(a, line, known, x, p);
             }
         }
     }
@@ -329,17 +331,17 @@ template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const Ex
         if (a.direct) {
         } else if (line.unit) {
             const int at_block = ex_div(x, heads);
-            const int i = x - (at_block - ex_sequence_at<ROWS, true>(a, line, first ? known : nullptr, at_block, p)) * heads;
+            const int i = x - (at_block - ex_sequence_at<true>(a, line, first ? known : nullptr, at_block, p)) * heads;
             const int h = ex_div_short(i, p.s.blocks); // (a sequence's items: its blocks times heads)
             p.item = i + ((h << gg_shift) + first_head - h) * p.s.blocks;
-            part = ex_part<ROWS>(a, p, 0, p.s.cost, 0);
+            part = ex_part(a, p, 0, p.s.cost, 0);
             next = x + step;
         } else {
             const int x1 = p.x0 + p.s.cost;
             if (end < x1) end = line.moved(end, p.x0, p.s.cost);
             if (x >= end) break;
             next = x1 < end ? x1 : end;
-            part = ex_part<ROWS>(a, p, x - p.x0, next - p.x0, k);
+            part = ex_part(a, p, x - p.x0, next - p.x0, k);
             if (x == p.x0 && next < x1) {
                 begun = make_int4(p.s.t0, part.row0, part.rows, part.kvh);
                 last = line.last_of(x1);
@@ -351,7 +353,7 @@ template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const Ex
         x = next;
         if (x >= end || line.unit) continue;
         if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
-        else ex_find<ROWS>(a, line, nullptr, x, p);
+        else ex_find(a, line, nullptr, x, p);
     }
     if (threadIdx.x == 0 && !a.direct && k < a.spans) { // (every span is answered for, also one that does not exist)
         a.desc[2 * k] = begun;
@@ -362,7 +364,9 @@ template <int ROWS, typename F> __device__ __forceinline__ void ex_walk(const Ex
 // ---- values that a row does not see ---------------------------------------------------------------------
 //
 // In the stages that the causal mask cuts, a row's weight of a later token is zero, and zero times an infinite or NaN value
-// is NaN.  Where a V operand of such a stage holds one, its product is made key by key, each added only to rows that see it.
+// is NaN.  Where a V operand of such a stage holds one (which is looked for there alone), the product is made without these
+// values, and what they do to the rows that see them is added apart: a product of "infinite, or NaN" with "seen" for either
+// sign, and an infinity for every place where it is not zero.  NaN has both.
 
 __device__ __forceinline__ bool ex_odd(bf16x8 v)
 {
@@ -372,13 +376,48 @@ __device__ __forceinline__ bool ex_odd(bf16x8 v)
     for (int i = 0; i < 4; i++) odd = odd || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
     return odd;
 }
-// The operand with only element e of its eight kept.
-__device__ __forceinline__ bf16x8 ex_only(bf16x8 v, bool lanes, int e)
+// v without them; plus, minus: one where v has an infinity of that sign or a NaN.
+__device__ __forceinline__ bf16x8 ex_even(bf16x8 v, u32x4 &plus, u32x4 &minus)
 {
     u32x4 w = __builtin_bit_cast(u32x4, v);
 #pragma unroll
-    for (int i = 0; i < 4; i++) w[i] &= lanes && (e >> 1) == i ? 0xffffu << (16 * (e & 1)) : 0u;
+    for (int i = 0; i < 4; i++) {
+        unsigned keep = 0, up = 0, down = 0;
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const unsigned x = (w[i] >> (16 * h)) & 0xffffu, m = x & 0x7fffu;
+            if (m < 0x7f80u) keep |= x << (16 * h);
+            if (x == 0x7f80u || m > 0x7f80u) up |= 0x3f80u << (16 * h);
+            if (x == 0xff80u || m > 0x7f80u) down |= 0x3f80u << (16 * h);
+        }
+        w[i] = keep, plus[i] = up, minus[i] = down;
+    }
     return __builtin_bit_cast(bf16x8, w);
+}
+// The second operand of such a product: one where the lane's row sees the key.  Slot e of half hh of the sixteen keys from
+// `key` on is key 8 (e / 4) + 4 hh + e % 4.
+__device__ __forceinline__ bf16x8 ex_seen(int key, int lim, int hh)
+{
+    u32x4 w;
+#pragma unroll
+    for (int i = 0; i < 4; i++) {
+        w[i] = 0;
+#pragma unroll
+        for (int h = 0; h < 2; h++) {
+            const int e = 2 * i + h;
+            if (key + 8 * (e >> 2) + 4 * hh + (e & 3) <= lim) w[i] |= 0x3f80u << (16 * h);
+        }
+    }
+    return __builtin_bit_cast(bf16x8, w);
+}
+__device__ __forceinline__ void ex_add_odd(f32x16 &o, u32x4 of, bf16x8 seen, float infinity)
+{
+    f32x16 w;
+#pragma unroll
+    for (int e = 0; e < 16; e++) w[e] = 0.f;
+    w = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, of), seen, w, 0, 0, 0);
+#pragma unroll
+    for (int e = 0; e < 16; e++) o[e] += w[e] > 0.f ? infinity : 0.f;
 }
 
 // ---- many rows ------------------------------------------------------------------------------------------
@@ -512,17 +551,10 @@ __device__ __forceinline__ void ex_step(PfState<D> &st, uint32_t k_next, uint32_
         const bf16x8 vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(vr[dt][kk][0], vr[dt][kk][1], 0, 1, 2, 3, 4, 5, 6, 7));
         const bf16x8 pf = __builtin_bit_cast(bf16x8, pw[kk]);
         if ((MASK || !NEXT) && __builtin_expect(__any(ex_odd(vf)), 0)) {
-#pragma unroll 1
-            for (int i = 0; i < 16; i++) { // key 8 (e / 4) + 4 h + e % 4 of the sixteen: element e of the lanes of half h
-                const int e = i & 7, h = i >> 3;
-                f32x16 t;
-#pragma unroll
-                for (int x = 0; x < 16; x++) t[x] = 0.f;
-                t = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ex_only(vf, hh == h, e), pf, t, 0, 0, 0);
-                const bool sees = key + 16 * kk + 8 * (e >> 2) + 4 * h + (e & 3) <= lim;
-#pragma unroll
-                for (int x = 0; x < 16; x++) st.o[dt][x] += sees ? t[x] : 0.f;
-            }
+            u32x4 plus, minus;
+            const bf16x8 even = ex_even(vf, plus, minus), seen = ex_seen(key + 16 * kk, lim, hh);
+            st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(even, pf, st.o[dt], 0, 0, 0);
+            ex_add_odd(st.o[dt], plus, seen, INFINITY), ex_add_odd(st.o[dt], minus, seen, -INFINITY);
         } else {
             st.o[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, st.o[dt], 0, 0, 0);
         }
@@ -546,6 +578,301 @@ __device__ __forceinline__ void ex_step(PfState<D> &st, uint32_t k_next, uint32_
 #undef EX_FENCE
 }
 
+// ---- few rows -------------------------------------------------------------------------------------------
+//
+// A block of up to 32 NG rows keeps one or two waves busy with a stage that all four wait for.  Here every wave multiplies
+// stages of its own (every fourth one of the part) with all the rows, as they land in a place of its own: K and V in turn,
+// each asked for as soon as the operands before it are in registers, so that a wave has 32 keys on the way while it works on
+// others and no wave waits for another.  What the waves have is added up in LDS.  The query rows, which all waves read, lie in
+// LDS like a K tile.
+
+template <int D, bool FP8> struct ExNarrowLds {
+    using G = Geo<D, FP8 ? 1 : 2>;
+    static constexpr int kWave = 4 * G::kTile;             // K and V of a stage, as stored
+    static constexpr int kScales = kExWaves * kWave;        // e4m3: each wave's scales
+    static constexpr int kNeeds = kScales + (FP8 ? kExWaves * 256 : 0);
+    static constexpr int kRows = 2 * 32 * D * 2;            // the query rows, behind the ring in the waves' areas
+    // in the end, over all of it: the waves' sums of 32 rows, 64 d of them at a time, and maximum and sum of these rows
+    static constexpr int kSum = 32 * 64 * 4, kStats = kExWaves * kSum, kEnds = kStats + kExWaves * 32 * 8;
+};
+
+template <int D, bool FP8, int NG, typename LC>
+__device__ __forceinline__ void ex_narrow(const ExtendLaunch &a, const ExPlace &p, const ExPart &t, const LC &lc, const PfLane<D> &pl, uint8_t *lds,
+                                          uint8_t *areas, int lane, int wave)
+{
+    using G = Geo<D, 2>;
+    using P = Geo<D, FP8 ? 1 : 2>;
+    using X = ExNarrowLds<D, FP8>;
+    typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
+    typedef bf16x8 __attribute__((address_space(3))) * lds_bf16x8;
+    typedef short s16x8 __attribute__((ext_vector_type(8)));
+    typedef int __attribute__((ext_vector_type(2))) i32x2;
+    typedef i32x2 __attribute__((address_space(3))) * lds_i32x2;
+    typedef float f32x2 __attribute__((ext_vector_type(2)));
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    constexpr int KS = D / 16, DT = D / 32, UM = G::kUnits - 1, PUM = P::kUnits - 1;
+    const int n = lane & 31, hh = lane >> 5, shift = p.s.L - p.s.n;
+    const uint32_t lds_addr = (uint32_t)(uintptr_t)lds, q_addr = (uint32_t)(uintptr_t)areas;
+    const uint32_t k_addr = lds_addr + wave * X::kWave, v_addr = k_addr + 2 * P::kTile, scale_addr = lds_addr + X::kScales + 256 * wave;
+
+    // the wave's stages of the part: wave, wave + 4, ...
+    const int left = t.hi - t.lo - wave, mine = left > 0 ? (left + kExWaves - 1) / kExWaves : 0;
+    const int32_t *const pages = a.table + (int64_t)p.b * a.max_pages;
+    const int count = (p.s.L + kPage - 1) / kPage, last_page = count > 0 ? count - 1 : 0;
+    const int64_t head_b = (int64_t)t.kvh * a.stride_head_b;
+    auto page_id = [&](int i, int h) __attribute__((always_inline)) { // (a page that does not exist takes the last one's place, and none of its rows are read)
+        const int g = 2 * (t.lo + wave + kExWaves * i) + h;
+        return uniform_load(pages, g < last_page ? g : last_page);
+    };
+    int id0 = 0, id1 = 0, next0 = 0, next1 = 0; // pages of the stage whose K was asked for last, and of the one after it
+    auto load_k = [&](int i) __attribute__((always_inline)) {
+        const int nv = p.s.L - 32 * (t.lo + wave + kExWaves * i);
+        id0 = next0, id1 = next1;
+        if (i + 1 < mine) next0 = page_id(i + 1, 0), next1 = page_id(i + 1, 1);
+        issue_tile<D, FP8 ? 1 : 2, true>(lc, a.k_pool + (int64_t)id0 * a.stride_page_b + head_b, nv, k_addr, a.zeros);
+        issue_tile<D, FP8 ? 1 : 2, true>(lc, a.k_pool + (int64_t)id1 * a.stride_page_b + head_b, nv - kPage, k_addr + P::kTile, a.zeros);
+        if (FP8) { // lanes 0..3 bring K and V scale of the first page, K and V scale of the second
+            const void *src = a.zeros;
+            if (lane < 4 && ((lane & 2) ? nv - kPage : nv) > 0) src = ((lane & 1) ? a.v_scale : a.k_scale) + (int64_t)((lane & 2) ? id1 : id0) * a.Hkv + t.kvh;
+            dma4(src, scale_addr);
+        }
+    };
+    auto load_v = [&](int i) __attribute__((always_inline)) { // (before K of the stage after it)
+        const int nv = p.s.L - 32 * (t.lo + wave + kExWaves * i);
+        issue_tile<D, FP8 ? 1 : 2, true>(lc, a.v_pool + (int64_t)id0 * a.stride_page_b + head_b, nv, v_addr, a.zeros);
+        issue_tile<D, FP8 ? 1 : 2, true>(lc, a.v_pool + (int64_t)id1 * a.stride_page_b + head_b, nv - kPage, v_addr + P::kTile, a.zeros);
+    };
+    constexpr int NK = 2 * P::kDmaPerTile + (FP8 ? 1 : 0), NV = 2 * P::kDmaPerTile; // loads of a stage's K and of its V
+    if (mine > 0) next0 = page_id(0, 0), next1 = page_id(0, 1);
+    __syncthreads(); // (the ring and the areas of the part before have been read)
+    if (mine > 0) load_k(0), load_v(0);
+    {
+        constexpr int UNITS = 32 * NG * G::kUnits;
+#pragma unroll
+        for (int x = 0; x < UNITS / (64 * kExWaves); x++) {
+            const int u = 64 * kExWaves * x + (int)threadIdx.x, r = u / G::kUnits, c = u % G::kUnits;
+            int row = t.row0 + r;
+            row = row < t.rows ? row : t.rows - 1;
+            const int token = ex_div_g(a, row);
+            const uint4 w = *(const uint4 *)(a.q + (int64_t)(p.s.t0 + token) * a.q_stride + (t.kvh * a.G + row - token * a.G) * D + 8 * c);
+            *(uint4 *)(areas + (r >> 4) * G::kTile + 16 * ((r & 15) * G::kUnits + (c ^ (swz(r & 15) & UM)))) = w;
+        }
+    }
+    __syncthreads();
+
+    int lim[NG];
+    f32x16 o[NG][DT];
+    float m[NG], l[NG];
+#pragma unroll
+    for (int g = 0; g < NG; g++) {
+        const int row = t.row0 + 32 * g + n;
+        lim[g] = shift + ex_div_g(a, row < t.rows ? row : t.rows - 1);
+        m[g] = kPfLowest, l[g] = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) {
+#pragma unroll
+            for (int e = 0; e < 16; e++) o[g][dt][e] = 0.f;
+        }
+    }
+    const int first_lim = shift + ex_div_g(a, t.row0); // (the first row sees the least)
+    // e4m3: sixteen codes of a K row at a time are the operands of two k-steps, d = 32 i + 16 hh .. + 7 and + 8 .. + 15; so are Q's
+    const int r16 = n & 15;
+    const int kq_base = FP8 ? (n >> 4) * G::kTile + G::kRowBytes * r16 + 16 * ((swz(r16) & UM) ^ (2 * hh)) : pl.k_base;
+    const int k8_base = (n >> 4) * P::kTile + P::kRowBytes * r16 + 16 * ((swz(r16) & PUM) ^ hh);
+    // e4m3: V through the transposing read of bytes: lane a of sixteen supplies row a / 2 of eight, keys 4 hh .. + 3 and 8 + 4 hh .. + 3
+    const int va = lane & 15, vrow = 4 * hh + ((va >> 1) & 3) + 8 * (va >> 3);
+    const int v8_base = P::kRowBytes * vrow + 16 * (((lane >> 4) & 1) ^ (swz(vrow) & PUM)) + 8 * (va & 1);
+
+#pragma unroll 1
+    for (int i = 0; i < mine; i++) {
+        const int key = 32 * (t.lo + wave + kExWaves * i);
+        const bool more = i + 1 < mine;
+        wait_vmcnt<NV>(); // K is there (V of the stage, asked for after it, may not be)
+        asm volatile("" ::: "memory");
+        float sk0 = a.scale_log2, sk1 = a.scale_log2, sv0 = 1.f, sv1 = 1.f;
+        if (FP8) {
+            f32x4 w = *(const f32x4 *)(lds + X::kScales + 256 * wave);
+            sk0 *= w[0] == 0.f ? 1e-30f : w[0], sk1 *= w[2] == 0.f ? 1e-30f : w[2]; // (zero times the mask's -inf would be NaN)
+            sv0 = w[1], sv1 = w[3];
+        }
+        bf16x8 kf[KS];
+        if (FP8) {
+#pragma unroll
+            for (int k = 0; k < KS / 2; k++) {
+                const uint4 c = *(const uint4 *)(lds + wave * X::kWave + (k8_base ^ (32 * k)));
+                kf[2 * k] = fp8x8_to_bf16((int)c.x, (int)c.y), kf[2 * k + 1] = fp8x8_to_bf16((int)c.z, (int)c.w);
+            }
+        } else {
+            uint32_t ka = k_addr + (uint32_t)pl.k_base;
+            asm volatile("" : "+v"(ka));
+#pragma unroll
+            for (int k = 0; k < KS; k++) kf[k] = *(lds_bf16x8)(ka ^ (uint32_t)(32 * k));
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) load_k(i + 1);
+        const bool masked = key + 31 > first_lim;
+        u32x4 pw[NG][2];
+        // (two chains of products either way: of two groups of rows, or of one in halves)
+        f32x16 sc[2];
+#pragma unroll
+        for (int e = 0; e < 16; e++) sc[0][e] = sc[1][e] = 0.f;
+        uint32_t qa = q_addr + (uint32_t)kq_base;
+        asm volatile("" : "+v"(qa));
+#pragma unroll
+        for (int k = 0; k < KS; k += 2) {
+#pragma unroll
+            for (int h = 0; h < 2; h++) {
+                // (e4m3: unit 2 k + 2 hh + h; else 2 (k + h) + hh)
+                const uint32_t at = qa ^ (uint32_t)(FP8 ? 32 * k + 16 * h : 32 * (k + h));
+#pragma unroll
+                for (int g = 0; g < NG; g++) {
+                    f32x16 &x = sc[NG == 2 ? g : h];
+                    x = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[k + h], *((lds_bf16x8)at + 2 * G::kTile * g / 16), x, 0, 0, 0);
+                }
+            }
+        }
+        if (NG == 1) sc[0] += sc[1];
+#pragma unroll
+        for (int g = 0; g < NG; g++) {
+            f32x16 &s = sc[g];
+            if (masked) {
+#pragma unroll
+                for (int e = 0; e < 16; e++) {
+                    if (key + 8 * (e / 4) + 4 * hh + (e % 4) > lim[g]) s[e] = -INFINITY;
+                }
+            }
+            float m0 = max3(first_max(s[0], s[1]), s[2], s[3]), m1 = max3(first_max(s[8], s[9]), s[10], s[11]);
+            m0 = max3(max3(m0, s[4], s[5]), s[6], s[7]), m1 = max3(max3(m1, s[12], s[13]), s[14], s[15]);
+            float mn = fmaxf(m0 * sk0, m1 * sk1);
+            const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(mn), __float_as_uint(mn), false, false);
+            mn = max3(__uint_as_float(r[0]), __uint_as_float(r[1]), __uint_as_float(r[1]));
+            const bool grew = mn > m[g] + kPfSlack;
+            if (__any(grew)) {
+                mn = grew ? mn : m[g];
+                const float alpha = __builtin_amdgcn_exp2f(m[g] - mn);
+                m[g] = mn;
+                l[g] *= alpha;
+#pragma unroll
+                for (int dt = 0; dt < DT; dt++) o[g][dt] *= alpha;
+            }
+            float acc0 = 0.f, acc1 = 0.f;
+#pragma unroll
+            for (int e = 0; e < 16; e += 2) {
+                float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], e < 8 ? sk0 : sk1, -m[g]));
+                float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], e < 8 ? sk0 : sk1, -m[g]));
+                acc0 += w0, acc1 += w1;
+                if (FP8) w0 *= e < 8 ? sv0 : sv1, w1 *= e < 8 ? sv0 : sv1;
+                pw[g][e >> 3][(e >> 1) & 3] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{w0, w1}), bf16x2));
+            }
+            l[g] += acc0 + acc1;
+        }
+        if (more) wait_vmcnt<NK>(); // V is there
+        else wait_vmcnt<0>();
+        asm volatile("" ::: "memory");
+        bf16x8 vf[DT][2];
+        uint32_t vb = v_addr + (uint32_t)(FP8 ? v8_base : pl.v_base);
+        asm volatile("" : "+v"(vb));
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) {
+#pragma unroll
+            for (int kk = 0; kk < 2; kk++) {
+                if (FP8) {
+                    const i32x2 c = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)(vb ^ (uint32_t)(32 * dt)) + kk * P::kTile / 8);
+                    vf[dt][kk] = fp8x8_to_bf16(c[0], c[1]);
+                } else {
+                    const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb ^ (uint32_t)pf_v_xor<D>(dt, 0)) + kk * G::kTile / 8);
+                    const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb ^ (uint32_t)pf_v_xor<D>(dt, 1)) + kk * G::kTile / 8);
+                    vf[dt][kk] = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(x, y, 0, 1, 2, 3, 4, 5, 6, 7));
+                }
+            }
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        if (more) load_v(i + 1);
+        bool odd = false;
+        if (masked) {
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) odd = odd || ex_odd(vf[dt][0]) || ex_odd(vf[dt][1]);
+            odd = __any(odd);
+        }
+        if (__builtin_expect(odd, 0)) {
+#pragma unroll
+            for (int dt = 0; dt < DT; dt++) {
+#pragma unroll
+                for (int kk = 0; kk < 2; kk++) {
+                    u32x4 plus, minus;
+                    vf[dt][kk] = ex_even(vf[dt][kk], plus, minus);
+#pragma unroll
+                    for (int g = 0; g < NG; g++) {
+                        const bf16x8 seen = ex_seen(key + 16 * kk, lim[g], hh);
+                        ex_add_odd(o[g][dt], plus, seen, INFINITY), ex_add_odd(o[g][dt], minus, seen, -INFINITY);
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int dt = 0; dt < DT; dt++) {
+#pragma unroll
+            for (int kk = 0; kk < 2; kk++) {
+#pragma unroll
+                for (int g = 0; g < NG; g++) o[g][dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[dt][kk], __builtin_bit_cast(bf16x8, pw[g][kk]), o[g][dt], 0, 0, 0);
+            }
+        }
+    }
+
+    // The waves' sums, 32 rows at a time, as the accumulators lie: 256 consecutive values (four of a lane) to a piece.
+    constexpr int PIECES = 8; // of 32 rows and 64 d
+    float2 *const stats = (float2 *)(lds + X::kStats);
+#pragma unroll
+    for (int g = 0; g < NG; g++) {
+        const int row = t.row0 + 32 * g + n;
+        float lg;
+        {
+            const u32x2 r = __builtin_amdgcn_permlane32_swap(__float_as_uint(l[g]), __float_as_uint(l[g]), false, false);
+            lg = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+        }
+        const int token = ex_div_g(a, row < t.rows ? row : t.rows - 1);
+        const int64_t rh = (int64_t)(p.s.t0 + token) * a.Hq + t.kvh * a.G + (row - token * a.G);
+        float f[kExWaves], mm = kPfLowest, ll = 0.f, inv = 0.f;
+#pragma unroll
+        for (int half = 0; half < D / 64; half++) {
+            __syncthreads(); // (nothing is on its way to the ring any more, and nothing of it is being read)
+#pragma unroll
+            for (int dt = 0; dt < 2; dt++) {
+#pragma unroll
+                for (int j = 0; j < 4; j++) {
+                    const f32x16 &x = o[g][2 * half + dt];
+                    *(f32x4 *)(lds + wave * X::kSum + 1024 * (4 * dt + j) + 16 * lane) = f32x4{x[4 * j], x[4 * j + 1], x[4 * j + 2], x[4 * j + 3]};
+                }
+            }
+            if (half == 0 && hh == 0) stats[32 * wave + n] = make_float2(m[g], lg);
+            __syncthreads();
+            if (half == 0) {
+                float2 ml[kExWaves];
+#pragma unroll
+                for (int w = 0; w < kExWaves; w++) ml[w] = stats[32 * w + n], mm = fmaxf(mm, ml[w].x);
+#pragma unroll
+                for (int w = 0; w < kExWaves; w++) f[w] = __builtin_amdgcn_exp2f(ml[w].x - mm), ll += f[w] * ml[w].y;
+                inv = ll > 0.f ? 1.0f / ll : ll == 0.f ? 0.f : ll; // (no key: zeros; NaN stays)
+            }
+#pragma unroll
+            for (int x = 0; x < PIECES / kExWaves; x++) {
+                const int c = PIECES / kExWaves * wave + x;
+                f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int w = 0; w < kExWaves; w++) acc += f[w] * *(const f32x4 *)(lds + w * X::kSum + 1024 * c + 16 * lane);
+                if (row >= t.rows) continue;
+                if (t.slot >= 0) *(f32x4 *)(a.part_o + (int64_t)t.slot * (kExRows * D) + g * (32 * D) + 256 * (PIECES * half + c) + 4 * lane) = acc;
+                else *(bf16x4 *)(a.out + rh * D + 64 * half + 32 * (c >> 2) + 8 * (c & 3) + 4 * hh) = __builtin_convertvector(acc * inv, bf16x4);
+            }
+        }
+        if (wave == 0 && hh == 0 && row < t.rows) {
+            if (t.slot >= 0) *(float2 *)(a.part_lse + 2 * ((int64_t)t.slot * kExRows + 32 * g + n)) = make_float2(mm, ll);
+            else a.lse[rh] = (mm + __builtin_amdgcn_logf(ll)) * 0.6931471805599453f;
+        }
+    }
+    __syncthreads(); // (the ring takes the next part's stages)
+}
+
 // The LDS of a workgroup: a ring of stages in bf16, and for each wave an area of its own, where e4m3 tiles land as they are
 // stored (a ring of its own loads) and results are put in order on their way out.
 template <int D, bool FP8> struct ExTileLds {
@@ -554,9 +881,14 @@ template <int D, bool FP8> struct ExTileLds {
     static constexpr int kArea = FP8 && kRaw * kRawSlot > kPfStageBytes ? kRaw * kRawSlot : kPfStageBytes;
     static constexpr int kAreas = kSlots * Geo<D, 2>::kStage; // the areas follow the ring
     static constexpr int kBytes = kAreas + kArea * kExWaves;
+    using N = ExNarrowLds<D, FP8>;
+    static_assert(N::kNeeds <= kAreas && N::kRows <= kArea * kExWaves && N::kEnds <= kBytes, "few rows find room in it");
 };
 
-template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_tile_kernel(EX_PARAMS)
+// What the rows of a kernel's sequences (of one kv head) are: any number; up to 32; up to 64.
+enum ExKind { kExAny, kEx32, kEx64 };
+
+template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_kernel(EX_PARAMS)
 {
     EX_TAKE(a);
     using G = Geo<D, 2>;
@@ -575,7 +907,8 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
     auto after = [](int slot) __attribute__((always_inline)) { return slot + 1 == X::kSlots ? 0 : slot + 1; };
     int slot0 = 0; // ring slot of the part's first stage; the others follow
 
-    ex_walk<kExTileRows>(a, lds, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
+    ex_walk(a, lds, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
+        if constexpr (KIND != kExAny) return ex_narrow<D, FP8, KIND == kEx64 ? 2 : 1>(a, p, t, lc, pl, lds, lds + X::kAreas, lane, wave);
         const int nst = t.hi - t.lo, row = t.row0 + kPfRows * wave + n; // this lane's row
         const bool exists = row < t.rows;
         const int token = ex_div_g(a, exists ? row : t.rows - 1), head = t.kvh * a.G + ((exists ? row : t.rows - 1) - token * a.G);
@@ -740,14 +1073,14 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
         if (row_lo >= t.rows) return;
         if (t.slot >= 0) {
             // a part: as the accumulators lie, which is whole lines
-            float *const o = a.part_o + (int64_t)t.slot * (kExTileRows * D) + wave * (kPfRows * D) + 4 * lane;
+            float *const o = a.part_o + (int64_t)t.slot * (kExRows * D) + wave * (kPfRows * D) + 4 * lane;
 #pragma unroll
             for (int dt = 0; dt < D / 32; dt++) {
 #pragma unroll
                 for (int j = 0; j < 4; j++)
                     if (exists) *(f32x4 *)(o + 256 * (4 * dt + j)) = f32x4{st.o[dt][4 * j], st.o[dt][4 * j + 1], st.o[dt][4 * j + 2], st.o[dt][4 * j + 3]};
             }
-            if (exists && hh == 0) *(float2 *)(a.part_lse + 2 * ((int64_t)t.slot * kExTileRows + kPfRows * wave + n)) = make_float2(st.m, l);
+            if (exists && hh == 0) *(float2 *)(a.part_lse + 2 * ((int64_t)t.slot * kExRows + kPfRows * wave + n)) = make_float2(st.m, l);
             return;
         }
         const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l; // (no key: zeros; NaN stays)
@@ -778,260 +1111,19 @@ template <int D, bool FP8> __global__ __launch_bounds__(64 * kExWaves, D == 64 ?
     wait_vmcnt<0>(); // nothing may land in LDS after the workgroup has left
 }
 
-// ---- few rows -------------------------------------------------------------------------------------------
-
-template <int D, int KVB> struct ExFewLds {
-    using G = Geo<D, KVB>;
-    static constexpr int kSlots = KVB == 2 ? 2 : 4;        // a wave's ring, in stages
-    static constexpr int kRing = kSlots * G::kStage;
-    static constexpr int kStats = kExWaves * kRing;         // what the waves' rows have as maximum and sum
-    static constexpr int kBytes = kStats + kExWaves * kExFewRows * 8;
-    static_assert(kRing >= kExFewRows * D * 4, "a wave's sums take the place of its ring");
-    static_assert((kSlots - 1) * G::kDmaPerStage < 64, "the vector-memory counter holds 6 bits");
-};
-
-// NQT: tiles of sixteen rows that a sequence and kv head has at most.
-template <int D, int KVB, int NQT> __global__ __launch_bounds__(64 * kExWaves, 1) void extend_few_kernel(EX_PARAMS)
-{
-    EX_TAKE(a);
-    using G = Geo<D, KVB>;
-    using X = ExFewLds<D, KVB>;
-    constexpr int NST = X::kSlots, DPS = G::kDmaPerStage, W = kExWaves;
-    extern __shared__ __attribute__((aligned(1024))) uint8_t lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int rn = lane & 15, j = lane >> 4;
-    uint8_t *const ring = lds + wave * X::kRing;
-    const uint32_t ring_addr = (uint32_t)(uintptr_t)ring;
-    LaneConst<D, KVB> lc;
-    lane_setup<D, KVB>(lc, lane, a.stride_token_b);
-
-    ex_walk<kExFewRows>(a, lds, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
-        const int ntiles = (t.rows + 15) >> 4, shift = p.s.L - p.s.n;
-        // the wave's stages of the part: wave, wave + 4, ...
-        const int left = t.hi - t.lo - wave, mine = left > 0 ? (left + W - 1) / W : 0;
-        const int32_t *const pages = a.table + (int64_t)p.b * a.max_pages;
-        const int count = (p.s.L + kPage - 1) / kPage;
-        const int64_t head_b = (int64_t)t.kvh * a.stride_head_b;
-        const int last_page = count > 0 ? count - 1 : 0; // (a page that does not exist takes its place, and none of its rows are read)
-        auto page_id = [&](int i, int h) __attribute__((always_inline)) {
-            const int g = 2 * (t.lo + wave + W * i) + h;
-            return uniform_load(pages, g < last_page ? g : last_page);
-        };
-        int issued = 0, id0 = 0, id1 = 0;
-        if (mine > 0) id0 = page_id(0, 0), id1 = page_id(0, 1);
-        auto issue = [&]() __attribute__((always_inline)) {
-            if (issued >= mine) return;
-            const int nv0 = p.s.L - 2 * kPage * (t.lo + wave + W * issued), nv1 = nv0 - kPage;
-            const int64_t off0 = (int64_t)id0 * a.stride_page_b + head_b, off1 = (int64_t)id1 * a.stride_page_b + head_b;
-            const uint32_t sb = ring_addr + (issued % NST) * G::kStage;
-            issue_tile<D, KVB, true>(lc, a.k_pool + off0, nv0, sb, a.zeros);
-            issue_tile<D, KVB, true>(lc, a.k_pool + off1, nv1, sb + G::kTile, a.zeros);
-            issue_tile<D, KVB, true>(lc, a.v_pool + off0, nv0, sb + 2 * G::kTile, a.zeros);
-            issue_tile<D, KVB, true>(lc, a.v_pool + off1, nv1, sb + 3 * G::kTile, a.zeros);
-            if (KVB == 1) { // the pages' scales land behind the tiles: lanes 0..3 bring k0, v0, k1, v1
-                const int pid = (lane & 2) ? id1 : id0;
-                const void *src = a.zeros;
-                if (lane < 4 && ((lane & 2) ? nv1 : nv0) > 0) src = ((lane & 1) ? a.v_scale : a.k_scale) + (int64_t)pid * a.Hkv + t.kvh;
-                dma4(src, sb + 4 * G::kTile);
-            }
-            issued++;
-            id0 = page_id(issued, 0), id1 = page_id(issued, 1);
-        };
-        // Query rows as the second operand of K . Q^T wants them: lane (row, j) holds the d values that its K operand holds.
-        bf16x8 qf[NQT][G::kKSteps];
-        int lim[NQT];
-#pragma unroll
-        for (int q = 0; q < NQT; q++) {
-            int r = 16 * q + rn;
-            r = r < t.rows ? r : t.rows - 1;
-            const int token = ex_div_g(a, r);
-            lim[q] = shift + token;
-            const uint16_t *const src = a.q + (int64_t)(p.s.t0 + token) * a.q_stride + (t.kvh * a.G + r - token * a.G) * D;
-#pragma unroll
-            for (int i = 0; i < G::kKSteps; i++) {
-                const int d0 = KVB == 2 ? 32 * i + 8 * j : 16 * (4 * (i / 2) + j) + 8 * (i % 2);
-                if (q < ntiles) qf[q][i] = *(const bf16x8 *)(src + d0);
-            }
-        }
-#pragma unroll
-        for (int i = 0; i < NST - 1; i++) issue();
-
-        f32x4 o[NQT][G::kDTiles];
-        float m[NQT], lsum[NQT];
-#pragma unroll
-        for (int q = 0; q < NQT; q++) {
-            m[q] = kPfLowest, lsum[q] = 0.f;
-#pragma unroll
-            for (int dt = 0; dt < G::kDTiles; dt++) o[q][dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-#pragma unroll 1
-        for (int it = 0; it < mine; it++) {
-            issue();
-            WaitTail<NST - 1, DPS>::run(issued - 1 - it);
-            const uint8_t *const st = ring + (it % NST) * G::kStage;
-            const int key = 32 * (t.lo + wave + W * it);
-            f32x4 s[NQT][2];
-#pragma unroll
-            for (int pg = 0; pg < 2; pg++) {
-#pragma unroll
-                for (int q = 0; q < NQT; q++) s[q][pg] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < G::kKReads; i++) {
-                    if (KVB == 2) {
-                        const bf16x8 kf = *(const bf16x8 *)(st + pg * G::kTile + lc.k_off[i]);
-#pragma unroll
-                        for (int q = 0; q < NQT; q++)
-                            if (q < ntiles) s[q][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[q][i], s[q][pg], 0, 0, 0);
-                    } else {
-                        const int4 kc = *(const int4 *)(st + pg * G::kTile + lc.k_off[i]); // 16 codes: two k-steps
-                        const bf16x8 k0 = fp8x8_to_bf16(kc.x, kc.y), k1 = fp8x8_to_bf16(kc.z, kc.w);
-#pragma unroll
-                        for (int q = 0; q < NQT; q++)
-                            if (q < ntiles) {
-                                s[q][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k0, qf[q][2 * i], s[q][pg], 0, 0, 0);
-                                s[q][pg] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k1, qf[q][2 * i + 1], s[q][pg], 0, 0, 0);
-                            }
-                    }
-                }
-            }
-            // e4m3: the K scale folds into the score's, the V scale into the weights before they are rounded to bf16 (the
-            // row sum keeps them unscaled)
-            float ks0 = a.scale_log2, ks1 = a.scale_log2, vs0 = 1.0f, vs1 = 1.0f;
-            if (KVB == 1) {
-                const f32x4 sc = *(const f32x4 *)(st + 4 * G::kTile);
-                ks0 *= sc[0], vs0 = sc[1], ks1 *= sc[2], vs1 = sc[3];
-            }
-            const bool masked = key + 31 > shift; // (the first row sees the least)
-            bf16x8 pf[NQT];
-#pragma unroll
-            for (int q = 0; q < NQT; q++) {
-                if (q >= ntiles) continue;
-                float v[8];
-#pragma unroll
-                for (int e = 0; e < 4; e++) v[e] = s[q][0][e] * ks0, v[4 + e] = s[q][1][e] * ks1;
-                if (masked) {
-#pragma unroll
-                    for (int e = 0; e < 4; e++) {
-                        if (key + 4 * j + e > lim[q]) v[e] = -INFINITY;
-                        if (key + kPage + 4 * j + e > lim[q]) v[4 + e] = -INFINITY;
-                    }
-                }
-                const float mx = row_max3(max3(max3(v[0], v[1], v[2]), max3(v[3], v[4], v[5]), max3(v[6], v[7], v[7])));
-                const float mn = max3(m[q], mx, mx);
-                f32x8 w;
-#pragma unroll
-                for (int e = 0; e < 8; e++) w[e] = __builtin_amdgcn_exp2f(v[e] - mn);
-                const float ws = ((w[0] + w[1]) + (w[2] + w[3])) + ((w[4] + w[5]) + (w[6] + w[7]));
-                if (KVB == 1) {
-#pragma unroll
-                    for (int e = 0; e < 4; e++) w[e] *= vs0, w[4 + e] *= vs1;
-                }
-                pf[q] = __builtin_convertvector(w, bf16x8);
-                if (__any(mn != m[q])) {
-                    const float alpha = __builtin_amdgcn_exp2f(m[q] - mn);
-                    m[q] = mn;
-                    lsum[q] *= alpha;
-#pragma unroll
-                    for (int dt = 0; dt < G::kDTiles; dt++) o[q][dt] *= alpha;
-                }
-                lsum[q] += ws;
-            }
-            typedef s16x4 __attribute__((address_space(3))) * lds_s16x4;
-            typedef int __attribute__((ext_vector_type(2))) i32x2;
-            typedef i32x2 __attribute__((address_space(3))) * lds_i32x2;
-            typedef short s16x8 __attribute__((ext_vector_type(8)));
-            const uint32_t vb = ring_addr + (it % NST) * G::kStage + 2 * G::kTile;
-#pragma unroll
-            for (int dt = 0; dt < G::kDTiles; dt++) {
-                bf16x8 vf;
-                if (KVB == 2) {
-                    const s16x4 v0 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + lc.v_off[dt]));
-                    const s16x4 v1 = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb + G::kTile + lc.v_off[dt]));
-                    vf = __builtin_bit_cast(bf16x8, (s16x8)__builtin_shufflevector(v0, v1, 0, 1, 2, 3, 4, 5, 6, 7));
-                } else {
-                    const i32x2 vc = __builtin_amdgcn_ds_read_tr8_b64_v2i32((lds_i32x2)((vb + lc.v_off[0]) ^ (uint32_t)(16 * dt)));
-                    vf = fp8x8_to_bf16(vc[0], vc[1]);
-                }
-                if (masked && __builtin_expect(__any(ex_odd(vf)), 0)) {
-#pragma unroll 1
-                    for (int i = 0; i < 32; i++) { // element e of lane group h: key 4 h + e of the first page, or 4 h + e - 4 of the second
-                        const int e = i & 7, h = i >> 3, at = key + 4 * h + (e & 3) + (e & 4 ? kPage : 0);
-                        const bf16x8 one = ex_only(vf, j == h, e);
-#pragma unroll
-                        for (int q = 0; q < NQT; q++) {
-                            if (q >= ntiles) continue;
-                            const f32x4 x = __builtin_amdgcn_mfma_f32_16x16x32_bf16(one, pf[q], (f32x4{0.f, 0.f, 0.f, 0.f}), 0, 0, 0);
-#pragma unroll
-                            for (int c = 0; c < 4; c++) o[q][dt][c] += at <= lim[q] ? x[c] : 0.f;
-                        }
-                    }
-                    continue;
-                }
-#pragma unroll
-                for (int q = 0; q < NQT; q++)
-                    if (q < ntiles) o[q][dt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf, pf[q], o[q][dt], 0, 0, 0);
-            }
-            // every LDS read of this stage has returned before a later load may overwrite it
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        }
-
-        // The four waves' sums: a row's 16-byte pieces lie XOR-swizzled by the row, in the wave's ring.
-        float *const mine_o = (float *)ring;
-        float2 *const stats = (float2 *)(lds + X::kStats);
-        constexpr int PIECES = D / 4;
-#pragma unroll
-        for (int q = 0; q < NQT; q++) {
-            if (q >= ntiles) continue;
-            const int r = 16 * q + rn;
-            const float l = row_sum(lsum[q]);
-#pragma unroll
-            for (int dt = 0; dt < G::kDTiles; dt++) *(f32x4 *)(mine_o + r * D + 4 * ((4 * dt + j) ^ rn)) = o[q][dt];
-            if (j == 0) stats[wave * kExFewRows + r] = make_float2(m[q], l);
-        }
-        __syncthreads();
-        for (int x = threadIdx.x; x < t.rows * PIECES; x += 64 * W) {
-            const int r = x / PIECES, c = x % PIECES;
-            float mm = kPfLowest, l = 0.f;
-            float2 ml[W];
-            f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-            for (int w = 0; w < W; w++) ml[w] = stats[w * kExFewRows + r], mm = fmaxf(mm, ml[w].x);
-#pragma unroll
-            for (int w = 0; w < W; w++) {
-                const float f = __builtin_amdgcn_exp2f(ml[w].x - mm);
-                l += f * ml[w].y;
-                acc += f * *(const f32x4 *)((const float *)(lds + w * X::kRing) + r * D + 4 * (c ^ (r & 15)));
-            }
-            if (t.slot >= 0) {
-                *(f32x4 *)(a.part_o + ((int64_t)t.slot * kExFewRows + r) * D + 4 * c) = acc;
-                if (c == 0) *(float2 *)(a.part_lse + 2 * ((int64_t)t.slot * kExFewRows + r)) = make_float2(mm, l);
-            } else {
-                const int token = ex_div_g(a, r);
-                const int64_t rh = (int64_t)(p.s.t0 + token) * a.Hq + t.kvh * a.G + (r - token * a.G);
-                const float inv = l > 0.f ? 1.0f / l : l == 0.f ? 0.f : l; // (no key: zeros; NaN stays)
-                *(bf16x4 *)(a.out + rh * D + 4 * c) = __builtin_convertvector(acc * inv, bf16x4);
-                if (c == 0) a.lse[rh] = (mm + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-            }
-        }
-        __syncthreads(); // (the rings take the next part's stages)
-    });
-    wait_vmcnt<0>();
-}
-
 // ---- what spans share -----------------------------------------------------------------------------------
 
 constexpr int kExMergeWgs = 2048, kExMaxSpans = 1024;
 constexpr int kExMergeFew = 12; // parts of an item that one wave adds up
 
 // Adds up the parts of the items that a cut goes through, 256 consecutive values of an item's parts at a time: a wave alone
-// where every item has few parts, else a workgroup's waves every fourth part each.  ROWS: those of the kernel that left them,
-// with its layout.
-template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(const int4 *__restrict__ desc, int spans, ExtendLaunch given)
+// where every item has few parts, else a workgroup's waves every fourth part each.
+template <int D> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(const int4 *__restrict__ desc, int spans, ExtendLaunch given)
 {
     ExtendLaunch a = given;
     a.desc = (int4 *)desc, a.spans = spans;
     touch_lines(given);
-    constexpr int W = kExWaves, CHUNKS = ROWS * D / 256, N = kExMaxSpans / (64 * W);
+    constexpr int W = kExWaves, CHUNKS = kExRows * D / 256, N = kExMaxSpans / (64 * W);
     __shared__ int list[kExMaxSpans];
     __shared__ int counts[W][N], longest[W];
     __shared__ f32x4 sums[W][64];
@@ -1078,11 +1170,9 @@ template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void exte
         const int4 item = a.desc[2 * k]; // {first packed token, first row, rows, kv head}
         const int last = a.desc[2 * k + 1].x;
         int r, d; // this lane's row of the block, and the first of its four values
-        if (ROWS == kExTileRows) {
+        {
             const int wv = chunk / (D / 8), c = chunk % (D / 8);
             r = kPfRows * wv + (lane & 31), d = 32 * (c >> 2) + 8 * (c & 3) + 4 * (lane >> 5);
-        } else {
-            r = chunk * (256 / D) + lane / (D / 4), d = 4 * (lane % (D / 4));
         }
         const int row = item.y + r;
         const bool exists = have && row < item.z;
@@ -1100,8 +1190,8 @@ template <int D, int ROWS> __global__ __launch_bounds__(64 * kExWaves) void exte
                     const int64_t slot = p == k ? 2 * (int64_t)k + 1 : 2 * (int64_t)p;
                     ml[i] = make_float2(kPfLowest, 0.f), o[i] = f32x4{0.f, 0.f, 0.f, 0.f};
                     if (p <= last) {
-                        ml[i] = *(const float2 *)(a.part_lse + 2 * (slot * ROWS + r));
-                        o[i] = *(const f32x4 *)(a.part_o + slot * (ROWS * D) + 256 * chunk + 4 * lane);
+                        ml[i] = *(const float2 *)(a.part_lse + 2 * (slot * kExRows + r));
+                        o[i] = *(const f32x4 *)(a.part_o + slot * (kExRows * D) + 256 * chunk + 4 * lane);
                     }
                 }
                 float top = mm;

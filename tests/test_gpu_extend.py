@@ -249,7 +249,7 @@ def test_graph_replays_read_what_the_buffers_hold(dec):
 
 
 def test_workspace_is_checked(dec):
-    x = Extension(Cache([900], 2, 128), [5], 8)
+    x = Extension(Cache([6000], 2, 128), [5], 8)
     need = ra.rollout_attn_extend_workspace_size(dec.ctx, x.c)
     ws = torch.empty(need, dtype=torch.uint8, device=DEV)
     for at, size, status in ((ws.data_ptr(), need - 1, ra.RA_ERR_WORKSPACE_TOO_SMALL), (0, need, ra.RA_ERR_INVALID_ARG),
