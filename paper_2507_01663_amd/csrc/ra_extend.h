@@ -103,29 +103,34 @@ __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
 // place.
 constexpr int kExKnown = 512;
 struct ExKnown {
-    int4 rec[kExKnown]; // {start on the line, blocks before, first packed token, new tokens}
+    int4 rec[kExKnown]; // {start on the line, -, first packed token, new tokens}
     int len[kExKnown];
+    int2 rank[kExKnown]; // {class, blocks of the class before}
 };
+constexpr int kExClasses = 4; // items that are left whole begin with the longest, in so many classes of length
 static_assert(sizeof(ExKnown) <= 3 * Geo<64, 2>::kStage, "it fits the smallest ring");
 
 struct ExLine {
     int lane, sub, chunks;   // sixty-fours of sequences in a chunk
     int unit;                // items are left whole (see measure)
     int before, total;       // start of this lane's chunk
-    int before_blocks, blocks; // ... counted in blocks of one kv head
+    int blocks;              // blocks of one kv head, of all sequences
+    int ranked[kExClasses], ranks[kExClasses]; // of an order by length: blocks of a class before this lane's chunk, and in all
     int q, r, spans, cut;    // span k starts at q k + min(k, r), before cuts are moved; items up to `cut` are not cut
 
     __device__ __forceinline__ void measure(const ExtendLaunch &a, ExKnown *known)
     {
         lane = threadIdx.x & 63;
-        before = before_blocks = total = blocks = 0;
+        before = total = blocks = 0;
         int longest = 0;
         sub = 1;
-        auto add = [&](const ExSeq &s, int &at, int &at_blocks) __attribute__((always_inline)) {
+        auto add = [&](const ExSeq &s) __attribute__((always_inline)) {
             int tc, tb;
-            at = total + wave_scan(a.Hkv * s.blocks * s.cost, lane, tc), at_blocks = blocks + wave_scan(s.blocks, lane, tb);
+            const int at = total + wave_scan(a.Hkv * s.blocks * s.cost, lane, tc);
+            (void)wave_scan(s.blocks, lane, tb);
             total += tc, blocks += tb;
             longest = longest > s.cost ? longest : s.cost;
+            return at;
         };
         if (a.B <= kExKnown) {
             chunks = (a.B + 63) >> 6;
@@ -143,10 +148,9 @@ struct ExLine {
                 for (int i = 0; i < AT; i++) {
                     if (c0 + i >= chunks) break;
                     const ExSeq s = ex_sequence(a, t0[i], t1[i], len[i]);
-                    if (lane == c0 + i) before = total, before_blocks = blocks;
-                    int at, at_blocks;
-                    add(s, at, at_blocks);
-                    known->rec[64 * (c0 + i) + lane] = make_int4(at, at_blocks, s.t0, s.n);
+                    if (lane == c0 + i) before = total;
+                    const int at = add(s);
+                    known->rec[64 * (c0 + i) + lane] = make_int4(at, 0, s.t0, s.n);
                     known->len[64 * (c0 + i) + lane] = s.L;
                 }
             }
@@ -155,12 +159,11 @@ struct ExLine {
             chunks = ex_div(a.B + 64 * sub - 1, 64 * sub);
 #pragma unroll 1
             for (int c = 0; c < chunks * sub; c++) {
-                if (lane * sub == c) before = total, before_blocks = blocks;
-                int at, at_blocks;
-                add(ex_sequence(a, 64 * c + lane), at, at_blocks);
+                if (lane * sub == c) before = total;
+                (void)add(ex_sequence(a, 64 * c + lane));
             }
         }
-        if (lane >= chunks) before = before_blocks = INT32_MAX;
+        if (lane >= chunks) before = INT32_MAX;
         spans = a.spans;
         if (total < a.least * a.spans) {
             spans = ex_div(total, a.least);
@@ -170,7 +173,33 @@ struct ExLine {
         r = total - q * spans;
         cut = q >> 3 > a.least ? q >> 3 : a.least;
         // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.
-        unit = blocks * a.Hkv >= 2 * a.spans && !__any(longest > q);
+        unit = a.B <= kExKnown && blocks * a.Hkv >= 2 * a.spans && !__any(longest > q);
+        if (!unit) return;
+        // (what is started last should be short: by length, in classes of a quarter of the longest)
+#pragma unroll
+        for (int sh = 32; sh >= 1; sh >>= 1) {
+            const int o = __shfl_xor(longest, sh);
+            longest = longest > o ? longest : o;
+        }
+#pragma unroll
+        for (int k = 0; k < kExClasses; k++) ranked[k] = INT32_MAX, ranks[k] = 0;
+#pragma unroll 1
+        for (int c = 0; c < chunks; c++) {
+            const int b = 64 * c + lane;
+            const int4 rec = known->rec[b];
+            const ExSeq s = ex_sequence(a, rec.z, rec.z + rec.w, known->len[b]);
+            const int cls = 4 * s.cost >= 3 * longest ? 0 : 2 * s.cost >= longest ? 1 : 4 * s.cost >= longest ? 2 : 3;
+            int mine = 0;
+#pragma unroll
+            for (int k = 0; k < kExClasses; k++) {
+                int t;
+                const int at = ranks[k] + wave_scan(cls == k ? s.blocks : 0, lane, t);
+                if (cls == k) mine = at;
+                if (lane == c) ranked[k] = ranks[k];
+                ranks[k] += t;
+            }
+            known->rank[b] = make_int2(cls, mine);
+        }
     }
     __device__ __forceinline__ int raw(int k) const { return q * k + (k < r ? k : r); }
     // The last span that an item which ends at x1 has a part in, if it is cut.
@@ -197,42 +226,56 @@ struct ExPlace {
     ExSeq s;         // (cost: the item's length on the line)
 };
 
-// The sequence that x lies in (0 <= x < total), x counted as the line is or (BLOCKS) in blocks of one kv head; returns x's
-// distance from its start.
-template <bool BLOCKS> __device__ __forceinline__ int ex_sequence_at(const ExtendLaunch &a, const ExLine &line, const ExKnown *known, int x, ExPlace &p)
+__device__ __forceinline__ void ex_place(const ExtendLaunch &a, const ExSeq &s, int base, int l, ExPlace &p)
 {
-    const int chunk_before = BLOCKS ? line.before_blocks : line.before;
-    const int c = 63 - __builtin_clzll(__ballot(chunk_before <= x));
+    p.b = base + l;
+    const int t0 = __builtin_amdgcn_readlane(s.t0, l);
+    p.s = ex_sequence(a, t0, t0 + __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.L, l));
+}
+
+// The item that x lies in (0 <= x < total).
+__device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine &line, const ExKnown *known, int x, ExPlace &p)
+{
+    const int c = 63 - __builtin_clzll(__ballot(line.before <= x));
     int base = 64 * c, before;
     ExSeq s = {0, 0, 0, 0, 0};
     if (known) {
         const int4 rec = known->rec[base + line.lane];
-        s.t0 = rec.z, s.n = rec.w, s.L = known->len[base + line.lane], before = BLOCKS ? rec.y : rec.x;
+        s.t0 = rec.z, s.n = rec.w, s.L = known->len[base + line.lane], before = rec.x;
     } else {
-        int start = __builtin_amdgcn_readlane(chunk_before, c);
+        int start = __builtin_amdgcn_readlane(line.before, c);
 #pragma unroll 1
         for (int i = 0;; i++) {
             base = (c * line.sub + i) * 64;
             s = ex_sequence(a, base + line.lane);
             int t;
-            before = start + wave_scan(BLOCKS ? s.blocks : a.Hkv * s.blocks * s.cost, line.lane, t);
+            before = start + wave_scan(a.Hkv * s.blocks * s.cost, line.lane, t);
             if (x < start + t || i + 1 == line.sub) break;
             start += t;
         }
     }
     const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && before <= x));
-    p.b = base + l;
-    const int t0 = __builtin_amdgcn_readlane(s.t0, l);
-    p.s = ex_sequence(a, t0, t0 + __builtin_amdgcn_readlane(s.n, l), __builtin_amdgcn_readlane(s.L, l));
-    return x - __builtin_amdgcn_readlane(before, l);
-}
-
-// The item that x lies in.
-__device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine &line, const ExKnown *known, int x, ExPlace &p)
-{
-    const int y = ex_sequence_at<false>(a, line, known, x, p);
+    ex_place(a, s, base, l, p);
+    const int y = x - __builtin_amdgcn_readlane(before, l);
     p.item = ex_div_short(y, p.s.cost);
     p.x0 = x - y + p.item * p.s.cost;
+}
+
+// The sequence that block x of one kv head lies in, in the order by length; returns x's distance from its start.
+__device__ __forceinline__ int ex_find_ranked(const ExtendLaunch &a, const ExLine &line, const ExKnown *known, int x, ExPlace &p)
+{
+    int cls = 0, ranked = line.ranked[0];
+#pragma unroll
+    for (int k = 0; k + 1 < kExClasses; k++) {
+        if (cls == k && x >= line.ranks[k]) x -= line.ranks[k], cls = k + 1, ranked = line.ranked[k + 1];
+    }
+    const int c = 63 - __builtin_clzll(__ballot(ranked <= x)), b = 64 * c + line.lane;
+    const int4 rec = known->rec[b];
+    const int2 rank = known->rank[b];
+    const ExSeq s = {rec.z, rec.w, known->len[b], 0, 0};
+    const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && rank.x == cls && rank.y <= x));
+    ex_place(a, s, 64 * c, l, p);
+    return x - __builtin_amdgcn_readlane(rank.y, l);
 }
 
 // A part of an item that a workgroup works on.
@@ -279,7 +322,8 @@ template <typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch
     ExPlace p;
     ExPart part;
     p.item = 0, p.x0 = 0;
-    int last = 0, x = 0, end = 0, step = 0, k = 0;
+    int last = 0, x = 0, end = 0, k = 0;
+    bool whole = false; // one item, and nothing else
     int4 begun = {0, 0, 0, 0};
     if (a.direct) {
         // Every item is short: a workgroup for each, and no line.  Blocks are numbered without counting them: sequence b's
@@ -306,14 +350,21 @@ template <typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch
         part.row0 = kExRows * j, part.rows = p.s.n * a.G;
         part.lo = 0, part.hi = ex_stages(a, p.s, j), part.slot = -1;
         part.hi = part.hi < 0 ? 0 : part.hi;
-        end = 1;
+        whole = true, end = 1;
     } else {
         line.measure(a, (ExKnown *)lds);
         const int per = (line.spans + 7) >> 3;
         k = at < per ? die * per + at : (int)blockIdx.x; // (past the spans: one that does not exist)
         if (line.unit) {
-            x = share, end = line.blocks * heads;
-            step = (int)gridDim.x >> 3 << s_shift; // (there are as many workgroups as items, if the call's sizes are what they say)
+            // (a workgroup for each item: there are as many, if the call's sizes are what they say)
+            const int number = ex_div_short(share, heads);
+            if (number < line.blocks) {
+                const int i = share - (number - ex_find_ranked(a, line, known, number, p)) * heads; // the sequence's items: its blocks times heads
+                const int h = ex_div_short(i, p.s.blocks);
+                p.item = i + ((h << gg_shift) + first_head - h) * p.s.blocks;
+                part = ex_part(a, p, 0, p.s.cost, 0);
+                whole = true, end = 1;
+            }
         } else if (line.total > 0 && at < per && k < line.spans) {
             // `end` is moved where the span gets to it
             end = k + 1 < line.spans ? line.raw(k + 1) : line.total, x = line.raw(k);
@@ -327,16 +378,8 @@ template <typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch
     }
     bool first = !a.direct;
     while (x < end) {
-        int next = 1;
-        if (a.direct) {
-        } else if (line.unit) {
-            const int at_block = ex_div(x, heads);
-            const int i = x - (at_block - ex_sequence_at<true>(a, line, first ? known : nullptr, at_block, p)) * heads;
-            const int h = ex_div_short(i, p.s.blocks); // (a sequence's items: its blocks times heads)
-            p.item = i + ((h << gg_shift) + first_head - h) * p.s.blocks;
-            part = ex_part(a, p, 0, p.s.cost, 0);
-            next = x + step;
-        } else {
+        int next = end;
+        if (!whole) {
             const int x1 = p.x0 + p.s.cost;
             if (end < x1) end = line.moved(end, p.x0, p.s.cost);
             if (x >= end) break;
@@ -351,7 +394,7 @@ template <typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch
         first = false;
         work(p, part);
         x = next;
-        if (x >= end || line.unit) continue;
+        if (x >= end) break;
         if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
         else ex_find(a, line, nullptr, x, p);
     }
