@@ -46,8 +46,8 @@ struct ExtendLaunch {
     float *part_o, *part_lse;    // partial results, two slots per span
     int4 *desc;                  // [spans][2] what the merge adds up
     // (set by carve_extend) workgroups that share the work, workgroups launched, length of a span at least, whether every
-    // sequence is one block, and whether no item is long enough to be cut
-    int32_t spans, grid, least, few, direct;
+    // sequence is one block, whether no item is long enough to be cut, and whether short sequences have a line of their own
+    int32_t spans, grid, least, few, direct, two;
 };
 // How a call is launched (from B, T, max_chunk, Hkv, G, D, max_pages and num_cus), and its workspace: the bytes; places the pointers
 // when base is not null.

@@ -78,6 +78,9 @@ __device__ __forceinline__ int ex_div_short(int x, int y)
 // The length on the line of a number of stages, where sequences have up to so many rows: few rows take four at a time.
 __host__ __device__ __forceinline__ int ex_weight(int stages, int most) { return most > 64 ? stages : stages * (most > 32 ? 14 : 9) >> 5; }
 
+// Where most sequences are far shorter than the longest: does one of n tokens have few rows?
+__device__ __forceinline__ bool ex_few(const ExtendLaunch &a, int n) { return a.two && n * a.G <= 32; }
+
 // What the sequence of t0, t1 (where its chunk starts and ends) and length L is.  (A workgroup comes past everything up to its
 // first keys once and alone, an instruction after the other: they are few.)
 __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int t1, int L)
@@ -90,7 +93,7 @@ __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int 
     s.L = L < 0 ? 0 : (L < most ? L : most);
     s.blocks = (s.n * a.G + kExRows - 1) / kExRows;
     const int mean = (s.L - (s.n >> 1) + 48) >> 5; // keys that a row sees, in stages
-    s.cost = kExFixed + 1 + (mean > 0 ? ex_weight(mean, a.max_chunk * a.G) : 0);
+    s.cost = kExFixed + 1 + (mean > 0 ? ex_weight(mean, ex_few(a, s.n) ? 32 : a.max_chunk * a.G) : 0);
     return s;
 }
 __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
@@ -110,10 +113,13 @@ struct ExKnown {
 constexpr int kExClasses = 4; // items that are left whole begin with the longest, in so many classes of length
 static_assert(sizeof(ExKnown) <= 3 * Geo<64, 2>::kStage, "it fits the smallest ring");
 
-struct ExLine {
+// Where some sequences have few rows and some have many (TWO), they are two lines, and the spans are divided between them.
+template <bool TWO> struct ExLine {
     int lane, sub, chunks;   // sixty-fours of sequences in a chunk
     int unit;                // items are left whole (see measure)
+    int few, base;           // which of two lines it is, and the number of its first span
     int before, total;       // start of this lane's chunk
+    int before_few, total_few; // (the other line's, as long as both are measured)
     int blocks;              // blocks of one kv head, of all sequences
     int ranked[kExClasses], ranks[kExClasses]; // of an order by length: blocks of a class before this lane's chunk, and in all
     int q, r, spans, cut;    // span k starts at q k + min(k, r), before cuts are moved; items up to `cut` are not cut
@@ -121,14 +127,22 @@ struct ExLine {
     __device__ __forceinline__ void measure(const ExtendLaunch &a, ExKnown *known)
     {
         lane = threadIdx.x & 63;
-        before = total = blocks = 0;
+        before = total = before_few = total_few = blocks = few = base = 0;
         int longest = 0;
         sub = 1;
         auto add = [&](const ExSeq &s) __attribute__((always_inline)) {
             int tc, tb;
-            const int at = total + wave_scan(a.Hkv * s.blocks * s.cost, lane, tc);
+            const int length = a.Hkv * s.blocks * s.cost;
+            const bool other = TWO && ex_few(a, s.n);
+            int at = total + wave_scan(other ? 0 : length, lane, tc);
+            total += tc;
+            if (TWO) {
+                const int at_few = total_few + wave_scan(other ? length : 0, lane, tc);
+                total_few += tc;
+                at = other ? at_few : at;
+            }
             (void)wave_scan(s.blocks, lane, tb);
-            total += tc, blocks += tb;
+            blocks += tb;
             longest = longest > s.cost ? longest : s.cost;
             return at;
         };
@@ -148,7 +162,7 @@ struct ExLine {
                 for (int i = 0; i < AT; i++) {
                     if (c0 + i >= chunks) break;
                     const ExSeq s = ex_sequence(a, t0[i], t1[i], len[i]);
-                    if (lane == c0 + i) before = total;
+                    if (lane == c0 + i) before = total, before_few = total_few;
                     const int at = add(s);
                     known->rec[64 * (c0 + i) + lane] = make_int4(at, 0, s.t0, s.n);
                     known->len[64 * (c0 + i) + lane] = s.L;
@@ -159,19 +173,18 @@ struct ExLine {
             chunks = ex_div(a.B + 64 * sub - 1, 64 * sub);
 #pragma unroll 1
             for (int c = 0; c < chunks * sub; c++) {
-                if (lane * sub == c) before = total;
+                if (lane * sub == c) before = total, before_few = total_few;
                 (void)add(ex_sequence(a, 64 * c + lane));
             }
         }
-        if (lane >= chunks) before = INT32_MAX;
+        if (lane >= chunks) before = before_few = INT32_MAX;
+        const int sum = total + total_few;
         spans = a.spans;
-        if (total < a.least * a.spans) {
-            spans = ex_div(total, a.least);
+        if (sum < a.least * a.spans) {
+            spans = ex_div(sum, a.least);
             spans = spans < 1 ? 1 : spans;
         }
-        q = ex_div(total, spans);
-        r = total - q * spans;
-        cut = q >> 3 > a.least ? q >> 3 : a.least;
+        divide(a, sum);
         // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.
         unit = a.B <= kExKnown && blocks * a.Hkv >= 2 * a.spans && !__any(longest > q);
         if (!unit) return;
@@ -200,6 +213,44 @@ struct ExLine {
             }
             known->rank[b] = make_int2(cls, mine);
         }
+    }
+    __device__ __forceinline__ void divide(const ExtendLaunch &a, int length)
+    {
+        q = ex_div(length, spans);
+        r = length - q * spans;
+        cut = q >> 3 > a.least ? q >> 3 : a.least;
+    }
+    // The span of the workgroup that is number `at` of a die, counted from the line's first (-1: there is none).  `number`: of
+    // all spans, and for workgroups without one the numbers that are left.
+    __device__ __forceinline__ int take(const ExtendLaunch &a, int die, int at, int &number)
+    {
+        int of_few = 0; // spans of the line of few rows, and after that of the other; both a multiple of eight, or up to eight
+        if (TWO && total_few > 0) {
+            if (total == 0) {
+                of_few = spans;
+            } else {
+                const int n = ex_uni((int)((float)spans * ((float)total_few / (float)(total + total_few)) + 0.5f));
+                const int most_few = ex_div(total_few, a.least), most = ex_div(total, a.least);
+                if (spans < 16) {
+                    of_few = n < 1 ? 1 : n < 8 ? n : 8;
+                    spans = spans - of_few < 1 ? 1 : spans - of_few < 8 ? spans - of_few : 8;
+                } else {
+                    spans &= ~7;
+                    of_few = (n + 4) & ~7;
+                    of_few = of_few < 8 ? 8 : of_few < spans - 8 ? of_few : spans - 8;
+                    spans -= of_few;
+                }
+                of_few = of_few < most_few ? of_few : most_few > 1 ? most_few : 1;
+                spans = spans < most ? spans : most > 1 ? most : 1;
+            }
+            const int per = (of_few + 7) >> 3;
+            if (at < per || total == 0) few = 1, total = total_few, before = before_few, spans = of_few;
+            else at -= per, base = 8 * per;
+            divide(a, total);
+        }
+        const int per = (spans + 7) >> 3, k = die * per + at;
+        if (at < per) number = base + k;
+        return at < per && k < spans && total > 0 ? k : -1;
     }
     __device__ __forceinline__ int raw(int k) const { return q * k + (k < r ? k : r); }
     // The last span that an item which ends at x1 has a part in, if it is cut.
@@ -234,7 +285,8 @@ __device__ __forceinline__ void ex_place(const ExtendLaunch &a, const ExSeq &s, 
 }
 
 // The item that x lies in (0 <= x < total).
-__device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine &line, const ExKnown *known, int x, ExPlace &p)
+template <bool TWO>
+__device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<TWO> &line, const ExKnown *known, int x, ExPlace &p)
 {
     const int c = 63 - __builtin_clzll(__ballot(line.before <= x));
     int base = 64 * c, before;
@@ -248,13 +300,14 @@ __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine &lin
         for (int i = 0;; i++) {
             base = (c * line.sub + i) * 64;
             s = ex_sequence(a, base + line.lane);
+            if (TWO && ex_few(a, s.n) != (line.few != 0)) s.n = s.blocks = 0;
             int t;
             before = start + wave_scan(a.Hkv * s.blocks * s.cost, line.lane, t);
             if (x < start + t || i + 1 == line.sub) break;
             start += t;
         }
     }
-    const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && before <= x));
+    const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && before <= x && (!TWO || ex_few(a, s.n) == (line.few != 0))));
     ex_place(a, s, base, l, p);
     const int y = x - __builtin_amdgcn_readlane(before, l);
     p.item = ex_div_short(y, p.s.cost);
@@ -262,7 +315,8 @@ __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine &lin
 }
 
 // The sequence that block x of one kv head lies in, in the order by length; returns x's distance from its start.
-__device__ __forceinline__ int ex_find_ranked(const ExtendLaunch &a, const ExLine &line, const ExKnown *known, int x, ExPlace &p)
+template <bool TWO>
+__device__ __forceinline__ int ex_find_ranked(const ExtendLaunch &a, const ExLine<TWO> &line, const ExKnown *known, int x, ExPlace &p)
 {
     int cls = 0, ranked = line.ranked[0];
 #pragma unroll
@@ -312,60 +366,60 @@ __device__ __forceinline__ ExPart ex_part(const ExtendLaunch &a, const ExPlace &
 // same keys run side by side on few of them.
 // Else: a die takes neighbouring spans.  Also tells the merge which items begin in a span and end in another: desc[2 k],
 // desc[2 k + 1] = {first packed token, first row, rows, kv head}, {last span, -, -, -}.
-template <typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, uint8_t *lds, F &&work)
+// `work_few`: the same for sequences of few rows, where there are both (TWO).
+template <bool TWO, typename F, typename FewF> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, uint8_t *lds, F &&work, FewF &&work_few)
 {
     const int die = (int)blockIdx.x & 7, at = (int)blockIdx.x >> 3;
     const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift, heads = a.Hkv >> gg_shift;
     const int first_head = die & ((1 << gg_shift) - 1), share = (at << s_shift) + (die >> gg_shift);
     const ExKnown *known = a.B <= kExKnown ? (ExKnown *)lds : nullptr;
-    ExLine line;
+    ExLine<TWO> line;
     ExPlace p;
     ExPart part;
     p.item = 0, p.x0 = 0;
-    int last = 0, x = 0, end = 0, k = 0;
+    int last = 0, x = 0, end = 0, k = -1, number = blockIdx.x;
     bool whole = false; // one item, and nothing else
     int4 begun = {0, 0, 0, 0};
     if (a.direct) {
         // Every item is short: a workgroup for each, and no line.  Blocks are numbered without counting them: sequence b's
         // are given the numbers from cu[b] G / kExRows + b on, which leaves it as many as it can have.
-        const int number = ex_div_short(share, heads), lane = threadIdx.x & 63;
+        const int block = ex_div_short(share, heads), lane = threadIdx.x & 63;
         int j = 0;
-        p.b = number;
+        p.b = block;
         if (!a.few) {
             p.b = -1;
 #pragma unroll 1
             for (int base = 0; base < a.B; base += 64) {
                 const int start = base + lane < a.B ? (int)((int64_t)a.cu[base + lane] * a.G / kExRows) + base + lane : INT32_MAX;
-                const unsigned long long m = __ballot(start <= number);
+                const unsigned long long m = __ballot(start <= block);
                 if (!m) break;
                 const int l = 63 - __builtin_clzll(m);
-                p.b = base + l, j = number - __builtin_amdgcn_readlane(start, l);
+                p.b = base + l, j = block - __builtin_amdgcn_readlane(start, l);
                 if (l < 63) break;
             }
         }
         if (p.b < 0 || p.b >= a.B) return;
         p.s = ex_sequence(a, uniform_load(a.cu, p.b), uniform_load(a.cu, p.b + 1), uniform_load(a.seq_lens, p.b));
         if (j < 0 || j >= p.s.blocks) return;
-        part.kvh = ((share - number * heads) << gg_shift) + first_head;
+        part.kvh = ((share - block * heads) << gg_shift) + first_head;
         part.row0 = kExRows * j, part.rows = p.s.n * a.G;
         part.lo = 0, part.hi = ex_stages(a, p.s, j), part.slot = -1;
         part.hi = part.hi < 0 ? 0 : part.hi;
         whole = true, end = 1;
     } else {
         line.measure(a, (ExKnown *)lds);
-        const int per = (line.spans + 7) >> 3;
-        k = at < per ? die * per + at : (int)blockIdx.x; // (past the spans: one that does not exist)
+        if (!line.unit) k = line.take(a, die, at, number);
         if (line.unit) {
             // (a workgroup for each item: there are as many, if the call's sizes are what they say)
-            const int number = ex_div_short(share, heads);
-            if (number < line.blocks) {
-                const int i = share - (number - ex_find_ranked(a, line, known, number, p)) * heads; // the sequence's items: its blocks times heads
+            const int block = ex_div_short(share, heads);
+            if (block < line.blocks) {
+                const int i = share - (block - ex_find_ranked(a, line, known, block, p)) * heads; // the sequence's items: its blocks times heads
                 const int h = ex_div_short(i, p.s.blocks);
                 p.item = i + ((h << gg_shift) + first_head - h) * p.s.blocks;
                 part = ex_part(a, p, 0, p.s.cost, 0);
                 whole = true, end = 1;
             }
-        } else if (line.total > 0 && at < per && k < line.spans) {
+        } else if (k >= 0) {
             // `end` is moved where the span gets to it
             end = k + 1 < line.spans ? line.raw(k + 1) : line.total, x = line.raw(k);
             ex_find(a, line, known, x, p);
@@ -376,31 +430,35 @@ template <typename F> __device__ __forceinline__ void ex_walk(const ExtendLaunch
             }
         }
     }
-    bool first = !a.direct;
-    while (x < end) {
-        int next = end;
-        if (!whole) {
-            const int x1 = p.x0 + p.s.cost;
-            if (end < x1) end = line.moved(end, p.x0, p.s.cost);
-            if (x >= end) break;
-            next = x1 < end ? x1 : end;
-            part = ex_part(a, p, x - p.x0, next - p.x0, k);
-            if (x == p.x0 && next < x1) {
-                begun = make_int4(p.s.t0, part.row0, part.rows, part.kvh);
-                last = line.last_of(x1);
+    auto go = [&](auto &&work) __attribute__((always_inline)) {
+        bool first = !a.direct;
+        while (x < end) {
+            int next = end;
+            if (!whole) {
+                const int x1 = p.x0 + p.s.cost;
+                if (end < x1) end = line.moved(end, p.x0, p.s.cost);
+                if (x >= end) break;
+                next = x1 < end ? x1 : end;
+                part = ex_part(a, p, x - p.x0, next - p.x0, number);
+                if (x == p.x0 && next < x1) {
+                    begun = make_int4(p.s.t0, part.row0, part.rows, part.kvh);
+                    last = line.base + line.last_of(x1);
+                }
             }
+            if (first) __syncthreads(); // (what the waves know of the line makes room for the ring)
+            first = false;
+            work(p, part);
+            x = next;
+            if (x >= end) break;
+            if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
+            else ex_find(a, line, nullptr, x, p);
         }
-        if (first) __syncthreads(); // (what the waves know of the line makes room for the ring)
-        first = false;
-        work(p, part);
-        x = next;
-        if (x >= end) break;
-        if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
-        else ex_find(a, line, nullptr, x, p);
-    }
-    if (threadIdx.x == 0 && !a.direct && k < a.spans) { // (every span is answered for, also one that does not exist)
-        a.desc[2 * k] = begun;
-        a.desc[2 * k + 1] = make_int4(last, 0, 0, 0);
+    };
+    if (TWO && (whole ? ex_few(a, p.s.n) : line.few != 0)) go(work_few);
+    else go(work);
+    if (!a.direct && threadIdx.x == 0 && number < a.spans) { // (every span is answered for, also one that does not exist)
+        a.desc[2 * number] = begun;
+        a.desc[2 * number + 1] = make_int4(last, 0, 0, 0);
     }
 }
 
@@ -928,8 +986,8 @@ template <int D, bool FP8> struct ExTileLds {
     static_assert(N::kNeeds <= kAreas && N::kRows <= kArea * kExWaves && N::kEnds <= kBytes, "few rows find room in it");
 };
 
-// What the rows of a kernel's sequences (of one kv head) are: any number; up to 32; up to 64.
-enum ExKind { kExAny, kEx32, kEx64 };
+// What the rows of a kernel's sequences (of one kv head) are: any number; up to 32; up to 64; up to 32 or any number.
+enum ExKind { kExAny, kEx32, kEx64, kExTwo };
 
 template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_kernel(EX_PARAMS)
 {
@@ -950,8 +1008,10 @@ template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWav
     auto after = [](int slot) __attribute__((always_inline)) { return slot + 1 == X::kSlots ? 0 : slot + 1; };
     int slot0 = 0; // ring slot of the part's first stage; the others follow
 
-    ex_walk(a, lds, [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
-        if constexpr (KIND != kExAny) return ex_narrow<D, FP8, KIND == kEx64 ? 2 : 1>(a, p, t, lc, pl, lds, lds + X::kAreas, lane, wave);
+    auto few = [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
+        ex_narrow<D, FP8, KIND == kEx64 ? 2 : 1>(a, p, t, lc, pl, lds, lds + X::kAreas, lane, wave);
+    };
+    auto many = [&](const ExPlace &p, const ExPart &t) __attribute__((always_inline)) {
         const int nst = t.hi - t.lo, row = t.row0 + kPfRows * wave + n; // this lane's row
         const bool exists = row < t.rows;
         const int token = ex_div_g(a, exists ? row : t.rows - 1), head = t.kvh * a.G + ((exists ? row : t.rows - 1) - token * a.G);
@@ -1150,7 +1210,10 @@ template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWav
             }
         }
         if (exists && hh == 0) a.lse[(int64_t)(p.s.t0 + token) * a.Hq + head] = (st.m + __builtin_amdgcn_logf(l)) * 0.6931471805599453f;
-    });
+    };
+    if constexpr (KIND == kExTwo) ex_walk<true>(a, lds, many, few);
+    else if constexpr (KIND == kExAny) ex_walk<false>(a, lds, many, many);
+    else ex_walk<false>(a, lds, few, few);
     wait_vmcnt<0>(); // nothing may land in LDS after the workgroup has left
 }
 

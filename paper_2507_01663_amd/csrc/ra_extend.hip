@@ -11,13 +11,14 @@ static void extend_shape(ExtendLaunch &a)
 {
     const int64_t rows = (int64_t)a.max_chunk * a.G; // of a kv head, at most
     a.few = rows <= kExRows;
+    a.two = rows > 64 && 4 * (int64_t)a.T <= (int64_t)a.B * a.max_chunk;
     const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExRows + a.B, items = blocks * a.Hkv;
     const int longest = kExFixed + 1 + ex_weight(a.max_pages / 2 + 1, (int)rows); // an item at most
     a.least = kExLeast;
     a.direct = longest <= kExShort;
     const int64_t resident = (int64_t)(a.num_cus < 8 ? 8 : a.num_cus & ~7) * (a.D == 64 ? 3 : 2);
     int64_t spans = (items * longest / a.least + 7) & ~(int64_t)7;
-    spans = spans < 8 ? 8 : spans < resident ? spans : resident;
+    spans = spans < 16 ? 16 : spans < resident ? spans : resident; // (two lines take eight each, at least)
     a.spans = (int)(spans < kExMaxSpans ? spans : kExMaxSpans);
     // (a workgroup for every item where items are left whole, or may be: see ex_walk, and ExLine::measure)
     const int gg_shift = (a.Hkv & 7) == 0 ? 3 : (a.Hkv & 3) == 0 ? 2 : (a.Hkv & 1) == 0 ? 1 : 0, s_shift = 3 - gg_shift;
@@ -42,7 +43,7 @@ size_t carve_extend(ExtendLaunch &a, void *base)
     return at;
 }
 
-#define RA_EX_KINDS(X, DD, F) X(DD, F, kExAny) X(DD, F, kEx32) X(DD, F, kEx64)
+#define RA_EX_KINDS(X, DD, F) X(DD, F, kExAny) X(DD, F, kEx32) X(DD, F, kEx64) X(DD, F, kExTwo)
 #define RA_EX_KERNELS(X) RA_EX_KINDS(X, 64, false) RA_EX_KINDS(X, 64, true) RA_EX_KINDS(X, 128, false) RA_EX_KINDS(X, 128, true)
 
 hipError_t extend_config()
@@ -59,7 +60,7 @@ hipError_t launch_extend(const ExtendLaunch &a, hipStream_t s)
 {
     const dim3 grid((unsigned)a.grid), block(64 * kExWaves);
     const int64_t rows = (int64_t)a.max_chunk * a.G;
-    const ExKind kind = rows <= 32 ? kEx32 : rows <= 64 ? kEx64 : kExAny;
+    const ExKind kind = rows <= 32 ? kEx32 : rows <= 64 ? kEx64 : a.two ? kExTwo : kExAny;
 #define RA_EX_LAUNCH(DD, F, K) \
     if (a.D == DD && (a.kv_fp8 != 0) == F && kind == K) hipLaunchKernelGGL((extend_kernel<DD, F, K>), grid, block, (ExTileLds<DD, F>::kBytes), s, EX_GIVE(a));
     RA_EX_KERNELS(RA_EX_LAUNCH)

@@ -80,3 +80,44 @@ def test_batches_of_every_size(dec, B, most):
 def test_an_item_of_many_parts(dec, D, Hq, chunk, length, kv):
     """Items of a dozen parts and more, beside one that is whole."""
     run(dec, "parts", [length, 33], [chunk, 1], Hq, 1, D, kv, 0)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("Hq,Hkv,D,singles,pieces,deep", [
+    (8, 1, 128, 1, [50], 40),                    # hardly any work: a span or two for either line
+    (28, 4, 128, 12, [61, 0, 90], 700),
+    (16, 2, 64, 20, [130], 900),
+    (4, 4, 64, 30, [200, 150], 300),             # one head for each kv head
+    (32, 1, 128, 9, [33], 1100),                 # a token's heads are all the rows that are few
+])
+def test_single_tokens_beside_pieces(dec, Hq, Hkv, D, singles, pieces, deep, kv):
+    """Steps of most sequences and pieces of some, which are worked on apart; contexts of every length, also none."""
+    chunks = [1] * singles + pieces + [1, 2, 1, 1, 1]
+    lens = [n + (97 * b) % deep for b, n in enumerate(chunks)]
+    lens[0] = 1
+    run(dec, "beside", lens, chunks, Hq, Hkv, D, kv, 0)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("chunks", [[1, 2, 1], [70, 64], [3]])
+def test_one_of_two_kinds_is_missing(dec, chunks, kv):
+    """A bound that promises long chunks, over short ones alone or long ones alone."""
+    x = Extension(Cache([800 + n for n in chunks], 2, 128, kv), chunks, 8, bound=600)
+    dec.extend(x.c)
+    x.check("missing")
+
+
+@pytest.mark.parametrize("at", [0, 60, 129])
+def test_later_tokens_have_no_part_beside_pieces(dec, at):
+    """A NaN in one sequence's pages stays with the tokens of that sequence that see it."""
+    chunks = [1, 1, 130, 2, 1, 1, 1, 1]
+    cache = Cache([n + 100 for n in chunks], 2, 128)
+    clean = Extension(cache, chunks, 8)
+    dec.extend(clean.c)
+    clean.check()
+    cache.v[int(cache.table[2, (100 + at) // 16]), :, (100 + at) % 16, 5:9] = float("nan")
+    x = Extension(cache, chunks, 8)
+    dec.extend(x.c)
+    torch.cuda.synchronize()
+    spoilt = torch.isnan(x.out).any(-1).any(-1)
+    assert spoilt.tolist() == [2 + at <= t < 132 for t in range(sum(chunks))]
