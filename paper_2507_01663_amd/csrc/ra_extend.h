@@ -40,12 +40,13 @@ constexpr int kExRows = kPfRows * kExWaves; // rows of a block
 
 struct ExSeq {
     int t0, n, L;  // first packed token, new tokens, tokens in all
-    int blocks, cost; // blocks of a kv head; the length of each on the line (stages, the mean of the sequence's blocks, and kFixed)
+    int blocks, cost, fixed; // blocks of a kv head; the length of each on the line (stages, the mean of the sequence's blocks, and ex_fixed)
 };
 
+constexpr int kExFixedMany = 8, kExFixedFew = 4;
 // What an item costs beside its stages, in stages: finding it, its query rows, the first trip to memory, its results.
-constexpr int kExFixed = 4;
-constexpr int kExEdge = 2; // no part of an item is shorter than this (a span is longer than kExFixed + 2 kExEdge)
+__host__ __device__ __forceinline__ int ex_fixed(int most, bool two) { return most > 64 && !two ? kExFixedMany : kExFixedFew; }
+constexpr int kExEdge = 2; // no part of an item is shorter than this (a span is longer than ex_fixed + 2 kExEdge)
 
 __device__ __forceinline__ int ex_uni(int x) { return __builtin_amdgcn_readfirstlane(x); } // (a quotient comes from the vector unit)
 // x / y for 0 <= x < 2^30, y > 0, both the wave's: the quotient by the reciprocal in binary32 is off by x / y 2^-22 at most, the
@@ -85,7 +86,7 @@ __device__ __forceinline__ bool ex_few(const ExtendLaunch &a, int n) { return a.
 // first keys once and alone, an instruction after the other: they are few.)
 __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int t1, int L)
 {
-    ExSeq s = {0, 0, 0, 0, 0};
+    ExSeq s = {0, 0, 0, 0, 0, 0};
     const int n = t1 - t0, most = a.max_pages * kPage;
     if (t0 < 0 || t0 > a.T || n <= 0 || n > a.T - t0) return s;
     s.t0 = t0;
@@ -93,12 +94,14 @@ __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int 
     s.L = L < 0 ? 0 : (L < most ? L : most);
     s.blocks = (s.n * a.G + kExRows - 1) / kExRows;
     const int mean = (s.L - (s.n >> 1) + 48) >> 5; // keys that a row sees, in stages
-    s.cost = kExFixed + 1 + (mean > 0 ? ex_weight(mean, ex_few(a, s.n) ? 32 : a.max_chunk * a.G) : 0);
+    const int most_rows = ex_few(a, s.n) ? 32 : a.max_chunk * a.G;
+    s.fixed = ex_fixed(most_rows, a.two);
+    s.cost = s.fixed + 1 + (mean > 0 ? ex_weight(mean, most_rows) : 0);
     return s;
 }
 __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int b)
 {
-    return b < a.B ? ex_sequence(a, a.cu[b], a.cu[b + 1], a.seq_lens[b]) : ExSeq{0, 0, 0, 0, 0};
+    return b < a.B ? ex_sequence(a, a.cu[b], a.cu[b + 1], a.seq_lens[b]) : ExSeq{0, 0, 0, 0, 0, 0};
 }
 
 // The line: lane c has chunk c of the sequences (64 of them, or a multiple of that in a very large batch).  Of a batch of up to
@@ -253,20 +256,26 @@ template <bool TWO> struct ExLine {
         return at < per && k < spans && total > 0 ? k : -1;
     }
     __device__ __forceinline__ int raw(int k) const { return q * k + (k < r ? k : r); }
-    // The last span that an item which ends at x1 has a part in, if it is cut.
+    // The last span that starts at y or before it, but for cuts that move.
+    __device__ __forceinline__ int span_of(int y) const
+    {
+        const int big = r * (q + 1);
+        const bool in_big = y < big;
+        return (in_big ? 0 : r) + ex_div(in_big ? y : y - big, in_big ? q + 1 : q);
+    }
+    // The first and the last span that an item which is cut and lies from x0 to x1 has a part in (cuts near its ends move there).
+    __device__ __forceinline__ int first_of(int x0, const ExSeq &s) const { return span_of(x0 + s.fixed + kExEdge - 1); }
     __device__ __forceinline__ int last_of(int x1) const
     {
-        const int y = x1 - 1, big = r * (q + 1);
-        const bool in_big = y < big;
-        const int k = (in_big ? 0 : r) + ex_div(in_big ? y : y - big, in_big ? q + 1 : q); // the last one that starts before x1
-        return x1 - raw(k) < kExEdge ? k - 1 : k;                          // (but for a cut that moves there)
+        const int k = span_of(x1 - 1);
+        return x1 - raw(k) < kExEdge ? k - 1 : k;
     }
     // Where a cut at x goes in the item of that length that starts at x0: nowhere into short items, and not so near an end of
     // others that a part would be next to nothing.
-    __device__ __forceinline__ int moved(int x, int x0, int cost) const
+    __device__ __forceinline__ int moved(int x, int x0, const ExSeq &s) const
     {
-        const int y = x - x0, left = cost - y;
-        const bool down = cost > cut ? y < kExFixed + kExEdge : y < left, up = cost > cut ? left < kExEdge : true;
+        const int y = x - x0, cost = s.cost, left = cost - y;
+        const bool down = cost > cut ? y < s.fixed + kExEdge : y < left, up = cost > cut ? left < kExEdge : true;
         return down ? x0 : up ? x0 + cost : x;
     }
 };
@@ -290,7 +299,7 @@ __device__ __forceinline__ void ex_find(const ExtendLaunch &a, const ExLine<TWO>
 {
     const int c = 63 - __builtin_clzll(__ballot(line.before <= x));
     int base = 64 * c, before;
-    ExSeq s = {0, 0, 0, 0, 0};
+    ExSeq s = {0, 0, 0, 0, 0, 0};
     if (known) {
         const int4 rec = known->rec[base + line.lane];
         s.t0 = rec.z, s.n = rec.w, s.L = known->len[base + line.lane], before = rec.x;
@@ -326,7 +335,7 @@ __device__ __forceinline__ int ex_find_ranked(const ExtendLaunch &a, const ExLin
     const int c = 63 - __builtin_clzll(__ballot(ranked <= x)), b = 64 * c + line.lane;
     const int4 rec = known->rec[b];
     const int2 rank = known->rank[b];
-    const ExSeq s = {rec.z, rec.w, known->len[b], 0, 0};
+    const ExSeq s = {rec.z, rec.w, known->len[b], 0, 0, 0};
     const int l = 63 - __builtin_clzll(__ballot(s.n > 0 && rank.x == cls && rank.y <= x));
     ex_place(a, s, 64 * c, l, p);
     return x - __builtin_amdgcn_readlane(rank.y, l);
@@ -351,7 +360,7 @@ __device__ __forceinline__ ExPart ex_part(const ExtendLaunch &a, const ExPlace &
     stages = stages < 0 ? 0 : stages;
     // (a place inside the item, in proportion: the same for the two parts that it divides)
     auto stage_at = [&](int y) __attribute__((always_inline)) {
-        return ex_uni((int)((float)stages * ((float)(y - kExFixed) * __builtin_amdgcn_rcpf((float)(p.s.cost - kExFixed)))));
+        return ex_uni((int)((float)stages * ((float)(y - p.s.fixed) * __builtin_amdgcn_rcpf((float)(p.s.cost - p.s.fixed)))));
     };
     t.lo = y0 == 0 ? 0 : stage_at(y0);
     t.hi = y1 == p.s.cost ? stages : stage_at(y1);
@@ -364,8 +373,8 @@ __device__ __forceinline__ ExPart ex_part(const ExtendLaunch &a, const ExPlace &
 // Items that are left whole: with gg = gcd(Hkv, 8), a die takes the kv heads congruent to it mod gg, and the 8 / gg dies that
 // take the same heads take their items in turn, so that every die has its share of every sequence, and blocks that read the
 // same keys run side by side on few of them.
-// Else: a die takes neighbouring spans.  Also tells the merge which items begin in a span and end in another: desc[2 k],
-// desc[2 k + 1] = {first packed token, first row, rows, kv head}, {last span, -, -, -}.
+// Else: a die takes neighbouring spans.  Also tells the merge which spans begin inside an item: desc[2 k], desc[2 k + 1] =
+// {first packed token, first row, rows, kv head}, {first span of the item or -1, its last, -, -}.
 // `work_few`: the same for sequences of few rows, where there are both (TWO).
 template <bool TWO, typename F, typename FewF> __device__ __forceinline__ void ex_walk(const ExtendLaunch &a, uint8_t *lds, F &&work, FewF &&work_few)
 {
@@ -377,7 +386,8 @@ template <bool TWO, typename F, typename FewF> __device__ __forceinline__ void e
     ExPlace p;
     ExPart part;
     p.item = 0, p.x0 = 0;
-    int last = 0, x = 0, end = 0, k = -1, number = blockIdx.x;
+    int x = 0, end = 0, k = -1, number = blockIdx.x;
+    int2 ends = {-1, 0};
     bool whole = false; // one item, and nothing else
     int4 begun = {0, 0, 0, 0};
     if (a.direct) {
@@ -423,7 +433,7 @@ template <bool TWO, typename F, typename FewF> __device__ __forceinline__ void e
             // `end` is moved where the span gets to it
             end = k + 1 < line.spans ? line.raw(k + 1) : line.total, x = line.raw(k);
             ex_find(a, line, known, x, p);
-            x = line.moved(x, p.x0, p.s.cost);
+            x = line.moved(x, p.x0, p.s);
             if (x == p.x0 + p.s.cost) {
                 if (p.item + 1 < a.Hkv * p.s.blocks) p.item++, p.x0 = x;
                 else if (x < end) ex_find(a, line, known, x, p);
@@ -436,13 +446,13 @@ template <bool TWO, typename F, typename FewF> __device__ __forceinline__ void e
             int next = end;
             if (!whole) {
                 const int x1 = p.x0 + p.s.cost;
-                if (end < x1) end = line.moved(end, p.x0, p.s.cost);
+                if (end < x1) end = line.moved(end, p.x0, p.s);
                 if (x >= end) break;
                 next = x1 < end ? x1 : end;
                 part = ex_part(a, p, x - p.x0, next - p.x0, number);
-                if (x == p.x0 && next < x1) {
+                if (x > p.x0) {
                     begun = make_int4(p.s.t0, part.row0, part.rows, part.kvh);
-                    last = line.base + line.last_of(x1);
+                    ends = make_int2(line.base + line.first_of(p.x0, p.s), line.base + line.last_of(x1));
                 }
             }
             if (first) __syncthreads(); // (what the waves know of the line makes room for the ring)
@@ -458,7 +468,7 @@ template <bool TWO, typename F, typename FewF> __device__ __forceinline__ void e
     else go(work);
     if (!a.direct && threadIdx.x == 0 && number < a.spans) { // (every span is answered for, also one that does not exist)
         a.desc[2 * number] = begun;
-        a.desc[2 * number + 1] = make_int4(last, 0, 0, 0);
+        a.desc[2 * number + 1] = make_int4(ends.x, ends.y, 0, 0);
     }
 }
 
@@ -1219,62 +1229,31 @@ template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWav
 
 // ---- what spans share -----------------------------------------------------------------------------------
 
-constexpr int kExMergeWgs = 2048, kExMaxSpans = 1024;
-constexpr int kExMergeFew = 12; // parts of an item that one wave adds up
+constexpr int kExMaxSpans = 1024, kExMergeWgs = 4; // workgroups of the merge for each span
+constexpr int kExMergeFew = 12;                    // parts of an item that one wave adds up
 
-// Adds up the parts of the items that a cut goes through, 256 consecutive values of an item's parts at a time: a wave alone
-// where every item has few parts, else a workgroup's waves every fourth part each.
-template <int D> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(const int4 *__restrict__ desc, int spans, ExtendLaunch given)
+// Adds up the parts of the items that a cut goes through, 256 consecutive values of an item's parts at a time.  An item of P
+// parts lies in P - 1 spans that begin inside it: each of them has every (P - 1)-th of the item's chunks of 256 values to add
+// up, so that all have as much to read.  A wave does so alone where the item has few parts, else a workgroup's waves take
+// every fourth part each.
+template <int D> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(const int4 *__restrict__ desc, ExtendLaunch given)
 {
     ExtendLaunch a = given;
-    a.desc = (int4 *)desc, a.spans = spans;
     touch_lines(given);
-    constexpr int W = kExWaves, CHUNKS = kExRows * D / 256, N = kExMaxSpans / (64 * W);
-    __shared__ int list[kExMaxSpans];
-    __shared__ int counts[W][N], longest[W];
+    constexpr int W = kExWaves, GROUP = D / 8; // chunks of 32 rows
     __shared__ f32x4 sums[W][64];
     __shared__ float2 stats[W][64];
     const int lane = threadIdx.x & 63, wave = ex_uni((int)threadIdx.x >> 6);
-    // the spans in which such an item begins, in order
-    int ends[N], most = 0, items = 0;
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        const int k = 64 * W * i + (int)threadIdx.x;
-        ends[i] = k < a.spans ? a.desc[2 * k + 1].x : 0;
-    }
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        const int k = 64 * W * i + (int)threadIdx.x;
-        most = most > ends[i] - k ? most : ends[i] - k;
-        const int n = __popcll(__ballot(ends[i] > k));
-        if (lane == 0) counts[wave][i] = n;
-    }
-    const bool long_ones = __any(most >= kExMergeFew);
-    if (lane == 0) longest[wave] = long_ones;
-    __syncthreads();
-    bool split = false;
-#pragma unroll
-    for (int w = 0; w < W; w++) split = split || longest[w];
-#pragma unroll
-    for (int i = 0; i < N; i++) {
-        const int k = 64 * W * i + (int)threadIdx.x;
-        int at = items;
-#pragma unroll
-        for (int w = 0; w < W; w++) {
-            if (w < wave) at += counts[w][i];
-            items += counts[w][i];
-        }
-        const unsigned long long m = __ballot(ends[i] > k);
-        if (ends[i] > k) list[at + __popcll(m & ((1ull << lane) - 1ull))] = k;
-    }
-    __syncthreads();
-    const int each = split ? 1 : W; // units of work that a workgroup takes at a time
-    for (int u0 = blockIdx.x * each; u0 < items * CHUNKS; u0 += gridDim.x * each) {
-        const int u = split ? u0 : u0 + wave, chunk = u % CHUNKS;
-        const bool have = u < items * CHUNKS;
-        const int k = list[have ? u / CHUNKS : 0];
-        const int4 item = a.desc[2 * k]; // {first packed token, first row, rows, kv head}
-        const int last = a.desc[2 * k + 1].x;
+    const int j = blockIdx.x / kExMergeWgs, sub = blockIdx.x % kExMergeWgs;
+    const int4 item = desc[2 * j], ends = desc[2 * j + 1];
+    const int k = ex_uni(ends.x), last = ex_uni(ends.y);
+    if (k < 0) return;
+    const int left = ex_uni(item.z - item.y), chunks = left >= kExRows ? GROUP * kExWaves : GROUP * ((left + 31) >> 5);
+    const bool split = last - k + 1 >= kExMergeFew;
+    const int share = last - k; // spans with a share of the item
+    for (int c0 = j - k - 1 + share * (split ? sub : W * sub); c0 < chunks; c0 += share * (split ? kExMergeWgs : W * kExMergeWgs)) {
+        const int chunk = split ? c0 : c0 + share * wave;
+        const bool have = chunk < chunks;
         int r, d; // this lane's row of the block, and the first of its four values
         {
             const int wv = chunk / (D / 8), c = chunk % (D / 8);

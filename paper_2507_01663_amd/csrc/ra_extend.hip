@@ -6,16 +6,16 @@ namespace ra {
 // How many workgroups a call takes, and how finely its work is cut.
 // An item of S stages that is cut in two saves half of them, and pays for a second workgroup's fixed part and for the merge, a
 // kernel of its own.  Where no item is longer than kExShort, none is cut.
-constexpr int kExLeast = 10, kExShort = 20;
+constexpr int kExLeast = 6, kExShort = 16;
 static void extend_shape(ExtendLaunch &a)
 {
     const int64_t rows = (int64_t)a.max_chunk * a.G; // of a kv head, at most
     a.few = rows <= kExRows;
     a.two = rows > 64 && 4 * (int64_t)a.T <= (int64_t)a.B * a.max_chunk;
     const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExRows + a.B, items = blocks * a.Hkv;
-    const int longest = kExFixed + 1 + ex_weight(a.max_pages / 2 + 1, (int)rows); // an item at most
-    a.least = kExLeast;
-    a.direct = longest <= kExShort;
+    const int most = rows <= 64 ? (int)rows : 65, fixed = ex_fixed(most, a.two), longest = fixed + 1 + ex_weight(a.max_pages / 2 + 1, most); // an item at most
+    a.least = kExLeast + fixed;
+    a.direct = longest <= kExShort + fixed;
     const int64_t resident = (int64_t)(a.num_cus < 8 ? 8 : a.num_cus & ~7) * (a.D == 64 ? 3 : 2);
     int64_t spans = (items * longest / a.least + 7) & ~(int64_t)7;
     spans = spans < 16 ? 16 : spans < resident ? spans : resident; // (two lines take eight each, at least)
@@ -67,8 +67,8 @@ hipError_t launch_extend(const ExtendLaunch &a, hipStream_t s)
 #undef RA_EX_LAUNCH
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.direct) return e;
-    if (a.D == 128) hipLaunchKernelGGL(extend_merge_kernel<128>, dim3(kExMergeWgs), block, 0, s, a.desc, a.spans, a);
-    else hipLaunchKernelGGL(extend_merge_kernel<64>, dim3(kExMergeWgs), block, 0, s, a.desc, a.spans, a);
+    if (a.D == 128) hipLaunchKernelGGL(extend_merge_kernel<128>, dim3((unsigned)(kExMergeWgs * a.spans)), block, 0, s, a.desc, a);
+    else hipLaunchKernelGGL(extend_merge_kernel<64>, dim3((unsigned)(kExMergeWgs * a.spans)), block, 0, s, a.desc, a);
     return hipGetLastError();
 }
 
