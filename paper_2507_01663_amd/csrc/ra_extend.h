@@ -1158,10 +1158,19 @@ template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWav
             };
             if (mine > 0) {
                 const int free = whole - t.lo < mine ? whole - t.lo : mine; // stages without a mask
+                // (two steps at a time: the scores need not change registers)
 #pragma unroll 1
-                for (; s + 1 < free; s++) {
+                for (; s + 2 < free; s++) {
                     open(s + 1);
                     EX_STEP(false, true);
+                    s++;
+                    open(s + 1);
+                    EX_STEP(false, true);
+                }
+                if (s + 1 < free) {
+                    open(s + 1);
+                    EX_STEP(false, true);
+                    s++;
                 }
 #pragma unroll 1
                 for (; s + 1 < mine; s++) {
