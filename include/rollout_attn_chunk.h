@@ -160,7 +160,8 @@ ra_status rollout_attn_check_extend(const ra_extend *extend, char *msg, size_t m
  * size for a 256-compute-unit device is returned.  0 (a batch of short sequences): none, and it may be NULL. */
 ra_status rollout_attn_extend_workspace_size(const ra_ctx *ctx, const ra_extend *shape_only, size_t *bytes);
 
-/* Enqueues the attention on hip_stream: at most three kernels.  workspace as for rollout_attn_decode: dev memory of at
+/* Enqueues the attention on hip_stream: one kernel, and a second where workgroups may share a sequence's work (a workspace size
+ * other than 0); a decode step's where it runs as one.  workspace as for rollout_attn_decode: dev memory of at
  * least rollout_attn_extend_workspace_size() bytes, 256-byte aligned, contents irrelevant on entry and undefined
  * afterwards; calls that overlap in time need distinct workspaces. */
 ra_status rollout_attn_extend(ra_ctx *ctx, const ra_extend *extend, void *workspace, size_t workspace_bytes, void *hip_stream);
