@@ -239,15 +239,22 @@ template <int D, RowsTo TO> static hipError_t launch_rows(RowsLaunch &a, int num
 {
     const int rows = a.Hq + a.Hkv + (TO == kToPages ? a.Hkv : 0);
     if (a.T == 0 || rows == 0) return hipSuccess;
-    // Few rows: as many waves as there are, a pass each.  Many: four passes, whose loads are on their way together.
+    // Few rows: as many waves as there are, a pass each.  Many, into a cache: four passes, which look for their place in it once
+    // (8 192 tokens of 64 + 8 + 8 heads: 75.4 -> 71.1 us; 256 tokens of 28 + 4 + 4: 4.5, with four passes 6.2).  Without a place to
+    // look for a pass each is the faster also there (7 000 rotated tokens of 34 heads, D = 64: 12.6 us, with four 14.9).
     int64_t units = rows_units<D>(a, rows, 1);
-    const bool many = units > 32 * (int64_t)num_cus;
+    const bool many = TO != kToRows && units > 32 * (int64_t)num_cus;
     if (many) units = rows_units<D>(a, rows, 4);
     const int64_t groups = (units + kRowWaves - 1) / kRowWaves;
     if (groups > INT32_MAX) return hipErrorInvalidValue;
 #define RA_ROWS(a) a.q, a.k, a.q_stride, a.k_stride, a.T, a.Hq, a.Hkv, a.slots_shift, a
-    if (many) hipLaunchKernelGGL((rows_kernel<D, TO, 4>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, RA_ROWS(a));
-    else hipLaunchKernelGGL((rows_kernel<D, TO, 1>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, RA_ROWS(a));
+    if constexpr (TO != kToRows) {
+        if (many) {
+            hipLaunchKernelGGL((rows_kernel<D, TO, 4>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, RA_ROWS(a));
+            return hipGetLastError();
+        }
+    }
+    hipLaunchKernelGGL((rows_kernel<D, TO, 1>), dim3((unsigned)groups), dim3(64 * kRowWaves), 0, s, RA_ROWS(a));
 #undef RA_ROWS
     return hipGetLastError();
 }
