@@ -5,8 +5,14 @@ namespace ra {
 
 // How many workgroups a call takes, and how finely its work is cut.
 // An item of S stages that is cut in two saves half of them, and pays for a second workgroup's fixed part and for the merge, a
-// kernel of its own.  Where no item is longer than kExShort, none is cut.
-constexpr int kExLeast = 6, kExShort = 16;
+// kernel of its own: about 10 us.  So none is cut where the page table has room for short items only, and a workgroup takes each
+// without looking at the others: up to kExShort stages beside the fixed part where there are few items, up to kExShortMany
+// where there is one for every compute unit.  (Times in us uncut and cut, 28 heads on four, D = 128, bf16: one item for every
+// second unit, 17 stages 28.8, 38.4, 24 36.2, 37.0, 34 45.8, 42.3; one for each, 24 stages 40.2, 46.8, 34 52.4, 59.8, 45 64.4,
+// 65.8; 320 of 36 stages and more than 64 rows, e4m3, D = 64: 62.0, 55.)
+// kExLeast: stages of a span at least, beside the fixed part.  (Eight items of 34 stages to 64 rows and 26 to 32: 6 is 26.7 and
+// 24.8 us, 3 25.2 and 24.4, 12 31.1 and 29.2; 36 stages 28.3, 33.5, 31.0.)
+constexpr int kExLeast = 6, kExShort = 20, kExShortMany = 36;
 static void extend_shape(ExtendLaunch &a)
 {
     const int64_t rows = (int64_t)a.max_chunk * a.G; // of a kv head, at most
@@ -15,7 +21,7 @@ static void extend_shape(ExtendLaunch &a)
     const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExRows + a.B, items = blocks * a.Hkv;
     const int most = rows <= 64 ? (int)rows : 65, fixed = ex_fixed(most, a.two), longest = fixed + 1 + ex_weight(a.max_pages / 2 + 1, most); // an item at most
     a.least = kExLeast + fixed;
-    a.direct = longest <= kExShort + fixed;
+    a.direct = longest <= (items < a.num_cus ? kExShort : kExShortMany) + fixed;
     const int64_t resident = (int64_t)(a.num_cus < 8 ? 8 : a.num_cus & ~7) * (a.D == 64 ? 3 : 2);
     int64_t spans = (items * longest / a.least + 7) & ~(int64_t)7;
     spans = spans < 16 ? 16 : spans < resident ? spans : resident; // (two lines take eight each, at least)

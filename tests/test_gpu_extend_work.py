@@ -51,7 +51,7 @@ def test_items_left_whole(dec, Hq, Hkv, D, B, most, kv):
     chunks = [(1 + b % 2) * (b % 11 != 3) for b in range(B)]
     chunks[B // 2] = most
     lens = [n + (29 * b) % 90 for b, n in enumerate(chunks)]
-    run(dec, "whole", lens, chunks, Hq, Hkv, D, kv, 130)
+    run(dec, "whole", lens, chunks, Hq, Hkv, D, kv, 420)
 
 
 @pytest.mark.parametrize("Hq,Hkv,D,most", [(8, 8, 128, 2), (16, 8, 128, 40)])
@@ -61,7 +61,7 @@ def test_one_long_sequence_among_many(dec, Hq, Hkv, D, most):
     chunks = [1 + b % 2 for b in range(B)]
     chunks[77] = most
     lens = [n + b % 13 for b, n in enumerate(chunks)]
-    lens[77] = 2900
+    lens[77] = 7900
     run(dec, "one long", lens, chunks, Hq, Hkv, D, "bf16", 0)
 
 
@@ -71,7 +71,7 @@ def test_batches_of_every_size(dec, B, most):
     chunks = [int(b % 5 != 2) for b in range(B)]
     chunks[B // 3], chunks[B - 1] = most, most
     lens = [n + b % 19 for b, n in enumerate(chunks)]
-    lens[5], lens[B // 3], lens[B - 2] = 1900, 2100, 600
+    lens[5], lens[B // 3], lens[B - 2] = 5900, 6100, 600
     run(dec, "size", lens, chunks, 1, 1, 64, "bf16", 0)
 
 
@@ -80,6 +80,16 @@ def test_batches_of_every_size(dec, B, most):
 def test_an_item_of_many_parts(dec, D, Hq, chunk, length, kv):
     """Items of a dozen parts and more, beside one that is whole."""
     run(dec, "parts", [length, 33], [chunk, 1], Hq, 1, D, kv, 0)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("B", [9, 270])
+@pytest.mark.parametrize("Hq,most,wide", [(4, 5, 0), (4, 5, 76), (4, 5, 100), (4, 12, 40), (4, 40, 16), (4, 40, 90)])
+def test_items_that_are_short_from_the_start(dec, B, Hq, most, wide, kv):
+    """Page tables on either side of the width up to which a workgroup takes an item without looking at the others."""
+    chunks = [(1 + (b * 7) % most) * (b % 5 != 1) for b in range(B)]
+    lens = [n + (17 * b) % 40 for b, n in enumerate(chunks)]
+    run(dec, "short", lens, chunks, Hq, 1, 64, kv, wide)
 
 
 @pytest.mark.parametrize("kv", ["bf16", "e4m3"])
