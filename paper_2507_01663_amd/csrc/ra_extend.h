@@ -7,8 +7,21 @@
 // A workgroup of four waves takes a block of up to 128 rows.  Many are bound by the matrix cores and the vector work between:
 // 32 to a wave, all waves multiplying every stage of 32 keys that streams through one LDS ring:
 //   S^T[key, row] = K . Q^T,   O^T[d, row] += V^T . P^T     (32x32x16 MFMA, binary32 sums, softmax running per row)
-// Where no sequence has more than 64, they are bound by the stream of pages: every wave multiplies stages of its own with all
-// the rows, and what the waves have is added up in LDS (ex_narrow).
+// Up to 64 are bound by the stream of pages: every wave multiplies stages of its own with all the rows, and what the waves have
+// is added up in LDS (ex_narrow).  Kernels of its own do so where no sequence has more, and one has both ways where most
+// sequences are far shorter than the longest.
+//
+// With q rows of D values, keys k_j and values v_j, a row's stages are taken with its running maximum m and sum l, all in
+// binary32: s_j = scale <q, k_j> log2 e, p_j = 2^(s_j - m), l += sum p_j, o += sum p_j v_j; where a maximum exceeds m by more
+// than 8, m moves there and o and l are multiplied by 2^(m_old - m_new) first.  p_j goes to the matrix cores as bf16, which
+// rounds it (relative 2^-8 at most, the part of a result's error that its own rounding does not explain) and keeps l's unrounded sum;
+// e4m3 codes go there as bf16 exactly, the page's scales into s_j and p_j before its rounding.
+//
+// What bounds it (stated sizes, MI355X): many rows, the vector instructions of the softmax beside the products and the clock
+// that the card's power leaves: 2048 new tokens over 14 000, 64 heads on eight, 1001 us, 1.0 PFLOP/s of the mask's products; 40
+// turns of 20 to 300 tokens over 1024 to 4000, 40 on eight, 431 to 449 us, 0.8 PFLOP/s, an eighth of it items' starts and ends.
+// Few rows: 64 drafts of five tokens over up to 4000, 28 heads on four, 79.7 us, 4.1 TB/s (of four tokens, 28 rows, 66.7 us).
+// Batches of little work each: finding it (3 to 4 us), rows and first pages (3), parts' results (2) and their merge (7 to 10).
 //
 // The work is a line of items, one per (sequence, kv head, block), each as long as it has stages, and the line is cut into
 // as many spans of one length as workgroups are resident, so that ragged lengths load them alike.  Every workgroup finds its
@@ -43,8 +56,10 @@ struct ExSeq {
     int blocks, cost, fixed; // blocks of a kv head; the length of each on the line (stages, the mean of the sequence's blocks, and ex_fixed)
 };
 
+// What an item costs beside its stages, in stages: finding it, its query rows, the first trip to memory, its results.  (8 to 9 us
+// beside 0.7 to 1.0 for a stage that waves share, 5 beside 0.28 for one of few rows: 96 short turns, D = 64, e4m3, with 8 63.6 us, with
+// 4 64.4.  A kernel that has both is the faster with 4 for either, 51.9 us against 56: the two kinds share compute units.)
 constexpr int kExFixedMany = 8, kExFixedFew = 4;
-// What an item costs beside its stages, in stages: finding it, its query rows, the first trip to memory, its results.
 __host__ __device__ __forceinline__ int ex_fixed(int most, bool two) { return most > 64 && !two ? kExFixedMany : kExFixedFew; }
 constexpr int kExEdge = 2; // no part of an item is shorter than this (a span is longer than ex_fixed + 2 kExEdge)
 
@@ -188,10 +203,11 @@ template <bool TWO> struct ExLine {
             spans = spans < 1 ? 1 : spans;
         }
         divide(a, sum);
-        // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.
+        // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.  (40
+        // turns, 2288 items: 431 us, cut into spans 538; 64 shorter ones, D = 64, 197 and 252.)
         unit = a.B <= kExKnown && blocks * a.Hkv >= 2 * a.spans && !__any(longest > q);
         if (!unit) return;
-        // (what is started last should be short: by length, in classes of a quarter of the longest)
+        // (what is started last should be short: by length, in classes of a quarter of the longest; the 40 turns 459 -> 449 us)
 #pragma unroll
         for (int sh = 32; sh >= 1; sh >>= 1) {
             const int o = __shfl_xor(longest, sh);
@@ -996,7 +1012,8 @@ template <int D, bool FP8> struct ExTileLds {
     static_assert(N::kNeeds <= kAreas && N::kRows <= kArea * kExWaves && N::kEnds <= kBytes, "few rows find room in it");
 };
 
-// What the rows of a kernel's sequences (of one kv head) are: any number; up to 32; up to 64; up to 32 or any number.
+// What the rows of a kernel's sequences (of one kv head) are: any number; up to 32; up to 64; up to 32 or any number.  (64 drafts of
+// 28 rows 66.7 us by kEx32, 83.1 by kExAny, e4m3 42.5 and 66; of 35 rows 79.7 by kEx64, 84.6; for kExTwo see extend_shape.)
 enum ExKind { kExAny, kEx32, kEx64, kExTwo };
 
 template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_kernel(EX_PARAMS)
@@ -1239,11 +1256,13 @@ template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWav
 // ---- what spans share -----------------------------------------------------------------------------------
 
 constexpr int kExMaxSpans = 1024, kExMergeWgs = 4; // workgroups of the merge for each span
-constexpr int kExMergeFew = 12;                    // parts of an item that one wave adds up
+constexpr int kExMergeFew = 12; // an item of fewer parts is one wave's to add up (one of 64 parts: 47.4 us in all, so too 55.6; all
+                                // items by four waves: 64 drafts 86.4 us, so 79.8)
 
 // Adds up the parts of the items that a cut goes through, 256 consecutive values of an item's parts at a time.  An item of P
 // parts lies in P - 1 spans that begin inside it: each of them has every (P - 1)-th of the item's chunks of 256 values to add
-// up, so that all have as much to read.  A wave does so alone where the item has few parts, else a workgroup's waves take
+// up, so that all have as much to read.  Its time is the launch, two trips and the parts: 7 us for 64
+// drafts (15 MB read), 8 for a mixed batch (24 MB), 9 for 96 short turns (31 MB), 4 where there are none.  A wave does so alone where the item has few parts, else a workgroup's waves take
 // every fourth part each.
 template <int D> __global__ __launch_bounds__(64 * kExWaves) void extend_merge_kernel(const int4 *__restrict__ desc, ExtendLaunch given)
 {

@@ -17,6 +17,9 @@ static void extend_shape(ExtendLaunch &a)
 {
     const int64_t rows = (int64_t)a.max_chunk * a.G; // of a kv head, at most
     a.few = rows <= kExRows;
+    // Many sequences far shorter than the longest: the short ones apart.  (64 sequences, 62, 56, 48, 32 of them single tokens, the
+    // others of 200, 32 heads on eight, e4m3: 55.8, 87.6, 130, 223 us, in one line 87.3, 117, 149, 233; bf16 84.4, 95.2, 130, 199, in one
+    // line 84.5, 117, 125, 197.)
     a.two = rows > 64 && 4 * (int64_t)a.T <= (int64_t)a.B * a.max_chunk;
     const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExRows + a.B, items = blocks * a.Hkv;
     const int most = rows <= 64 ? (int)rows : 65, fixed = ex_fixed(most, a.two), longest = fixed + 1 + ex_weight(a.max_pages / 2 + 1, most); // an item at most
