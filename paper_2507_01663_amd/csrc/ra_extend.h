@@ -18,9 +18,9 @@
 // e4m3 codes go there as bf16 exactly, the page's scales into s_j and p_j before its rounding.
 //
 // What bounds it (stated sizes, MI355X): many rows, the vector instructions of the softmax beside the products and the clock
-// that the card's power leaves: 2048 new tokens over 14 000, 64 heads on eight, 1001 us, 1.0 PFLOP/s of the mask's products; 40
-// turns of 20 to 300 tokens over 1024 to 4000, 40 on eight, 431 to 449 us, 0.8 PFLOP/s, an eighth of it items' starts and ends.
-// Few rows: 64 drafts of five tokens over up to 4000, 28 heads on four, 79.7 us, 4.1 TB/s (of four tokens, 28 rows, 66.7 us).
+// that the card's power leaves: 2048 new tokens over 14 000, 64 heads on eight, 971 us, 1.04 PFLOP/s of the mask's products; 40
+// turns of 20 to 300 tokens over 1024 to 4000, 40 on eight, 430.5 us, 0.83 PFLOP/s, an eighth of it items' starts and ends.
+// Few rows: 64 drafts of five tokens over up to 4000, 28 heads on four, 79.1 us, 4.1 TB/s (of four tokens, 28 rows, 66.7 us).
 // Batches of little work each: finding it (3 to 4 us), rows and first pages (3), parts' results (2) and their merge (7 to 10).
 //
 // The work is a line of items, one per (sequence, kv head, block), each as long as it has stages, and the line is cut into
