@@ -494,6 +494,11 @@ template <bool TWO, typename F, typename FewF> __device__ __forceinline__ void e
 // is NaN.  Where a V operand of such a stage holds one (which is looked for there alone), the product is made without these
 // values, and what they do to the rows that see them is added apart: a product of "infinite, or NaN" with "seen" for either
 // sign, and an infinity for every place where it is not zero.  NaN has both.
+//
+// The scale of an e4m3 page may be infinite or NaN as well (an appended infinity makes it infinite).  Where one of such a stage is
+// (which is looked for there alone), the page's scores are multiplied by it before the mask, so that later tokens' are -inf, and
+// V's scale has no part in the weights, all zero, of a row that does not see the page.  (A row that sees any of it is not finite
+// anyway: finite values have code zero there.  By the weights one by one instead: 64 drafts of five, e4m3, 59 -> 67 us; so 60.)
 
 __device__ __forceinline__ bool ex_odd(bf16x8 v)
 {
@@ -502,6 +507,17 @@ __device__ __forceinline__ bool ex_odd(bf16x8 v)
 #pragma unroll
     for (int i = 0; i < 4; i++) odd = odd || (w[i] & 0x7f80u) == 0x7f80u || (w[i] & 0x7f800000u) == 0x7f800000u;
     return odd;
+}
+// Is one of a stage's scales infinite or NaN?  (None is negative.)
+__device__ __forceinline__ bool ex_odd(float k0, float k1, float v0, float v1) { return __any(!(k0 + k1 + v0 + v1 < INFINITY)); }
+// Takes K scales that are into the stage's scores: of the page's keys that the lane's row sees; the others' are -inf.
+__device__ __forceinline__ void ex_scale_seen(f32x16 &s, float k0, float k1, int key, int lim, int hh)
+{
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+        const float k = e < 8 ? k0 : k1;
+        if (!(k < INFINITY)) s[e] = key + 8 * (e >> 2) + 4 * hh + (e & 3) > lim ? -INFINITY : s[e] * k;
+    }
 }
 // v without them; plus, minus: one where v has an infinity of that sign or a NaN.
 __device__ __forceinline__ bf16x8 ex_even(bf16x8 v, u32x4 &plus, u32x4 &minus)
@@ -557,7 +573,7 @@ struct ExScale {
 // One step of a wave's software pipeline: the weights of a stage (whose scores are st.s) and the scores of the next
 // (NEXT; MASK: the causal mask cuts one of the two), then O += P V of the first and the maxima of the new scores.
 // key, key_next: first keys of the two stages; lim: the last key that the lane's row sees.
-// As pf_step, but for the scales of e4m3 pages (their codes lie in the ring as bf16, exactly) and what MASK does with V.
+// As pf_step, but for the scales of e4m3 pages (their codes lie in the ring as bf16, exactly) and what MASK does with V and with them.
 template <int D, bool FP8, bool MASK, bool NEXT>
 __device__ __forceinline__ void ex_step(PfState<D> &st, uint32_t k_next, uint32_t v_addr, const PfLane<D> &pl, const ExScale &sc, const ExScale &sn_,
                                         int key, int key_next, int lim)
@@ -589,14 +605,21 @@ __device__ __forceinline__ void ex_step(PfState<D> &st, uint32_t k_next, uint32_
             vr[dt][kk][rd] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4)(vb ^ (uint32_t)pf_v_xor<D>(dt, rd)) + kk * G::kTile / 8);
     };
     EX_FENCE();
+    const bool odd_scale = FP8 && (MASK || !NEXT) && ex_odd(sc.k0, sc.k1, sc.v0, sc.v1);
+    float k0 = sc.k0, k1 = sc.k1, v0 = sc.v0, v1 = sc.v1;
+    if (__builtin_expect(odd_scale, 0)) {
+        ex_scale_seen(st.s, k0, k1, key, lim, hh);
+        k0 = k0 < INFINITY ? k0 : 1.f, k1 = k1 < INFINITY ? k1 : 1.f;
+        v0 = key > lim ? 1.f : v0, v1 = key + kPage > lim ? 1.f : v1;
+    }
     u32x4 pw[2];
     float pprev = 0.f, acc0 = 0.f, acc1 = 0.f;
     auto w_item = [&](int k) {
         if (k < 16) {
-            float pk = __builtin_amdgcn_exp2f(__builtin_fmaf(st.s[k], k < 8 ? sc.k0 : sc.k1, -st.m));
+            float pk = __builtin_amdgcn_exp2f(__builtin_fmaf(st.s[k], k < 8 ? k0 : k1, -st.m));
             if (k & 1) acc1 = k == 1 ? pk : acc1 + pk;
             else acc0 = k == 0 ? pk : acc0 + pk;
-            if (FP8) pk *= k < 8 ? sc.v0 : sc.v1;
+            if (FP8) pk *= k < 8 ? v0 : v1;
             if (k & 1) pw[k >> 3][(k >> 1) & 3] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{pprev, pk}), bf16x2));
             else pprev = pk;
         } else {
@@ -671,7 +694,7 @@ __device__ __forceinline__ void ex_step(PfState<D> &st, uint32_t k_next, uint32_
         else if (k == 7) mx = max3(first_max(sn[8], sn[9]), sn[10], sn[11]);
         else if (k == 8) mx = max3(mx, sn[12], sn[13]);
         else if (k == 9) mx = max3(mx, sn[14], sn[15]);
-        else if (k == 10) mx = fmaxf(mx0 * sn_.k0, mx * sn_.k1);
+        else if (k == 10) mx = fmaxf(mx0 * sn_.k0, mx * sn_.k1); // (-inf by a scale that is NaN: no part in the maximum)
         else if (k >= 12) m_item(k);
     };
     constexpr int NMI = NEXT ? 14 : 0, NPV = 2 * DT;
@@ -822,11 +845,12 @@ __device__ __forceinline__ void ex_narrow(const ExtendLaunch &a, const ExPlace &
         const bool more = i + 1 < mine;
         wait_vmcnt<NV>(); // K is there (V of the stage, asked for after it, may not be)
         asm volatile("" ::: "memory");
-        float sk0 = a.scale_log2, sk1 = a.scale_log2, sv0 = 1.f, sv1 = 1.f;
+        float sk0 = a.scale_log2, sk1 = a.scale_log2, sv0[NG], sv1[NG];
         if (FP8) {
             f32x4 w = *(const f32x4 *)(lds + X::kScales + 256 * wave);
             sk0 *= w[0] == 0.f ? 1e-30f : w[0], sk1 *= w[2] == 0.f ? 1e-30f : w[2]; // (zero times the mask's -inf would be NaN)
-            sv0 = w[1], sv1 = w[3];
+#pragma unroll
+            for (int g = 0; g < NG; g++) sv0[g] = w[1], sv1[g] = w[3];
         }
         bf16x8 kf[KS];
         if (FP8) {
@@ -865,6 +889,15 @@ __device__ __forceinline__ void ex_narrow(const ExtendLaunch &a, const ExPlace &
             }
         }
         if (NG == 1) sc[0] += sc[1];
+        const bool odd_scale = FP8 && masked && ex_odd(sk0, sk1, sv0[0], sv1[0]);
+        if (__builtin_expect(odd_scale, 0)) {
+#pragma unroll
+            for (int g = 0; g < NG; g++) {
+                ex_scale_seen(sc[g], sk0, sk1, key, lim[g], hh);
+                sv0[g] = key > lim[g] ? 1.f : sv0[g], sv1[g] = key + kPage > lim[g] ? 1.f : sv1[g];
+            }
+            sk0 = sk0 < INFINITY ? sk0 : 1.f, sk1 = sk1 < INFINITY ? sk1 : 1.f;
+        }
 #pragma unroll
         for (int g = 0; g < NG; g++) {
             f32x16 &s = sc[g];
@@ -894,7 +927,7 @@ __device__ __forceinline__ void ex_narrow(const ExtendLaunch &a, const ExPlace &
                 float w0 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], e < 8 ? sk0 : sk1, -m[g]));
                 float w1 = __builtin_amdgcn_exp2f(__builtin_fmaf(s[e + 1], e < 8 ? sk0 : sk1, -m[g]));
                 acc0 += w0, acc1 += w1;
-                if (FP8) w0 *= e < 8 ? sv0 : sv1, w1 *= e < 8 ? sv0 : sv1;
+                if (FP8) w0 *= e < 8 ? sv0[g] : sv1[g], w1 *= e < 8 ? sv0[g] : sv1[g];
                 pw[g][e >> 3][(e >> 1) & 3] = __builtin_bit_cast(unsigned, __builtin_convertvector((f32x2{w0, w1}), bf16x2));
             }
             l[g] += acc0 + acc1;
