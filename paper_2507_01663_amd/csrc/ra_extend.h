@@ -848,7 +848,8 @@ __device__ __forceinline__ void ex_narrow(const ExtendLaunch &a, const ExPlace &
         float sk0 = a.scale_log2, sk1 = a.scale_log2, sv0[NG], sv1[NG];
         if (FP8) {
             f32x4 w = *(const f32x4 *)(lds + X::kScales + 256 * wave);
-            sk0 *= w[0] == 0.f ? 1e-30f : w[0], sk1 *= w[2] == 0.f ? 1e-30f : w[2]; // (zero times the mask's -inf would be NaN)
+            sk0 *= w[0], sk1 *= w[2];
+            sk0 = sk0 == 0.f ? 1e-30f : sk0, sk1 = sk1 == 0.f ? 1e-30f : sk1; // (zero times the mask's -inf would be NaN)
 #pragma unroll
             for (int g = 0; g < NG; g++) sv0[g] = w[1], sv1[g] = w[3];
         }
@@ -1148,7 +1149,7 @@ template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWav
                 const int bits = ex_uni(__float_as_int(f));
                 return __int_as_float(k && (bits & 0x7fffffff) == 0 ? 0x0da24260 : bits); // (1e-30: zero times the mask's -inf would be NaN)
             };
-            sc_put = {scale(w[0], true) * a.scale_log2, scale(w[2], true) * a.scale_log2, scale(w[1], false), scale(w[3], false)};
+            sc_put = {scale(w[0] * a.scale_log2, true), scale(w[2] * a.scale_log2, true), scale(w[1], false), scale(w[3], false)};
             raw_slot = raw_slot + 1 == X::kRaw ? 0 : raw_slot + 1;
             put_slot = after(put_slot);
         };

@@ -1,5 +1,6 @@
 """e4m3 pages that a token does not see: whatever their scales are has no part in the token's result.  A page's scale becomes
 infinite when an infinite value is appended; a NaN is one that nothing appended."""
+import numpy as np
 import pytest
 import torch
 
@@ -108,3 +109,15 @@ def test_an_infinite_value_on_its_way_through_the_cache(dec, Hq, n, before, at, 
     assert same > 0
     assert torch.equal(bits(x.out[:same]), bits(clean.out[:same])) and torch.equal(bits(x.lse[:same]), bits(clean.lse[:same]))
     assert not torch.isfinite(x.out[at - before:, :, 7] if which == "v" else x.out[at - before:]).any()
+
+@pytest.mark.parametrize("Hq,chunk,L", [(8, 8, 148), (8, 16, 152), (8, 70, 150)])
+def test_scores_that_underflow(dec, Hq, chunk, L):
+    """A page's scale times the softmax scale is below the smallest number: all scores are zero, and every key that is seen
+    weighs the same."""
+    cache = Cache([L], 2, 128, "e4m3")
+    cache.ks.fill_(1e-20)
+    x = Extension(cache, [chunk], Hq)
+    x.scale = float(np.float32(1e-30))
+    x.c.softmax_scale = x.scale
+    dec.extend(x.c)
+    x.check("underflow")
