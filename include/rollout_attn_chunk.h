@@ -128,9 +128,10 @@ ra_status rollout_attn_append_chunk(ra_ctx *ctx, const ra_append_chunk *append, 
  * Layout: q bf16, element (t, head, d) at t * q_stride_token + head * D + d; out bf16 [T][Hq][D] and lse fp32 [T][Hq]
  * contiguous, T = total_tokens = cu_seqlens[num_seqs].  cu_seqlens as for ra_append_chunk.  max_chunk_len is a HOST-side
  * upper bound of every chunk's length (the launch is sized by it and by total_tokens; a chunk's tokens at or past it may
- * be left unprocessed).
+ * be left unprocessed, those before it are what they are in the whole chunk).
  * One new token for every sequence (max_chunk_len == 1 and total_tokens == num_seqs) is a decode step, and runs as one
- * without a prompt-group hint where rollout_attn_decode supports the shape and q is contiguous.
+ * without a prompt-group hint where rollout_attn_decode supports the shape and q is contiguous.  Of such a call the bound
+ * must hold: cu_seqlens is not read, and token b is sequence b's.
  * Supported: page_size == 16; D in {64, 128}; Hq % Hkv == 0; Hq / Hkv <= 128.
  */
 typedef struct {

@@ -52,7 +52,7 @@ constexpr int kExRows = kPfRows * kExWaves; // rows of a block
 // ---- the line of items and its spans ------------------------------------------------------------------
 
 struct ExSeq {
-    int t0, n, L;  // first packed token, new tokens, tokens in all
+    int t0, n, L;  // first packed token, new tokens (up to max_chunk), tokens in all up to the last of them
     int blocks, cost, fixed; // blocks of a kv head; the length of each on the line (stages, the mean of the sequence's blocks, and ex_fixed)
 };
 
@@ -106,7 +106,8 @@ __device__ __forceinline__ ExSeq ex_sequence(const ExtendLaunch &a, int t0, int 
     if (t0 < 0 || t0 > a.T || n <= 0 || n > a.T - t0) return s;
     s.t0 = t0;
     s.n = n < a.max_chunk ? n : a.max_chunk;
-    s.L = L < 0 ? 0 : (L < most ? L : most);
+    s.L = (L < 0 ? 0 : (L < most ? L : most)) - (n - s.n);
+    s.L = s.L > 0 ? s.L : 0; // (none sees a key then)
     s.blocks = (s.n * a.G + kExRows - 1) / kExRows;
     const int mean = (s.L - (s.n >> 1) + 48) >> 5; // keys that a row sees, in stages
     const int most_rows = ex_few(a, s.n) ? 32 : a.max_chunk * a.G;
