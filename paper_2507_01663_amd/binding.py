@@ -508,9 +508,8 @@ class Decoder:
         self.ctx = rollout_attn_create(device_ordinal)
         self._ws = None
         self._ws_at = None           # its address and size, always those of one tensor
-        self._chunk_ws = None        # extend's (a schedule that decode keeps in the other one outlives it)
-        self._chunk_ws_at = None
-        self._retired = []
+        self._chunk_ws_at = None     # extend's (a schedule that decode keeps in the other one outlives it)
+        self._retired = []           # tensors that enqueued work may use: every one of extend's, decode's former ones
         self._raw_stream = None
 
     def close(self):
@@ -519,7 +518,7 @@ class Decoder:
             torch.cuda.synchronize(self.device_ordinal)      # nothing enqueued may outlive the buffers
             rollout_attn_destroy(self.ctx)
             self.ctx = None
-            self._ws = self._ws_at = self._chunk_ws = self._chunk_ws_at = None
+            self._ws = self._ws_at = self._chunk_ws_at = None
             self._retired = []
 
     def __del__(self):
@@ -607,11 +606,12 @@ class Decoder:
                 _check(status, self.ctx)
         import torch
         need = max(256, rollout_attn_extend_workspace_size(self.ctx, extend))
-        if self._chunk_ws is not None:
-            self._retired.append(self._chunk_ws)
-        self._chunk_ws = torch.empty(need, dtype=torch.uint8, device="cuda:%d" % self.device_ordinal)
-        self._chunk_ws_at = (self._chunk_ws.data_ptr(), need)
-        rollout_attn_extend(self.ctx, extend, ctypes.c_void_p(self._chunk_ws.data_ptr()), need, ctypes.c_void_p(s))
+        ws = torch.empty(need, dtype=torch.uint8, device="cuda:%d" % self.device_ordinal)
+        self._retired.append(ws)
+        mine, at = (ws.data_ptr(), need), self._chunk_ws_at
+        if at is None or at[1] < need:
+            self._chunk_ws_at = mine
+        rollout_attn_extend(self.ctx, extend, ctypes.c_void_p(mine[0]), mine[1], ctypes.c_void_p(s))
 
     def debug_gather(self, problem, b, kv_head, k_out, v_out, stream=None):
         import torch
