@@ -165,10 +165,10 @@ void fill_shape(ra::ExtendLaunch &a, const ra_extend *p, int num_cus)
     a.max_pages = p->max_pages_per_seq, a.num_cus = num_cus;
 }
 
-// One new token for every sequence, in a shape that the decode step has: what it is asked then.
+// One new token for every sequence, in a shape that the decode step has: what it is asked then, if q is contiguous.
 bool as_decode(const ra_extend *p, ra_problem &d)
 {
-    if (p->max_chunk_len != 1 || p->total_tokens != p->num_seqs || p->q_stride_token != (int64_t)p->Hq * p->D || p->Hq / p->Hkv > 16) return false;
+    if (p->max_chunk_len != 1 || p->total_tokens != p->num_seqs || p->Hq / p->Hkv > 16) return false;
     memset(&d, 0, sizeof d);
     d.B = p->num_seqs, d.Hq = p->Hq, d.Hkv = p->Hkv, d.D = p->D, d.page_size = p->page_size, d.num_pages = p->num_pages;
     d.max_pages_per_seq = p->max_pages_per_seq;
@@ -263,7 +263,8 @@ ra_status rollout_attn_extend(ra_ctx *c, const ra_extend *p, void *workspace, si
         return RA_ERR_WORKSPACE_TOO_SMALL;
     }
     ra_problem d;
-    if (as_decode(p, d) && rollout_attn_check_problem(&d, nullptr, 0) == RA_OK) return rollout_attn_decode(c, &d, workspace, workspace_bytes, stream);
+    if (p->q_stride_token == (int64_t)p->Hq * p->D && as_decode(p, d) && rollout_attn_check_problem(&d, nullptr, 0) == RA_OK)
+        return rollout_attn_decode(c, &d, workspace, workspace_bytes, stream);
     const int es = p->kv_dtype == RA_KV_FP8_E4M3 ? 1 : 2;
     ra::ExtendLaunch a;
     memset(&a, 0, sizeof a);
