@@ -1,6 +1,7 @@
 """ctypes binding of the rollout_attn C ABI (include/rollout_attn.h, include/rollout_attn_chunk.h).  Argument marshalling only: every
 step of the decode path runs in the library's kernels.  There is no fallback: if the shared library is
 missing the import of a symbol raises."""
+import contextlib
 import ctypes
 import os
 
@@ -527,13 +528,19 @@ class Decoder:
         except Exception:
             pass
 
-    def workspace(self, problem):
+    def _bytes(self, n, stream):
+        """Device memory for calls on the given (or the current) torch stream: a block from that stream's own, since one that
+        another stream gave back may still be read by what is enqueued there."""
         import torch
+        with torch.cuda.stream(stream) if isinstance(stream, torch.cuda.Stream) else contextlib.nullcontext():
+            return torch.empty(n, dtype=torch.uint8, device="cuda:%d" % self.device_ordinal)
+
+    def workspace(self, problem, stream=None):
         need = rollout_attn_workspace_size(self.ctx, problem)
         if self._ws is None or self._ws.numel() < need:
             if self._ws is not None:
                 self._retired.append(self._ws)
-            self._ws = torch.empty(need, dtype=torch.uint8, device="cuda:%d" % self.device_ordinal)
+            self._ws = self._bytes(need, stream)
             self._ws_at = (self._ws.data_ptr(), need)
         return self._ws
 
@@ -560,7 +567,7 @@ class Decoder:
                 return
             if status != RA_ERR_WORKSPACE_TOO_SMALL:
                 _check(status, self.ctx)
-        ws = self.workspace(problem)
+        ws = self.workspace(problem, stream)
         rollout_attn_decode(self.ctx, problem, ctypes.c_void_p(ws.data_ptr()), ws.numel(), ctypes.c_void_p(s))
 
     def decode_static(self, problem, stream=None):
@@ -570,7 +577,7 @@ class Decoder:
     def schedule(self, problem, stream=None):
         """Runs only the schedule; returns (ra_schedule_info, the workspace tensor it was written to)."""
         import torch
-        ws = self.workspace(problem)
+        ws = self.workspace(problem, stream)
         s = stream if stream is not None else torch.cuda.current_stream(self.device_ordinal)
         info = rollout_attn_debug_schedule(self.ctx, problem, ctypes.c_void_p(ws.data_ptr()), ws.numel(), ctypes.c_void_p(s.cuda_stream))
         return info, ws
@@ -604,9 +611,8 @@ class Decoder:
                 return
             if status != RA_ERR_WORKSPACE_TOO_SMALL:
                 _check(status, self.ctx)
-        import torch
         need = max(256, rollout_attn_extend_workspace_size(self.ctx, extend))
-        ws = torch.empty(need, dtype=torch.uint8, device="cuda:%d" % self.device_ordinal)
+        ws = self._bytes(need, stream)
         self._retired.append(ws)
         mine, at = (ws.data_ptr(), need), self._chunk_ws_at
         if at is None or at[1] < need:
