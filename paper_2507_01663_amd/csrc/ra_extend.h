@@ -18,10 +18,12 @@
 // e4m3 codes go there as bf16 exactly, the page's scales into s_j and p_j before its rounding.
 //
 // What bounds it (stated sizes, MI355X): many rows, the vector instructions of the softmax beside the products and the clock
-// that the card's power leaves: 2048 new tokens over 14 000, 64 heads on eight, 971 us, 1.04 PFLOP/s of the mask's products; 40
-// turns of 20 to 300 tokens over 1024 to 4000, 40 on eight, 430.5 us, 0.83 PFLOP/s, an eighth of it items' starts and ends.
-// Few rows: 64 drafts of five tokens over up to 4000, 28 heads on four, 79.1 us, 4.1 TB/s (of four tokens, 28 rows, 66.7 us).
-// Batches of little work each: finding it (3 to 4 us), rows and first pages (3), parts' results (2) and their merge (7 to 10).
+// that the card's power leaves: 2048 new tokens over 14 000, 64 heads on eight, 969 us, 1.04 PFLOP/s of the mask's products (e4m3
+// 1167 us); 40 turns of 20 to 300 tokens over 1024 to 4000, 40 on eight, 431 us, 0.83 PFLOP/s (e4m3 505 us), an eighth of it items'
+// starts and ends.  Few rows: 64 drafts of five tokens over up to 4000, 28 heads on four, 79.1 us, 4.1 TB/s (of four tokens, 28
+// rows, 59.8 us; e4m3 60.1 and 43.4).  Batches of little work each: finding it (3 to 4 us), rows and first pages (3), parts'
+// results (2) and their merge (7 to 10), beside the stages; about 16 us of some 50 to 60 are in none of these parts.
+// Times here are of calls in a row whose inputs change; where two forms are compared both were timed in turn on one card.
 //
 // The work is a line of items, one per (sequence, kv head, block), each as long as it has stages, and the line is cut into
 // as many spans of one length as workgroups are resident, so that ragged lengths load them alike.  Every workgroup finds its
@@ -57,8 +59,8 @@ struct ExSeq {
 };
 
 // What an item costs beside its stages, in stages: finding it, its query rows, the first trip to memory, its results.  (8 to 9 us
-// beside 0.7 to 1.0 for a stage that waves share, 5 beside 0.28 for one of few rows: 96 short turns, D = 64, e4m3, with 8 63.6 us, with
-// 4 64.4.  A kernel that has both is the faster with 4 for either, 51.9 us against 56: the two kinds share compute units.)
+// beside 0.7 to 1.0 for a stage that waves share, 5 beside 0.28 for one of few rows: 96 short turns, D = 64, e4m3, with 8 58.9 us, with
+// 4 60.7.  A kernel that has both is the faster with 4 for either, 51.2 us against 55.6: the two kinds share compute units.)
 constexpr int kExFixedMany = 8, kExFixedFew = 4;
 __host__ __device__ __forceinline__ int ex_fixed(int most, bool two) { return most > 64 && !two ? kExFixedMany : kExFixedFew; }
 constexpr int kExEdge = 2; // no part of an item is shorter than this (a span is longer than ex_fixed + 2 kExEdge)
@@ -205,10 +207,10 @@ template <bool TWO> struct ExLine {
         }
         divide(a, sum);
         // Many items, none of them longer than what a workgroup has on average: they are left whole, a workgroup for each.  (40
-        // turns, 2288 items: 431 us, cut into spans 538; 64 shorter ones, D = 64, 197 and 252.)
+        // turns, 2288 items: 431 us, cut into spans 528; 64 over 100 to 2000, 32 heads on eight, D = 64, 200 and 237.)
         unit = a.B <= kExKnown && blocks * a.Hkv >= 2 * a.spans && !__any(longest > q);
         if (!unit) return;
-        // (what is started last should be short: by length, in classes of a quarter of the longest; the 40 turns 459 -> 449 us)
+        // (what is started last should be short: by length, in classes of a quarter of the longest; the 40 turns 441 -> 431 us)
 #pragma unroll
         for (int sh = 32; sh >= 1; sh >>= 1) {
             const int o = __shfl_xor(longest, sh);
@@ -630,8 +632,8 @@ __device__ __forceinline__ void ex_step(PfState<D> &st, uint32_t k_next, uint32_
     constexpr int NW = 17;
     f32x16 sn;
     // (Of two waves on a SIMD the one further on goes first, which keeps one in products while the other has its weights to make:
-    // 2048 tokens over 14 000 1068 -> 1015 us, 40 turns 466 -> 460, 96 short ones, e4m3, 60.6 -> 59.3; for the second half alone
-    // 1015, 460, 60.2, the same for all of a step 1060, 467, 59.4.)
+    // 2048 tokens over 14 000 1006 -> 968 us, 40 turns 443 -> 431, 96 short ones, e4m3, 60.5 -> 58.9; for the second half alone
+    // 963, 433, 60.2, the same for all of a step 1002, 443, 59.5.)
     __builtin_amdgcn_s_setprio(1);
     if (NEXT) {
 #pragma unroll
@@ -937,7 +939,7 @@ __device__ __forceinline__ void ex_narrow(const ExtendLaunch &a, const ExPlace &
         if (more) wait_vmcnt<NK>(); // V is there
         else wait_vmcnt<0>();
         asm volatile("" ::: "memory");
-        __builtin_amdgcn_s_setprio(1); // (as in ex_step: 64 drafts 79.6 -> 79.0 us)
+        __builtin_amdgcn_s_setprio(1); // (as in ex_step: 64 drafts 79.8 -> 79.1 us)
         bf16x8 vf[DT][2];
         uint32_t vb = v_addr + (uint32_t)(FP8 ? v8_base : pl.v_base);
         asm volatile("" : "+v"(vb));
@@ -1056,7 +1058,8 @@ template <int D, bool FP8> struct ExTileLds {
 };
 
 // What the rows of a kernel's sequences (of one kv head) are: any number; up to 32; up to 64; up to 32 or any number.  (64 drafts of
-// 28 rows 66.7 us by kEx32, 83.1 by kExAny, e4m3 42.5 and 66; of 35 rows 79.7 by kEx64, 84.6; for kExTwo see extend_shape.)
+// 28 rows 59.8 us by kEx32, 91.3 by kExAny, e4m3 43.4 and 120; of 35 rows 79.1 by kEx64, 85.5, e4m3 60.1 and 68.0; for kExTwo see
+// extend_shape.)
 enum ExKind { kExAny, kEx32, kEx64, kExTwo };
 
 template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWaves, D == 64 ? 3 : 2) void extend_kernel(EX_PARAMS)
@@ -1299,8 +1302,8 @@ template <int D, bool FP8, ExKind KIND> __global__ __launch_bounds__(64 * kExWav
 // ---- what spans share -----------------------------------------------------------------------------------
 
 constexpr int kExMaxSpans = 1024, kExMergeWgs = 4; // workgroups of the merge for each span
-constexpr int kExMergeFew = 12; // an item of fewer parts is one wave's to add up (one of 64 parts: 47.4 us in all, so too 55.6; all
-                                // items by four waves: 64 drafts 86.4 us, so 79.8)
+constexpr int kExMergeFew = 12; // an item of fewer parts is one wave's to add up (one of 64 parts: 47.3 us in all, so too 55.4; all
+                                // items by four waves: 64 drafts 85.6 us, so 79.1)
 
 // Adds up the parts of the items that a cut goes through, 256 consecutive values of an item's parts at a time.  An item of P
 // parts lies in P - 1 spans that begin inside it: each of them has every (P - 1)-th of the item's chunks of 256 values to add

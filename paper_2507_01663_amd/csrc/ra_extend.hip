@@ -8,18 +8,18 @@ namespace ra {
 // kernel of its own: about 10 us.  So none is cut where the page table has room for short items only, and a workgroup takes each
 // without looking at the others: up to kExShort stages beside the fixed part where there are few items, up to kExShortMany
 // where there is one for every compute unit.  (Times in us uncut and cut, 28 heads on four, D = 128, bf16: one item for every
-// second unit, 17 stages 28.8, 38.4, 24 36.2, 37.0, 34 45.8, 42.3; one for each, 24 stages 40.2, 46.8, 34 52.4, 59.8, 45 64.4,
-// 65.8; 320 of 36 stages and more than 64 rows, e4m3, D = 64: 62.0, 55.)
-// kExLeast: stages of a span at least, beside the fixed part.  (Eight items of 34 stages to 64 rows and 26 to 32: 6 is 26.7 and
-// 24.8 us, 3 25.2 and 24.4, 12 31.1 and 29.2; 36 stages 28.3, 33.5, 31.0.)
+// second unit, 17 stages of few rows 19.6, 32.0, 24 21.7, 27.7, 34 27.5, 33.6, 45 33.4, 37.0; one for each, 17 stages 23.2, 38.0, 24
+// 27.0, 37.0, 34 34.9, 48.8, 45 43.0, 55.5; 320 of 36 stages and more than 64 rows, e4m3, D = 64: 44.2, 41.8.)
+// kExLeast: stages of a span at least, beside the fixed part.  (Eight items of 34 stages to 64 rows and 26 to 32, cut: 6 is 23.1
+// and 21.3 us, 5 24.5 and 19.6, 12 32.5 and 28.5; 36 stages 23.0, 26.4, 33.0.)
 constexpr int kExLeast = 6, kExShort = 20, kExShortMany = 36;
 static void extend_shape(ExtendLaunch &a)
 {
     const int64_t rows = (int64_t)a.max_chunk * a.G; // of a kv head, at most
     a.few = rows <= kExRows;
     // Many sequences far shorter than the longest: the short ones apart.  (64 sequences, 62, 56, 48, 32 of them single tokens, the
-    // others of 200, 32 heads on eight, e4m3: 55.8, 87.6, 130, 223 us, in one line 87.3, 117, 149, 233; bf16 84.4, 95.2, 130, 199, in one
-    // line 84.5, 117, 125, 197.)
+    // others of 200, 32 heads on eight, e4m3: 55.0, 84.8, 143, 223 us, in one line 76.0, 107, 143, 223; bf16 80.5, 94.5, 120, 192, in one
+    // line 77.5, 98.8, 121, 193.)
     a.two = rows > 64 && 4 * (int64_t)a.T <= (int64_t)a.B * a.max_chunk;
     const int64_t blocks = a.few ? a.B : (int64_t)a.T * a.G / kExRows + a.B, items = blocks * a.Hkv;
     const int most = rows <= 64 ? (int)rows : 65, fixed = ex_fixed(most, a.two), longest = fixed + 1 + ex_weight(a.max_pages / 2 + 1, most); // an item at most

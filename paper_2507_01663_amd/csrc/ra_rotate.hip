@@ -6,9 +6,9 @@
 // one lane: units j and j + rot / 16 where a pair is half the rotated part apart, neighbours where it is a pair of
 // neighbours.  The only step across lanes is the sum of squares, over a row's eight or four.
 //
-// Measured: 16 384 tokens of 28 + 4 heads, D = 128, 54.8 us, 4.9 TB/s read and written (a copy of 1 GiB: 5.1); 7 201 of 32 + 2 heads, D =
-// 64, ragged, 13.0 us; a handful 4.2 us, which is the launch and three trips.  Into pages: 8 192 tokens of 64 + 8 + 8 heads 71.1 us,
-// 4.8 TB/s; one token for each of 256 sequences 4.5 us; 6 424 tokens of 40 + 8 + 8 heads into e4m3 pages 44 us, 4.0 TB/s.
+// Measured: 16 384 tokens of 28 + 4 heads, D = 128, 53.3 us, 5.0 TB/s read and written (a copy of 1 GiB: 5.1); 7 201 of 32 + 2 heads, D =
+// 64, ragged, 12.8 us; a handful 4.4 us, which is the launch and three trips.  Into pages: 8 192 tokens of 64 + 8 + 8 heads 69.3 us,
+// 4.9 TB/s; one token for each of 256 sequences 4.3 us, into e4m3 pages 8.0; 6 424 tokens of 40 + 8 + 8 heads into those 44 us, 4.0 TB/s.
 #include "ra_chunk.h"
 #include "ra_device.h"
 
