@@ -122,7 +122,8 @@ ra_status rollout_attn_append_chunk(ra_ctx *ctx, const ra_append_chunk *append, 
  *   out[.,h] = sum_j softmax(s)_j * v_j          (bf16)
  *   lse[.,h] = ln sum_j exp(s_j)                 (fp32, natural log)
  * A token that sees no key (L - n + i < 0) gives out = 0 and lse = -inf.  What a token does not see has no part in its
- * result, whatever it holds: keys and values of later tokens, slots at or past L (either may be infinite or NaN).  seq_lens
+ * result, whatever it holds: keys and values of later tokens, slots at or past L (either may be infinite or NaN; an e4m3
+ * page's scale is a part of every value in the page, and of a page without a token that is seen it has none).  seq_lens
  * outside [0, max_pages_per_seq * page_size] count as the nearest of the two; block-table entries at or past
  * ceil(L / page_size) are not read, the others must be in [0, num_pages).
  * Layout: q bf16, element (t, head, d) at t * q_stride_token + head * D + d; out bf16 [T][Hq][D] and lse fp32 [T][Hq]
