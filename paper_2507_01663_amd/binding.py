@@ -1,6 +1,6 @@
-"""ctypes binding of the rollout_attn C ABI (include/rollout_attn.h, include/rollout_attn_chunk.h).  Argument marshalling only: every
-step of the decode path runs in the library's kernels.  There is no fallback: if the shared library is
-missing the import of a symbol raises."""
+"""ctypes binding of the rollout_attn C ABI (include/rollout_attn.h, include/rollout_attn_chunk.h,
+include/rollout_attn_step.h).  Argument marshalling only: every step of the decode path runs in the library's
+kernels.  There is no fallback: if the shared library is missing the import of a symbol raises."""
 import contextlib
 import ctypes
 import os
@@ -11,6 +11,7 @@ _lib = None
 
 RA_OK, RA_ERR_INVALID_ARG, RA_ERR_UNSUPPORTED, RA_ERR_WORKSPACE_TOO_SMALL, RA_ERR_OUT_OF_RANGE, RA_ERR_DEVICE = range(6)
 RA_KV_BF16, RA_KV_FP8_E4M3 = 0, 1
+RA_LOGITS_BF16, RA_LOGITS_FP32 = 0, 1
 RA_FLAG_VALIDATE, RA_FLAG_NO_PREFIX_SHARING, RA_FLAG_REUSE_SCHEDULE = 1, 2, 4
 _STATUS_NAMES = ["RA_OK", "RA_ERR_INVALID_ARG", "RA_ERR_UNSUPPORTED", "RA_ERR_WORKSPACE_TOO_SMALL",
                  "RA_ERR_OUT_OF_RANGE", "RA_ERR_DEVICE"]
@@ -93,6 +94,40 @@ class ra_extend(ctypes.Structure):
     ]
 
 
+class ra_place(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("total_tokens", ctypes.c_int32),
+        ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("seq_lens", ctypes.c_void_p), ("new_tokens", ctypes.c_void_p), ("held", ctypes.c_void_p),
+        ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p),
+        ("num_groups", ctypes.c_int32),
+        ("seq_group", ctypes.c_void_p), ("prefix_page_offsets", ctypes.c_void_p), ("prefix_pages", ctypes.c_void_p),
+        ("block_table", ctypes.c_void_p), ("cu_seqlens", ctypes.c_void_p), ("lens_out", ctypes.c_void_p),
+        ("held_out", ctypes.c_void_p), ("free_count_out", ctypes.c_void_p),
+        ("positions", ctypes.c_void_p), ("slots", ctypes.c_void_p), ("seqs", ctypes.c_void_p),
+    ]
+
+
+class ra_release(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("page_size", ctypes.c_int32), ("num_pages", ctypes.c_int32), ("max_pages_per_seq", ctypes.c_int32),
+        ("keep_lens", ctypes.c_void_p), ("held", ctypes.c_void_p), ("block_table", ctypes.c_void_p),
+        ("num_groups", ctypes.c_int32), ("seq_group", ctypes.c_void_p), ("prefix_page_offsets", ctypes.c_void_p),
+        ("free_pages", ctypes.c_void_p), ("free_count", ctypes.c_void_p), ("held_out", ctypes.c_void_p), ("free_count_out", ctypes.c_void_p),
+    ]
+
+
+class ra_verify(ctypes.Structure):
+    _fields_ = [
+        ("num_seqs", ctypes.c_int32), ("total_rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("logits_dtype", ctypes.c_int32),
+        ("logits", ctypes.c_void_p), ("logits_stride", ctypes.c_int64), ("cu_rows", ctypes.c_void_p), ("tokens", ctypes.c_void_p),
+        ("draft_logits", ctypes.c_void_p), ("draft_stride", ctypes.c_int64), ("draft_dtype", ctypes.c_int32),
+        ("total_draft_rows", ctypes.c_int32), ("draft_rows", ctypes.c_void_p),
+        ("temperature", ctypes.c_void_p), ("accept_uniform", ctypes.c_void_p), ("draw_uniform", ctypes.c_void_p),
+        ("accepted", ctypes.c_void_p), ("out_tokens", ctypes.c_void_p), ("out_logprobs", ctypes.c_void_p), ("next_tokens", ctypes.c_void_p),
+    ]
+
+
 def library_path():
     return _LIB_PATH
 
@@ -151,14 +186,16 @@ def load_library():
     lib.rollout_attn_set_timing.argtypes = [ctypes.c_void_p, ctypes.c_int]
     lib.rollout_attn_get_timing.restype = ctypes.c_int
     lib.rollout_attn_get_timing.argtypes = [ctypes.c_void_p, P(ctypes.c_float)]
-    for name, kind in (("rotate", ra_rotate), ("append_chunk", ra_append_chunk), ("extend", ra_extend)):
+    for name, kind in (("rotate", ra_rotate), ("append_chunk", ra_append_chunk), ("extend", ra_extend), ("place", ra_place),
+                       ("release", ra_release), ("verify", ra_verify)):
         check = getattr(lib, "rollout_attn_check_" + name)
         check.restype, check.argtypes = ctypes.c_int, [P(kind), ctypes.c_char_p, ctypes.c_size_t]
         call = getattr(lib, "rollout_attn_" + name)
         call.restype, call.argtypes = ctypes.c_int, [ctypes.c_void_p, P(kind), ctypes.c_void_p]
-    lib.rollout_attn_extend.argtypes = [ctypes.c_void_p, P(ra_extend), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
-    lib.rollout_attn_extend_workspace_size.restype = ctypes.c_int
-    lib.rollout_attn_extend_workspace_size.argtypes = [ctypes.c_void_p, P(ra_extend), P(ctypes.c_size_t)]
+    for name, kind in (("extend", ra_extend), ("verify", ra_verify)):    # those with a workspace
+        getattr(lib, "rollout_attn_" + name).argtypes = [ctypes.c_void_p, P(kind), ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p]
+        size = getattr(lib, "rollout_attn_%s_workspace_size" % name)
+        size.restype, size.argtypes = ctypes.c_int, [ctypes.c_void_p, P(kind), P(ctypes.c_size_t)]
     _lib = lib
     return lib
 
@@ -274,6 +311,39 @@ def rollout_attn_extend_workspace_size(ctx, extend):
 
 def rollout_attn_extend(ctx, extend, workspace_ptr, workspace_bytes, hip_stream=None):
     _check(load_library().rollout_attn_extend(ctx, ctypes.byref(extend), workspace_ptr, workspace_bytes, hip_stream), ctx)
+
+
+def rollout_attn_check_place(place):
+    """Returns (status, message) of the host-side argument check of a placing."""
+    return _check_only("rollout_attn_check_place", place)
+
+
+def rollout_attn_check_release(release):
+    """Returns (status, message) of the host-side argument check of a release."""
+    return _check_only("rollout_attn_check_release", release)
+
+
+def rollout_attn_check_verify(verify):
+    """Returns (status, message) of the host-side argument check of a verification."""
+    return _check_only("rollout_attn_check_verify", verify)
+
+
+def rollout_attn_place(ctx, place, hip_stream=None):
+    _check(load_library().rollout_attn_place(ctx, ctypes.byref(place), hip_stream), ctx)
+
+
+def rollout_attn_release(ctx, release, hip_stream=None):
+    _check(load_library().rollout_attn_release(ctx, ctypes.byref(release), hip_stream), ctx)
+
+
+def rollout_attn_verify_workspace_size(ctx, verify):
+    n = ctypes.c_size_t()
+    _check(load_library().rollout_attn_verify_workspace_size(ctx, ctypes.byref(verify), ctypes.byref(n)), ctx)
+    return int(n.value)
+
+
+def rollout_attn_verify(ctx, verify, workspace_ptr, workspace_bytes, hip_stream=None):
+    _check(load_library().rollout_attn_verify(ctx, ctypes.byref(verify), workspace_ptr, workspace_bytes, hip_stream), ctx)
 
 
 def rollout_attn_balance(weights, k, equal_count=False):
@@ -493,6 +563,105 @@ def extend_from_tensors(q, k_pool, v_pool, cu_seqlens, max_chunk_len, block_tabl
     return p
 
 
+def _int32(t, n, name):
+    """Address of a contiguous int32 tensor of n elements."""
+    import torch
+    assert t.dtype == torch.int32 and t.is_contiguous() and t.numel() == n, name
+    return _ptr(t)
+
+
+def _fill_groups(p, seq_group, prefix_page_offsets):
+    if seq_group is not None:
+        p.num_groups = prefix_page_offsets.numel() - 1
+        p.seq_group = _int32(seq_group, p.num_seqs, "seq_group")
+        p.prefix_page_offsets = _int32(prefix_page_offsets, p.num_groups + 1, "prefix_page_offsets")
+
+
+def place_from_tensors(seq_lens, new_tokens, held, block_table, free_pages, free_count, cu_seqlens, lens_out, held_out, free_count_out,
+                       positions=None, slots=None, seqs=None, total_tokens=None, seq_group=None, prefix_page_offsets=None, prefix_pages=None,
+                       page_size=16):
+    """Fills a ra_place from device tensors, int32 but for slots (int64): seq_lens, new_tokens, held, lens_out, held_out [n];
+    block_table [n,max_pages]; free_pages [num_pages]; free_count, free_count_out [1]; cu_seqlens [n+1]; positions, slots and seqs
+    [total_tokens] (each may be None); total_tokens: the bound on the new tokens (None: the length of positions, slots or seqs, or what
+    the table has room for); the group hint as for problem_from_tensors."""
+    import torch
+    p = ra_place()
+    p.num_seqs, p.page_size, p.num_pages = seq_lens.numel(), page_size, free_pages.numel()
+    assert block_table.dim() == 2 and block_table.shape[0] == p.num_seqs
+    p.max_pages_per_seq = block_table.shape[1]
+    if total_tokens is None:
+        given = [t.numel() for t in (positions, slots, seqs) if t is not None]
+        total_tokens = given[0] if given else min(2 ** 31 - 1, page_size * block_table.numel())
+    p.total_tokens = int(total_tokens)
+    for f, t in (("seq_lens", seq_lens), ("new_tokens", new_tokens), ("held", held), ("lens_out", lens_out), ("held_out", held_out)):
+        setattr(p, f, _int32(t, p.num_seqs, f))
+    p.block_table, p.cu_seqlens = _int32(block_table, block_table.numel(), "block_table"), _int32(cu_seqlens, p.num_seqs + 1, "cu_seqlens")
+    p.free_pages, p.free_count, p.free_count_out = _int32(free_pages, p.num_pages, "free_pages"), _int32(free_count, 1, "free_count"), _int32(free_count_out, 1, "free_count_out")
+    for f, t in (("positions", positions), ("seqs", seqs)):
+        if t is not None:
+            setattr(p, f, _int32(t, p.total_tokens, f))
+    if slots is not None:
+        assert slots.dtype == torch.int64 and slots.is_contiguous() and slots.numel() == p.total_tokens
+        p.slots = _ptr(slots)
+    _fill_groups(p, seq_group, prefix_page_offsets)
+    if seq_group is not None:
+        p.prefix_pages = _int32(prefix_pages, prefix_pages.numel(), "prefix_pages")
+    return p
+
+
+def release_from_tensors(keep_lens, held, block_table, free_pages, free_count, held_out, free_count_out, seq_group=None, prefix_page_offsets=None,
+                         page_size=16):
+    """Fills a ra_release from device tensors (int32): keep_lens, held, held_out [n]; the rest as for place_from_tensors."""
+    p = ra_release()
+    p.num_seqs, p.page_size, p.num_pages = keep_lens.numel(), page_size, free_pages.numel()
+    assert block_table.dim() == 2 and block_table.shape[0] == p.num_seqs
+    p.max_pages_per_seq = block_table.shape[1]
+    for f, t in (("keep_lens", keep_lens), ("held", held), ("held_out", held_out)):
+        setattr(p, f, _int32(t, p.num_seqs, f))
+    p.block_table = _int32(block_table, block_table.numel(), "block_table")
+    p.free_pages, p.free_count, p.free_count_out = _int32(free_pages, p.num_pages, "free_pages"), _int32(free_count, 1, "free_count"), _int32(free_count_out, 1, "free_count_out")
+    _fill_groups(p, seq_group, prefix_page_offsets)
+    return p
+
+
+def _logits(t, vocab, name):
+    """(address, row stride, ra_logits_dtype) of logits [rows, vocab], rows any stride apart."""
+    import torch
+    assert t.dim() == 2 and t.shape[1] == vocab and t.dtype in (torch.bfloat16, torch.float32), name
+    assert t.shape[0] == 0 or vocab == 1 or t.stride(1) == 1, name
+    # (a single row's stride means nothing; torch may have any there)
+    return _ptr(t), t.stride(0) if t.shape[0] > 1 else vocab, RA_LOGITS_FP32 if t.dtype == torch.float32 else RA_LOGITS_BF16
+
+
+def verify_from_tensors(logits, cu_rows, tokens, accept_uniform, draw_uniform, accepted, out_tokens, out_logprobs=None, next_tokens=None,
+                        temperature=None, draft_logits=None, draft_rows=None):
+    """Fills a ra_verify from device tensors: logits bf16 or float32 [R,vocab] (rows any stride apart); cu_rows int32 [n+1]; tokens int32
+    [R]; accept_uniform float32 [R]; draw_uniform float32 [n]; accepted, next_tokens int32 [n]; out_tokens int32 [R]; out_logprobs
+    float32 [R]; temperature float32 [n] (None: 1); draft_logits like logits (either type) with draft_rows int32 [n], the first row
+    of each sequence there (None: drafts are plain guesses)."""
+    import torch
+    p = ra_verify()
+    p.num_seqs = cu_rows.numel() - 1
+    p.total_rows, p.vocab = logits.shape
+    p.logits, p.logits_stride, p.logits_dtype = _logits(logits, p.vocab, "logits")
+    for f, t, n in (("cu_rows", cu_rows, p.num_seqs + 1), ("tokens", tokens, p.total_rows), ("accepted", accepted, p.num_seqs),
+                    ("out_tokens", out_tokens, p.total_rows), ("next_tokens", next_tokens, p.num_seqs)):
+        if t is not None:
+            setattr(p, f, _int32(t, n, f))
+    for f, t, n in (("accept_uniform", accept_uniform, p.total_rows), ("draw_uniform", draw_uniform, p.num_seqs), ("temperature", temperature, p.num_seqs),
+                    ("out_logprobs", out_logprobs, p.total_rows)):
+        if t is not None:
+            assert t.dtype == torch.float32 and t.is_contiguous() and t.numel() == n, f
+            setattr(p, f, _ptr(t))
+    if draft_logits is not None:
+        p.total_draft_rows = draft_logits.shape[0]
+        p.draft_logits, p.draft_stride, p.draft_dtype = _logits(draft_logits, p.vocab, "draft_logits")
+        if not p.total_draft_rows:                           # (torch gives an empty tensor no address, which would say that there are none)
+            p.draft_logits, p.draft_stride, p.draft_dtype = p.logits, p.logits_stride, p.logits_dtype
+        p.draft_rows = _int32(draft_rows, p.num_seqs, "draft_rows")
+    return p
+
+
 class ra_schedule_info(ctypes.Structure):
     _fields_ = [("header_offset", ctypes.c_int64), ("work_list_offset", ctypes.c_int64), ("merge_desc_offset", ctypes.c_int64),
                 ("waves", ctypes.c_int32), ("segments_per_chunk", ctypes.c_int32)]
@@ -503,6 +672,8 @@ class Decoder:
     the tensors it outgrew stay alive until close(), because work already enqueued (or a HIP graph captured earlier)
     may still use them.  A captured graph and a schedule that RA_FLAG_REUSE_SCHEDULE reuses are tied to the workspace
     they were made with: after the workspace has grown, capture or schedule again."""
+
+    _verify_ws_at = None             # the address and size of verify's workspace, as _chunk_ws_at is extend's
 
     def __init__(self, device_ordinal=0):
         self.device_ordinal = device_ordinal
@@ -519,7 +690,7 @@ class Decoder:
             torch.cuda.synchronize(self.device_ordinal)      # nothing enqueued may outlive the buffers
             rollout_attn_destroy(self.ctx)
             self.ctx = None
-            self._ws = self._ws_at = self._chunk_ws_at = None
+            self._ws = self._ws_at = self._chunk_ws_at = self._verify_ws_at = None
             self._retired = []
 
     def __del__(self):
@@ -618,6 +789,33 @@ class Decoder:
         if at is None or at[1] < need:
             self._chunk_ws_at = mine
         rollout_attn_extend(self.ctx, extend, ctypes.c_void_p(mine[0]), mine[1], ctypes.c_void_p(s))
+
+    def place(self, place, stream=None):
+        """Enqueues the placing of new tokens: pages from the stack, block table, packed offsets, positions, slots."""
+        _check(load_library().rollout_attn_place(self.ctx, place, self._hip_stream(stream)), self.ctx)
+
+    def release(self, release, stream=None):
+        """Enqueues the return of pages to the stack."""
+        _check(load_library().rollout_attn_release(self.ctx, release, self._hip_stream(stream)), self.ctx)
+
+    def verify(self, verify, stream=None):
+        """Enqueues the verification of drafts and the choice of the next tokens.  Its workspace grows and is shared as extend's
+        is: put calls that overlap in time on one stream, or take a Decoder for each."""
+        s = self._hip_stream(stream)
+        at = self._verify_ws_at      # (read once: another thread's call may put a larger one there)
+        if at is not None:
+            status = load_library().rollout_attn_verify(self.ctx, verify, at[0], at[1], s)
+            if status == RA_OK:
+                return
+            if status != RA_ERR_WORKSPACE_TOO_SMALL:
+                _check(status, self.ctx)
+        need = max(256, rollout_attn_verify_workspace_size(self.ctx, verify))
+        ws = self._bytes(need, stream)
+        self._retired.append(ws)
+        mine, at = (ws.data_ptr(), need), self._verify_ws_at
+        if at is None or at[1] < need:
+            self._verify_ws_at = mine
+        rollout_attn_verify(self.ctx, verify, ctypes.c_void_p(mine[0]), mine[1], ctypes.c_void_p(s))
 
     def debug_gather(self, problem, b, kv_head, k_out, v_out, stream=None):
         import torch

@@ -5,7 +5,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "librollout_attn.so")
-SOURCES = ["ra_kernels.hip", "ra_prefill.hip", "ra_prefill_four.hip", "ra_rotate.hip", "ra_extend.hip", "ra_api.cpp", "ra_chunk_api.cpp", "ra_balance.cpp"]
+SOURCES = ["ra_kernels.hip", "ra_prefill.hip", "ra_prefill_four.hip", "ra_rotate.hip", "ra_extend.hip", "ra_pages.hip", "ra_verify.hip",
+           "ra_api.cpp", "ra_chunk_api.cpp", "ra_step_api.cpp", "ra_balance.cpp"]
 COMMON = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-x", "hip",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
           "-Wall", "-Wno-inline-asm", "-Wno-int-to-pointer-cast", "-Wno-unused-command-line-argument", "-Wno-unknown-warning-option"]

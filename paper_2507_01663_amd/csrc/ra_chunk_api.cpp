@@ -1,32 +1,16 @@
 // C-ABI of the operators for chunks of new tokens (see include/rollout_attn_chunk.h): argument checks, launches.
 #include "../../include/rollout_attn_chunk.h"
+#include "ra_check.h"
 #include "ra_chunk.h"
-#include "ra_context.h"
 
 #include <cmath>
-#include <cstdarg>
-#include <cstdio>
 #include <cstring>
 
+using ra::Fail;
+using ra::on_device;
 using ra::set_err;
 
 namespace {
-
-// A failed check: its status, and its text in msg.
-struct Fail {
-    char *msg;
-    size_t n;
-    __attribute__((format(printf, 3, 4))) ra_status operator()(ra_status st, const char *fmt, ...) const
-    {
-        if (msg && n) {
-            va_list ap;
-            va_start(ap, fmt);
-            vsnprintf(msg, n, fmt, ap);
-            va_end(ap);
-        }
-        return st;
-    }
-};
 
 ra_status check_rows(const ra_rotate *p, const Fail &fail, bool append)
 {
@@ -178,18 +162,6 @@ bool as_decode(const ra_extend *p, ra_problem &d)
     d.block_table = p->block_table, d.seq_lens = p->seq_lens;
     d.softmax_scale = p->softmax_scale, d.out = p->out, d.lse = p->lse;
     return true;
-}
-
-// Runs `launch` on the context's device.
-template <typename F> ra_status on_device(ra_ctx *c, F launch)
-{
-    int prev = 0;
-    hipError_t e = hipGetDevice(&prev);
-    if (e == hipSuccess && prev != c->device) e = hipSetDevice(c->device);
-    if (e == hipSuccess) e = launch();
-    if (prev != c->device) (void)hipSetDevice(prev);
-    if (e != hipSuccess) { set_err(c, "HIP: %s", hipGetErrorString(e)); return RA_ERR_DEVICE; }
-    return RA_OK;
 }
 
 } // namespace

@@ -1,0 +1,192 @@
+// gfx950 kernels of the pages of a batch: places of new tokens (block table, packed offsets, positions, slots) and pages back to
+// the stack of free ones.
+//
+// Integers only.  A sequence's share of the stack and of the packed arrays is a running sum over the sequences before it, so a
+// workgroup goes over all sequences, 1024 at a time with one to a thread, and then over the tokens (or the pages) of that tile: each
+// finds its sequence by bisection of the tile's running sums in LDS.  A page of the stack that a sequence takes begins at one of its
+// new tokens, so the token that begins a page also writes it into the table.
+#include "ra_device.h"
+#include "ra_step.h"
+
+namespace ra {
+
+constexpr int kTileSeqs = 1024, kTileWaves = kTileSeqs / 64;
+
+// Inclusive sums over the 1024 threads of a workgroup, on top of what was carried in; the new totals are carried out.
+struct TwoSums {
+    int32_t pages;
+    int64_t tokens;
+};
+struct ScanLds {
+    int32_t pages[kTileWaves];
+    int64_t tokens[kTileWaves];
+};
+__device__ __forceinline__ TwoSums scan(TwoSums x, TwoSums &carry, ScanLds &lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int32_t p = __shfl_up(x.pages, d);
+        const int64_t t = __shfl_up((long long)x.tokens, d);
+        if (lane >= d) x.pages += p, x.tokens += t;
+    }
+    if (lane == 63) lds.pages[wave] = x.pages, lds.tokens[wave] = x.tokens;
+    __syncthreads();
+    TwoSums before = carry, all = carry;
+#pragma unroll
+    for (int w = 0; w < kTileWaves; w++) {
+        const int32_t p = lds.pages[w];
+        const int64_t t = lds.tokens[w];
+        if (w < wave) before.pages += p, before.tokens += t;
+        all.pages += p, all.tokens += t;
+    }
+    __syncthreads();
+    x.pages += before.pages, x.tokens += before.tokens;
+    carry = all;
+    return x;
+}
+
+// Pages that sequence b's group shares, and where they are listed.
+__device__ __forceinline__ int shared_pages(const PagesLaunch &a, int b, int &at)
+{
+    at = 0;
+    if (a.num_groups <= 0) return 0;
+    const int g = a.group[b];
+    if (g < 0 || g >= a.num_groups) return 0;
+    at = a.pfx_off[g];
+    const int n = a.pfx_off[g + 1] - at;
+    return n > 0 ? n : 0;
+}
+
+__device__ __forceinline__ int stack_height(const PagesLaunch &a)
+{
+    const int n = a.free_count[0];
+    return n < 0 ? 0 : n > a.num_pages ? a.num_pages : n;
+}
+
+// The last of the tile's sequences whose sum of those before it is at most x (a sequence without any has the sum of the next).
+__device__ __forceinline__ int owner(const int32_t *before, int x)
+{
+    int lo = 0;
+#pragma unroll
+    for (int step = kTileSeqs / 2; step > 0; step /= 2)
+        if (before[lo + step] <= x) lo += step;
+    return lo;
+}
+
+// PARTS: workgroups that share the tokens (workgroup w has every PARTS-th block of 1024 of them); STATE: the new lengths, counts and
+// offsets are written.  Both at once only with one workgroup: lengths and counts may be written where they are read.
+template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void place_kernel(PagesLaunch a)
+{
+    __shared__ ScanLds sums;
+    __shared__ int32_t first[kTileSeqs];                        // tokens before the sequence
+    __shared__ int4 row[kTileSeqs];                             // {tokens held, pages held, pages with the group's, stack's entry of the first taken}
+    __shared__ int32_t listed[kTileSeqs];                       // where its group's pages are
+    const int tid = threadIdx.x, free = stack_height(a);
+    TwoSums wanted = {0, 0}, given = {0, 0};
+    for (int base = 0; base < a.B; base += kTileSeqs) {
+        const int b = base + tid;
+        int L = 0, n = 0, H = 0, F = 0, at = 0;
+        if (b < a.B) L = a.lens[b], n = a.asked[b], H = a.held[b], F = shared_pages(a, b, at);
+        const int S = H > F ? H : F;
+        const int64_t end = (int64_t)L + n;
+        const int64_t P = (end + kPage - 1) / kPage;
+        const bool fine = n > 0 && L >= 0 && H >= 0 && S <= a.max_pages && P <= a.max_pages && L <= (int64_t)kPage * S;
+        TwoSums mine = {0, 0};
+        if (fine) mine = {P > S ? (int32_t)P - S : 0, n};
+        const TwoSums upto = scan(mine, wanted, sums);
+        const bool served = fine && (mine.pages == 0 || upto.pages <= free) && upto.tokens <= a.T;
+        if (!served) mine = {0, 0};
+        const TwoSums incl = scan(mine, given, sums);
+        const int32_t cu = (int32_t)(incl.tokens - mine.tokens);
+        if (STATE && b < a.B) {
+            a.cu[b] = cu;
+            a.lens_out[b] = L + (int32_t)mine.tokens;
+            a.held_out[b] = served && P > S ? (int32_t)P : served ? S : H;
+        }
+        if (TOKENS) {
+            const int top = free - 1 - (incl.pages - mine.pages);
+            first[tid] = cu, row[tid] = make_int4(L, H, S, top), listed[tid] = at;
+            __syncthreads();
+            const int t0 = first[0], t1 = (int)given.tokens;
+            if (served && F > H && (cu / kTileSeqs) % gridDim.x == blockIdx.x)
+                for (int i = H; i < F; i++) a.table[(int64_t)b * a.max_pages + i] = a.pfx_pages[at + i];
+            for (int blk = t0 / kTileSeqs; (int64_t)blk * kTileSeqs < t1; blk++) {
+                if (blk % gridDim.x != blockIdx.x) continue;
+                const int t = blk * kTileSeqs + tid;
+                if (t < t0 || t >= t1) continue;
+                const int s = owner(first, t);
+                const int4 r = row[s];
+                const int place = r.x + t - first[s], i = place / kPage;
+                int32_t *const entries = a.table + (int64_t)(base + s) * a.max_pages;
+                int page;
+                if (i < r.y) page = entries[i];
+                else if (i < r.z) page = a.pfx_pages[listed[s] + i];
+                else {
+                    page = a.stack[r.w - (i - r.z)];
+                    if (place % kPage == 0) entries[i] = page;
+                }
+                if (a.positions) a.positions[t] = place;
+                if (a.slots) a.slots[t] = (int64_t)page * kPage + place % kPage;
+                if (a.seqs) a.seqs[t] = base + s;
+            }
+            __syncthreads();
+        }
+    }
+    if (TOKENS)
+        for (int64_t t = given.tokens + (int64_t)blockIdx.x * kTileSeqs + tid; t < a.T; t += (int64_t)gridDim.x * kTileSeqs) {
+            if (a.positions) a.positions[t] = -1;
+            if (a.slots) a.slots[t] = -1;
+            if (a.seqs) a.seqs[t] = -1;
+        }
+    if (STATE && tid == 0) a.cu[a.B] = (int32_t)given.tokens, a.free_out[0] = free - given.pages;
+}
+
+template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void release_kernel(PagesLaunch a)
+{
+    __shared__ ScanLds sums;
+    __shared__ int32_t first[kTileSeqs], begin[kTileSeqs];      // pages before the sequence's, and its first that goes back
+    const int tid = threadIdx.x, free = stack_height(a);
+    TwoSums back = {0, 0};
+    for (int base = 0; base < a.B; base += kTileSeqs) {
+        const int b = base + tid, before = back.pages;
+        int keep = 0, H = 0, F = 0, at;
+        if (b < a.B) keep = a.lens[b], H = a.held[b], F = shared_pages(a, b, at);
+        const int kept = keep > 0 ? (int)(((int64_t)keep + kPage - 1) / kPage) : 0, K = kept < H ? kept : H;
+        const bool fine = H >= 0 && H <= a.max_pages;
+        const int from = K > F ? K : F;
+        const TwoSums mine = {fine && from < H ? H - from : 0, 0};
+        const TwoSums incl = scan(mine, back, sums);
+        if (STATE && b < a.B) a.held_out[b] = fine ? K : H;
+        if (PAGES) {
+            first[tid] = incl.pages - mine.pages, begin[tid] = from;
+            __syncthreads();
+            for (int blk = before / kTileSeqs; (int64_t)blk * kTileSeqs < back.pages; blk++) {
+                if (blk % gridDim.x != blockIdx.x) continue;
+                const int e = blk * kTileSeqs + tid;
+                if (e < before || e >= back.pages) continue;
+                const int s = owner(first, e);
+                const int64_t to = (int64_t)free + e;
+                if (to < a.num_pages) a.stack[to] = a.table[(int64_t)(base + s) * a.max_pages + begin[s] + e - first[s]];
+            }
+            __syncthreads();
+        }
+    }
+    if (STATE && tid == 0) a.free_out[0] = (int64_t)free + back.pages < a.num_pages ? free + back.pages : a.num_pages;
+}
+
+hipError_t launch_place(const PagesLaunch &a, int num_cus, hipStream_t s)
+{
+    (void)num_cus;
+    hipLaunchKernelGGL((place_kernel<true, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_release(const PagesLaunch &a, int num_cus, hipStream_t s)
+{
+    (void)num_cus;
+    hipLaunchKernelGGL((release_kernel<true, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+    return hipGetLastError();
+}
+
+} // namespace ra

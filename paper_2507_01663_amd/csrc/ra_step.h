@@ -1,0 +1,46 @@
+// Internal interface between ra_step_api.cpp and the kernels of both ends of a step (ra_pages.hip, ra_verify.hip).
+#pragma once
+#include "ra_internal.h"
+
+namespace ra {
+
+// Pages of the sequences of a batch (ra_place, ra_release).
+struct PagesLaunch {
+    int32_t B, T, num_pages, max_pages, num_groups;
+    const int32_t *lens;         // place: tokens held; release: tokens kept
+    const int32_t *asked;        // place
+    const int32_t *held;
+    const int32_t *group, *pfx_off, *pfx_pages;
+    const int32_t *free_count;
+    int32_t *stack;              // free pages; place only reads them
+    int32_t *table;              // release only reads it
+    int32_t *cu, *lens_out, *held_out, *free_out;
+    int32_t *positions, *seqs;   // place, each may be null
+    int64_t *slots;
+};
+hipError_t launch_place(const PagesLaunch &a, int num_cus, hipStream_t s);
+hipError_t launch_release(const PagesLaunch &a, int num_cus, hipStream_t s);
+
+// What is known of one part of a row of logits: the largest, and the sum of the weights 2^((l - largest) log2(e) / T), or for a
+// greedy row the first index of the largest.
+struct RowPart {
+    double sum;
+    float top;                   // -inf: nothing but -inf; NaN: a NaN among them
+    int32_t first;
+};
+struct VerifyLaunch {
+    int32_t B, R, V, parts, part_len; // a row's parts, and the values of a part
+    int32_t fp32, draft_fp32, total_draft_rows;
+    const void *logits, *draft;
+    int64_t stride, draft_stride;
+    const int32_t *cu, *tokens, *draft_rows;
+    const float *temperature, *u, *v;
+    int32_t *accepted, *out, *next;
+    float *logprobs;
+    RowPart *row, *draft_row;    // [R][parts]
+};
+// How a call is divided (from B, R, V), and its workspace: the bytes; places the pointers when base is not null.
+size_t carve_verify(VerifyLaunch &a, int num_cus, bool drafted, void *base);
+hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s);
+
+} // namespace ra

@@ -1,0 +1,156 @@
+"""CPU-side checks of the C ABI of both ends of a step: exported symbols, struct layouts, the host-only argument checks, the
+workspace's size."""
+import ctypes
+import os
+import re
+
+import pytest
+
+import paper_2507_01663_amd as ra
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+BAD, NOT = ra.RA_ERR_INVALID_ARG, ra.RA_ERR_UNSUPPORTED
+
+
+def test_library_exports_every_declared_symbol():
+    text = open(os.path.join(ROOT, "include", "rollout_attn_step.h")).read()
+    text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
+    names = sorted(set(re.findall(r"\b(rollout_attn_[a-z_]+)\s*\(", text)))
+    assert len(names) == 7, names
+    lib = ra.load_library()
+    for n in names:
+        assert getattr(lib, n) is not None and hasattr(ra, n)
+
+
+def test_struct_layouts():
+    assert ctypes.sizeof(ra.ra_place) == 24 + 5 * 8 + 8 + 3 * 8 + 5 * 8 + 3 * 8
+    assert ctypes.sizeof(ra.ra_release) == 16 + 3 * 8 + 8 + 2 * 8 + 4 * 8
+    assert ctypes.sizeof(ra.ra_verify) == 16 + 16 + 16 + 16 + 8 + 8 + 24 + 32
+
+
+def place():
+    p = ra.ra_place()
+    p.num_seqs, p.total_tokens, p.page_size, p.num_pages, p.max_pages_per_seq, p.num_groups = 3, 40, 16, 64, 8, 2
+    for i, f in enumerate(("seq_lens", "new_tokens", "held", "free_pages", "free_count", "seq_group", "prefix_page_offsets", "prefix_pages", "block_table",
+                           "cu_seqlens", "lens_out", "held_out", "free_count_out", "positions", "slots", "seqs")):
+        setattr(p, f, 0x10000 * (i + 1))
+    return p
+
+
+def release():
+    p = ra.ra_release()
+    p.num_seqs, p.page_size, p.num_pages, p.max_pages_per_seq, p.num_groups = 3, 16, 64, 8, 2
+    for i, f in enumerate(("keep_lens", "held", "block_table", "seq_group", "prefix_page_offsets", "free_pages", "free_count", "held_out", "free_count_out")):
+        setattr(p, f, 0x10000 * (i + 1))
+    return p
+
+
+def verify(drafted=True):
+    p = ra.ra_verify()
+    p.num_seqs, p.total_rows, p.vocab = 2, 7, 1000
+    p.logits_stride = p.draft_stride = 1000
+    for i, f in enumerate(("logits", "cu_rows", "tokens", "temperature", "accept_uniform", "draw_uniform", "accepted", "out_tokens", "out_logprobs", "next_tokens")):
+        setattr(p, f, 0x10000 * (i + 1))
+    if drafted:
+        p.draft_logits, p.draft_rows, p.total_draft_rows = 0xF0000, 0x100000, 5
+    return p
+
+
+def refused(check, make, changes):
+    assert check(make()) == (ra.RA_OK, "")
+    assert check(None)[0] == BAD
+    for change, status, word in changes:
+        p = make()
+        for k, v in change.items():
+            setattr(p, k, v)
+        st, msg = check(p)
+        assert st == status and word in msg, (change, st, msg)
+
+
+PAGES = [(dict(num_seqs=-1), BAD, "dimension"), (dict(page_size=0), BAD, "dimension"), (dict(num_pages=-1), BAD, "dimension"),
+         (dict(max_pages_per_seq=-1), BAD, "dimension"), (dict(num_groups=-1), BAD, "dimension"), (dict(page_size=32), NOT, "page_size"),
+         (dict(num_seqs=2 ** 20, max_pages_per_seq=2 ** 12), NOT, "large"), (dict(max_pages_per_seq=2 ** 28), NOT, "large"),
+         (dict(free_count=None), BAD, "pointer"), (dict(free_count_out=None), BAD, "pointer"), (dict(held=None), BAD, "pointer"), (dict(held_out=None), BAD, "pointer"),
+         (dict(block_table=None), BAD, "pointer"), (dict(free_pages=None), BAD, "pointer"), (dict(seq_group=None), BAD, "hint"),
+         (dict(prefix_page_offsets=None), BAD, "hint")]
+
+
+def test_check_place():
+    refused(ra.rollout_attn_check_place, place, PAGES + [
+        (dict(total_tokens=-1), BAD, "total_tokens"), (dict(cu_seqlens=None), BAD, "pointer"), (dict(seq_lens=None), BAD, "pointer"),
+        (dict(new_tokens=None), BAD, "pointer"), (dict(lens_out=None), BAD, "pointer"), (dict(prefix_pages=None), BAD, "hint"), (dict(slots=0xF0004), BAD, "aligned")])
+    p = place()
+    p.num_groups = 0
+    for f in ("seq_group", "prefix_page_offsets", "prefix_pages", "positions", "slots", "seqs"):
+        setattr(p, f, None)
+    assert ra.rollout_attn_check_place(p) == (ra.RA_OK, "")
+    p = ra.ra_place()                                        # nothing to place: the counts and the offsets' one entry are still written
+    p.page_size, p.free_count, p.free_count_out, p.cu_seqlens = 16, 0x10000, 0x10000, 0x20000
+    assert ra.rollout_attn_check_place(p) == (ra.RA_OK, "")
+
+
+def test_check_release():
+    refused(ra.rollout_attn_check_release, release, PAGES + [(dict(keep_lens=None), BAD, "pointer")])
+
+
+def test_check_verify():
+    changes = [(dict(num_seqs=-1), BAD, "dimension"), (dict(total_rows=-1), BAD, "dimension"), (dict(vocab=0), BAD, "dimension"), (dict(vocab=2 ** 24 + 1), NOT, "vocab"),
+               (dict(total_rows=2 ** 22 + 1), NOT, "large"), (dict(num_seqs=2 ** 22 + 1), NOT, "large"), (dict(logits_dtype=2), BAD, "dtype"), (dict(logits=None), BAD, "pointer"),
+               (dict(logits=0x10001), BAD, "aligned"), (dict(logits=0x10002, logits_dtype=ra.RA_LOGITS_FP32), BAD, "aligned"), (dict(logits_stride=999), BAD, "stride"),
+               (dict(logits_stride=2 ** 40), NOT, "stride"), (dict(cu_rows=None), BAD, "pointer"), (dict(tokens=None), BAD, "pointer"),
+               (dict(accept_uniform=None), BAD, "pointer"), (dict(draw_uniform=None), BAD, "pointer"), (dict(accepted=None), BAD, "pointer"),
+               (dict(out_tokens=None), BAD, "pointer")]
+    refused(ra.rollout_attn_check_verify, verify, changes + [
+        (dict(draft_dtype=-1), BAD, "dtype"), (dict(draft_logits=0xF0001), BAD, "aligned"), (dict(draft_stride=5), BAD, "stride"), (dict(total_draft_rows=-1), BAD, "total_draft_rows"),
+        (dict(draft_rows=None), BAD, "draft_rows")])
+    refused(ra.rollout_attn_check_verify, lambda: verify(False), changes)
+    p = verify(False)
+    p.temperature = p.out_logprobs = p.next_tokens = None
+    assert ra.rollout_attn_check_verify(p) == (ra.RA_OK, "")
+
+
+def test_verify_workspace_size():
+    sizes = {}
+    for rows in (0, 1, 5, 1000, 100000):
+        for drafted in (False, True):
+            p = verify(drafted)
+            p.total_rows = rows
+            n = sizes[rows, drafted] = ra.rollout_attn_verify_workspace_size(None, p)
+            assert n % 256 == 0
+    assert sizes[1000, True] > sizes[1000, False] > 0
+    p = verify()
+    p.vocab = 0
+    with pytest.raises(ra.RolloutAttnError) as e:
+        ra.rollout_attn_verify_workspace_size(None, p)
+    assert e.value.status == BAD
+    p.vocab = 2 ** 25
+    with pytest.raises(ra.RolloutAttnError) as e:
+        ra.rollout_attn_verify_workspace_size(None, p)
+    assert e.value.status == NOT
+
+
+def test_calls_without_a_context_are_rejected():
+    for call, desc, more in ((ra.rollout_attn_place, place(), ()), (ra.rollout_attn_release, release(), ()), (ra.rollout_attn_verify, verify(), (None, 0))):
+        with pytest.raises(ra.RolloutAttnError) as e:
+            call(None, desc, *more)
+        assert e.value.status == BAD
+
+
+def test_descriptors_refuse_tensors_of_other_shapes():
+    import torch
+    i = lambda *s: torch.zeros(s, dtype=torch.int32)
+    f = lambda *s: torch.zeros(s)
+    good = lambda: dict(logits=f(4, 10), cu_rows=i(3), tokens=i(4), accept_uniform=f(4), draw_uniform=f(2), accepted=i(2), out_tokens=i(4))
+    p = ra.verify_from_tensors(**good())
+    assert (p.num_seqs, p.total_rows, p.vocab, p.logits_stride, p.logits_dtype) == (2, 4, 10, 10, ra.RA_LOGITS_FP32)
+    for bad in (dict(logits=f(4, 10).half()), dict(logits=f(10, 4).t()), dict(tokens=i(3)), dict(tokens=i(4).long()), dict(draw_uniform=f(4)), dict(accept_uniform=f(4).double()),
+                dict(out_tokens=i(8)[::2]), dict(draft_logits=f(2, 9), draft_rows=i(2)), dict(draft_logits=f(2, 10), draft_rows=i(1)), dict(temperature=f(1))):
+        with pytest.raises(AssertionError):
+            ra.verify_from_tensors(**{**good(), **bad})
+    good = lambda: dict(seq_lens=i(2), new_tokens=i(2), held=i(2), block_table=i(2, 5), free_pages=i(9), free_count=i(1), cu_seqlens=i(3), lens_out=i(2), held_out=i(2),
+                        free_count_out=i(1))
+    assert ra.place_from_tensors(**good()).total_tokens == 160       # (what the table has room for)
+    for bad in (dict(held=i(3)), dict(block_table=i(5, 2)), dict(block_table=i(2, 10)[:, ::2]), dict(free_count=i(2)), dict(cu_seqlens=i(2)), dict(slots=i(4)),
+                dict(positions=i(4), seqs=i(5)), dict(seq_group=i(1), prefix_page_offsets=i(2), prefix_pages=i(3))):
+        with pytest.raises(AssertionError):
+            ra.place_from_tensors(**{**good(), **bad})
