@@ -38,9 +38,12 @@ struct VerifyLaunch {
     int32_t *accepted, *out, *next;
     float *logprobs;
     RowPart *row, *draft_row;    // [R][parts]
+    double *rest;                // [R][parts]  sums of max(p - q, 0), of the rows whose draft is turned down
+    int32_t *tickets;            // [B]         parts of those that have been added up
 };
 // How a call is divided (from B, R, V), and its workspace: the bytes; places the pointers when base is not null.
 size_t carve_verify(VerifyLaunch &a, int num_cus, bool drafted, void *base);
+bool verify_fits(const VerifyLaunch &a, bool drafted); // in one launch each
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s);
 
 } // namespace ra

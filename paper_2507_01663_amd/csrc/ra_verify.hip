@@ -9,6 +9,8 @@
 namespace ra {
 
 constexpr int kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
+constexpr int kDrawThreads = 512, kDrawWaves = kDrawThreads / 64;
+constexpr int kMostPart = 64 * kDrawThreads;                     // values of a part at most: a wave then looks at a thread's stretch at once
 constexpr int kVec = 8;                                          // values that a lane loads at a time
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -146,15 +148,15 @@ template <bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int beg
     return r;
 }
 
-// The sequence that row t belongs to: the number of those whose rows end at or before it.
+// The sequence that row t belongs to: the number of those whose rows end at or before it, by 64 looks at a time.
 __device__ __forceinline__ int sequence_of_row(const VerifyLaunch &a, int t, int lane)
 {
-    int b = 0;
-    for (int base = 0; base < a.B; base += 64) {
-        const int s = base + lane;
-        const int n = __popcll(__ballot(s < a.B && a.cu[s + 1] <= t));
-        b += n;
-        if (n < 64) break;
+    int b = 0, n = a.B;
+    while (n > 0) {
+        const int step = (n + 63) / 64, s = b + (lane + 1) * step - 1;
+        const int ended = __popcll(__ballot(s < a.B && a.cu[s + 1] <= t));
+        b += ended * step;
+        n = step == 1 ? 0 : a.B - b < step ? a.B - b : step;
     }
     return b;
 }
@@ -191,6 +193,8 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunc
         const uint8_t *const at = row_at(a.draft, a.draft_stride, a.draft_fp32, d);
         r = a.draft_fp32 ? part_of_row(Row<true>{at}, begin, end, temper) : part_of_row(Row<false>{at}, begin, end, temper);
     }
+    // (this many parts of the sequence's rest have been added up: none; see verify_draw_kernel)
+    if (threadIdx.x == 0 && !drafted && k == 0 && t == a.cu[b] && a.draft) a.tickets[b] = 0;
     if (threadIdx.x == 0) (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
 }
 
@@ -234,30 +238,108 @@ __device__ __forceinline__ float logit_at(const void *logits, int64_t stride, in
 // How a token is drawn from a row.
 enum DrawFrom { kNothing, kTop, kRow, kRowWithout, kRest }; // no distribution; greedy; p; p without the draft; max(p - q, 0)
 struct Draw {
-    int from, x, dfp32;          // x: the draft that was turned down
+    int from, x, row;            // x: the draft that was turned down, or the greedy token; row: of logits
     const uint8_t *p, *q;        // the rows
     double p_top, p_scale, q_top, q_scale; // p = weight(l, p_top) * p_scale
     Temper t;
 };
 
-// The weight of value i in the sum that the token is drawn by.
-template <bool FP32, bool QFP32> struct Weights {
-    Draw d;
-    __device__ __forceinline__ double operator()(int i) const
-    {
-#pragma clang fp contract(off)
-        // (each product rounded by itself: where p and q are the same, nothing is left)
-        double w = weight(Row<FP32>{d.p}[i], d.p_top, d.t) * d.p_scale;
-        if (d.from == kRest) {
-            w -= weight(Row<QFP32>{d.q}[i], d.q_top, d.t) * d.q_scale;
-            w = w > 0.0 ? w : 0.0;
-        }
-        return d.from == kRowWithout && i == d.x ? 0.0 : w;
-    }
-};
-
-__device__ __forceinline__ double block_sum_before(double x, double *lds, double &total)
+// What row `row` of sequence b says to its draft, and how a token is drawn from it if that does not stay.  All lanes of a wave.
+__device__ __forceinline__ Draw judge(const VerifyLaunch &a, int b, int row, int end, const Temper &t, int lane, bool &stays, double &lp)
 {
+    const Whole p = whole_row(a.row + (int64_t)row * a.parts, a.parts, t, lane);
+    const int x = row + 1 == end ? -1 : a.tokens[row + 1];
+    const bool token = x >= 0 && x < a.V;
+    Draw d = {};
+    d.row = row, d.x = x, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, row), d.p_top = p.top, d.p_scale = 1.0 / p.sum;
+    stays = false, lp = 0.0;
+    if (!is_finite(p.top)) {
+        d.from = kNothing;
+        return d;
+    }
+    if (t.c == 0.0) {
+        d.from = kTop, stays = token && x == p.first, d.x = p.first;
+        return d;
+    }
+    d.from = kRow;
+    if (!token) return d;
+    const float l = logit_at(a.logits, a.stride, a.fp32, row, x);
+    const double px = weight(l, p.top, t) / p.sum;
+    lp = ((double)l - (double)p.top) * t.c / kLog2e - log(p.sum);
+    if (!a.draft) {
+        stays = (double)a.u[row] < px;
+        d.from = kRowWithout;
+        return d;
+    }
+    const int64_t r = draft_row_of(a, b, row);
+    if (r < 0) return d;
+    const Whole q = whole_row(a.draft_row + (int64_t)row * a.parts, a.parts, t, lane);
+    if (!is_finite(q.top)) return d;
+    d.from = kRest, d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, r), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+    const double qx = weight(logit_at(a.draft, a.draft_stride, a.draft_fp32, r, x), q.top, t) / q.sum;
+    stays = (double)a.u[row] * qx < px;
+    return d;
+}
+
+// The rows of sequence b, as many at a time as there are waves, up to the first that keeps no draft: that one's draw.  The whole
+// workgroup; `write`: this one writes the drafts that stay.
+__device__ __forceinline__ Draw decide(const VerifyLaunch &a, int b, int begin, int end, const Temper &t, bool write)
+{
+    __shared__ Draw draws[kDrawWaves];
+    __shared__ int stay[kDrawWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    for (int base = begin;; base += kDrawWaves) {
+        const int row = base + wave;
+        bool stays = false;
+        double lp = 0.0;
+        if (row < end) {
+            const Draw d = judge(a, b, row, end, t, lane, stays, lp);
+            if (lane == 0) draws[wave] = d;
+        }
+        if (lane == 0) stay[wave] = stays;
+        __syncthreads();
+        int n = 0;
+        while (n < kDrawWaves && stay[n]) n++;
+        if (write && wave < n && lane == 0) {
+            a.out[row] = a.tokens[row + 1];
+            if (a.logprobs) a.logprobs[row] = (float)lp;
+        }
+        if (n < kDrawWaves) return draws[n];                    // (the last row keeps none, so there is one)
+        __syncthreads();
+    }
+}
+
+// ---- a token from its weights ---------------------------------------------------------------------------
+
+// Weights of values i .. i + 7 (those at or past end are 0) in the sum that the token is drawn by.
+template <bool FP32, bool QFP32> __device__ __forceinline__ void weights(double (&w)[kVec], const Draw &d, int i, int end)
+{
+    float x[kVec], y[kVec];
+    Row<FP32>{d.p}.load_some(x, i, end);
+    if (d.from == kRest) {
+        Row<QFP32>{d.q}.load_some(y, i, end);
+#pragma unroll
+        for (int j = 0; j < kVec; j++) {
+#pragma clang fp contract(off)
+            // (each product rounded by itself: where p and q are the same, nothing is left)
+            const double r = weight(x[j], d.p_top, d.t) * d.p_scale - weight(y[j], d.q_top, d.t) * d.q_scale;
+            w[j] = r > 0.0 ? r : 0.0;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < kVec; j++) w[j] = d.from == kRowWithout && i + j == d.x ? 0.0 : weight(x[j], d.p_top, d.t) * d.p_scale;
+    }
+}
+__device__ __forceinline__ void weights_at(double (&w)[kVec], const VerifyLaunch &a, const Draw &d, int i, int end)
+{
+    if (a.fp32) a.draft_fp32 ? weights<true, true>(w, d, i, end) : weights<true, false>(w, d, i, end);
+    else a.draft_fp32 ? weights<false, true>(w, d, i, end) : weights<false, false>(w, d, i, end);
+}
+
+// The sum of x over the workgroup's threads before this one; total: over all.
+__device__ __forceinline__ double sum_before(double x, double &total)
+{
+    __shared__ double sums[kDrawWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     double s = x;
 #pragma unroll
@@ -265,179 +347,225 @@ __device__ __forceinline__ double block_sum_before(double x, double *lds, double
         const double o = __shfl_up(s, d);
         if (lane >= d) s += o;
     }
-    if (lane == 63) lds[wave] = s;
+    if (lane == 63) sums[wave] = s;
     __syncthreads();
     double before = 0.0;
     total = 0.0;
 #pragma unroll
-    for (int w = 0; w < kVerifyWaves; w++) {
-        if (w < wave) before += lds[w];
-        total += lds[w];
+    for (int w = 0; w < kDrawWaves; w++) {
+        if (w < wave) before += sums[w];
+        total += sums[w];
     }
     __syncthreads();
-    return before + s - x;
+    const double up = __shfl_up(s, 1);
+    return before + (lane ? up : 0.0);
 }
 
-// The token: the first value at which the running sum passes v times the whole.  Every thread has one stretch of the row; the one
-// that holds the border walks it again.
-template <typename W> __device__ int draw(const W &w, int V, double v, bool &nothing)
+// The thread whose share of a running sum holds the border: the first that the sum with it exceeds it in, or the last with any
+// share where rounding (or a number of 1) leaves none; -1: no thread has any.
+__device__ __forceinline__ int holder(double before, double mine, double border)
 {
-    __shared__ double lds[kVerifyWaves];
-    __shared__ int found, last;
-    const int tid = threadIdx.x, len = (V + kVerifyThreads - 1) / kVerifyThreads;
-    const int begin = tid * len < V ? tid * len : V, end = begin + len < V ? begin + len : V;
-    if (tid == 0) found = INT32_MAX, last = -1;
-    double mine = 0.0, total;
-    for (int i = begin; i < end; i++) mine += w(i);
-    const double before = block_sum_before(mine, lds, total);
-    const double border = v * total;
-    if (mine > 0.0) atomicMax(&last, tid);
-    if (before <= border && before + mine > border) atomicMin(&found, tid);
+    __shared__ int over[kDrawWaves], some[kDrawWaves];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint64_t any = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && before + mine > border);
+    if (lane == 0) over[wave] = past ? wave * 64 + __builtin_ctzll(past) : INT32_MAX, some[wave] = any ? wave * 64 + 63 - __builtin_clzll(any) : -1;
     __syncthreads();
-    nothing = !(total > 0.0);
-    const int who = found < last ? found : last;
+    int first = INT32_MAX, last = -1;
+#pragma unroll
+    for (int w = 0; w < kDrawWaves; w++) first = over[w] < first ? over[w] : first, last = some[w] > last ? some[w] : last;
     __syncthreads();
-    if (tid == who) {
-        double run = before;
-        int token = -1;
-        for (int i = begin; i < end; i++) {
-            const double x = w(i);
-            if (!(x > 0.0)) continue;
-            token = i, run += x;
-            if (run > border) break;
+    return first < INT32_MAX ? first : last;
+}
+
+// The first value of part k at which the running sum of the part's weights passes the border.
+__device__ int token_of_part(const VerifyLaunch &a, const Draw &d, int k, double border)
+{
+    __shared__ int token;
+    __shared__ double from;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int begin = k * a.part_len, end = begin + a.part_len < a.V ? begin + a.part_len : a.V;
+    const int len = a.part_len / kDrawThreads;                  // a multiple of 8, at most 64
+    const int mine = begin + tid * len, stop = mine + len < end ? mine + len : end;
+    double sum = 0.0, total, w[kVec];
+    for (int i = mine; i < stop; i += kVec) {
+        weights_at(w, a, d, i, stop);
+#pragma unroll
+        for (int j = 0; j < kVec; j++) sum += w[j];
+    }
+    const double before = sum_before(sum, total);
+    const int who = holder(before, sum, border);
+    if (who < 0) return -1;
+    if (tid == who) from = before;
+    __syncthreads();
+    if (tid < 64) {                                             // that thread's stretch, a value to a lane
+        const int at = begin + who * len, i = at + lane;
+        weights_at(w, a, d, i, i < end && lane < len ? i + 1 : i);
+        double run = w[0];
+#pragma unroll
+        for (int s = 1; s < 64; s *= 2) {
+            const double o = __shfl_up(run, s);
+            if (lane >= s) run += o;
         }
-        found = token;
+        const uint64_t any = __ballot(w[0] > 0.0), past = __ballot(w[0] > 0.0 && from + run > border);
+        if (lane == 0) token = past ? at + __builtin_ctzll(past) : any ? at + 63 - __builtin_clzll(any) : -1;
     }
     __syncthreads();
-    return found;
-}
-
-template <bool FP32, bool QFP32> __device__ int draw_from(Draw &d, int V, double v)
-{
-    bool nothing = false;
-    int token = draw(Weights<FP32, QFP32>{d}, V, v, nothing);
-    if (nothing) {
-        __syncthreads();
-        d.from = kRow;
-        token = draw(Weights<FP32, QFP32>{d}, V, v, nothing);
-    }
     return token;
 }
 
-// One workgroup for each sequence: which drafts stay, and the token behind them.
-__global__ __launch_bounds__(kVerifyThreads) void verify_draw_kernel(VerifyLaunch a)
+// A part's share in the sum; one below 2^-996 is none (its weights might all have vanished).
+__device__ __forceinline__ double share_of_part(const VerifyLaunch &a, const Draw &d, int k)
 {
-    __shared__ Draw shared;
-    __shared__ int kept, done;
-    const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    int begin = a.cu[b], end = a.cu[b + 1];
+    double s;
+    if (d.from == kRest) s = a.rest[(int64_t)d.row * a.parts + k];
+    else {
+        const RowPart r = a.row[(int64_t)d.row * a.parts + k];
+        s = is_finite(r.top) ? r.sum * exp2(((double)r.top - d.p_top) * d.t.c) * d.p_scale : 0.0;
+    }
+    return s > 1e-300 ? s : 0.0;
+}
+
+__device__ double sum_of_part(const VerifyLaunch &a, const Draw &d, int k)
+{
+    const int begin = k * a.part_len, end = begin + a.part_len < a.V ? begin + a.part_len : a.V;
+    double sum = 0.0, total, w[kVec];
+    for (int i = begin + threadIdx.x * kVec; i < end; i += kDrawThreads * kVec) {
+        weights_at(w, a, d, i, end);
+#pragma unroll
+        for (int j = 0; j < kVec; j++) sum += w[j];
+    }
+    (void)sum_before(sum, total);
+    return total;
+}
+
+// The token that v draws, from the parts' sums and then from the part that holds the border.  The whole workgroup.
+__device__ int draw(const VerifyLaunch &a, Draw d, double v)
+{
+    __shared__ double border_in_part;
+    __shared__ int part;
+    const int tid = threadIdx.x, each = (a.parts + kDrawThreads - 1) / kDrawThreads;
+    for (;;) {
+        // (the part that the draft is in, anew: what is left of it may be far less than a difference of sums could say)
+        const int without = d.from == kRowWithout ? d.x / a.part_len : -1;
+        double left = without >= 0 ? sum_of_part(a, d, without) : 0.0;
+        left = left > 1e-300 ? left : 0.0;
+        double mine = 0.0, total;
+        for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) mine += k == without ? left : share_of_part(a, d, k);
+        const double before = sum_before(mine, total), border = v * total;
+        const int who = holder(before, mine, border);
+        if (who < 0) {                                          // nothing is left of p - q: p
+            if (d.from == kRow) return -1;                      // (no row of a well-formed call)
+            d.from = kRow;
+            continue;
+        }
+        if (tid == who) {
+            double run = before;
+            for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) {
+                const double s = k == without ? left : share_of_part(a, d, k);
+                if (!(s > 0.0)) continue;
+                part = k, border_in_part = border - run;
+                run += s;
+                if (run > border) break;
+            }
+        }
+        __syncthreads();
+        return token_of_part(a, d, part, border_in_part);
+    }
+}
+
+// Which drafts stay, and the token behind them.  With a draft model's logits every sequence has a workgroup for each part of a row: all
+// see which draft was turned down, and add up what is left of its part; the last to arrive draws.  Where nothing is to be added up, and
+// without a draft model, a sequence's first (only) workgroup draws.
+__global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyLaunch a)
+{
+    __shared__ int arrived;
+    const int tid = threadIdx.x;
+    const int b = a.draft ? blockIdx.x / (unsigned)a.parts : blockIdx.x, k = a.draft ? blockIdx.x % (unsigned)a.parts : 0;
+    const int begin = a.cu[b], end = a.cu[b + 1];
     if (begin < 0 || end > a.R || begin >= end) {
-        if (tid == 0) {
+        if (k == 0 && tid == 0) {
             a.accepted[b] = 0;
             if (a.next) a.next[b] = -1;
         }
         return;
     }
     const Temper t = temper_of(a, b);
-    if (tid == 0) done = 0;
-    __syncthreads();
-    // rows one after the other, until one accepts no draft
-    for (int row = begin; row < end; row++) {
-        if (wave == 0) {
-            const Whole p = whole_row(a.row + (int64_t)row * a.parts, a.parts, t, lane);
-            const bool last = row + 1 == end;
-            const int x = last ? -1 : a.tokens[row + 1];
-            const bool token = x >= 0 && x < a.V;
-            Draw d = {};
-            d.x = x, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, row), d.p_top = p.top, d.p_scale = 1.0 / p.sum;
-            bool stays = false;
-            double lp = 0.0;
-            if (!is_finite(p.top)) d.from = kNothing;
-            else if (t.c == 0.0) {
-                d.from = kTop, stays = token && x == p.first;
-                d.x = p.first;
-            } else {
-                d.from = kRow;
-                double px = 0.0;
-                if (token) {
-                    const float l = logit_at(a.logits, a.stride, a.fp32, row, x);
-                    px = weight(l, p.top, t) / p.sum;
-                    lp = ((double)l - (double)p.top) * t.c / kLog2e - log(p.sum);
-                }
-                if (token && !a.draft) {
-                    stays = (double)a.u[row] < px;
-                    d.from = kRowWithout;
-                } else if (token) {
-                    const int64_t r = draft_row_of(a, b, row);
-                    if (r >= 0) {
-                        const Whole q = whole_row(a.draft_row + (int64_t)row * a.parts, a.parts, t, lane);
-                        if (is_finite(q.top)) {
-                            d.from = kRest, d.dfp32 = a.draft_fp32, d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, r);
-                            d.q_top = q.top, d.q_scale = 1.0 / q.sum;
-                            const double qx = weight(logit_at(a.draft, a.draft_stride, a.draft_fp32, r, x), q.top, t) / q.sum;
-                            stays = (double)a.u[row] * qx < px;
-                        }
-                    }
-                }
-            }
-            if (lane == 0) {
-                if (stays) {
-                    a.out[row] = x;
-                    if (a.logprobs) a.logprobs[row] = (float)lp;
-                } else shared = d, kept = row - begin, done = 1;
-            }
+    const Draw d = decide(a, b, begin, end, t, k == 0);
+    if (d.from == kRest) {
+        const double sum = sum_of_part(a, d, k);
+        if (tid == 0) {
+            a.rest[(int64_t)d.row * a.parts + k] = sum;
+            arrived = __hip_atomic_fetch_add(a.tickets + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
         }
         __syncthreads();
-        const bool all = done != 0;
-        __syncthreads();                                        // (before the first wave goes on to the next row)
-        if (all) break;
-    }
-    const int at = begin + kept;
-    Draw d = shared;
+        if (arrived != a.parts - 1) return;
+    } else if (k != 0) return;
     double v = a.v[b];
     v = v > 0.0 ? v < 1.0 ? v : 1.0 : 0.0;
     int token = -1;
     if (d.from == kTop) token = d.x;
-    else if (d.from != kNothing) {
-        if (a.fp32) token = a.draft_fp32 ? draw_from<true, true>(d, a.V, v) : draw_from<true, false>(d, a.V, v);
-        else token = a.draft_fp32 ? draw_from<false, true>(d, a.V, v) : draw_from<false, false>(d, a.V, v);
-    }
+    else if (d.from != kNothing) token = draw(a, d, v);
     if (tid == 0) {
-        a.accepted[b] = kept;
+        a.accepted[b] = d.row - begin;
         if (a.next) a.next[b] = token;
-        a.out[at] = token;
+        a.out[d.row] = token;
         if (a.logprobs) {
             double lp = d.from == kTop ? 0.0 : __builtin_nan("");
             if (d.from != kTop && token >= 0)
-                lp = ((double)logit_at(a.logits, a.stride, a.fp32, at, token) - d.p_top) * t.c / kLog2e + log(d.p_scale);
-            a.logprobs[at] = (float)lp;
+                lp = ((double)logit_at(a.logits, a.stride, a.fp32, d.row, token) - d.p_top) * t.c / kLog2e + log(d.p_scale);
+            a.logprobs[d.row] = (float)lp;
         }
     }
-    for (int i = at + 1 + tid; i < end; i += kVerifyThreads) {
+    for (int i = d.row + 1 + tid; i < end; i += kDrawThreads) {
         a.out[i] = -1;
         if (a.logprobs) a.logprobs[i] = 0.f;
     }
 }
 
+// How rows are cut into parts: so many that the workgroups of the rows fill the device several times, of whole loads of a workgroup each.
+static void verify_shape(VerifyLaunch &a, int num_cus, bool drafted)
+{
+    const int64_t rows = (int64_t)a.R * (drafted ? 2 : 1), unit = kDrawThreads * kVec;
+    const int64_t units = (a.V + unit - 1) / unit, wanted = rows > 0 ? ((int64_t)num_cus * 32 + rows - 1) / rows : 1;
+    int64_t each = units / (wanted > 1 ? wanted : 1);
+    each = each < 1 ? 1 : each > kMostPart / unit ? kMostPart / unit : each;
+    a.part_len = (int)(each * unit);
+    a.parts = (int)((units + each - 1) / each);
+}
+
 size_t carve_verify(VerifyLaunch &a, int num_cus, bool drafted, void *base)
 {
-    (void)num_cus;
-    a.parts = 1, a.part_len = a.V;
-    const size_t rows = ((size_t)a.R * a.parts * sizeof(RowPart) + 255) & ~(size_t)255;
-    a.row = (RowPart *)base;
-    a.draft_row = base && drafted ? (RowPart *)((char *)base + rows) : nullptr;
-    return drafted ? 2 * rows : rows;
+    verify_shape(a, num_cus, drafted);
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        void *const p = base ? (char *)base + at : nullptr;
+        at += (bytes + 255) & ~(size_t)255;
+        return p;
+    };
+    const size_t parts = (size_t)a.R * a.parts;
+    a.row = (RowPart *)take(parts * sizeof(RowPart));
+    if (drafted) {
+        a.draft_row = (RowPart *)take(parts * sizeof(RowPart));
+        a.rest = (double *)take(parts * sizeof(double));
+        a.tickets = (int32_t *)take((size_t)a.B * 4);
+    }
+    return at;
+}
+
+// (a launch has less than 2^32 threads)
+bool verify_fits(const VerifyLaunch &a, bool drafted)
+{
+    return (int64_t)a.R * a.parts * (drafted ? 2 : 1) * kVerifyThreads < (int64_t)1 << 32 && (int64_t)a.B * (drafted ? a.parts : 1) * kDrawThreads < (int64_t)1 << 32;
 }
 
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
 {
     if (a.R > 0) {
-        const unsigned blocks = (unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u); // (at most 2^23: R is at most 2^22, parts 1 there)
-        hipLaunchKernelGGL(verify_rows_kernel, dim3(blocks), dim3(kVerifyThreads), 0, s, a);
+        hipLaunchKernelGGL(verify_rows_kernel, dim3((unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u)), dim3(kVerifyThreads), 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(verify_draw_kernel, dim3((unsigned)a.B), dim3(kVerifyThreads), 0, s, a);
+    hipLaunchKernelGGL(verify_draw_kernel, dim3((unsigned)a.B * (a.draft ? (unsigned)a.parts : 1u)), dim3(kDrawThreads), 0, s, a);
     return hipGetLastError();
 }
 
