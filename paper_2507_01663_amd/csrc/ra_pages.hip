@@ -74,7 +74,14 @@ __device__ __forceinline__ int owner(const int32_t *before, int x)
     return lo;
 }
 
-// PARTS: workgroups that share the tokens (workgroup w has every PARTS-th block of 1024 of them); STATE: the new lengths, counts and
+// This workgroup's first block of 1024 from the one that x is in: workgroup w of n has those whose number is w more than a multiple of n.
+__device__ __forceinline__ int64_t first_block(int x)
+{
+    const unsigned n = gridDim.x, b = (unsigned)x / kTileSeqs, mine = b % n;
+    return (int64_t)b + (blockIdx.x >= mine ? blockIdx.x - mine : blockIdx.x + n - mine);
+}
+
+// TOKENS: the tokens are placed, by workgroups that share the tokens in blocks of 1024; STATE: the new lengths, counts and
 // offsets are written.  Both at once only with one workgroup: lengths and counts may be written where they are read.
 template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void place_kernel(PagesLaunch a)
 {
@@ -111,10 +118,10 @@ template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void 
             const int t0 = first[0], t1 = (int)given.tokens;
             if (served && F > H && (cu / kTileSeqs) % gridDim.x == blockIdx.x)
                 for (int i = H; i < F; i++) a.table[(int64_t)b * a.max_pages + i] = a.pfx_pages[at + i];
-            for (int blk = t0 / kTileSeqs; (int64_t)blk * kTileSeqs < t1; blk++) {
-                if (blk % gridDim.x != blockIdx.x) continue;
-                const int t = blk * kTileSeqs + tid;
-                if (t < t0 || t >= t1) continue;
+            for (int64_t blk = first_block(t0); blk * kTileSeqs < t1; blk += gridDim.x) {
+                const int64_t at64 = blk * kTileSeqs + tid;
+                if (at64 < t0 || at64 >= t1) continue;
+                const int t = (int)at64;
                 const int s = owner(first, t);
                 const int4 r = row[s];
                 const int place = r.x + t - first[s], i = place / kPage;
@@ -161,10 +168,10 @@ template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void r
         if (PAGES) {
             first[tid] = incl.pages - mine.pages, begin[tid] = from;
             __syncthreads();
-            for (int blk = before / kTileSeqs; (int64_t)blk * kTileSeqs < back.pages; blk++) {
-                if (blk % gridDim.x != blockIdx.x) continue;
-                const int e = blk * kTileSeqs + tid;
-                if (e < before || e >= back.pages) continue;
+            for (int64_t blk = first_block(before); blk * kTileSeqs < back.pages; blk += gridDim.x) {
+                const int64_t at64 = blk * kTileSeqs + tid;
+                if (at64 < before || at64 >= back.pages) continue;
+                const int e = (int)at64;
                 const int s = owner(first, e);
                 const int64_t to = (int64_t)free + e;
                 if (to < a.num_pages) a.stack[to] = a.table[(int64_t)(base + s) * a.max_pages + begin[s] + e - first[s]];
@@ -175,17 +182,40 @@ template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void r
     if (STATE && tid == 0) a.free_out[0] = (int64_t)free + back.pages < a.num_pages ? free + back.pages : a.num_pages;
 }
 
+// Workgroups that share n tokens (or pages): one up to kAlone of them, which then writes the state too; else one for each kEach and a
+// kernel for the state, since lengths and counts may be written where the others still read them.
+constexpr int kAlone = 4096, kEach = 2048;
+static unsigned workgroups(int64_t n, int num_cus)
+{
+    const int64_t w = (n + kEach - 1) / kEach;
+    return n <= kAlone ? 1u : w < num_cus ? (unsigned)w : (unsigned)num_cus;
+}
+
 hipError_t launch_place(const PagesLaunch &a, int num_cus, hipStream_t s)
 {
-    (void)num_cus;
-    hipLaunchKernelGGL((place_kernel<true, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+    const unsigned n = workgroups(a.T, num_cus);
+    if (n == 1) {
+        hipLaunchKernelGGL((place_kernel<true, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((place_kernel<true, false>), dim3(n), dim3(kTileSeqs), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((place_kernel<false, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
     return hipGetLastError();
 }
 
 hipError_t launch_release(const PagesLaunch &a, int num_cus, hipStream_t s)
 {
-    (void)num_cus;
-    hipLaunchKernelGGL((release_kernel<true, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+    const unsigned n = workgroups((int64_t)a.B * a.max_pages, num_cus);
+    if (n == 1) {
+        hipLaunchKernelGGL((release_kernel<true, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL((release_kernel<true, false>), dim3(n), dim3(kTileSeqs), 0, s, a);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL((release_kernel<false, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
     return hipGetLastError();
 }
 

@@ -51,8 +51,7 @@ __device__ __forceinline__ double power(double d, double c)
 // The weight of logit l against top, which is finite and not smaller by much: 0 for -inf.
 __device__ __forceinline__ double weight(float l, double top, const Temper &t)
 {
-    const double d = (double)l - top;
-    return power(d > t.low ? d : t.low, t.c);
+    return power(__builtin_fmax((double)l - top, t.low), t.c);
 }
 
 // The larger of the two, or NaN if one is.
@@ -103,9 +102,13 @@ template <bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int beg
     float top = -INFINITY, mine = -__FLT_MAX__;
     int first = INT32_MAX;
     double sum = 0.0, against = mine;
+    float next[kVec];
+    if (begin + tid * kVec < end) row.load_some(next, begin + tid * kVec, end);
     for (int i = begin + tid * kVec; i < end; i += kVerifyThreads * kVec) {
         float x[kVec];
-        row.load_some(x, i, end);
+#pragma unroll
+        for (int j = 0; j < kVec; j++) x[j] = next[j];
+        if (i + kVerifyThreads * kVec < end) row.load_some(next, i + kVerifyThreads * kVec, end);
         float m = x[0];
 #pragma unroll
         for (int j = 1; j < kVec; j++) m = top_of(m, x[j]);
