@@ -134,12 +134,14 @@ typedef enum { RA_LOGITS_BF16 = 0, RA_LOGITS_FP32 = 1 } ra_logits_dtype;
  *   w = p_t                    if t is the last row,
  *   w = max(p_t - q_t, 0)      if its draft was turned down (without draft_logits: p_t without x); p_t if that is all zeros,
  * the token being the first one i with w_0 + .. + w_i > v * (w_0 + .. + w_{V-1}).  (With numbers that are independent and even on [0, 1) every
- * token is then distributed as if sampled from p alone.)  All of this is held in binary64, so that the sums of many small weights
- * move no border; the exponential is right to 2^-38.
+ * token is then distributed as if sampled from p alone.)  All of this is as in binary64, so that the sums of many small weights move
+ * no border: with weights that are right to 2^-38; or, in large batches, with sums of binary32 weights where what they may be off by
+ * settles the comparison, and in binary64 for the tests and draws that they leave open.
  *   T == 0 (or less, or NaN): greedy.  p_t is all on the largest logit, the first of equals; draft_logits are not read: a draft is
  *   accepted if it is that token.  T counts as the nearest of 1e-30 and 1e30 outside them.
  *   out_tokens[t]     for the sequence's rows: the accepted drafts, then the token drawn, then -1
- *   out_logprobs[t]   ln p_t(out_tokens[t]), 0 where out_tokens[t] is -1                     (NULL: not written)
+ *   out_logprobs[t]   ln p_t(out_tokens[t]), 0 where out_tokens[t] is -1; rounded to binary32, and off by 2^-17 at most where sums
+ *                     were of binary32 weights                                             (NULL: not written)
  *   next_tokens[b]    the token drawn                                                      (NULL: not written)
  * Logits of -inf have probability 0, whatever masks them; a row that has a NaN or +inf in it, or nothing but -inf, has no
  * distribution: p_t of such a row accepts no draft, and the token drawn from it is -1, with a log-probability of NaN; q_t of such a
@@ -180,7 +182,9 @@ ra_status rollout_attn_check_verify(const ra_verify *verify, char *msg, size_t m
  * is NULL are read).  ctx may be NULL: the size for a 256-compute-unit device is returned. */
 ra_status rollout_attn_verify_workspace_size(const ra_ctx *ctx, const ra_verify *shape_only, size_t *bytes);
 
-/* Enqueues the verification on hip_stream.  workspace as for rollout_attn_decode: dev memory of at least
+/* Enqueues the verification on hip_stream: two kernels, in large batches three or four.  The environment's
+ * ROLLOUT_ATTN_VERIFY_FEW=n, read by rollout_attn_create, is the number of logits (target's and draft model's) up to which all sums
+ * are binary64 from the start.  workspace as for rollout_attn_decode: dev memory of at least
  * rollout_attn_verify_workspace_size() bytes, 256-byte aligned, contents irrelevant on entry and undefined afterwards; calls
  * that overlap in time need distinct workspaces. */
 ra_status rollout_attn_verify(ra_ctx *ctx, const ra_verify *verify, void *workspace, size_t workspace_bytes, void *hip_stream);

@@ -184,6 +184,11 @@ ra_status rollout_attn_create(ra_ctx **out, int device)
         if (v >= 0 && v <= 64) c->prefill_stay = v;
     }
     c->self_plan = 1;
+    c->verify_few = ra::kVerifyFew;
+    if (const char *ev = getenv("ROLLOUT_ATTN_VERIFY_FEW")) {
+        const long long v = atoll(ev);
+        if (v >= 0) c->verify_few = v;
+    }
     if (const char *ev = getenv("ROLLOUT_ATTN_SELF_PLAN")) c->self_plan = atoi(ev) != 0;
     c->direct = 1;
     if (const char *ev = getenv("ROLLOUT_ATTN_DIRECT")) c->direct = atoi(ev) != 0;

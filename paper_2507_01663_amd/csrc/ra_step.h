@@ -39,10 +39,13 @@ struct VerifyLaunch {
     float *logprobs;
     RowPart *row, *draft_row;    // [R][parts]
     double *rest;                // [R][parts]  sums of max(p - q, 0), of the rows whose draft is turned down
-    int32_t *tickets;            // [B]         parts of those that have been added up
+    int32_t *tickets;            // [B]         workgroups that have added up a part
+    int4 *open;                  // [B]         draws that binary32 sums do not settle: {how, row, draft, -}
+    int32_t exact;               // all sums in binary64 from the start
+    double eps;                  // else: what a sum may be off by, in parts of the row's
 };
 // How a call is divided (from B, R, V), and its workspace: the bytes; places the pointers when base is not null.
-size_t carve_verify(VerifyLaunch &a, int num_cus, bool drafted, void *base);
+size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, void *base);
 bool verify_fits(const VerifyLaunch &a, bool drafted); // in one launch each
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s);
 

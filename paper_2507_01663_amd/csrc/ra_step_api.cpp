@@ -151,7 +151,7 @@ ra_status rollout_attn_verify_workspace_size(const ra_ctx *c, const ra_verify *p
     if (st != RA_OK) { set_err(err, "%s", msg); return st; }
     ra::VerifyLaunch a;
     fill_shape(a, p);
-    *bytes = ra::carve_verify(a, c ? c->num_cus : 256, p->draft_logits != nullptr, nullptr);
+    *bytes = ra::carve_verify(a, c ? c->num_cus : 256, c ? c->verify_few : ra::kVerifyFew, p->draft_logits != nullptr, nullptr);
     if (!ra::verify_fits(a, p->draft_logits != nullptr)) { set_err(err, "batch too large"); return RA_ERR_UNSUPPORTED; }
     return RA_OK;
 }
@@ -163,7 +163,7 @@ ra_status rollout_attn_verify(ra_ctx *c, const ra_verify *p, void *workspace, si
     if (st != RA_OK || p->num_seqs == 0) return st;
     ra::VerifyLaunch a;
     fill_shape(a, p);
-    const size_t need = ra::carve_verify(a, c->num_cus, p->draft_logits != nullptr, workspace);
+    const size_t need = ra::carve_verify(a, c->num_cus, c->verify_few, p->draft_logits != nullptr, workspace);
     if (!ra::verify_fits(a, p->draft_logits != nullptr)) { set_err(c, "batch too large"); return RA_ERR_UNSUPPORTED; }
     if (need && (!workspace || ((uintptr_t)workspace & 255))) { set_err(c, "workspace is NULL or not 256-byte aligned"); return RA_ERR_INVALID_ARG; }
     if (workspace_bytes < need) {

@@ -8,7 +8,7 @@
 
 namespace ra {
 
-constexpr int kVerifyThreads = 256, kVerifyWaves = kVerifyThreads / 64;
+constexpr int kVerifyThreads = 256;
 constexpr int kDrawThreads = 512, kDrawWaves = kDrawThreads / 64;
 constexpr int kMostPart = 64 * kDrawThreads;                     // values of a part at most: a wave then looks at a thread's stretch at once
 constexpr int kVec = 8;                                          // values that a lane loads at a time
@@ -54,6 +54,14 @@ __device__ __forceinline__ double weight(float l, double top, const Temper &t)
     return power(__builtin_fmax((double)l - top, t.low), t.c);
 }
 
+// The same in binary32, off by no more than (3 ln 2 |y| + 2) 2^-24 of it, y = (l - top) c: the difference, c and the product are rounded,
+// and the instruction's own step.
+__device__ __forceinline__ float weight32(float l, float top, const Temper &t) { return __builtin_amdgcn_exp2f((l - top) * t.cf); }
+__device__ __forceinline__ float sum_of_eight(const float (&x)[kVec])
+{
+    return ((x[0] + x[1]) + (x[2] + x[3])) + ((x[4] + x[5]) + (x[6] + x[7]));
+}
+
 // The larger of the two, or NaN if one is.
 __device__ __forceinline__ float top_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 
@@ -91,12 +99,14 @@ __device__ __forceinline__ bool is_finite(float x) { return __builtin_isfinite(x
 // ---- a part of a row ----------------------------------------------------------------------------------
 
 // The largest of values [begin, end) of a row and the sum of their weights against it; of a greedy row, the first of the largest.  A thread's
-// sum stands against the first value that it met (binary64 has room for weights of 2^500); the block's against the largest.
-template <bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int begin, int end, const Temper &t)
+// sum stands against a value that it met, and moves to a larger one only where weights would grow past 2^500 (in binary32: 2^8); the
+// workgroup's stands against the largest.
+template <bool EXACT, int THREADS, bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int begin, int end, const Temper &t)
 {
-    __shared__ float tops[kVerifyWaves];
-    __shared__ double part_sums[kVerifyWaves];
-    __shared__ int firsts[kVerifyWaves];
+    constexpr int WAVES = THREADS / 64;
+    __shared__ float tops[WAVES];
+    __shared__ double part_sums[WAVES];
+    __shared__ int firsts[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool greedy = t.c == 0.0;
     float top = -INFINITY, mine = -__FLT_MAX__;
@@ -104,11 +114,11 @@ template <bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int beg
     double sum = 0.0, against = mine;
     float next[kVec];
     if (begin + tid * kVec < end) row.load_some(next, begin + tid * kVec, end);
-    for (int i = begin + tid * kVec; i < end; i += kVerifyThreads * kVec) {
+    for (int i = begin + tid * kVec; i < end; i += THREADS * kVec) {
         float x[kVec];
 #pragma unroll
         for (int j = 0; j < kVec; j++) x[j] = next[j];
-        if (i + kVerifyThreads * kVec < end) row.load_some(next, i + kVerifyThreads * kVec, end);
+        if (i + THREADS * kVec < end) row.load_some(next, i + THREADS * kVec, end);
         float m = x[0];
 #pragma unroll
         for (int j = 1; j < kVec; j++) m = top_of(m, x[j]);
@@ -118,12 +128,18 @@ template <bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int beg
                 for (int j = kVec - 1; j >= 0; j--)
                     if (x[j] == m) first = i + j;
         } else {
-            if ((m - mine) * t.cf > 500.f) {                    // (also the first time)
+            if ((m - mine) * t.cf > (EXACT ? 500.f : 8.f)) {    // (also the first time)
                 sum *= exp2(((double)mine - (double)m) * t.c);
                 mine = m, against = m;
             }
+            if constexpr (EXACT) {
 #pragma unroll
-            for (int j = 0; j < kVec; j++) sum += weight(x[j], against, t);
+                for (int j = 0; j < kVec; j++) sum += weight(x[j], against, t);
+            } else {
+#pragma unroll
+                for (int j = 0; j < kVec; j++) x[j] = weight32(x[j], mine, t);
+                sum += (double)sum_of_eight(x);
+            }
         }
         top = top_of(top, m);
     }
@@ -134,7 +150,7 @@ template <bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int beg
     __syncthreads();
     all = tops[0];
 #pragma unroll
-    for (int w = 1; w < kVerifyWaves; w++) all = top_of(all, tops[w]);
+    for (int w = 1; w < WAVES; w++) all = top_of(all, tops[w]);
     sum = is_finite(all) ? sum * exp2(((double)mine - (double)all) * t.c) : 0.0;
     if (top != all) first = INT32_MAX;
 #pragma unroll
@@ -147,7 +163,8 @@ template <bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int beg
     __syncthreads();
     RowPart r = {part_sums[0], all, firsts[0]};
 #pragma unroll
-    for (int w = 1; w < kVerifyWaves; w++) r.sum += part_sums[w], r.first = firsts[w] < r.first ? firsts[w] : r.first;
+    for (int w = 1; w < WAVES; w++) r.sum += part_sums[w], r.first = firsts[w] < r.first ? firsts[w] : r.first;
+    __syncthreads();
     return r;
 }
 
@@ -176,8 +193,14 @@ __device__ __forceinline__ int64_t draft_row_of(const VerifyLaunch &a, int b, in
     return r >= 0 && r < a.total_draft_rows ? r : -1;
 }
 
+template <bool EXACT, int THREADS> __device__ __forceinline__ RowPart part_of(const uint8_t *at, int fp32, int begin, int end, const Temper &t)
+{
+    return fp32 ? part_of_row<EXACT, THREADS>(Row<true>{at}, begin, end, t) : part_of_row<EXACT, THREADS>(Row<false>{at}, begin, end, t);
+}
+__device__ __forceinline__ int part_end(const VerifyLaunch &a, int k) { return k + 1 < a.parts ? (k + 1) * a.part_len : a.V; }
+
 // A part of a target row, or of the draft's row that belongs to it: the workgroups of the target's rows come first.
-__global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
+template <bool EXACT> __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
 {
     const unsigned rows = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
     const bool drafted = rows >= (unsigned)a.R;
@@ -185,20 +208,17 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunc
     const int b = sequence_of_row(a, t, lane);
     if (b >= a.B || t < a.cu[b]) return;
     const Temper temper = temper_of(a, b);
-    const int begin = (int)k * a.part_len, end = begin + a.part_len < a.V ? begin + a.part_len : a.V;
-    RowPart r;
-    if (!drafted) {
-        const uint8_t *const at = row_at(a.logits, a.stride, a.fp32, t);
-        r = a.fp32 ? part_of_row(Row<true>{at}, begin, end, temper) : part_of_row(Row<false>{at}, begin, end, temper);
-    } else {
+    const uint8_t *at = row_at(a.logits, a.stride, a.fp32, t);
+    if (drafted) {
         const int64_t d = draft_row_of(a, b, t);
         if (t + 1 >= a.cu[b + 1] || d < 0 || temper.c == 0.0) return;
-        const uint8_t *const at = row_at(a.draft, a.draft_stride, a.draft_fp32, d);
-        r = a.draft_fp32 ? part_of_row(Row<true>{at}, begin, end, temper) : part_of_row(Row<false>{at}, begin, end, temper);
+        at = row_at(a.draft, a.draft_stride, a.draft_fp32, d);
     }
-    // (this many parts of the sequence's rest have been added up: none; see verify_draw_kernel)
-    if (threadIdx.x == 0 && !drafted && k == 0 && t == a.cu[b] && a.draft) a.tickets[b] = 0;
-    if (threadIdx.x == 0) (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
+    const RowPart r = part_of<EXACT, kVerifyThreads>(at, drafted ? a.draft_fp32 : a.fp32, k * a.part_len, part_end(a, k), temper);
+    if (threadIdx.x) return;
+    // (this many parts of the sequence's rest have been added up: none; see the draws)
+    if (!drafted && k == 0 && t == a.cu[b] && a.tickets) a.tickets[b] = 0;
+    (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
 }
 
 // ---- decisions ----------------------------------------------------------------------------------------
@@ -248,20 +268,20 @@ struct Draw {
 };
 
 // What row `row` of sequence b says to its draft, and how a token is drawn from it if that does not stay.  All lanes of a wave.
-__device__ __forceinline__ Draw judge(const VerifyLaunch &a, int b, int row, int end, const Temper &t, int lane, bool &stays, double &lp)
+enum Verdict { kGoes, kStays, kUnsure };
+__device__ __forceinline__ Draw judge(const VerifyLaunch &a, int b, int row, int end, const Temper &t, const Whole &p, const Whole &q, double unsure, Verdict &says, double &lp)
 {
-    const Whole p = whole_row(a.row + (int64_t)row * a.parts, a.parts, t, lane);
     const int x = row + 1 == end ? -1 : a.tokens[row + 1];
     const bool token = x >= 0 && x < a.V;
     Draw d = {};
     d.row = row, d.x = x, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, row), d.p_top = p.top, d.p_scale = 1.0 / p.sum;
-    stays = false, lp = 0.0;
+    says = kGoes, lp = 0.0;
     if (!is_finite(p.top)) {
         d.from = kNothing;
         return d;
     }
     if (t.c == 0.0) {
-        d.from = kTop, stays = token && x == p.first, d.x = p.first;
+        d.from = kTop, says = token && x == p.first ? kStays : kGoes, d.x = p.first;
         return d;
     }
     d.from = kRow;
@@ -269,41 +289,67 @@ __device__ __forceinline__ Draw judge(const VerifyLaunch &a, int b, int row, int
     const float l = logit_at(a.logits, a.stride, a.fp32, row, x);
     const double px = weight(l, p.top, t) / p.sum;
     lp = ((double)l - (double)p.top) * t.c / kLog2e - log(p.sum);
-    if (!a.draft) {
-        stays = (double)a.u[row] < px;
-        d.from = kRowWithout;
-        return d;
+    double against = (double)a.u[row];
+    if (!a.draft) d.from = kRowWithout;
+    else {
+        const int64_t r = draft_row_of(a, b, row);
+        if (r < 0 || !is_finite(q.top)) return d;
+        d.from = kRest, d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, r), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+        against *= weight(logit_at(a.draft, a.draft_stride, a.draft_fp32, r, x), q.top, t) / q.sum;
     }
-    const int64_t r = draft_row_of(a, b, row);
-    if (r < 0) return d;
-    const Whole q = whole_row(a.draft_row + (int64_t)row * a.parts, a.parts, t, lane);
-    if (!is_finite(q.top)) return d;
-    d.from = kRest, d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, r), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
-    const double qx = weight(logit_at(a.draft, a.draft_stride, a.draft_fp32, r, x), q.top, t) / q.sum;
-    stays = (double)a.u[row] * qx < px;
+    says = against < px ? kStays : kGoes;
+    // (where px is 0 or the number is not positive, no error of the sums changes the answer)
+    if (px > 0.0 && against > 0.0 && __builtin_fabs(against - px) <= unsure * px) says = kUnsure;
     return d;
 }
+// The sums of the row and of its draft's, as the first kernel (or resum) left them.
+__device__ __forceinline__ Draw judge_row(const VerifyLaunch &a, int b, int row, int end, const Temper &t, int lane, double unsure, Verdict &says, double &lp)
+{
+    const Whole p = whole_row(a.row + (int64_t)row * a.parts, a.parts, t, lane);
+    Whole q = {1.0, -INFINITY, 0};
+    if (a.draft && row + 1 < end && t.c != 0.0 && draft_row_of(a, b, row) >= 0) q = whole_row(a.draft_row + (int64_t)row * a.parts, a.parts, t, lane);
+    return judge(a, b, row, end, t, p, q, unsure, says, lp);
+}
 
-// The rows of sequence b, as many at a time as there are waves, up to the first that keeps no draft: that one's draw.  The whole
-// workgroup; `write`: this one writes the drafts that stay.
-__device__ __forceinline__ Draw decide(const VerifyLaunch &a, int b, int begin, int end, const Temper &t, bool write)
+// A whole row, all over again in binary64, by a workgroup of the draws.
+__device__ Whole exact_row(const VerifyLaunch &a, const uint8_t *at, int fp32, const Temper &t)
+{
+    const RowPart r = part_of<true, kDrawThreads>(at, fp32, 0, a.V, t);
+    return {r.sum, r.top, r.first};
+}
+
+// The rows of sequence b, as many at a time as there are waves, up to the first that keeps no draft: that one's draw.  The drafts that stay
+// are written.  The whole workgroup.
+template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch &a, int b, int begin, int end, const Temper &t)
 {
     __shared__ Draw draws[kDrawWaves];
-    __shared__ int stay[kDrawWaves];
+    __shared__ Verdict verdict[kDrawWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int base = begin;; base += kDrawWaves) {
         const int row = base + wave;
-        bool stays = false;
+        Verdict says = kGoes;
         double lp = 0.0;
         if (row < end) {
-            const Draw d = judge(a, b, row, end, t, lane, stays, lp);
+            const Draw d = judge_row(a, b, row, end, t, lane, EXACT ? 0.0 : 4.0 * a.eps, says, lp);
+            if (EXACT && says == kUnsure) says = kGoes;         // (equal: not less)
             if (lane == 0) draws[wave] = d;
         }
-        if (lane == 0) stay[wave] = stays;
+        if (lane == 0) verdict[wave] = says;
         __syncthreads();
         int n = 0;
-        while (n < kDrawWaves && stay[n]) n++;
-        if (write && wave < n && lane == 0) {
+        for (;; n++) {
+            while (n < kDrawWaves && verdict[n] == kStays) n++;
+            if (EXACT || n == kDrawWaves || verdict[n] == kGoes) break;
+            // too near to be told apart by sums of binary32 weights: a few in a hundred thousand
+            const Draw d = draws[n];
+            const Whole p = exact_row(a, d.p, a.fp32, t);
+            const Whole q = d.from == kRest ? exact_row(a, d.q, a.draft_fp32, t) : Whole{1.0, -INFINITY, 0};
+            Verdict sure;
+            double unused;
+            (void)judge(a, b, d.row, end, t, p, q, 0.0, sure, unused);
+            if (sure != kStays) break;
+        }
+        if (wave < n && lane == 0) {
             a.out[row] = a.tokens[row + 1];
             if (a.logprobs) a.logprobs[row] = (float)lp;
         }
@@ -380,13 +426,14 @@ __device__ __forceinline__ int holder(double before, double mine, double border)
     return first < INT32_MAX ? first : last;
 }
 
-// The first value of part k at which the running sum of the part's weights passes the border.
-__device__ int token_of_part(const VerifyLaunch &a, const Draw &d, int k, double border)
+// The first value of part k at which the running sum of the part's weights passes the border; -1 where the sum is within `unsure` of
+// the border at it or before it.
+__device__ int token_of_part(const VerifyLaunch &a, const Draw &d, int k, double border, double unsure)
 {
     __shared__ int token;
     __shared__ double from;
     const int tid = threadIdx.x, lane = tid & 63;
-    const int begin = k * a.part_len, end = begin + a.part_len < a.V ? begin + a.part_len : a.V;
+    const int begin = k * a.part_len, end = part_end(a, k);
     const int len = a.part_len / kDrawThreads;                  // a multiple of 8, at most 64
     const int mine = begin + tid * len, stop = mine + len < end ? mine + len : end;
     double sum = 0.0, total, w[kVec];
@@ -410,7 +457,10 @@ __device__ int token_of_part(const VerifyLaunch &a, const Draw &d, int k, double
             if (lane >= s) run += o;
         }
         const uint64_t any = __ballot(w[0] > 0.0), past = __ballot(w[0] > 0.0 && from + run > border);
-        if (lane == 0) token = past ? at + __builtin_ctzll(past) : any ? at + 63 - __builtin_clzll(any) : -1;
+        const int which = past ? __builtin_ctzll(past) : any ? 63 - __builtin_clzll(any) : -1;
+        const bool near = from + run - border <= unsure || border - (from + run - w[0]) <= unsure;
+        const bool told = unsure == 0.0 || !(__ballot(near) >> (which & 63) & 1);
+        if (lane == 0) token = which >= 0 && told ? at + which : -1;
     }
     __syncthreads();
     return token;
@@ -430,7 +480,7 @@ __device__ __forceinline__ double share_of_part(const VerifyLaunch &a, const Dra
 
 __device__ double sum_of_part(const VerifyLaunch &a, const Draw &d, int k)
 {
-    const int begin = k * a.part_len, end = begin + a.part_len < a.V ? begin + a.part_len : a.V;
+    const int begin = k * a.part_len, end = part_end(a, k);
     double sum = 0.0, total, w[kVec];
     for (int i = begin + threadIdx.x * kVec; i < end; i += kDrawThreads * kVec) {
         weights_at(w, a, d, i, end);
@@ -441,8 +491,35 @@ __device__ double sum_of_part(const VerifyLaunch &a, const Draw &d, int k)
     return total;
 }
 
-// The token that v draws, from the parts' sums and then from the part that holds the border.  The whole workgroup.
-__device__ int draw(const VerifyLaunch &a, Draw d, double v)
+// What is left of a part of p - q, in binary32 products.
+template <bool FP32, bool QFP32> __device__ __forceinline__ double rest32(const Draw &d, int begin, int end)
+{
+    const Row<FP32> p = {d.p};
+    const Row<QFP32> q = {d.q};
+    const float p_top = (float)d.p_top, q_top = (float)d.q_top, p_scale = (float)d.p_scale, q_scale = (float)d.q_scale;
+    double sum = 0.0;
+    float x[kVec], y[kVec];
+    for (int i = begin + threadIdx.x * kVec; i < end; i += kDrawThreads * kVec) {
+        p.load_some(x, i, end), q.load_some(y, i, end);
+#pragma unroll
+        for (int j = 0; j < kVec; j++) x[j] = fmaxf(weight32(x[j], p_top, d.t) * p_scale - weight32(y[j], q_top, d.t) * q_scale, 0.f);
+        sum += (double)sum_of_eight(x);
+    }
+    return sum;
+}
+__device__ double rest32_of_part(const VerifyLaunch &a, const Draw &d, int k)
+{
+    const int begin = k * a.part_len, end = part_end(a, k);
+    double sum, total;
+    if (a.fp32) sum = a.draft_fp32 ? rest32<true, true>(d, begin, end) : rest32<true, false>(d, begin, end);
+    else sum = a.draft_fp32 ? rest32<false, true>(d, begin, end) : rest32<false, false>(d, begin, end);
+    (void)sum_before(sum, total);
+    return total;
+}
+
+// The token that v draws, from the parts' sums and then from the part that holds the border.  The whole workgroup.  -1 where the sums
+// may be off by as much as the border is from the nearest token's (`unsure`).
+__device__ int draw(const VerifyLaunch &a, Draw d, double v, double unsure)
 {
     __shared__ double border_in_part;
     __shared__ int part;
@@ -457,7 +534,7 @@ __device__ int draw(const VerifyLaunch &a, Draw d, double v)
         const double before = sum_before(mine, total), border = v * total;
         const int who = holder(before, mine, border);
         if (who < 0) {                                          // nothing is left of p - q: p
-            if (d.from == kRow) return -1;                      // (no row of a well-formed call)
+            if (d.from == kRow || unsure > 0.0) return -1;      // (the first: no row of a well-formed call)
             d.from = kRow;
             continue;
         }
@@ -472,42 +549,20 @@ __device__ int draw(const VerifyLaunch &a, Draw d, double v)
             }
         }
         __syncthreads();
-        return token_of_part(a, d, part, border_in_part);
+        return token_of_part(a, d, part, border_in_part, unsure);
     }
 }
 
-// Which drafts stay, and the token behind them.  With a draft model's logits every sequence has a workgroup for each part of a row: all
-// see which draft was turned down, and add up what is left of its part; the last to arrive draws.  Where nothing is to be added up, and
-// without a draft model, a sequence's first (only) workgroup draws.
-__global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyLaunch a)
+__device__ __forceinline__ double number_of(const VerifyLaunch &a, int b)
 {
-    __shared__ int arrived;
+    const double v = a.v[b];
+    return v > 0.0 ? v < 1.0 ? v : 1.0 : 0.0;
+}
+
+// What comes out of sequence b, but for the drafts that stay.  The whole workgroup.
+__device__ __forceinline__ void finish(const VerifyLaunch &a, int b, int begin, int end, const Draw &d, int token)
+{
     const int tid = threadIdx.x;
-    const int b = a.draft ? blockIdx.x / (unsigned)a.parts : blockIdx.x, k = a.draft ? blockIdx.x % (unsigned)a.parts : 0;
-    const int begin = a.cu[b], end = a.cu[b + 1];
-    if (begin < 0 || end > a.R || begin >= end) {
-        if (k == 0 && tid == 0) {
-            a.accepted[b] = 0;
-            if (a.next) a.next[b] = -1;
-        }
-        return;
-    }
-    const Temper t = temper_of(a, b);
-    const Draw d = decide(a, b, begin, end, t, k == 0);
-    if (d.from == kRest) {
-        const double sum = sum_of_part(a, d, k);
-        if (tid == 0) {
-            a.rest[(int64_t)d.row * a.parts + k] = sum;
-            arrived = __hip_atomic_fetch_add(a.tickets + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
-        }
-        __syncthreads();
-        if (arrived != a.parts - 1) return;
-    } else if (k != 0) return;
-    double v = a.v[b];
-    v = v > 0.0 ? v < 1.0 ? v : 1.0 : 0.0;
-    int token = -1;
-    if (d.from == kTop) token = d.x;
-    else if (d.from != kNothing) token = draw(a, d, v);
     if (tid == 0) {
         a.accepted[b] = d.row - begin;
         if (a.next) a.next[b] = token;
@@ -515,7 +570,7 @@ __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyLaunch 
         if (a.logprobs) {
             double lp = d.from == kTop ? 0.0 : __builtin_nan("");
             if (d.from != kTop && token >= 0)
-                lp = ((double)logit_at(a.logits, a.stride, a.fp32, d.row, token) - d.p_top) * t.c / kLog2e + log(d.p_scale);
+                lp = ((double)logit_at(a.logits, a.stride, a.fp32, d.row, token) - d.p_top) * d.t.c / kLog2e + log(d.p_scale);
             a.logprobs[d.row] = (float)lp;
         }
     }
@@ -525,8 +580,101 @@ __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyLaunch 
     }
 }
 
+// Whether this workgroup is the last of `all` to come here for sequence b, on top of `came` before.  Its sums, written by its first
+// thread, are there for the last one.
+__device__ __forceinline__ bool last_to_arrive(const VerifyLaunch &a, int b, int came, int all)
+{
+    __shared__ int arrived;
+    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(a.tickets + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    __syncthreads();
+    return arrived == came + all - 1;
+}
+
+// Which drafts stay, and the token behind them where the row's sums tell it: a workgroup for each sequence.  What is left open: draws
+// from p - q, and those that binary32 sums do not settle.
+template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyLaunch a)
+{
+    const int tid = threadIdx.x, b = blockIdx.x;
+    const int begin = a.cu[b], end = a.cu[b + 1];
+    if (begin < 0 || end > a.R || begin >= end) {
+        if (tid == 0) {
+            a.accepted[b] = 0;
+            if (a.next) a.next[b] = -1;
+            if (a.open) a.open[b] = make_int4(kNothing, 0, 0, 0);
+        }
+        return;
+    }
+    const Temper t = temper_of(a, b);
+    const Draw d = decide<EXACT>(a, b, begin, end, t);
+    int token = -1;
+    if (d.from == kTop) token = d.x;
+    // (prefixes and totals are off by eps of the row each)
+    else if (d.from == kRow || d.from == kRowWithout) token = draw(a, d, number_of(a, b), EXACT ? 0.0 : 3.0 * a.eps);
+    const bool left_open = d.from == kRest || (!EXACT && token < 0 && d.from != kNothing);
+    if (a.open && tid == 0) a.open[b] = left_open ? make_int4(d.from, d.row, d.x, 0) : make_int4(kNothing, 0, 0, 0);
+    if (!left_open) finish(a, b, begin, end, d, token);
+}
+
+// What is known of an open draw.
+__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, int b, int4 o, const Temper &t)
+{
+    const int lane = threadIdx.x & 63, row = o.y;
+    Draw d = {};
+    d.from = o.x, d.row = row, d.x = o.z, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, row);
+    const Whole p = whole_row(a.row + (int64_t)row * a.parts, a.parts, t, lane);
+    d.p_top = p.top, d.p_scale = 1.0 / p.sum;
+    if (o.x == kRest) {
+        const Whole q = whole_row(a.draft_row + (int64_t)row * a.parts, a.parts, t, lane);
+        d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, draft_row_of(a, b, row)), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+    }
+    return d;
+}
+
+// The draws from p - q: a workgroup adds up what is left of each part, the last to arrive draws.  Not EXACT: in binary32, and draws that
+// those sums do not settle stay open; and the draws from p that are open have their sums made anew, in binary64.
+template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch a, int came)
+{
+    const int tid = threadIdx.x, b = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
+    const int4 o = a.open[b];
+    if (o.x == kNothing) return;
+    const Temper t = temper_of(a, b);
+    double unsure = 0.0;
+    Draw d;
+    if (EXACT || o.x == kRest) {
+        d = open_draw(a, b, o, t);
+        const double sum = EXACT ? sum_of_part(a, d, k) : rest32_of_part(a, d, k);
+        if (tid == 0) a.rest[(int64_t)o.y * a.parts + k] = sum;
+        // (p and q: twice eps each, by their weights and by their scales; so for a prefix and for the whole)
+        if (!EXACT) unsure = 10.0 * a.eps;
+        if (!last_to_arrive(a, b, came, a.parts)) return;
+    } else {
+        const RowPart p = part_of<true, kDrawThreads>(row_at(a.logits, a.stride, a.fp32, o.y), a.fp32, k * a.part_len, part_end(a, k), t);
+        if (tid == 0) a.row[(int64_t)o.y * a.parts + k] = p;
+        if (!last_to_arrive(a, b, came, a.parts)) return;
+        d = open_draw(a, b, o, t);
+    }
+    const int token = draw(a, d, number_of(a, b), unsure);
+    if (unsure > 0.0 && token < 0) return;
+    if (!EXACT && tid == 0) a.open[b].x = kNothing;             // (all of its workgroups have read it)
+    finish(a, b, a.cu[b], a.cu[b + 1], d, token);
+}
+
+// The sums of p and of q anew, in binary64, for the draws from p - q that are still open.
+__global__ __launch_bounds__(kDrawThreads) void verify_resum_kernel(VerifyLaunch a)
+{
+    const int tid = threadIdx.x, b = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
+    const int4 o = a.open[b];
+    if (o.x != kRest) return;
+    const Temper t = temper_of(a, b);
+    const int row = o.y, begin = k * a.part_len, end = part_end(a, k);
+    const RowPart p = part_of<true, kDrawThreads>(row_at(a.logits, a.stride, a.fp32, row), a.fp32, begin, end, t);
+    const RowPart q = part_of<true, kDrawThreads>(row_at(a.draft, a.draft_stride, a.draft_fp32, draft_row_of(a, b, row)), a.draft_fp32, begin, end, t);
+    if (tid == 0) a.row[(int64_t)row * a.parts + k] = p, a.draft_row[(int64_t)row * a.parts + k] = q;
+}
+
 // How rows are cut into parts: so many that the workgroups of the rows fill the device several times, of whole loads of a workgroup each.
-static void verify_shape(VerifyLaunch &a, int num_cus, bool drafted)
+// Whether all sums are binary64 from the start: where that costs less than the two kernels for the draws that binary32 leaves open.
+static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted)
 {
     const int64_t rows = (int64_t)a.R * (drafted ? 2 : 1), unit = kDrawThreads * kVec;
     const int64_t units = (a.V + unit - 1) / unit, wanted = rows > 0 ? ((int64_t)num_cus * 32 + rows - 1) / rows : 1;
@@ -534,11 +682,19 @@ static void verify_shape(VerifyLaunch &a, int num_cus, bool drafted)
     each = each < 1 ? 1 : each > kMostPart / unit ? kMostPart / unit : each;
     a.part_len = (int)(each * unit);
     a.parts = (int)((units + each - 1) / each);
+    a.exact = rows * a.V <= few;
+    // The error of a sum of weights as weight32 gives them, in parts of the row's whole sum W: a weight w is off by (3 ln 2 |y| + 2) 2^-24
+    // of it and a sum of eight by 3 2^-24; y is against the thread's value, which is at most 8 / c below one it met: |y| is at most 8
+    // more than against the row's largest.  Against that, log2(W) + sum(w |y|) / W is the entropy of the row in bits, at most log2(V),
+    // and W >= 1: so sum(w |y|) <= log2(V) W.  All together (3 ln 2 (log2(V) + 8) + 5) 2^-24, and a twentieth more for second orders.
+    int bits = 0;
+    while ((int64_t)1 << bits < a.V) bits++;
+    a.eps = 1.05 * (2.08 * (bits + 8) + 5.0) * 0x1p-24;
 }
 
-size_t carve_verify(VerifyLaunch &a, int num_cus, bool drafted, void *base)
+size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, void *base)
 {
-    verify_shape(a, num_cus, drafted);
+    verify_shape(a, num_cus, few, drafted);
     size_t at = 0;
     auto take = [&](size_t bytes) {
         void *const p = base ? (char *)base + at : nullptr;
@@ -550,7 +706,10 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, bool drafted, void *base)
     if (drafted) {
         a.draft_row = (RowPart *)take(parts * sizeof(RowPart));
         a.rest = (double *)take(parts * sizeof(double));
+    }
+    if (drafted || !a.exact) {
         a.tickets = (int32_t *)take((size_t)a.B * 4);
+        a.open = (int4 *)take((size_t)a.B * sizeof(int4));
     }
     return at;
 }
@@ -558,17 +717,30 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, bool drafted, void *base)
 // (a launch has less than 2^32 threads)
 bool verify_fits(const VerifyLaunch &a, bool drafted)
 {
-    return (int64_t)a.R * a.parts * (drafted ? 2 : 1) * kVerifyThreads < (int64_t)1 << 32 && (int64_t)a.B * (drafted ? a.parts : 1) * kDrawThreads < (int64_t)1 << 32;
+    return (int64_t)a.R * a.parts * (drafted ? 2 : 1) * kVerifyThreads < (int64_t)1 << 32 && (int64_t)a.B * a.parts * kDrawThreads < (int64_t)1 << 32;
 }
 
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
 {
+    const dim3 rows((unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u)), seqs((unsigned)a.B), parts((unsigned)a.B * (unsigned)a.parts);
+    const dim3 threads(kDrawThreads);
     if (a.R > 0) {
-        hipLaunchKernelGGL(verify_rows_kernel, dim3((unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u)), dim3(kVerifyThreads), 0, s, a);
+        if (a.exact) hipLaunchKernelGGL(verify_rows_kernel<true>, rows, dim3(kVerifyThreads), 0, s, a);
+        else hipLaunchKernelGGL(verify_rows_kernel<false>, rows, dim3(kVerifyThreads), 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    hipLaunchKernelGGL(verify_draw_kernel, dim3((unsigned)a.B * (a.draft ? (unsigned)a.parts : 1u)), dim3(kDrawThreads), 0, s, a);
+    if (a.exact) {
+        hipLaunchKernelGGL(verify_draw_kernel<true>, seqs, threads, 0, s, a);
+        if (a.draft) hipLaunchKernelGGL(verify_rest_kernel<true>, parts, threads, 0, s, a, 0);
+        return hipGetLastError();
+    }
+    hipLaunchKernelGGL(verify_draw_kernel<false>, seqs, threads, 0, s, a);
+    hipLaunchKernelGGL(verify_rest_kernel<false>, parts, threads, 0, s, a, 0);
+    if (a.draft) {
+        hipLaunchKernelGGL(verify_resum_kernel, parts, threads, 0, s, a);
+        hipLaunchKernelGGL(verify_rest_kernel<true>, parts, threads, 0, s, a, a.parts);
+    }
     return hipGetLastError();
 }
 

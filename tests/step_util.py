@@ -216,7 +216,7 @@ def verify(logits, cu, tokens, u, v, T=None, draft=None, draft_rows=None):
 
 
 class Verifying:
-    """A batch of rows on the device.  rows: rows of each sequence; behind: rows of nobody at the end; logits, draft: float64 [R, V] that
+    """A batch of rows on the device.  exact: all sums are binary64 (the library's choice for few logits).  rows: rows of each sequence; behind: rows of nobody at the end; logits, draft: float64 [R, V] that
     are values of their types.  pad: elements between two rows; shift: elements before the first."""
 
     def __init__(self, rows, logits, tokens, u, v, T=None, draft=None, draft_rows=None, dtype="bf16", draft_dtype=None, pad=0, shift=0, lead=0):
@@ -236,6 +236,8 @@ class Verifying:
         self.c = ra.verify_from_tensors(self.logits, self.cu, self.tokens, self.u, self.v, self.accepted, self.out, self.lps, self.next, self.T,
                                         self.draft, self.draft_rows)
 
+    exact = True
+
     @staticmethod
     def _device(x, dtype, pad, shift):
         kind = torch.bfloat16 if dtype == "bf16" else torch.float32
@@ -247,7 +249,12 @@ class Verifying:
 
     def check(self, what=""):
         """Tokens and counts are those of the reference.  A log-probability is rounded once to binary32 (2^-24 of it); beside that the
-        weights' 2^-38 in the sum of a row, and binary64 steps in (l - top) / T of a size up to 1e4 (1e4 2^-52)."""
+        weights' 2^-38 in the sum of a row, and binary64 steps in (l - top) / T of a size up to 1e4 (1e4 2^-52).  A row's sum of binary32
+        weights w = 2^y is off by (3 ln 2 |y| + 2) 2^-24 w for each (the difference, the factor and the product are rounded, and the
+        power's step) and 3 2^-24 for adding eight up; y is against a value up to 8 below the largest, and sum(w |y|) <= log2(V)
+        sum(w) where the largest weighs 1 (the entropy in bits): (3 ln 2 (log2(V) + 8) + 5) 2^-24 of the sum, 5.7e-5 2^-4 = 3.6e-6 for
+        V = 2^17, and as much in its logarithm."""
+        sums = 0.0 if self.exact else 1.05 * (3 * math.log(2) * (math.log2(max(2, self.c.vocab)) + 8) + 5) * 2.0 ** -24
         torch.cuda.synchronize()
         accepted, out, lps, nexts = verify(*self.host)
         assert self.accepted.tolist() == accepted, (what, self.accepted.tolist(), accepted)
@@ -261,7 +268,7 @@ class Verifying:
             if math.isnan(lp):
                 assert math.isnan(glp[t]), (what, t)
             else:
-                assert abs(glp[t] - lp) <= 2.0 ** -24 * abs(lp) + 2.0 ** -37, (what, t, glp[t], lp)
+                assert abs(glp[t] - lp) <= 2.0 ** -24 * abs(lp) + 2.0 ** -37 + sums, (what, t, glp[t], lp)
         return self
 
 

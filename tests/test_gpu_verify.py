@@ -4,6 +4,7 @@ import pytest
 import torch
 
 import paper_2507_01663_amd as ra
+from gpu_util import context
 from step_util import DEV, Verifying, distribution, drafting, rounded, rows_of
 
 pytestmark = pytest.mark.gpu
@@ -11,14 +12,18 @@ pytestmark = pytest.mark.gpu
 INF, NAN = float("inf"), float("nan")
 
 
-@pytest.fixture(scope="module")
-def dec():
-    d = ra.Decoder(0)
+@pytest.fixture(scope="module", params=["binary64 sums", "binary32 sums first"])
+def dec(request):
+    """The library's choice for the few logits of most of these tests, and the way that it takes with many."""
+    exact = request.param == "binary64 sums"
+    d = context() if exact else context(VERIFY_FEW=0)
+    d.exact = exact
     yield d
     d.close()
 
 
 def run(dec, x, what=""):
+    x.exact = dec.exact
     dec.verify(x.c)
     return x.check(what)
 
@@ -182,6 +187,7 @@ def test_sizes_of_logits_and_temperatures(dec, scale):
     dec.verify(x.c)
     torch.cuda.synchronize()
     # (a log-probability of (l - top) / T in the thousands is known to 2^-24 of its size, which check() allows for)
+    x.exact = dec.exact
     x.check(scale)
 
 
