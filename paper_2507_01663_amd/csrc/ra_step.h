@@ -41,6 +41,7 @@ struct VerifyLaunch {
     double *rest;                // [R][parts]  sums of max(p - q, 0), of the rows whose draft is turned down
     int32_t *tickets;            // [B]         workgroups that have added up a part
     int4 *open;                  // [B]         draws that binary32 sums do not settle: {how, row, draft, -}
+    int32_t alone;               // a part to a wave, not to a workgroup
     int32_t exact;               // all sums in binary64 from the start
     double eps;                  // else: what a sum may be off by, in parts of the row's
 };

@@ -10,7 +10,6 @@ namespace ra {
 
 constexpr int kVerifyThreads = 256;
 constexpr int kDrawThreads = 512, kDrawWaves = kDrawThreads / 64;
-constexpr int kMostPart = 64 * kDrawThreads;                     // values of a part at most: a wave then looks at a thread's stretch at once
 constexpr int kVec = 8;                                          // values that a lane loads at a time
 constexpr double kLog2e = 1.4426950408889634074;
 
@@ -98,27 +97,14 @@ __device__ __forceinline__ bool is_finite(float x) { return __builtin_isfinite(x
 
 // ---- a part of a row ----------------------------------------------------------------------------------
 
-// The largest of values [begin, end) of a row and the sum of their weights against it; of a greedy row, the first of the largest.  A thread's
-// sum stands against a value that it met, and moves to a larger one only where weights would grow past 2^500 (in binary32: 2^8); the
-// workgroup's stands against the largest.
-template <bool EXACT, int THREADS, bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int begin, int end, const Temper &t)
-{
-    constexpr int WAVES = THREADS / 64;
-    __shared__ float tops[WAVES];
-    __shared__ double part_sums[WAVES];
-    __shared__ int firsts[WAVES];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const bool greedy = t.c == 0.0;
+// What a thread knows of the values that it has met: the largest, their weights' sum against `mine`, and for a greedy row the first of the
+// largest.  `mine` is a value that it met, and moves to a larger one only where weights would grow past 2^500 (in binary32: 2^8).
+template <bool EXACT> struct Met {
     float top = -INFINITY, mine = -__FLT_MAX__;
     int first = INT32_MAX;
-    double sum = 0.0, against = mine;
-    float next[kVec];
-    if (begin + tid * kVec < end) row.load_some(next, begin + tid * kVec, end);
-    for (int i = begin + tid * kVec; i < end; i += THREADS * kVec) {
-        float x[kVec];
-#pragma unroll
-        for (int j = 0; j < kVec; j++) x[j] = next[j];
-        if (i + THREADS * kVec < end) row.load_some(next, i + THREADS * kVec, end);
+    double sum = 0.0, against = -__FLT_MAX__;
+    __device__ __forceinline__ void meet(float (&x)[kVec], int i, const Temper &t, bool greedy)
+    {
         float m = x[0];
 #pragma unroll
         for (int j = 1; j < kVec; j++) m = top_of(m, x[j]);
@@ -143,27 +129,73 @@ template <bool EXACT, int THREADS, bool FP32> __device__ RowPart part_of_row(con
         }
         top = top_of(top, m);
     }
-    float all = top;
+};
+
+// Values [begin, end) of a row, by THREADS threads of which this is number tid: two loads of eight values at a time, then one, then what is
+// left of a load, a value to a thread.
+template <bool EXACT, int THREADS, bool FP32> __device__ __forceinline__ Met<EXACT> meet_all(const Row<FP32> row, int begin, int end, const Temper &t, int tid)
+{
+    const bool greedy = t.c == 0.0;
+    const int whole = begin + ((end - begin) & ~(kVec - 1));
+    Met<EXACT> met;
+    float x[kVec], y[kVec];
+    int i = begin + tid * kVec;
+    for (; i + THREADS * kVec < whole; i += 2 * THREADS * kVec) {
+        row.load(x, i), row.load(y, i + THREADS * kVec);
+        met.meet(x, i, t, greedy), met.meet(y, i + THREADS * kVec, t, greedy);
+    }
+    if (i < whole) {
+        row.load(x, i);
+        met.meet(x, i, t, greedy);
+    }
+    if (whole + tid < end) {
+        x[0] = row[whole + tid];
 #pragma unroll
-    for (int d = 32; d > 0; d /= 2) all = top_of(all, __shfl_xor(all, d));
+        for (int j = 1; j < kVec; j++) x[j] = -INFINITY;
+        met.meet(x, whole + tid, t, greedy);
+    }
+    return met;
+}
+
+// The lanes of a wave together: `all` is the largest over whatever the sum is to stand against.
+__device__ __forceinline__ float wave_top(float x)
+{
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) x = top_of(x, __shfl_xor(x, d));
+    return x;
+}
+template <bool EXACT> __device__ __forceinline__ RowPart wave_part(const Met<EXACT> &met, float all, const Temper &t)
+{
+    RowPart r = {is_finite(all) ? met.sum * exp2(((double)met.mine - (double)all) * t.c) : 0.0, all, met.top == all ? met.first : INT32_MAX};
+#pragma unroll
+    for (int d = 32; d > 0; d /= 2) {
+        r.sum += __shfl_xor(r.sum, d);
+        const int other = __shfl_xor(r.first, d);
+        r.first = other < r.first ? other : r.first;
+    }
+    return r;
+}
+
+// A part of a row by a workgroup.
+template <bool EXACT, int THREADS, bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int begin, int end, const Temper &t)
+{
+    constexpr int WAVES = THREADS / 64;
+    __shared__ float tops[WAVES];
+    __shared__ RowPart sums[WAVES];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const Met<EXACT> met = meet_all<EXACT, THREADS>(row, begin, end, t, tid);
+    float all = wave_top(met.top);
     if (lane == 0) tops[wave] = all;
     __syncthreads();
     all = tops[0];
 #pragma unroll
     for (int w = 1; w < WAVES; w++) all = top_of(all, tops[w]);
-    sum = is_finite(all) ? sum * exp2(((double)mine - (double)all) * t.c) : 0.0;
-    if (top != all) first = INT32_MAX;
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-        sum += __shfl_xor(sum, d);
-        const int other = __shfl_xor(first, d);
-        first = other < first ? other : first;
-    }
-    if (lane == 0) part_sums[wave] = sum, firsts[wave] = first;
+    RowPart r = wave_part(met, all, t);
+    if (lane == 0) sums[wave] = r;
     __syncthreads();
-    RowPart r = {part_sums[0], all, firsts[0]};
+    r = sums[0];
 #pragma unroll
-    for (int w = 1; w < WAVES; w++) r.sum += part_sums[w], r.first = firsts[w] < r.first ? firsts[w] : r.first;
+    for (int w = 1; w < WAVES; w++) r.sum += sums[w].sum, r.first = sums[w].first < r.first ? sums[w].first : r.first;
     __syncthreads();
     return r;
 }
@@ -197,14 +229,24 @@ template <bool EXACT, int THREADS> __device__ __forceinline__ RowPart part_of(co
 {
     return fp32 ? part_of_row<EXACT, THREADS>(Row<true>{at}, begin, end, t) : part_of_row<EXACT, THREADS>(Row<false>{at}, begin, end, t);
 }
+template <bool EXACT> __device__ __forceinline__ RowPart part_by_wave(const uint8_t *at, int fp32, int begin, int end, const Temper &t)
+{
+    const int lane = threadIdx.x & 63;
+    const Met<EXACT> met = fp32 ? meet_all<EXACT, 64>(Row<true>{at}, begin, end, t, lane) : meet_all<EXACT, 64>(Row<false>{at}, begin, end, t, lane);
+    return wave_part(met, wave_top(met.top), t);
+}
 __device__ __forceinline__ int part_end(const VerifyLaunch &a, int k) { return k + 1 < a.parts ? (k + 1) * a.part_len : a.V; }
 
-// A part of a target row, or of the draft's row that belongs to it: the workgroups of the target's rows come first.
-template <bool EXACT> __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
+// A part of a target row, or of the draft's row that belongs to it, for each workgroup, or for each of its waves (ALONE): the target's rows
+// come first.
+template <bool EXACT, bool ALONE> __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
 {
-    const unsigned rows = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
+    const int lane = threadIdx.x & 63;
+    const unsigned n = __builtin_amdgcn_readfirstlane(ALONE ? blockIdx.x * (kVerifyThreads / 64) + threadIdx.x / 64 : blockIdx.x);
+    const unsigned rows = n / (unsigned)a.parts, k = n % (unsigned)a.parts;
     const bool drafted = rows >= (unsigned)a.R;
-    const int t = (int)(drafted ? rows - a.R : rows), lane = threadIdx.x & 63;
+    if (ALONE && rows >= (unsigned)a.R * (a.draft ? 2u : 1u)) return;
+    const int t = (int)(drafted ? rows - a.R : rows);
     const int b = sequence_of_row(a, t, lane);
     if (b >= a.B || t < a.cu[b]) return;
     const Temper temper = temper_of(a, b);
@@ -214,8 +256,9 @@ template <bool EXACT> __global__ __launch_bounds__(kVerifyThreads) void verify_r
         if (t + 1 >= a.cu[b + 1] || d < 0 || temper.c == 0.0) return;
         at = row_at(a.draft, a.draft_stride, a.draft_fp32, d);
     }
-    const RowPart r = part_of<EXACT, kVerifyThreads>(at, drafted ? a.draft_fp32 : a.fp32, k * a.part_len, part_end(a, k), temper);
-    if (threadIdx.x) return;
+    const int begin = k * a.part_len, end = part_end(a, k), fp32 = drafted ? a.draft_fp32 : a.fp32;
+    const RowPart r = ALONE ? part_by_wave<EXACT>(at, fp32, begin, end, temper) : part_of<EXACT, kVerifyThreads>(at, fp32, begin, end, temper);
+    if (ALONE ? lane : threadIdx.x) return;
     // (this many parts of the sequence's rest have been added up: none; see the draws)
     if (!drafted && k == 0 && t == a.cu[b] && a.tickets) a.tickets[b] = 0;
     (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
@@ -233,8 +276,7 @@ __device__ __forceinline__ Whole whole_row(const RowPart *part, int parts, const
 {
     float top = -INFINITY;
     for (int k = lane; k < parts; k += 64) top = top_of(top, part[k].top);
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) top = top_of(top, __shfl_xor(top, d));
+    top = wave_top(top);
     double sum = 0.0;
     int first = INT32_MAX;
     if (is_finite(top))
@@ -672,16 +714,14 @@ __global__ __launch_bounds__(kDrawThreads) void verify_resum_kernel(VerifyLaunch
     if (tid == 0) a.row[(int64_t)row * a.parts + k] = p, a.draft_row[(int64_t)row * a.parts + k] = q;
 }
 
-// How rows are cut into parts: so many that the workgroups of the rows fill the device several times, of whole loads of a workgroup each.
+// Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
 // Whether all sums are binary64 from the start: where that costs less than the two kernels for the draws that binary32 leaves open.
 static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted)
 {
-    const int64_t rows = (int64_t)a.R * (drafted ? 2 : 1), unit = kDrawThreads * kVec;
-    const int64_t units = (a.V + unit - 1) / unit, wanted = rows > 0 ? ((int64_t)num_cus * 32 + rows - 1) / rows : 1;
-    int64_t each = units / (wanted > 1 ? wanted : 1);
-    each = each < 1 ? 1 : each > kMostPart / unit ? kMostPart / unit : each;
-    a.part_len = (int)(each * unit);
-    a.parts = (int)((units + each - 1) / each);
+    const int64_t rows = (int64_t)a.R * (drafted ? 2 : 1);
+    a.part_len = kDrawThreads * kVec;
+    a.parts = (a.V + a.part_len - 1) / a.part_len;
+    a.alone = rows * a.parts >= (int64_t)num_cus * 32;
     a.exact = rows * a.V <= few;
     // The error of a sum of weights as weight32 gives them, in parts of the row's whole sum W: a weight w is off by (3 ln 2 |y| + 2) 2^-24
     // of it and a sum of eight by 3 2^-24; y is against the thread's value, which is at most 8 / c below one it met: |y| is at most 8
@@ -717,16 +757,19 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, voi
 // (a launch has less than 2^32 threads)
 bool verify_fits(const VerifyLaunch &a, bool drafted)
 {
-    return (int64_t)a.R * a.parts * (drafted ? 2 : 1) * kVerifyThreads < (int64_t)1 << 32 && (int64_t)a.B * a.parts * kDrawThreads < (int64_t)1 << 32;
+    return (int64_t)a.R * a.parts * (drafted ? 2 : 1) * 64 < (int64_t)1 << 32 && (int64_t)a.B * a.parts * kDrawThreads < (int64_t)1 << 32;
 }
 
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
 {
-    const dim3 rows((unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u)), seqs((unsigned)a.B), parts((unsigned)a.B * (unsigned)a.parts);
-    const dim3 threads(kDrawThreads);
+    const unsigned rows = (unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u), each = kVerifyThreads / 64;
+    const dim3 seqs((unsigned)a.B), parts((unsigned)a.B * (unsigned)a.parts), threads(kDrawThreads);
     if (a.R > 0) {
-        if (a.exact) hipLaunchKernelGGL(verify_rows_kernel<true>, rows, dim3(kVerifyThreads), 0, s, a);
-        else hipLaunchKernelGGL(verify_rows_kernel<false>, rows, dim3(kVerifyThreads), 0, s, a);
+        const dim3 grid(a.alone ? (rows + each - 1) / each : rows);
+        if (a.exact && a.alone) hipLaunchKernelGGL((verify_rows_kernel<true, true>), grid, dim3(kVerifyThreads), 0, s, a);
+        else if (a.exact) hipLaunchKernelGGL((verify_rows_kernel<true, false>), grid, dim3(kVerifyThreads), 0, s, a);
+        else if (a.alone) hipLaunchKernelGGL((verify_rows_kernel<false, true>), grid, dim3(kVerifyThreads), 0, s, a);
+        else hipLaunchKernelGGL((verify_rows_kernel<false, false>), grid, dim3(kVerifyThreads), 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
