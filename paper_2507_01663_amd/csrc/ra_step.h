@@ -28,6 +28,12 @@ struct RowPart {
     float top;                   // -inf: nothing but -inf; NaN: a NaN among them
     int32_t first;
 };
+// A draw from p - q, or one that binary32 sums did not settle (from: 0: none; see DrawFrom).
+struct OpenDraw {
+    int32_t from, row, x;        // x: the draft that was turned down
+    float p_top, q_top;
+    double p_scale, q_scale;
+};
 struct VerifyLaunch {
     int32_t B, R, V, parts, part_len; // a row's parts, and the values of a part
     int32_t fp32, draft_fp32, total_draft_rows;
@@ -38,9 +44,9 @@ struct VerifyLaunch {
     int32_t *accepted, *out, *next;
     float *logprobs;
     RowPart *row, *draft_row;    // [R][parts]
-    double *rest;                // [R][parts]  sums of max(p - q, 0), of the rows whose draft is turned down
+    double *rest;                // [R][parts]  sums of the parts of the rows that open draws are from
     int32_t *tickets;            // [B]         workgroups that have added up a part
-    int4 *open;                  // [B]         draws that binary32 sums do not settle: {how, row, draft, -}
+    OpenDraw *open;              // [B]
     int32_t alone;               // a part to a wave, not to a workgroup
     int32_t exact;               // all sums in binary64 from the start
     double eps;                  // else: what a sum may be off by, in parts of the row's

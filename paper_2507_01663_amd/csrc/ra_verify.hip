@@ -305,7 +305,8 @@ enum DrawFrom { kNothing, kTop, kRow, kRowWithout, kRest }; // no distribution; 
 struct Draw {
     int from, x, row;            // x: the draft that was turned down, or the greedy token; row: of logits
     const uint8_t *p, *q;        // the rows
-    double p_top, p_scale, q_top, q_scale; // p = weight(l, p_top) * p_scale
+    float p_top, q_top;
+    double p_scale, q_scale;     // p = weight(l, p_top) * p_scale
     Temper t;
 };
 
@@ -508,11 +509,14 @@ __device__ int token_of_part(const VerifyLaunch &a, const Draw &d, int k, double
     return token;
 }
 
-// A part's share in the sum; one below 2^-996 is none (its weights might all have vanished).
-__device__ __forceinline__ double share_of_part(const VerifyLaunch &a, const Draw &d, int k)
+__device__ __forceinline__ double published(const double *at);
+
+// A part's share in the sum, from the row's or (SUMS) as workgroups published it; one below 2^-996 is none (its weights might all have
+// vanished).
+template <bool SUMS> __device__ __forceinline__ double share_of_part(const VerifyLaunch &a, const Draw &d, int k)
 {
     double s;
-    if (d.from == kRest) s = a.rest[(int64_t)d.row * a.parts + k];
+    if (SUMS) s = published(a.rest + (int64_t)d.row * a.parts + k);
     else {
         const RowPart r = a.row[(int64_t)d.row * a.parts + k];
         s = is_finite(r.top) ? r.sum * exp2(((double)r.top - d.p_top) * d.t.c) * d.p_scale : 0.0;
@@ -561,29 +565,30 @@ __device__ double rest32_of_part(const VerifyLaunch &a, const Draw &d, int k)
 
 // The token that v draws, from the parts' sums and then from the part that holds the border.  The whole workgroup.  -1 where the sums
 // may be off by as much as the border is from the nearest token's (`unsure`).
-__device__ int draw(const VerifyLaunch &a, Draw d, double v, double unsure)
+template <bool SUMS> __device__ int draw(const VerifyLaunch &a, Draw d, double v, double unsure)
 {
     __shared__ double border_in_part;
     __shared__ int part;
     const int tid = threadIdx.x, each = (a.parts + kDrawThreads - 1) / kDrawThreads;
+    bool rowwise = false;                                       // (by the row's own sums after all)
     for (;;) {
         // (the part that the draft is in, anew: what is left of it may be far less than a difference of sums could say)
         const int without = d.from == kRowWithout ? d.x / a.part_len : -1;
         double left = without >= 0 ? sum_of_part(a, d, without) : 0.0;
         left = left > 1e-300 ? left : 0.0;
         double mine = 0.0, total;
-        for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) mine += k == without ? left : share_of_part(a, d, k);
+        for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) mine += k == without ? left : d.from == kRow && rowwise ? share_of_part<false>(a, d, k) : share_of_part<SUMS>(a, d, k);
         const double before = sum_before(mine, total), border = v * total;
         const int who = holder(before, mine, border);
         if (who < 0) {                                          // nothing is left of p - q: p
             if (d.from == kRow || unsure > 0.0) return -1;      // (the first: no row of a well-formed call)
-            d.from = kRow;
+            d.from = kRow, rowwise = true;
             continue;
         }
         if (tid == who) {
             double run = before;
             for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) {
-                const double s = k == without ? left : share_of_part(a, d, k);
+                const double s = k == without ? left : d.from == kRow && rowwise ? share_of_part<false>(a, d, k) : share_of_part<SUMS>(a, d, k);
                 if (!(s > 0.0)) continue;
                 part = k, border_in_part = border - run;
                 run += s;
@@ -622,12 +627,19 @@ __device__ __forceinline__ void finish(const VerifyLaunch &a, int b, int begin, 
     }
 }
 
-// Whether this workgroup is the last of `all` to come here for sequence b, on top of `came` before.  Its sums, written by its first
-// thread, are there for the last one.
+// A sum for whichever workgroup draws, and whether that is this one: the last of `all` to come here for sequence b, on top of `came`
+// before.  The sum goes past the caches to where every die sees it, is waited for, and only then counts; it is read the same way.
+// (A release and an acquire would write back and drop the die's whole cache for these eight bytes: 0.1 ms for 1 700 workgroups.)
+__device__ __forceinline__ void publish(double *at, double x)
+{
+    __hip_atomic_store(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+}
+__device__ __forceinline__ double published(const double *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ bool last_to_arrive(const VerifyLaunch &a, int b, int came, int all)
 {
     __shared__ int arrived;
-    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(a.tickets + b, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(a.tickets + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
     return arrived == came + all - 1;
 }
@@ -642,7 +654,7 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_dra
         if (tid == 0) {
             a.accepted[b] = 0;
             if (a.next) a.next[b] = -1;
-            if (a.open) a.open[b] = make_int4(kNothing, 0, 0, 0);
+            if (a.open) a.open[b].from = kNothing;
         }
         return;
     }
@@ -651,24 +663,19 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_dra
     int token = -1;
     if (d.from == kTop) token = d.x;
     // (prefixes and totals are off by eps of the row each)
-    else if (d.from == kRow || d.from == kRowWithout) token = draw(a, d, number_of(a, b), EXACT ? 0.0 : 3.0 * a.eps);
+    else if (d.from == kRow || d.from == kRowWithout) token = draw<false>(a, d, number_of(a, b), EXACT ? 0.0 : 3.0 * a.eps);
     const bool left_open = d.from == kRest || (!EXACT && token < 0 && d.from != kNothing);
-    if (a.open && tid == 0) a.open[b] = left_open ? make_int4(d.from, d.row, d.x, 0) : make_int4(kNothing, 0, 0, 0);
+    if (a.open && tid == 0) a.open[b] = {left_open ? d.from : kNothing, d.row, d.x, d.p_top, d.q_top, d.p_scale, d.q_scale};
     if (!left_open) finish(a, b, begin, end, d, token);
 }
 
-// What is known of an open draw.
-__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, int b, int4 o, const Temper &t)
+// An open draw as the draws' kernel left it.
+__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, int b, const OpenDraw &o, const Temper &t)
 {
-    const int lane = threadIdx.x & 63, row = o.y;
     Draw d = {};
-    d.from = o.x, d.row = row, d.x = o.z, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, row);
-    const Whole p = whole_row(a.row + (int64_t)row * a.parts, a.parts, t, lane);
-    d.p_top = p.top, d.p_scale = 1.0 / p.sum;
-    if (o.x == kRest) {
-        const Whole q = whole_row(a.draft_row + (int64_t)row * a.parts, a.parts, t, lane);
-        d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, draft_row_of(a, b, row)), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
-    }
+    d.from = o.from, d.row = o.row, d.x = o.x, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, o.row);
+    d.p_top = o.p_top, d.p_scale = o.p_scale, d.q_top = o.q_top, d.q_scale = o.q_scale;
+    if (o.from == kRest) d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, draft_row_of(a, b, o.row));
     return d;
 }
 
@@ -677,27 +684,31 @@ __device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, int b, int4 o, 
 template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch a, int came)
 {
     const int tid = threadIdx.x, b = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
-    const int4 o = a.open[b];
-    if (o.x == kNothing) return;
+    const OpenDraw o = a.open[b];
+    if (o.from == kNothing) return;
     const Temper t = temper_of(a, b);
     double unsure = 0.0;
-    Draw d;
-    if (EXACT || o.x == kRest) {
-        d = open_draw(a, b, o, t);
+    Draw d = open_draw(a, b, o, t);
+    double *const rest = a.rest + (int64_t)o.row * a.parts;
+    if (d.from == kRest) {
+        if (EXACT && came) {                                    // (their sums have been made anew)
+            const int lane = tid & 63;
+            const Whole p = whole_row(a.row + (int64_t)o.row * a.parts, a.parts, t, lane), q = whole_row(a.draft_row + (int64_t)o.row * a.parts, a.parts, t, lane);
+            d.p_top = p.top, d.p_scale = 1.0 / p.sum, d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+        }
         const double sum = EXACT ? sum_of_part(a, d, k) : rest32_of_part(a, d, k);
-        if (tid == 0) a.rest[(int64_t)o.y * a.parts + k] = sum;
+        if (tid == 0) publish(rest + k, sum);
         // (p and q: twice eps each, by their weights and by their scales; so for a prefix and for the whole)
         if (!EXACT) unsure = 10.0 * a.eps;
-        if (!last_to_arrive(a, b, came, a.parts)) return;
     } else {
-        const RowPart p = part_of<true, kDrawThreads>(row_at(a.logits, a.stride, a.fp32, o.y), a.fp32, k * a.part_len, part_end(a, k), t);
-        if (tid == 0) a.row[(int64_t)o.y * a.parts + k] = p;
-        if (!last_to_arrive(a, b, came, a.parts)) return;
-        d = open_draw(a, b, o, t);
+        const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, k * a.part_len, part_end(a, k), t);
+        // (against the row's largest, which is that of the sums at hand)
+        if (tid == 0) publish(rest + k, is_finite(p.top) ? p.sum * exp2(((double)p.top - d.p_top) * t.c) * d.p_scale : 0.0);
     }
-    const int token = draw(a, d, number_of(a, b), unsure);
+    if (!last_to_arrive(a, b, came, a.parts)) return;
+    const int token = draw<true>(a, d, number_of(a, b), unsure);
     if (unsure > 0.0 && token < 0) return;
-    if (!EXACT && tid == 0) a.open[b].x = kNothing;             // (all of its workgroups have read it)
+    if (!EXACT && tid == 0) a.open[b].from = kNothing;          // (all of its workgroups have read it)
     finish(a, b, a.cu[b], a.cu[b + 1], d, token);
 }
 
@@ -705,13 +716,14 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_res
 __global__ __launch_bounds__(kDrawThreads) void verify_resum_kernel(VerifyLaunch a)
 {
     const int tid = threadIdx.x, b = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
-    const int4 o = a.open[b];
-    if (o.x != kRest) return;
+    const OpenDraw o = a.open[b];
+    if (o.from != kRest) return;
     const Temper t = temper_of(a, b);
-    const int row = o.y, begin = k * a.part_len, end = part_end(a, k);
-    const RowPart p = part_of<true, kDrawThreads>(row_at(a.logits, a.stride, a.fp32, row), a.fp32, begin, end, t);
-    const RowPart q = part_of<true, kDrawThreads>(row_at(a.draft, a.draft_stride, a.draft_fp32, draft_row_of(a, b, row)), a.draft_fp32, begin, end, t);
-    if (tid == 0) a.row[(int64_t)row * a.parts + k] = p, a.draft_row[(int64_t)row * a.parts + k] = q;
+    const Draw d = open_draw(a, b, o, t);
+    const int begin = k * a.part_len, end = part_end(a, k);
+    const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, begin, end, t);
+    const RowPart q = part_of<true, kDrawThreads>(d.q, a.draft_fp32, begin, end, t);
+    if (tid == 0) a.row[(int64_t)o.row * a.parts + k] = p, a.draft_row[(int64_t)o.row * a.parts + k] = q;
 }
 
 // Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
@@ -743,13 +755,11 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, voi
     };
     const size_t parts = (size_t)a.R * a.parts;
     a.row = (RowPart *)take(parts * sizeof(RowPart));
-    if (drafted) {
-        a.draft_row = (RowPart *)take(parts * sizeof(RowPart));
-        a.rest = (double *)take(parts * sizeof(double));
-    }
+    if (drafted) a.draft_row = (RowPart *)take(parts * sizeof(RowPart));
     if (drafted || !a.exact) {
+        a.rest = (double *)take(parts * sizeof(double));
         a.tickets = (int32_t *)take((size_t)a.B * 4);
-        a.open = (int4 *)take((size_t)a.B * sizeof(int4));
+        a.open = (OpenDraw *)take((size_t)a.B * sizeof(OpenDraw));
     }
     return at;
 }
