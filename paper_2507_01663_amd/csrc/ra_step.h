@@ -28,10 +28,11 @@ struct RowPart {
     float top;                   // -inf: nothing but -inf; NaN: a NaN among them
     int32_t first;
 };
-// A draw from p - q, or one that binary32 sums did not settle (from: 0: none; see DrawFrom).
+// A draw from p - q, or one that binary32 sums did not settle.
 struct OpenDraw {
-    int32_t from, row, x;        // x: the draft that was turned down
-    float p_top, q_top;
+    int32_t b, from, row, x;     // from: see DrawFrom; x: the draft that was turned down
+    int32_t q_row, arrived;      // row of the draft model's logits; workgroups that have added up their part
+    float T, p_top, q_top;
     double p_scale, q_scale;
 };
 struct VerifyLaunch {
@@ -45,8 +46,9 @@ struct VerifyLaunch {
     float *logprobs;
     RowPart *row, *draft_row;    // [R][parts]
     double *rest;                // [R][parts]  sums of the parts of the rows that open draws are from
-    int32_t *tickets;            // [B]         workgroups that have added up a part
-    OpenDraw *open;              // [B]
+    int32_t *opened;             // [2]         draws on either list
+    OpenDraw *open, *still_open; // [B]
+    int32_t num_cus;
     int32_t alone;               // a part to a wave, not to a workgroup
     int32_t exact;               // all sums in binary64 from the start
     double eps;                  // else: what a sum may be off by, in parts of the row's

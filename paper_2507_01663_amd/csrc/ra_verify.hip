@@ -19,15 +19,14 @@ struct Temper {
     double low;                  // differences at or below this weigh nothing: 2^-1100
     float cf;
 };
-__device__ __forceinline__ Temper temper_of(const VerifyLaunch &a, int b)
+__device__ __forceinline__ Temper temper_from(float T)
 {
-    float T = a.temperature ? a.temperature[b] : 1.f;
-    Temper t;
     if (!(T > 0.f)) return {0.0, 0.0, 0.f};
     T = T < 1e-30f ? 1e-30f : T > 1e30f ? 1e30f : T;
-    t.c = kLog2e / (double)T, t.low = -1100.0 / t.c, t.cf = (float)t.c;
-    return t;
+    const double c = kLog2e / (double)T;
+    return {c, -1100.0 / kLog2e * (double)T, (float)c};
 }
+__device__ __forceinline__ Temper temper_of(const VerifyLaunch &a, int b) { return temper_from(a.temperature ? a.temperature[b] : 1.f); }
 
 // 2^x for x = d * c >= -1100, right to 2^-39: to the nearest whole number (by an addition that leaves it in the low bits), and for the
 // rest the polynomial of degree eight through 2^x at nine Chebyshev nodes of [-1/2, 1/2], with the constant term at 1.
@@ -63,6 +62,65 @@ __device__ __forceinline__ float sum_of_eight(const float (&x)[kVec])
 
 // The larger of the two, or NaN if one is.
 __device__ __forceinline__ float top_of(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// What a sum against `from` has to be multiplied by to stand against `to`, which is not smaller.
+__device__ __forceinline__ double rescale(float from, float to, const Temper &t)
+{
+    return power(__builtin_fmax((double)from - (double)to, t.low), t.c);
+}
+
+// Over the lanes of a wave by steps inside the vector unit: rows of sixteen lanes, then the last lane of a row to the next, then of the
+// lower half to the upper.
+template <int CTRL, int ROWS> __device__ __forceinline__ int from_lane(int x, int none) { return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xf, false); }
+template <int CTRL, int ROWS> __device__ __forceinline__ double from_lane(double x)
+{
+    const int2 w = {__double2loint(x), __double2hiint(x)};
+    return __hiloint2double(from_lane<CTRL, ROWS>(w.y, 0), from_lane<CTRL, ROWS>(w.x, 0));
+}
+__device__ __forceinline__ double wave_scan(double x)           // the sum up to this lane, itself included
+{
+    x += from_lane<0x111, 0xf>(x);
+    x += from_lane<0x112, 0xf>(x);
+    x += from_lane<0x114, 0xf>(x);
+    x += from_lane<0x118, 0xf>(x);
+    x += from_lane<0x142, 0xa>(x);
+    x += from_lane<0x143, 0xc>(x);
+    return x;
+}
+__device__ __forceinline__ double last_lane(double x)
+{
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), 63), __builtin_amdgcn_readlane(__double2loint(x), 63));
+}
+__device__ __forceinline__ double wave_sum(double x) { return last_lane(wave_scan(x)); }
+template <int CTRL, int ROWS> __device__ __forceinline__ float top_from_lane(float x)
+{
+    return top_of(x, __int_as_float(from_lane<CTRL, ROWS>(__float_as_int(x), __float_as_int(-INFINITY))));
+}
+__device__ __forceinline__ float wave_top(float x)
+{
+    x = top_from_lane<0x111, 0xf>(x);
+    x = top_from_lane<0x112, 0xf>(x);
+    x = top_from_lane<0x114, 0xf>(x);
+    x = top_from_lane<0x118, 0xf>(x);
+    x = top_from_lane<0x142, 0xa>(x);
+    x = top_from_lane<0x143, 0xc>(x);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(x), 63));
+}
+template <int CTRL, int ROWS> __device__ __forceinline__ int less_from_lane(int x)
+{
+    const int o = from_lane<CTRL, ROWS>(x, INT32_MAX);
+    return o < x ? o : x;
+}
+__device__ __forceinline__ int wave_least(int x)
+{
+    x = less_from_lane<0x111, 0xf>(x);
+    x = less_from_lane<0x112, 0xf>(x);
+    x = less_from_lane<0x114, 0xf>(x);
+    x = less_from_lane<0x118, 0xf>(x);
+    x = less_from_lane<0x142, 0xa>(x);
+    x = less_from_lane<0x143, 0xc>(x);
+    return __builtin_amdgcn_readlane(x, 63);
+}
 
 template <bool FP32> struct Row {
     const uint8_t *at;
@@ -115,7 +173,7 @@ template <bool EXACT> struct Met {
                     if (x[j] == m) first = i + j;
         } else {
             if ((m - mine) * t.cf > (EXACT ? 500.f : 8.f)) {    // (also the first time)
-                sum *= exp2(((double)mine - (double)m) * t.c);
+                sum *= rescale(mine, m, t);
                 mine = m, against = m;
             }
             if constexpr (EXACT) {
@@ -158,21 +216,11 @@ template <bool EXACT, int THREADS, bool FP32> __device__ __forceinline__ Met<EXA
 }
 
 // The lanes of a wave together: `all` is the largest over whatever the sum is to stand against.
-__device__ __forceinline__ float wave_top(float x)
-{
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) x = top_of(x, __shfl_xor(x, d));
-    return x;
-}
 template <bool EXACT> __device__ __forceinline__ RowPart wave_part(const Met<EXACT> &met, float all, const Temper &t)
 {
-    RowPart r = {is_finite(all) ? met.sum * exp2(((double)met.mine - (double)all) * t.c) : 0.0, all, met.top == all ? met.first : INT32_MAX};
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-        r.sum += __shfl_xor(r.sum, d);
-        const int other = __shfl_xor(r.first, d);
-        r.first = other < r.first ? other : r.first;
-    }
+    RowPart r = {0.0, all, INT32_MAX};
+    if (t.c == 0.0) r.first = wave_least(met.top == all ? met.first : INT32_MAX);
+    else if (is_finite(all)) r.sum = wave_sum(met.sum * rescale(met.mine, all, t));
     return r;
 }
 
@@ -242,6 +290,7 @@ __device__ __forceinline__ int part_end(const VerifyLaunch &a, int k) { return k
 template <bool EXACT, bool ALONE> __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
 {
     const int lane = threadIdx.x & 63;
+    if (blockIdx.x == 0 && threadIdx.x < 2 && a.opened) a.opened[threadIdx.x] = 0;
     const unsigned n = __builtin_amdgcn_readfirstlane(ALONE ? blockIdx.x * (kVerifyThreads / 64) + threadIdx.x / 64 : blockIdx.x);
     const unsigned rows = n / (unsigned)a.parts, k = n % (unsigned)a.parts;
     const bool drafted = rows >= (unsigned)a.R;
@@ -259,8 +308,6 @@ template <bool EXACT, bool ALONE> __global__ __launch_bounds__(kVerifyThreads) v
     const int begin = k * a.part_len, end = part_end(a, k), fp32 = drafted ? a.draft_fp32 : a.fp32;
     const RowPart r = ALONE ? part_by_wave<EXACT>(at, fp32, begin, end, temper) : part_of<EXACT, kVerifyThreads>(at, fp32, begin, end, temper);
     if (ALONE ? lane : threadIdx.x) return;
-    // (this many parts of the sequence's rest have been added up: none; see the draws)
-    if (!drafted && k == 0 && t == a.cu[b] && a.tickets) a.tickets[b] = 0;
     (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
 }
 
@@ -274,24 +321,23 @@ struct Whole {
 };
 __device__ __forceinline__ Whole whole_row(const RowPart *part, int parts, const Temper &t, int lane)
 {
-    float top = -INFINITY;
-    for (int k = lane; k < parts; k += 64) top = top_of(top, part[k].top);
+    RowPart r = {0.0, -INFINITY, INT32_MAX};
+    if (lane < parts) r = part[lane];
+    float top = r.top;
+    for (int k = lane + 64; k < parts; k += 64) top = top_of(top, part[k].top);
     top = wave_top(top);
-    double sum = 0.0;
-    int first = INT32_MAX;
-    if (is_finite(top))
-        for (int k = lane; k < parts; k += 64) {
-            const RowPart r = part[k];
-            if (r.top == top && r.first < first) first = r.first;
-            if (is_finite(r.top)) sum += r.sum * exp2(((double)r.top - (double)top) * t.c);
-        }
-#pragma unroll
-    for (int d = 32; d > 0; d /= 2) {
-        sum += __shfl_xor(sum, d);
-        const int other = __shfl_xor(first, d);
-        first = other < first ? other : first;
+    Whole w = {0.0, top, INT32_MAX};
+    if (!is_finite(top)) return w;
+    for (int k = lane;;) {
+        if (t.c == 0.0) w.first = r.top == top && r.first < w.first ? r.first : w.first;
+        else if (is_finite(r.top)) w.sum += r.sum * rescale(r.top, top, t);
+        k += 64;
+        if (k >= parts) break;
+        r = part[k];
     }
-    return {sum, top, first};
+    if (t.c == 0.0) w.first = wave_least(w.first);
+    else w.sum = wave_sum(w.sum);
+    return w;
 }
 
 __device__ __forceinline__ float logit_at(const void *logits, int64_t stride, int fp32, int64_t t, int i)
@@ -304,6 +350,7 @@ __device__ __forceinline__ float logit_at(const void *logits, int64_t stride, in
 enum DrawFrom { kNothing, kTop, kRow, kRowWithout, kRest }; // no distribution; greedy; p; p without the draft; max(p - q, 0)
 struct Draw {
     int from, x, row;            // x: the draft that was turned down, or the greedy token; row: of logits
+    int q_row;                   // ... of draft_logits
     const uint8_t *p, *q;        // the rows
     float p_top, q_top;
     double p_scale, q_scale;     // p = weight(l, p_top) * p_scale
@@ -337,7 +384,7 @@ __device__ __forceinline__ Draw judge(const VerifyLaunch &a, int b, int row, int
     else {
         const int64_t r = draft_row_of(a, b, row);
         if (r < 0 || !is_finite(q.top)) return d;
-        d.from = kRest, d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, r), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+        d.from = kRest, d.q_row = (int)r, d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, r), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
         against *= weight(logit_at(a.draft, a.draft_stride, a.draft_fp32, r, x), q.top, t) / q.sum;
     }
     says = against < px ? kStays : kGoes;
@@ -403,10 +450,10 @@ template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch 
 
 // ---- a token from its weights ---------------------------------------------------------------------------
 
-// Weights of values i .. i + 7 (those at or past end are 0) in the sum that the token is drawn by.
-template <bool FP32, bool QFP32> __device__ __forceinline__ void weights(double (&w)[kVec], const Draw &d, int i, int end)
+// Weights of values i .. i + 7 (those at or past end are 0) in the sum that the token is drawn by, and the target's logits.
+template <bool FP32, bool QFP32> __device__ __forceinline__ void weights(double (&w)[kVec], float (&x)[kVec], const Draw &d, int i, int end)
 {
-    float x[kVec], y[kVec];
+    float y[kVec];
     Row<FP32>{d.p}.load_some(x, i, end);
     if (d.from == kRest) {
         Row<QFP32>{d.q}.load_some(y, i, end);
@@ -422,88 +469,90 @@ template <bool FP32, bool QFP32> __device__ __forceinline__ void weights(double 
         for (int j = 0; j < kVec; j++) w[j] = d.from == kRowWithout && i + j == d.x ? 0.0 : weight(x[j], d.p_top, d.t) * d.p_scale;
     }
 }
-__device__ __forceinline__ void weights_at(double (&w)[kVec], const VerifyLaunch &a, const Draw &d, int i, int end)
+__device__ __forceinline__ void weights_at(double (&w)[kVec], float (&x)[kVec], const VerifyLaunch &a, const Draw &d, int i, int end)
 {
-    if (a.fp32) a.draft_fp32 ? weights<true, true>(w, d, i, end) : weights<true, false>(w, d, i, end);
-    else a.draft_fp32 ? weights<false, true>(w, d, i, end) : weights<false, false>(w, d, i, end);
+    if (a.fp32) a.draft_fp32 ? weights<true, true>(w, x, d, i, end) : weights<true, false>(w, x, d, i, end);
+    else a.draft_fp32 ? weights<false, true>(w, x, d, i, end) : weights<false, false>(w, x, d, i, end);
+}
+// This thread's eight weights of part k, and their sum.
+__device__ __forceinline__ double weights_of_part(double (&w)[kVec], float (&x)[kVec], const VerifyLaunch &a, const Draw &d, int k)
+{
+    weights_at(w, x, a, d, k * a.part_len + threadIdx.x * kVec, part_end(a, k));
+    double sum = 0.0;
+#pragma unroll
+    for (int j = 0; j < kVec; j++) sum += w[j];
+    return sum;
 }
 
-// The sum of x over the workgroup's threads before this one; total: over all.
-__device__ __forceinline__ double sum_before(double x, double &total)
+struct DrawLds {
+    double sums[kDrawWaves];
+    int over[kDrawWaves], some[kDrawWaves];
+};
+__device__ __forceinline__ double block_sum(double x, DrawLds &lds)
 {
-    __shared__ double sums[kDrawWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    double s = x;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double o = __shfl_up(s, d);
-        if (lane >= d) s += o;
-    }
-    if (lane == 63) sums[wave] = s;
+    x = wave_sum(x);
     __syncthreads();
-    double before = 0.0;
-    total = 0.0;
+    if ((threadIdx.x & 63) == 0) lds.sums[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double total = 0.0;
+#pragma unroll
+    for (int w = 0; w < kDrawWaves; w++) total += lds.sums[w];
+    return total;
+}
+// The thread whose share (mine) of a running sum over the workgroup holds the border: the first that the sum with it exceeds it in, or the
+// last with any share where rounding (or a number of 1) leaves none; -1: no thread has any.  border: of the sum; v given: v times
+// the sum of all.  before: the sum of the threads before this one.
+__device__ __forceinline__ int holder(double mine, double &before, double &border, const double *v, DrawLds &lds)
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const double scan = wave_scan(mine);
+    __syncthreads();
+    if (lane == 63) lds.sums[wave] = scan;
+    __syncthreads();
+    before = 0.0;
+    double total = 0.0;
 #pragma unroll
     for (int w = 0; w < kDrawWaves; w++) {
-        if (w < wave) before += sums[w];
-        total += sums[w];
+        if (w == wave) before = total;
+        total += lds.sums[w];
     }
-    __syncthreads();
-    const double up = __shfl_up(s, 1);
-    return before + (lane ? up : 0.0);
-}
-
-// The thread whose share of a running sum holds the border: the first that the sum with it exceeds it in, or the last with any
-// share where rounding (or a number of 1) leaves none; -1: no thread has any.
-__device__ __forceinline__ int holder(double before, double mine, double border)
-{
-    __shared__ int over[kDrawWaves], some[kDrawWaves];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const uint64_t any = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && before + mine > border);
-    if (lane == 0) over[wave] = past ? wave * 64 + __builtin_ctzll(past) : INT32_MAX, some[wave] = any ? wave * 64 + 63 - __builtin_clzll(any) : -1;
+    if (v) border = *v * total;
+    const uint64_t any = __ballot(mine > 0.0), past = __ballot(mine > 0.0 && before + scan > border);
+    const double up = from_lane<0x138, 0xf>(scan);              // (the lane before; none for the first)
+    before += up;
+    if (lane == 0) lds.over[wave] = past ? wave * 64 + __builtin_ctzll(past) : INT32_MAX, lds.some[wave] = any ? wave * 64 + 63 - __builtin_clzll(any) : -1;
     __syncthreads();
     int first = INT32_MAX, last = -1;
 #pragma unroll
-    for (int w = 0; w < kDrawWaves; w++) first = over[w] < first ? over[w] : first, last = some[w] > last ? some[w] : last;
-    __syncthreads();
+    for (int w = 0; w < kDrawWaves; w++) first = lds.over[w] < first ? lds.over[w] : first, last = lds.some[w] > last ? lds.some[w] : last;
     return first < INT32_MAX ? first : last;
 }
 
-// The first value of part k at which the running sum of the part's weights passes the border; -1 where the sum is within `unsure` of
+// A token that was drawn, and its logit; -1: none, or the draw stays open.
+struct Token {
+    int id;
+    float logit;
+};
+// The first value of part k at which the running sum of the part's weights passes the border; none where the sum is within `unsure` of
 // the border at it or before it.
-__device__ int token_of_part(const VerifyLaunch &a, const Draw &d, int k, double border, double unsure)
+__device__ Token token_of_part(const VerifyLaunch &a, const Draw &d, int k, double border, double unsure, DrawLds &lds)
 {
-    __shared__ int token;
-    __shared__ double from;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int begin = k * a.part_len, end = part_end(a, k);
-    const int len = a.part_len / kDrawThreads;                  // a multiple of 8, at most 64
-    const int mine = begin + tid * len, stop = mine + len < end ? mine + len : end;
-    double sum = 0.0, total, w[kVec];
-    for (int i = mine; i < stop; i += kVec) {
-        weights_at(w, a, d, i, stop);
+    __shared__ Token token;
+    const int tid = threadIdx.x;
+    double w[kVec], before;
+    float x[kVec];
+    const double sum = weights_of_part(w, x, a, d, k);
+    const int who = holder(sum, before, border, nullptr, lds);
+    if (who < 0) return {-1, 0.f};
+    if (tid == who) {
+        double run = before, under = before;
+        int which = -1;
+        float logit = 0.f;
 #pragma unroll
-        for (int j = 0; j < kVec; j++) sum += w[j];
-    }
-    const double before = sum_before(sum, total);
-    const int who = holder(before, sum, border);
-    if (who < 0) return -1;
-    if (tid == who) from = before;
-    __syncthreads();
-    if (tid < 64) {                                             // that thread's stretch, a value to a lane
-        const int at = begin + who * len, i = at + lane;
-        weights_at(w, a, d, i, i < end && lane < len ? i + 1 : i);
-        double run = w[0];
-#pragma unroll
-        for (int s = 1; s < 64; s *= 2) {
-            const double o = __shfl_up(run, s);
-            if (lane >= s) run += o;
-        }
-        const uint64_t any = __ballot(w[0] > 0.0), past = __ballot(w[0] > 0.0 && from + run > border);
-        const int which = past ? __builtin_ctzll(past) : any ? 63 - __builtin_clzll(any) : -1;
-        const bool near = from + run - border <= unsure || border - (from + run - w[0]) <= unsure;
-        const bool told = unsure == 0.0 || !(__ballot(near) >> (which & 63) & 1);
-        if (lane == 0) token = which >= 0 && told ? at + which : -1;
+        for (int j = 0; j < kVec; j++)
+            if (w[j] > 0.0 && (which < 0 || run <= border)) which = j, logit = x[j], under = run, run += w[j];
+        const bool near = run - border <= unsure || border - under <= unsure;
+        token = {which >= 0 && (unsure == 0.0 || !near) ? k * a.part_len + tid * kVec + which : -1, logit};
     }
     __syncthreads();
     return token;
@@ -519,76 +568,60 @@ template <bool SUMS> __device__ __forceinline__ double share_of_part(const Verif
     if (SUMS) s = published(a.rest + (int64_t)d.row * a.parts + k);
     else {
         const RowPart r = a.row[(int64_t)d.row * a.parts + k];
-        s = is_finite(r.top) ? r.sum * exp2(((double)r.top - d.p_top) * d.t.c) * d.p_scale : 0.0;
+        s = is_finite(r.top) ? r.sum * rescale(r.top, d.p_top, d.t) * d.p_scale : 0.0;
     }
     return s > 1e-300 ? s : 0.0;
 }
 
-__device__ double sum_of_part(const VerifyLaunch &a, const Draw &d, int k)
+// This thread's share of what is left of part k of p - q, in binary32 products.
+template <bool FP32, bool QFP32> __device__ __forceinline__ double rest32(const Draw &d, int i, int end)
 {
-    const int begin = k * a.part_len, end = part_end(a, k);
-    double sum = 0.0, total, w[kVec];
-    for (int i = begin + threadIdx.x * kVec; i < end; i += kDrawThreads * kVec) {
-        weights_at(w, a, d, i, end);
-#pragma unroll
-        for (int j = 0; j < kVec; j++) sum += w[j];
-    }
-    (void)sum_before(sum, total);
-    return total;
-}
-
-// What is left of a part of p - q, in binary32 products.
-template <bool FP32, bool QFP32> __device__ __forceinline__ double rest32(const Draw &d, int begin, int end)
-{
-    const Row<FP32> p = {d.p};
-    const Row<QFP32> q = {d.q};
-    const float p_top = (float)d.p_top, q_top = (float)d.q_top, p_scale = (float)d.p_scale, q_scale = (float)d.q_scale;
-    double sum = 0.0;
+    const float p_scale = (float)d.p_scale, q_scale = (float)d.q_scale;
     float x[kVec], y[kVec];
-    for (int i = begin + threadIdx.x * kVec; i < end; i += kDrawThreads * kVec) {
-        p.load_some(x, i, end), q.load_some(y, i, end);
+    Row<FP32>{d.p}.load_some(x, i, end), Row<QFP32>{d.q}.load_some(y, i, end);
 #pragma unroll
-        for (int j = 0; j < kVec; j++) x[j] = fmaxf(weight32(x[j], p_top, d.t) * p_scale - weight32(y[j], q_top, d.t) * q_scale, 0.f);
-        sum += (double)sum_of_eight(x);
-    }
-    return sum;
+    for (int j = 0; j < kVec; j++) x[j] = fmaxf(weight32(x[j], d.p_top, d.t) * p_scale - weight32(y[j], d.q_top, d.t) * q_scale, 0.f);
+    return (double)sum_of_eight(x);
 }
-__device__ double rest32_of_part(const VerifyLaunch &a, const Draw &d, int k)
+__device__ __forceinline__ double rest32_of_part(const VerifyLaunch &a, const Draw &d, int k)
 {
-    const int begin = k * a.part_len, end = part_end(a, k);
-    double sum, total;
-    if (a.fp32) sum = a.draft_fp32 ? rest32<true, true>(d, begin, end) : rest32<true, false>(d, begin, end);
-    else sum = a.draft_fp32 ? rest32<false, true>(d, begin, end) : rest32<false, false>(d, begin, end);
-    (void)sum_before(sum, total);
-    return total;
+    const int i = k * a.part_len + threadIdx.x * kVec, end = part_end(a, k);
+    if (a.fp32) return a.draft_fp32 ? rest32<true, true>(d, i, end) : rest32<true, false>(d, i, end);
+    return a.draft_fp32 ? rest32<false, true>(d, i, end) : rest32<false, false>(d, i, end);
 }
 
-// The token that v draws, from the parts' sums and then from the part that holds the border.  The whole workgroup.  -1 where the sums
+// The token that v draws, from the parts' sums and then from the part that holds the border.  The whole workgroup.  None where the sums
 // may be off by as much as the border is from the nearest token's (`unsure`).
-template <bool SUMS> __device__ int draw(const VerifyLaunch &a, Draw d, double v, double unsure)
+template <bool SUMS> __device__ Token draw(const VerifyLaunch &a, Draw d, double v, double unsure)
 {
+    __shared__ DrawLds lds;
     __shared__ double border_in_part;
     __shared__ int part;
     const int tid = threadIdx.x, each = (a.parts + kDrawThreads - 1) / kDrawThreads;
-    bool rowwise = false;                                       // (by the row's own sums after all)
+    bool own = !SUMS;                                           // by the row's own sums
     for (;;) {
         // (the part that the draft is in, anew: what is left of it may be far less than a difference of sums could say)
         const int without = d.from == kRowWithout ? d.x / a.part_len : -1;
-        double left = without >= 0 ? sum_of_part(a, d, without) : 0.0;
-        left = left > 1e-300 ? left : 0.0;
-        double mine = 0.0, total;
-        for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) mine += k == without ? left : d.from == kRow && rowwise ? share_of_part<false>(a, d, k) : share_of_part<SUMS>(a, d, k);
-        const double before = sum_before(mine, total), border = v * total;
-        const int who = holder(before, mine, border);
+        double left = 0.0;
+        if (without >= 0) {
+            double w[kVec];
+            float x[kVec];
+            left = block_sum(weights_of_part(w, x, a, d, without), lds);
+            left = left > 1e-300 ? left : 0.0;
+        }
+        auto share = [&](int k) { return k == without ? left : own ? share_of_part<false>(a, d, k) : share_of_part<SUMS>(a, d, k); };
+        double mine = 0.0, before, border;
+        for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) mine += share(k);
+        const int who = holder(mine, before, border, &v, lds);
         if (who < 0) {                                          // nothing is left of p - q: p
-            if (d.from == kRow || unsure > 0.0) return -1;      // (the first: no row of a well-formed call)
-            d.from = kRow, rowwise = true;
+            if (d.from == kRow || unsure > 0.0) return {-1, 0.f}; // (the first: no row of a well-formed call)
+            d.from = kRow, own = true;
             continue;
         }
         if (tid == who) {
             double run = before;
             for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) {
-                const double s = k == without ? left : d.from == kRow && rowwise ? share_of_part<false>(a, d, k) : share_of_part<SUMS>(a, d, k);
+                const double s = each == 1 ? mine : share(k);
                 if (!(s > 0.0)) continue;
                 part = k, border_in_part = border - run;
                 run += s;
@@ -596,7 +629,7 @@ template <bool SUMS> __device__ int draw(const VerifyLaunch &a, Draw d, double v
             }
         }
         __syncthreads();
-        return token_of_part(a, d, part, border_in_part, unsure);
+        return token_of_part(a, d, part, border_in_part, unsure, lds);
     }
 }
 
@@ -607,17 +640,16 @@ __device__ __forceinline__ double number_of(const VerifyLaunch &a, int b)
 }
 
 // What comes out of sequence b, but for the drafts that stay.  The whole workgroup.
-__device__ __forceinline__ void finish(const VerifyLaunch &a, int b, int begin, int end, const Draw &d, int token)
+__device__ __forceinline__ void finish(const VerifyLaunch &a, int b, int begin, int end, const Draw &d, Token token)
 {
     const int tid = threadIdx.x;
     if (tid == 0) {
         a.accepted[b] = d.row - begin;
-        if (a.next) a.next[b] = token;
-        a.out[d.row] = token;
+        if (a.next) a.next[b] = token.id;
+        a.out[d.row] = token.id;
         if (a.logprobs) {
             double lp = d.from == kTop ? 0.0 : __builtin_nan("");
-            if (d.from != kTop && token >= 0)
-                lp = ((double)logit_at(a.logits, a.stride, a.fp32, d.row, token) - d.p_top) * d.t.c / kLog2e + log(d.p_scale);
+            if (d.from != kTop && token.id >= 0) lp = ((double)token.logit - (double)d.p_top) * d.t.c / kLog2e + log(d.p_scale);
             a.logprobs[d.row] = (float)lp;
         }
     }
@@ -627,21 +659,28 @@ __device__ __forceinline__ void finish(const VerifyLaunch &a, int b, int begin, 
     }
 }
 
-// A sum for whichever workgroup draws, and whether that is this one: the last of `all` to come here for sequence b, on top of `came`
-// before.  The sum goes past the caches to where every die sees it, is waited for, and only then counts; it is read the same way.
-// (A release and an acquire would write back and drop the die's whole cache for these eight bytes: 0.1 ms for 1 700 workgroups.)
+// A sum for whichever workgroup draws, and whether that is this one: the last of an open draw's workgroups, one a part.  The sum goes past
+// the caches to where every die sees it, is waited for, and only then counts; it is read the same way.  (A release and an acquire
+// would write back and drop the die's whole cache for these eight bytes: 0.1 ms for 1 700 workgroups.)
 __device__ __forceinline__ void publish(double *at, double x)
 {
     __hip_atomic_store(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
 }
 __device__ __forceinline__ double published(const double *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ bool last_to_arrive(const VerifyLaunch &a, int b, int came, int all)
+__device__ __forceinline__ bool last_to_arrive(const VerifyLaunch &a, OpenDraw &o)
 {
     __shared__ int arrived;
-    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(a.tickets + b, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(&o.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     __syncthreads();
-    return arrived == came + all - 1;
+    return arrived == a.parts - 1;
+}
+
+// Puts a draw on list `which` of those that are open.  (In any order: draws do not look at each other.)
+__device__ __forceinline__ void leave_open(const VerifyLaunch &a, int which, const OpenDraw &o)
+{
+    const int at = atomicAdd(a.opened + which, 1);
+    (which ? a.still_open : a.open)[at] = o;
 }
 
 // Which drafts stay, and the token behind them where the row's sums tell it: a workgroup for each sequence.  What is left open: draws
@@ -654,76 +693,88 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_dra
         if (tid == 0) {
             a.accepted[b] = 0;
             if (a.next) a.next[b] = -1;
-            if (a.open) a.open[b].from = kNothing;
         }
         return;
     }
-    const Temper t = temper_of(a, b);
+    const float T = a.temperature ? a.temperature[b] : 1.f;
+    const Temper t = temper_from(T);
     const Draw d = decide<EXACT>(a, b, begin, end, t);
-    int token = -1;
-    if (d.from == kTop) token = d.x;
+    Token token = {d.from == kTop ? d.x : -1, 0.f};
     // (prefixes and totals are off by eps of the row each)
-    else if (d.from == kRow || d.from == kRowWithout) token = draw<false>(a, d, number_of(a, b), EXACT ? 0.0 : 3.0 * a.eps);
-    const bool left_open = d.from == kRest || (!EXACT && token < 0 && d.from != kNothing);
-    if (a.open && tid == 0) a.open[b] = {left_open ? d.from : kNothing, d.row, d.x, d.p_top, d.q_top, d.p_scale, d.q_scale};
-    if (!left_open) finish(a, b, begin, end, d, token);
+    if (d.from == kRow || d.from == kRowWithout) token = draw<false>(a, d, number_of(a, b), EXACT ? 0.0 : 3.0 * a.eps);
+    if (d.from == kRest || (!EXACT && token.id < 0 && d.from != kNothing)) {
+        if (tid == 0) leave_open(a, 0, {b, d.from, d.row, d.x, d.q_row, 0, T, d.p_top, d.q_top, d.p_scale, d.q_scale});
+    } else finish(a, b, begin, end, d, token);
 }
 
-// An open draw as the draws' kernel left it.
-__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, int b, const OpenDraw &o, const Temper &t)
+// An open draw as it was left.
+__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, const OpenDraw &o)
 {
     Draw d = {};
-    d.from = o.from, d.row = o.row, d.x = o.x, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, o.row);
+    d.from = o.from, d.row = o.row, d.x = o.x, d.q_row = o.q_row, d.t = temper_from(o.T), d.p = row_at(a.logits, a.stride, a.fp32, o.row);
     d.p_top = o.p_top, d.p_scale = o.p_scale, d.q_top = o.q_top, d.q_scale = o.q_scale;
-    if (o.from == kRest) d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, draft_row_of(a, b, o.row));
+    if (o.from == kRest) d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row);
     return d;
 }
 
-// The draws from p - q: a workgroup adds up what is left of each part, the last to arrive draws.  Not EXACT: in binary32, and draws that
-// those sums do not settle stay open; and the draws from p that are open have their sums made anew, in binary64.
-template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch a, int came)
+// The open draws: a workgroup adds up what is left of a part of p - q, and the last to arrive draws.  Not EXACT: in binary32, and draws
+// that those sums do not settle stay open; and draws from p have their sums made anew, in binary64.  again: the rows' sums have been made
+// anew by now.
+template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch a, int again)
 {
-    const int tid = threadIdx.x, b = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
-    const OpenDraw o = a.open[b];
-    if (o.from == kNothing) return;
-    const Temper t = temper_of(a, b);
-    double unsure = 0.0;
-    Draw d = open_draw(a, b, o, t);
-    double *const rest = a.rest + (int64_t)o.row * a.parts;
-    if (d.from == kRest) {
-        if (EXACT && came) {                                    // (their sums have been made anew)
-            const int lane = tid & 63;
-            const Whole p = whole_row(a.row + (int64_t)o.row * a.parts, a.parts, t, lane), q = whole_row(a.draft_row + (int64_t)o.row * a.parts, a.parts, t, lane);
-            d.p_top = p.top, d.p_scale = 1.0 / p.sum, d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+    __shared__ DrawLds lds;
+    OpenDraw *const list = again ? a.still_open : a.open;
+    const int tid = threadIdx.x, lane = tid & 63;
+    OpenDraw o = list[blockIdx.x / (unsigned)a.parts];          // (there is one, if of nothing: asked for beside their number)
+    const unsigned n = (unsigned)a.opened[again] * (unsigned)a.parts;
+    for (unsigned j = blockIdx.x; j < n;) {
+        const unsigned at = j / (unsigned)a.parts;
+        const int k = j % (unsigned)a.parts;
+        Draw d = open_draw(a, o);
+        double unsure = 0.0, sum;
+        if (d.from == kRest) {
+            if (EXACT && again) {
+                const Whole p = whole_row(a.row + (int64_t)o.row * a.parts, a.parts, d.t, lane), q = whole_row(a.draft_row + (int64_t)o.row * a.parts, a.parts, d.t, lane);
+                d.p_top = p.top, d.p_scale = 1.0 / p.sum, d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+            }
+            // (p and q: twice eps each, by their weights and by their scales; so for a prefix and for the whole)
+            if (!EXACT) unsure = 10.0 * a.eps;
         }
-        const double sum = EXACT ? sum_of_part(a, d, k) : rest32_of_part(a, d, k);
-        if (tid == 0) publish(rest + k, sum);
-        // (p and q: twice eps each, by their weights and by their scales; so for a prefix and for the whole)
-        if (!EXACT) unsure = 10.0 * a.eps;
-    } else {
-        const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, k * a.part_len, part_end(a, k), t);
-        // (against the row's largest, which is that of the sums at hand)
-        if (tid == 0) publish(rest + k, is_finite(p.top) ? p.sum * exp2(((double)p.top - d.p_top) * t.c) * d.p_scale : 0.0);
+        if (!EXACT && d.from == kRest) sum = rest32_of_part(a, d, k);
+        else {
+            double w[kVec];
+            float x[kVec];
+            Draw whole = d;
+            if (d.from == kRowWithout) whole.from = kRow;       // (the part that the draft is in is looked at by itself)
+            sum = weights_of_part(w, x, a, whole, k);
+        }
+        sum = block_sum(sum, lds);
+        if (tid == 0) publish(a.rest + (int64_t)o.row * a.parts + k, sum);
+        if (last_to_arrive(a, list[at])) {
+            const Token token = draw<true>(a, d, number_of(a, o.b), unsure);
+            if (unsure > 0.0 && token.id < 0) {
+                o.arrived = 0;
+                if (tid == 0) leave_open(a, 1, o);
+            } else finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, token);
+        }
+        j += gridDim.x;
+        if (j < n) o = list[j / (unsigned)a.parts];
+        __syncthreads();
     }
-    if (!last_to_arrive(a, b, came, a.parts)) return;
-    const int token = draw<true>(a, d, number_of(a, b), unsure);
-    if (unsure > 0.0 && token < 0) return;
-    if (!EXACT && tid == 0) a.open[b].from = kNothing;          // (all of its workgroups have read it)
-    finish(a, b, a.cu[b], a.cu[b + 1], d, token);
 }
 
 // The sums of p and of q anew, in binary64, for the draws from p - q that are still open.
 __global__ __launch_bounds__(kDrawThreads) void verify_resum_kernel(VerifyLaunch a)
 {
-    const int tid = threadIdx.x, b = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
-    const OpenDraw o = a.open[b];
-    if (o.from != kRest) return;
-    const Temper t = temper_of(a, b);
-    const Draw d = open_draw(a, b, o, t);
-    const int begin = k * a.part_len, end = part_end(a, k);
-    const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, begin, end, t);
-    const RowPart q = part_of<true, kDrawThreads>(d.q, a.draft_fp32, begin, end, t);
-    if (tid == 0) a.row[(int64_t)o.row * a.parts + k] = p, a.draft_row[(int64_t)o.row * a.parts + k] = q;
+    const unsigned n = (unsigned)a.opened[1] * (unsigned)a.parts;
+    for (unsigned j = blockIdx.x; j < n; j += gridDim.x) {
+        const OpenDraw o = a.still_open[j / (unsigned)a.parts];
+        const int k = j % (unsigned)a.parts, begin = k * a.part_len, end = part_end(a, k);
+        const Draw d = open_draw(a, o);
+        const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, begin, end, d.t);
+        const RowPart q = part_of<true, kDrawThreads>(d.q, a.draft_fp32, begin, end, d.t);
+        if (threadIdx.x == 0) a.row[(int64_t)o.row * a.parts + k] = p, a.draft_row[(int64_t)o.row * a.parts + k] = q;
+    }
 }
 
 // Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
@@ -731,9 +782,10 @@ __global__ __launch_bounds__(kDrawThreads) void verify_resum_kernel(VerifyLaunch
 static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted)
 {
     const int64_t rows = (int64_t)a.R * (drafted ? 2 : 1);
+    a.num_cus = num_cus;
     a.part_len = kDrawThreads * kVec;
     a.parts = (a.V + a.part_len - 1) / a.part_len;
-    a.alone = rows * a.parts >= (int64_t)num_cus * 32;
+    a.alone = rows * a.parts >= (int64_t)num_cus * 16;
     a.exact = rows * a.V <= few;
     // The error of a sum of weights as weight32 gives them, in parts of the row's whole sum W: a weight w is off by (3 ln 2 |y| + 2) 2^-24
     // of it and a sum of eight by 3 2^-24; y is against the thread's value, which is at most 8 / c below one it met: |y| is at most 8
@@ -758,8 +810,9 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, voi
     if (drafted) a.draft_row = (RowPart *)take(parts * sizeof(RowPart));
     if (drafted || !a.exact) {
         a.rest = (double *)take(parts * sizeof(double));
-        a.tickets = (int32_t *)take((size_t)a.B * 4);
+        a.opened = (int32_t *)take(2 * sizeof(int32_t));
         a.open = (OpenDraw *)take((size_t)a.B * sizeof(OpenDraw));
+        if (drafted && !a.exact) a.still_open = (OpenDraw *)take((size_t)a.B * sizeof(OpenDraw));
     }
     return at;
 }
@@ -773,7 +826,8 @@ bool verify_fits(const VerifyLaunch &a, bool drafted)
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
 {
     const unsigned rows = (unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u), each = kVerifyThreads / 64;
-    const dim3 seqs((unsigned)a.B), parts((unsigned)a.B * (unsigned)a.parts), threads(kDrawThreads);
+    const unsigned items = (unsigned)a.B * (unsigned)a.parts, most = (unsigned)(4 * a.num_cus);
+    const dim3 seqs((unsigned)a.B), parts(items < most ? items : most), threads(kDrawThreads);
     if (a.R > 0) {
         const dim3 grid(a.alone ? (rows + each - 1) / each : rows);
         if (a.exact && a.alone) hipLaunchKernelGGL((verify_rows_kernel<true, true>), grid, dim3(kVerifyThreads), 0, s, a);
@@ -785,14 +839,15 @@ hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
     }
     if (a.exact) {
         hipLaunchKernelGGL(verify_draw_kernel<true>, seqs, threads, 0, s, a);
-        if (a.draft) hipLaunchKernelGGL(verify_rest_kernel<true>, parts, threads, 0, s, a, 0);
+        if (a.draft && a.R > 0) hipLaunchKernelGGL(verify_rest_kernel<true>, parts, threads, 0, s, a, 0);
         return hipGetLastError();
     }
     hipLaunchKernelGGL(verify_draw_kernel<false>, seqs, threads, 0, s, a);
+    if (a.R == 0) return hipGetLastError();                     // (nothing is open, nor has anything said so)
     hipLaunchKernelGGL(verify_rest_kernel<false>, parts, threads, 0, s, a, 0);
     if (a.draft) {
         hipLaunchKernelGGL(verify_resum_kernel, parts, threads, 0, s, a);
-        hipLaunchKernelGGL(verify_rest_kernel<true>, parts, threads, 0, s, a, a.parts);
+        hipLaunchKernelGGL(verify_rest_kernel<true>, parts, threads, 0, s, a, 1);
     }
     return hipGetLastError();
 }
