@@ -31,9 +31,8 @@ struct RowPart {
 // A draw from p - q, or one that binary32 sums did not settle.
 struct OpenDraw {
     int32_t b, from, row, x;     // from: see DrawFrom; x: the draft that was turned down
-    int32_t q_row, arrived;      // row of the draft model's logits; workgroups that have added up their part
-    float T, p_top, q_top;
-    double p_scale, q_scale;
+    int32_t q_row;               // row of the draft model's logits
+    float T;
 };
 struct VerifyLaunch {
     int32_t B, R, V, parts, part_len; // a row's parts, and the values of a part
@@ -45,9 +44,9 @@ struct VerifyLaunch {
     int32_t *accepted, *out, *next;
     float *logprobs;
     RowPart *row, *draft_row;    // [R][parts]
-    double *rest;                // [R][parts]  sums of the parts of the rows that open draws are from
-    int32_t *opened;             // [2]         draws on either list
-    OpenDraw *open, *still_open; // [B]
+    double *rest;                // [R][parts]  sums of max(p - q, 0), of rows that open draws are from
+    int32_t *opened;             // [1]         open draws
+    OpenDraw *open;              // [B]
     int32_t num_cus;
     int32_t alone;               // a part to a wave, not to a workgroup
     int32_t exact;               // all sums in binary64 from the start

@@ -290,7 +290,7 @@ __device__ __forceinline__ int part_end(const VerifyLaunch &a, int k) { return k
 template <bool EXACT, bool ALONE> __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
 {
     const int lane = threadIdx.x & 63;
-    if (blockIdx.x == 0 && threadIdx.x < 2 && a.opened) a.opened[threadIdx.x] = 0;
+    if (blockIdx.x == 0 && threadIdx.x == 0 && a.opened) a.opened[0] = 0;
     const unsigned n = __builtin_amdgcn_readfirstlane(ALONE ? blockIdx.x * (kVerifyThreads / 64) + threadIdx.x / 64 : blockIdx.x);
     const unsigned rows = n / (unsigned)a.parts, k = n % (unsigned)a.parts;
     const bool drafted = rows >= (unsigned)a.R;
@@ -558,14 +558,11 @@ __device__ Token token_of_part(const VerifyLaunch &a, const Draw &d, int k, doub
     return token;
 }
 
-__device__ __forceinline__ double published(const double *at);
-
-// A part's share in the sum, from the row's or (SUMS) as workgroups published it; one below 2^-996 is none (its weights might all have
-// vanished).
-template <bool SUMS> __device__ __forceinline__ double share_of_part(const VerifyLaunch &a, const Draw &d, int k)
+// A part's share in the sum; one below 2^-996 is none (its weights might all have vanished).
+__device__ __forceinline__ double share_of_part(const VerifyLaunch &a, const Draw &d, int k)
 {
     double s;
-    if (SUMS) s = published(a.rest + (int64_t)d.row * a.parts + k);
+    if (d.from == kRest) s = a.rest[(int64_t)d.row * a.parts + k];
     else {
         const RowPart r = a.row[(int64_t)d.row * a.parts + k];
         s = is_finite(r.top) ? r.sum * rescale(r.top, d.p_top, d.t) * d.p_scale : 0.0;
@@ -573,32 +570,14 @@ template <bool SUMS> __device__ __forceinline__ double share_of_part(const Verif
     return s > 1e-300 ? s : 0.0;
 }
 
-// This thread's share of what is left of part k of p - q, in binary32 products.
-template <bool FP32, bool QFP32> __device__ __forceinline__ double rest32(const Draw &d, int i, int end)
-{
-    const float p_scale = (float)d.p_scale, q_scale = (float)d.q_scale;
-    float x[kVec], y[kVec];
-    Row<FP32>{d.p}.load_some(x, i, end), Row<QFP32>{d.q}.load_some(y, i, end);
-#pragma unroll
-    for (int j = 0; j < kVec; j++) x[j] = fmaxf(weight32(x[j], d.p_top, d.t) * p_scale - weight32(y[j], d.q_top, d.t) * q_scale, 0.f);
-    return (double)sum_of_eight(x);
-}
-__device__ __forceinline__ double rest32_of_part(const VerifyLaunch &a, const Draw &d, int k)
-{
-    const int i = k * a.part_len + threadIdx.x * kVec, end = part_end(a, k);
-    if (a.fp32) return a.draft_fp32 ? rest32<true, true>(d, i, end) : rest32<true, false>(d, i, end);
-    return a.draft_fp32 ? rest32<false, true>(d, i, end) : rest32<false, false>(d, i, end);
-}
-
 // The token that v draws, from the parts' sums and then from the part that holds the border.  The whole workgroup.  None where the sums
 // may be off by as much as the border is from the nearest token's (`unsure`).
-template <bool SUMS> __device__ Token draw(const VerifyLaunch &a, Draw d, double v, double unsure)
+__device__ Token draw(const VerifyLaunch &a, Draw d, double v, double unsure)
 {
     __shared__ DrawLds lds;
     __shared__ double border_in_part;
     __shared__ int part;
     const int tid = threadIdx.x, each = (a.parts + kDrawThreads - 1) / kDrawThreads;
-    bool own = !SUMS;                                           // by the row's own sums
     for (;;) {
         // (the part that the draft is in, anew: what is left of it may be far less than a difference of sums could say)
         const int without = d.from == kRowWithout ? d.x / a.part_len : -1;
@@ -609,13 +588,13 @@ template <bool SUMS> __device__ Token draw(const VerifyLaunch &a, Draw d, double
             left = block_sum(weights_of_part(w, x, a, d, without), lds);
             left = left > 1e-300 ? left : 0.0;
         }
-        auto share = [&](int k) { return k == without ? left : own ? share_of_part<false>(a, d, k) : share_of_part<SUMS>(a, d, k); };
+        auto share = [&](int k) { return k == without ? left : share_of_part(a, d, k); };
         double mine = 0.0, before, border;
         for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) mine += share(k);
         const int who = holder(mine, before, border, &v, lds);
         if (who < 0) {                                          // nothing is left of p - q: p
-            if (d.from == kRow || unsure > 0.0) return {-1, 0.f}; // (the first: no row of a well-formed call)
-            d.from = kRow, own = true;
+            if (d.from == kRow) return {-1, 0.f};               // (no row of a well-formed call)
+            d.from = kRow;
             continue;
         }
         if (tid == who) {
@@ -659,30 +638,6 @@ __device__ __forceinline__ void finish(const VerifyLaunch &a, int b, int begin, 
     }
 }
 
-// A sum for whichever workgroup draws, and whether that is this one: the last of an open draw's workgroups, one a part.  The sum goes past
-// the caches to where every die sees it, is waited for, and only then counts; it is read the same way.  (A release and an acquire
-// would write back and drop the die's whole cache for these eight bytes: 0.1 ms for 1 700 workgroups.)
-__device__ __forceinline__ void publish(double *at, double x)
-{
-    __hip_atomic_store(at, x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-}
-__device__ __forceinline__ double published(const double *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
-__device__ __forceinline__ bool last_to_arrive(const VerifyLaunch &a, OpenDraw &o)
-{
-    __shared__ int arrived;
-    if (threadIdx.x == 0) arrived = __hip_atomic_fetch_add(&o.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-    __syncthreads();
-    return arrived == a.parts - 1;
-}
-
-// Puts a draw on list `which` of those that are open.  (In any order: draws do not look at each other.)
-__device__ __forceinline__ void leave_open(const VerifyLaunch &a, int which, const OpenDraw &o)
-{
-    const int at = atomicAdd(a.opened + which, 1);
-    (which ? a.still_open : a.open)[at] = o;
-}
-
 // Which drafts stay, and the token behind them where the row's sums tell it: a workgroup for each sequence.  What is left open: draws
 // from p - q, and those that binary32 sums do not settle.
 template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyLaunch a)
@@ -701,80 +656,78 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_dra
     const Draw d = decide<EXACT>(a, b, begin, end, t);
     Token token = {d.from == kTop ? d.x : -1, 0.f};
     // (prefixes and totals are off by eps of the row each)
-    if (d.from == kRow || d.from == kRowWithout) token = draw<false>(a, d, number_of(a, b), EXACT ? 0.0 : 3.0 * a.eps);
+    if (d.from == kRow || d.from == kRowWithout) token = draw(a, d, number_of(a, b), EXACT ? 0.0 : 3.0 * a.eps);
     if (d.from == kRest || (!EXACT && token.id < 0 && d.from != kNothing)) {
-        if (tid == 0) leave_open(a, 0, {b, d.from, d.row, d.x, d.q_row, 0, T, d.p_top, d.q_top, d.p_scale, d.q_scale});
+        // (in any order: draws do not look at each other)
+        if (tid == 0) a.open[atomicAdd(a.opened, 1)] = {b, d.from, d.row, d.x, d.q_row, T};
     } else finish(a, b, begin, end, d, token);
 }
 
-// An open draw as it was left.
-__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, const OpenDraw &o)
+// The open draws of the kernels below, an item for each part: workgroups of four waves, an item to a wave at a time.
+template <typename F> __device__ __forceinline__ void every_item(const VerifyLaunch &a, F f)
+{
+    const unsigned waves = gridDim.x * (kVerifyThreads / 64), n = (unsigned)a.opened[0] * (unsigned)a.parts;
+    for (unsigned j = __builtin_amdgcn_readfirstlane(blockIdx.x * (kVerifyThreads / 64) + threadIdx.x / 64); j < n; j += waves)
+        f(a.open[j / (unsigned)a.parts], (int)(j % (unsigned)a.parts));
+}
+
+// Sums of the rows of open draws, p and q, anew, in binary64.
+__global__ __launch_bounds__(kVerifyThreads) void verify_resum_kernel(VerifyLaunch a)
+{
+    const int lane = threadIdx.x & 63;
+    every_item(a, [&](const OpenDraw &o, int k) {
+        const Temper t = temper_from(o.T);
+        const int begin = k * a.part_len, end = part_end(a, k);
+        const RowPart p = part_by_wave<true>(row_at(a.logits, a.stride, a.fp32, o.row), a.fp32, begin, end, t);
+        if (lane == 0) a.row[(int64_t)o.row * a.parts + k] = p;
+        if (o.from != kRest) return;
+        const RowPart q = part_by_wave<true>(row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row), a.draft_fp32, begin, end, t);
+        if (lane == 0) a.draft_row[(int64_t)o.row * a.parts + k] = q;
+    });
+}
+
+// An open draw with what the sums of its rows say.
+__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, const OpenDraw &o, int lane)
 {
     Draw d = {};
-    d.from = o.from, d.row = o.row, d.x = o.x, d.q_row = o.q_row, d.t = temper_from(o.T), d.p = row_at(a.logits, a.stride, a.fp32, o.row);
-    d.p_top = o.p_top, d.p_scale = o.p_scale, d.q_top = o.q_top, d.q_scale = o.q_scale;
-    if (o.from == kRest) d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row);
+    d.from = o.from, d.row = o.row, d.x = o.x, d.t = temper_from(o.T), d.p = row_at(a.logits, a.stride, a.fp32, o.row);
+    const Whole p = whole_row(a.row + (int64_t)o.row * a.parts, a.parts, d.t, lane);
+    d.p_top = p.top, d.p_scale = 1.0 / p.sum;
+    if (o.from == kRest) {
+        const Whole q = whole_row(a.draft_row + (int64_t)o.row * a.parts, a.parts, d.t, lane);
+        d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+    }
     return d;
 }
 
-// The open draws: a workgroup adds up what is left of a part of p - q, and the last to arrive draws.  Not EXACT: in binary32, and draws
-// that those sums do not settle stay open; and draws from p have their sums made anew, in binary64.  again: the rows' sums have been made
-// anew by now.
-template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch a, int again)
+// What is left of each part of p - q.
+__global__ __launch_bounds__(kVerifyThreads) void verify_rest_kernel(VerifyLaunch a)
 {
-    __shared__ DrawLds lds;
-    OpenDraw *const list = again ? a.still_open : a.open;
-    const int tid = threadIdx.x, lane = tid & 63;
-    OpenDraw o = list[blockIdx.x / (unsigned)a.parts];          // (there is one, if of nothing: asked for beside their number)
-    const unsigned n = (unsigned)a.opened[again] * (unsigned)a.parts;
-    for (unsigned j = blockIdx.x; j < n;) {
-        const unsigned at = j / (unsigned)a.parts;
-        const int k = j % (unsigned)a.parts;
-        Draw d = open_draw(a, o);
-        double unsure = 0.0, sum;
-        if (d.from == kRest) {
-            if (EXACT && again) {
-                const Whole p = whole_row(a.row + (int64_t)o.row * a.parts, a.parts, d.t, lane), q = whole_row(a.draft_row + (int64_t)o.row * a.parts, a.parts, d.t, lane);
-                d.p_top = p.top, d.p_scale = 1.0 / p.sum, d.q_top = q.top, d.q_scale = 1.0 / q.sum;
-            }
-            // (p and q: twice eps each, by their weights and by their scales; so for a prefix and for the whole)
-            if (!EXACT) unsure = 10.0 * a.eps;
+    const int lane = threadIdx.x & 63;
+    every_item(a, [&](const OpenDraw &o, int k) {
+        if (o.from != kRest) return;
+        const Draw d = open_draw(a, o, lane);
+        const int end = part_end(a, k);
+        double sum = 0.0, w[kVec];
+        float x[kVec];
+        for (int i = k * a.part_len + lane * kVec; i < end; i += 64 * kVec) {
+            weights_at(w, x, a, d, i, end);
+#pragma unroll
+            for (int j = 0; j < kVec; j++) sum += w[j];
         }
-        if (!EXACT && d.from == kRest) sum = rest32_of_part(a, d, k);
-        else {
-            double w[kVec];
-            float x[kVec];
-            Draw whole = d;
-            if (d.from == kRowWithout) whole.from = kRow;       // (the part that the draft is in is looked at by itself)
-            sum = weights_of_part(w, x, a, whole, k);
-        }
-        sum = block_sum(sum, lds);
-        if (tid == 0) publish(a.rest + (int64_t)o.row * a.parts + k, sum);
-        if (last_to_arrive(a, list[at])) {
-            const Token token = draw<true>(a, d, number_of(a, o.b), unsure);
-            if (unsure > 0.0 && token.id < 0) {
-                o.arrived = 0;
-                if (tid == 0) leave_open(a, 1, o);
-            } else finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, token);
-        }
-        j += gridDim.x;
-        if (j < n) o = list[j / (unsigned)a.parts];
-        __syncthreads();
-    }
+        sum = wave_sum(sum);
+        if (lane == 0) a.rest[(int64_t)o.row * a.parts + k] = sum;
+    });
 }
 
-// The sums of p and of q anew, in binary64, for the draws from p - q that are still open.
-__global__ __launch_bounds__(kDrawThreads) void verify_resum_kernel(VerifyLaunch a)
+// The tokens of the open draws, a workgroup each.
+__global__ __launch_bounds__(kDrawThreads) void verify_close_kernel(VerifyLaunch a)
 {
-    const unsigned n = (unsigned)a.opened[1] * (unsigned)a.parts;
-    for (unsigned j = blockIdx.x; j < n; j += gridDim.x) {
-        const OpenDraw o = a.still_open[j / (unsigned)a.parts];
-        const int k = j % (unsigned)a.parts, begin = k * a.part_len, end = part_end(a, k);
-        const Draw d = open_draw(a, o);
-        const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, begin, end, d.t);
-        const RowPart q = part_of<true, kDrawThreads>(d.q, a.draft_fp32, begin, end, d.t);
-        if (threadIdx.x == 0) a.row[(int64_t)o.row * a.parts + k] = p, a.draft_row[(int64_t)o.row * a.parts + k] = q;
-    }
+    const int n = a.opened[0];
+    if ((int)blockIdx.x >= n) return;
+    const OpenDraw o = a.open[blockIdx.x];
+    const Draw d = open_draw(a, o, threadIdx.x & 63);
+    finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, draw(a, d, number_of(a, o.b), 0.0));
 }
 
 // Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
@@ -808,11 +761,10 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, voi
     const size_t parts = (size_t)a.R * a.parts;
     a.row = (RowPart *)take(parts * sizeof(RowPart));
     if (drafted) a.draft_row = (RowPart *)take(parts * sizeof(RowPart));
+    if (drafted) a.rest = (double *)take(parts * sizeof(double));
     if (drafted || !a.exact) {
-        a.rest = (double *)take(parts * sizeof(double));
-        a.opened = (int32_t *)take(2 * sizeof(int32_t));
+        a.opened = (int32_t *)take(sizeof(int32_t));
         a.open = (OpenDraw *)take((size_t)a.B * sizeof(OpenDraw));
-        if (drafted && !a.exact) a.still_open = (OpenDraw *)take((size_t)a.B * sizeof(OpenDraw));
     }
     return at;
 }
@@ -820,14 +772,14 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, voi
 // (a launch has less than 2^32 threads)
 bool verify_fits(const VerifyLaunch &a, bool drafted)
 {
-    return (int64_t)a.R * a.parts * (drafted ? 2 : 1) * 64 < (int64_t)1 << 32 && (int64_t)a.B * a.parts * kDrawThreads < (int64_t)1 << 32;
+    return (int64_t)a.R * a.parts * (drafted ? 2 : 1) * 64 < (int64_t)1 << 32 && (int64_t)a.B * a.parts < (int64_t)1 << 32;
 }
 
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
 {
     const unsigned rows = (unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u), each = kVerifyThreads / 64;
-    const unsigned items = (unsigned)a.B * (unsigned)a.parts, most = (unsigned)(4 * a.num_cus);
-    const dim3 seqs((unsigned)a.B), parts(items < most ? items : most), threads(kDrawThreads);
+    const int64_t items = ((int64_t)a.B * a.parts + each - 1) / each, most = 8 * a.num_cus;
+    const dim3 seqs((unsigned)a.B), threads(kDrawThreads), open((unsigned)(items < most ? items : most)), open_threads(kVerifyThreads);
     if (a.R > 0) {
         const dim3 grid(a.alone ? (rows + each - 1) / each : rows);
         if (a.exact && a.alone) hipLaunchKernelGGL((verify_rows_kernel<true, true>), grid, dim3(kVerifyThreads), 0, s, a);
@@ -837,18 +789,12 @@ hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
-    if (a.exact) {
-        hipLaunchKernelGGL(verify_draw_kernel<true>, seqs, threads, 0, s, a);
-        if (a.draft && a.R > 0) hipLaunchKernelGGL(verify_rest_kernel<true>, parts, threads, 0, s, a, 0);
-        return hipGetLastError();
-    }
-    hipLaunchKernelGGL(verify_draw_kernel<false>, seqs, threads, 0, s, a);
-    if (a.R == 0) return hipGetLastError();                     // (nothing is open, nor has anything said so)
-    hipLaunchKernelGGL(verify_rest_kernel<false>, parts, threads, 0, s, a, 0);
-    if (a.draft) {
-        hipLaunchKernelGGL(verify_resum_kernel, parts, threads, 0, s, a);
-        hipLaunchKernelGGL(verify_rest_kernel<true>, parts, threads, 0, s, a, 1);
-    }
+    if (a.exact) hipLaunchKernelGGL(verify_draw_kernel<true>, seqs, threads, 0, s, a);
+    else hipLaunchKernelGGL(verify_draw_kernel<false>, seqs, threads, 0, s, a);
+    if (!a.opened || a.R == 0) return hipGetLastError();        // (nothing is left open)
+    if (!a.exact) hipLaunchKernelGGL(verify_resum_kernel, open, open_threads, 0, s, a);
+    if (a.draft) hipLaunchKernelGGL(verify_rest_kernel, open, open_threads, 0, s, a);
+    hipLaunchKernelGGL(verify_close_kernel, seqs, threads, 0, s, a);
     return hipGetLastError();
 }
 
