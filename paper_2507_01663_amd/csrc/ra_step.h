@@ -31,8 +31,9 @@ struct RowPart {
 // A draw from p - q, or one that binary32 sums did not settle.
 struct OpenDraw {
     int32_t b, from, row, x;     // from: see DrawFrom; x: the draft that was turned down
-    int32_t q_row;               // row of the draft model's logits
-    float T;
+    int32_t q_row, arrived;      // row of the draft model's logits; workgroups that have added up their part
+    float T, p_top;
+    double p_scale;
 };
 struct VerifyLaunch {
     int32_t B, R, V, parts, part_len; // a row's parts, and the values of a part
@@ -44,7 +45,7 @@ struct VerifyLaunch {
     int32_t *accepted, *out, *next;
     float *logprobs;
     RowPart *row, *draft_row;    // [R][parts]
-    double *rest;                // [R][parts]  sums of max(p - q, 0), of rows that open draws are from
+    double *rest;                // [R][parts]  sums of what open draws are from
     int32_t *opened;             // [1]         open draws
     OpenDraw *open;              // [B]
     int32_t num_cus;

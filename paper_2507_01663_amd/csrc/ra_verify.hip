@@ -91,6 +91,10 @@ __device__ __forceinline__ double last_lane(double x)
 {
     return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), 63), __builtin_amdgcn_readlane(__double2loint(x), 63));
 }
+__device__ __forceinline__ double lane_of(double x, int lane)
+{
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), lane), __builtin_amdgcn_readlane(__double2loint(x), lane));
+}
 __device__ __forceinline__ double wave_sum(double x) { return last_lane(wave_scan(x)); }
 template <int CTRL, int ROWS> __device__ __forceinline__ float top_from_lane(float x)
 {
@@ -319,10 +323,8 @@ struct Whole {
     float top;                   // finite: the row has a distribution
     int first;
 };
-__device__ __forceinline__ Whole whole_row(const RowPart *part, int parts, const Temper &t, int lane)
+__device__ __forceinline__ Whole whole_row(const RowPart *part, RowPart r, int parts, const Temper &t, int lane) // r: part[lane]
 {
-    RowPart r = {0.0, -INFINITY, INT32_MAX};
-    if (lane < parts) r = part[lane];
     float top = r.top;
     for (int k = lane + 64; k < parts; k += 64) top = top_of(top, part[k].top);
     top = wave_top(top);
@@ -392,13 +394,61 @@ __device__ __forceinline__ Draw judge(const VerifyLaunch &a, int b, int row, int
     if (px > 0.0 && against > 0.0 && __builtin_fabs(against - px) <= unsure * px) says = kUnsure;
     return d;
 }
-// The sums of the row and of its draft's, as the first kernel (or resum) left them.
-__device__ __forceinline__ Draw judge_row(const VerifyLaunch &a, int b, int row, int end, const Temper &t, int lane, double unsure, Verdict &says, double &lp)
+// A part of a row and what is left of the border there.
+struct Border {
+    int part;                    // -1: no part has a share
+    double at;
+};
+// The part that holds v times the sum of all parts' shares: the first that the running sum exceeds it in, or the last with any share
+// where rounding (or a number of 1) leaves none.  share(k): part k's, asked for by lane k % 64, once if there are 64 parts at most.  A share
+// below 2^-996 is none (its weights might all have vanished).  All lanes of a wave.
+template <typename F> __device__ __forceinline__ Border border_of(F share, int parts, double v, int lane)
 {
-    const Whole p = whole_row(a.row + (int64_t)row * a.parts, a.parts, t, lane);
+    auto some = [&](int k) {
+        const double s = k < parts ? share(k) : 0.0;
+        return s > 1e-300 ? s : 0.0;
+    };
+    double x = some(lane), total = wave_sum(x);
+    for (int k = lane + 64; k < parts + lane; k += 64) total += wave_sum(some(k));
+    const double border = v * total;
+    Border found = {-1, 0.0};
+    double run = 0.0;
+    for (int base = 0;;) {
+        const double scan = wave_scan(x), before = run + from_lane<0x138, 0xf>(scan); // (the lane before's; none for the first)
+        const uint64_t any = __ballot(x > 0.0), past = __ballot(x > 0.0 && run + scan > border);
+        if (any) {
+            const int at = past ? __builtin_ctzll(past) : 63 - __builtin_clzll(any);
+            found = {base + at, border - lane_of(before, at)};
+        }
+        if (past) break;
+        run += last_lane(scan);
+        base += 64;
+        if (base >= parts) break;
+        x = some(base + lane);
+    }
+    return found;
+}
+
+// The weight of a part of row p in parts of the whole row's.
+__device__ __forceinline__ double share_of(const RowPart &r, const Draw &d)
+{
+    return is_finite(r.top) ? r.sum * rescale(r.top, d.p_top, d.t) * d.p_scale : 0.0;
+}
+
+// Row `row` of sequence b by the sums that the first kernel left: the draw from it, what it says to its draft, and where v lies in it.
+__device__ __forceinline__ Draw judge_row(const VerifyLaunch &a, int b, int row, int end, const Temper &t, double v, int lane, double unsure, Verdict &says, double &lp, Border &border)
+{
+    const RowPart *const parts = a.row + (int64_t)row * a.parts;
+    const RowPart mine = lane < a.parts ? parts[lane] : RowPart{0.0, -INFINITY, INT32_MAX};
+    const Whole p = whole_row(parts, mine, a.parts, t, lane);
     Whole q = {1.0, -INFINITY, 0};
-    if (a.draft && row + 1 < end && t.c != 0.0 && draft_row_of(a, b, row) >= 0) q = whole_row(a.draft_row + (int64_t)row * a.parts, a.parts, t, lane);
-    return judge(a, b, row, end, t, p, q, unsure, says, lp);
+    if (a.draft && row + 1 < end && t.c != 0.0 && draft_row_of(a, b, row) >= 0) {
+        const RowPart *const theirs = a.draft_row + (int64_t)row * a.parts;
+        q = whole_row(theirs, lane < a.parts ? theirs[lane] : RowPart{0.0, -INFINITY, INT32_MAX}, a.parts, t, lane);
+    }
+    const Draw d = judge(a, b, row, end, t, p, q, unsure, says, lp);
+    if (d.from == kRow) border = border_of([&](int k) { return share_of(k == lane ? mine : parts[k], d); }, a.parts, v, lane);
+    return d;
 }
 
 // A whole row, all over again in binary64, by a workgroup of the draws.
@@ -410,19 +460,21 @@ __device__ Whole exact_row(const VerifyLaunch &a, const uint8_t *at, int fp32, c
 
 // The rows of sequence b, as many at a time as there are waves, up to the first that keeps no draft: that one's draw.  The drafts that stay
 // are written.  The whole workgroup.
-template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch &a, int b, int begin, int end, const Temper &t)
+template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch &a, int b, int begin, int end, const Temper &t, double v, Border &border)
 {
     __shared__ Draw draws[kDrawWaves];
     __shared__ Verdict verdict[kDrawWaves];
+    __shared__ Border borders[kDrawWaves];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     for (int base = begin;; base += kDrawWaves) {
         const int row = base + wave;
         Verdict says = kGoes;
         double lp = 0.0;
         if (row < end) {
-            const Draw d = judge_row(a, b, row, end, t, lane, EXACT ? 0.0 : 4.0 * a.eps, says, lp);
+            Border in_row = {-1, 0.0};
+            const Draw d = judge_row(a, b, row, end, t, v, lane, EXACT ? 0.0 : 4.0 * a.eps, says, lp, in_row);
             if (EXACT && says == kUnsure) says = kGoes;         // (equal: not less)
-            if (lane == 0) draws[wave] = d;
+            if (lane == 0) draws[wave] = d, borders[wave] = in_row;
         }
         if (lane == 0) verdict[wave] = says;
         __syncthreads();
@@ -443,7 +495,10 @@ template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch 
             a.out[row] = a.tokens[row + 1];
             if (a.logprobs) a.logprobs[row] = (float)lp;
         }
-        if (n < kDrawWaves) return draws[n];                    // (the last row keeps none, so there is one)
+        if (n < kDrawWaves) {                                   // (the last row keeps none, so there is one)
+            border = borders[n];
+            return draws[n];
+        }
         __syncthreads();
     }
 }
@@ -533,12 +588,14 @@ struct Token {
     int id;
     float logit;
 };
-// The first value of part k at which the running sum of the part's weights passes the border; none where the sum is within `unsure` of
+// The first value of the border's part at which the running sum of the part's weights passes the border; none where the sum is within `unsure` of
 // the border at it or before it.
-__device__ Token token_of_part(const VerifyLaunch &a, const Draw &d, int k, double border, double unsure, DrawLds &lds)
+__device__ Token token_of_part(const VerifyLaunch &a, const Draw &d, Border at, double unsure, DrawLds &lds)
 {
     __shared__ Token token;
-    const int tid = threadIdx.x;
+    const int tid = threadIdx.x, k = at.part;
+    double border = at.at;
+    if (k < 0) return {-1, 0.f};
     double w[kVec], before;
     float x[kVec];
     const double sum = weights_of_part(w, x, a, d, k);
@@ -558,58 +615,16 @@ __device__ Token token_of_part(const VerifyLaunch &a, const Draw &d, int k, doub
     return token;
 }
 
-// A part's share in the sum; one below 2^-996 is none (its weights might all have vanished).
-__device__ __forceinline__ double share_of_part(const VerifyLaunch &a, const Draw &d, int k)
+// The token that v draws from p without the draft, by the parts' shares in p.  The part that the draft is in is added up anew: what is left
+// of it may be far less than a difference of sums could say.  The whole workgroup.
+template <typename F> __device__ __forceinline__ Token draw_without(const VerifyLaunch &a, const Draw &d, F share, double v, double unsure, DrawLds &lds)
 {
-    double s;
-    if (d.from == kRest) s = a.rest[(int64_t)d.row * a.parts + k];
-    else {
-        const RowPart r = a.row[(int64_t)d.row * a.parts + k];
-        s = is_finite(r.top) ? r.sum * rescale(r.top, d.p_top, d.t) * d.p_scale : 0.0;
-    }
-    return s > 1e-300 ? s : 0.0;
-}
-
-// The token that v draws, from the parts' sums and then from the part that holds the border.  The whole workgroup.  None where the sums
-// may be off by as much as the border is from the nearest token's (`unsure`).
-__device__ Token draw(const VerifyLaunch &a, Draw d, double v, double unsure)
-{
-    __shared__ DrawLds lds;
-    __shared__ double border_in_part;
-    __shared__ int part;
-    const int tid = threadIdx.x, each = (a.parts + kDrawThreads - 1) / kDrawThreads;
-    for (;;) {
-        // (the part that the draft is in, anew: what is left of it may be far less than a difference of sums could say)
-        const int without = d.from == kRowWithout ? d.x / a.part_len : -1;
-        double left = 0.0;
-        if (without >= 0) {
-            double w[kVec];
-            float x[kVec];
-            left = block_sum(weights_of_part(w, x, a, d, without), lds);
-            left = left > 1e-300 ? left : 0.0;
-        }
-        auto share = [&](int k) { return k == without ? left : share_of_part(a, d, k); };
-        double mine = 0.0, before, border;
-        for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) mine += share(k);
-        const int who = holder(mine, before, border, &v, lds);
-        if (who < 0) {                                          // nothing is left of p - q: p
-            if (d.from == kRow) return {-1, 0.f};               // (no row of a well-formed call)
-            d.from = kRow;
-            continue;
-        }
-        if (tid == who) {
-            double run = before;
-            for (int k = tid * each; k < (tid + 1) * each && k < a.parts; k++) {
-                const double s = each == 1 ? mine : share(k);
-                if (!(s > 0.0)) continue;
-                part = k, border_in_part = border - run;
-                run += s;
-                if (run > border) break;
-            }
-        }
-        __syncthreads();
-        return token_of_part(a, d, part, border_in_part, unsure, lds);
-    }
+    const int lane = threadIdx.x & 63, without = d.x / a.part_len;
+    double w[kVec];
+    float x[kVec];
+    const double left = block_sum(weights_of_part(w, x, a, d, without), lds);
+    const Border at = border_of([&](int k) { return k == without ? left : share(k); }, a.parts, v, lane);
+    return token_of_part(a, d, at, unsure, lds);
 }
 
 __device__ __forceinline__ double number_of(const VerifyLaunch &a, int b)
@@ -642,6 +657,7 @@ __device__ __forceinline__ void finish(const VerifyLaunch &a, int b, int begin, 
 // from p - q, and those that binary32 sums do not settle.
 template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyLaunch a)
 {
+    __shared__ DrawLds lds;
     const int tid = threadIdx.x, b = blockIdx.x;
     const int begin = a.cu[b], end = a.cu[b + 1];
     if (begin < 0 || end > a.R || begin >= end) {
@@ -652,82 +668,176 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_dra
         return;
     }
     const float T = a.temperature ? a.temperature[b] : 1.f;
+    const double v = number_of(a, b), unsure = EXACT ? 0.0 : 3.0 * a.eps; // (prefixes and totals are off by eps of the row each)
     const Temper t = temper_from(T);
-    const Draw d = decide<EXACT>(a, b, begin, end, t);
+    Border at;
+    const Draw d = decide<EXACT>(a, b, begin, end, t, v, at);
     Token token = {d.from == kTop ? d.x : -1, 0.f};
-    // (prefixes and totals are off by eps of the row each)
-    if (d.from == kRow || d.from == kRowWithout) token = draw(a, d, number_of(a, b), EXACT ? 0.0 : 3.0 * a.eps);
+    if (d.from == kRow) token = token_of_part(a, d, at, unsure, lds);
+    else if (d.from == kRowWithout) {
+        const RowPart *const parts = a.row + (int64_t)d.row * a.parts;
+        token = draw_without(a, d, [&](int k) { return share_of(parts[k], d); }, v, unsure, lds);
+        if (EXACT && token.id < 0) {                            // nothing is left: p
+            Draw p = d;
+            p.from = kRow;
+            token = token_of_part(a, p, border_of([&](int k) { return share_of(parts[k], d); }, a.parts, v, tid & 63), 0.0, lds);
+        }
+    }
     if (d.from == kRest || (!EXACT && token.id < 0 && d.from != kNothing)) {
         // (in any order: draws do not look at each other)
-        if (tid == 0) a.open[atomicAdd(a.opened, 1)] = {b, d.from, d.row, d.x, d.q_row, T};
+        if (tid == 0) a.open[atomicAdd(a.opened, 1)] = {b, d.from, d.row, d.x, d.q_row, 0, T, d.p_top, d.p_scale};
     } else finish(a, b, begin, end, d, token);
 }
 
-// The open draws of the kernels below, an item for each part: workgroups of four waves, an item to a wave at a time.
+// A sum for whichever workgroup draws, and whether that is this one: the last of an open draw's workgroups, one a part.  The sum goes past
+// the caches to where every die sees it, is waited for, and only then counts; it is read the same way.  (A release and an acquire
+// would write back and drop the die's whole cache for these eight bytes: 0.1 ms for 1 700 workgroups.)
+__device__ __forceinline__ bool last_to_publish(const VerifyLaunch &a, OpenDraw &o, double *at, double sum)
+{
+    __shared__ int arrived;
+    if (threadIdx.x == 0) {
+        __hip_atomic_store(at, sum, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        arrived = __hip_atomic_fetch_add(&o.arrived, 1, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    __syncthreads();
+    return arrived == a.parts - 1;
+}
+__device__ __forceinline__ double published(const double *at) { return __hip_atomic_load(at, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+
+// Every part of every open draw, an item to a workgroup at a time.
 template <typename F> __device__ __forceinline__ void every_item(const VerifyLaunch &a, F f)
 {
-    const unsigned waves = gridDim.x * (kVerifyThreads / 64), n = (unsigned)a.opened[0] * (unsigned)a.parts;
-    for (unsigned j = __builtin_amdgcn_readfirstlane(blockIdx.x * (kVerifyThreads / 64) + threadIdx.x / 64); j < n; j += waves)
-        f(a.open[j / (unsigned)a.parts], (int)(j % (unsigned)a.parts));
+    unsigned at = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
+    OpenDraw o = a.open[at];                                    // (there is one, if of nothing: asked for beside their number)
+    const unsigned n = (unsigned)a.opened[0] * (unsigned)a.parts;
+    for (unsigned j = blockIdx.x; j < n;) {
+        f(o, a.open[at], (int)k);
+        j += gridDim.x, at = j / (unsigned)a.parts, k = j % (unsigned)a.parts;
+        if (j < n) o = a.open[at];
+        __syncthreads();
+    }
 }
 
-// Sums of the rows of open draws, p and q, anew, in binary64.
-__global__ __launch_bounds__(kVerifyThreads) void verify_resum_kernel(VerifyLaunch a)
+// The rows of an open draw and their sums; its shares are known by `share`, or by the row's sums where it is from p.  The whole workgroup, and
+// all of it knows the same.
+struct Opened {
+    Draw d;
+    const RowPart *parts;
+    RowPart mine;                // parts[lane]
+};
+__device__ __forceinline__ Opened open_draw(const VerifyLaunch &a, const OpenDraw &o, int lane)
+{
+    const RowPart none = {0.0, -INFINITY, INT32_MAX};
+    Opened r;
+    r.parts = a.row + (int64_t)o.row * a.parts, r.mine = lane < a.parts ? r.parts[lane] : none;
+    r.d = {};
+    r.d.from = o.from, r.d.row = o.row, r.d.x = o.x, r.d.t = temper_from(o.T), r.d.p = row_at(a.logits, a.stride, a.fp32, o.row);
+    if (o.from == kRest) {
+        const RowPart *const qs = a.draft_row + (int64_t)o.row * a.parts;
+        const Whole q = whole_row(qs, lane < a.parts ? qs[lane] : none, a.parts, r.d.t, lane);
+        r.d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row), r.d.q_top = q.top, r.d.q_scale = 1.0 / q.sum;
+    }
+    const Whole p = whole_row(r.parts, r.mine, a.parts, r.d.t, lane);
+    r.d.p_top = p.top, r.d.p_scale = 1.0 / p.sum;
+    return r;
+}
+template <typename F> __device__ __forceinline__ void close_draw(const VerifyLaunch &a, const OpenDraw &o, Opened &r, F share, DrawLds &lds)
 {
     const int lane = threadIdx.x & 63;
-    every_item(a, [&](const OpenDraw &o, int k) {
-        const Temper t = temper_from(o.T);
-        const int begin = k * a.part_len, end = part_end(a, k);
-        const RowPart p = part_by_wave<true>(row_at(a.logits, a.stride, a.fp32, o.row), a.fp32, begin, end, t);
-        if (lane == 0) a.row[(int64_t)o.row * a.parts + k] = p;
-        if (o.from != kRest) return;
-        const RowPart q = part_by_wave<true>(row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row), a.draft_fp32, begin, end, t);
-        if (lane == 0) a.draft_row[(int64_t)o.row * a.parts + k] = q;
+    const double v = number_of(a, o.b);
+    auto in_row = [&](int k) { return share_of(k == lane ? r.mine : r.parts[k], r.d); };
+    Token token = {-1, 0.f};
+    if (r.d.from == kRowWithout) token = draw_without(a, r.d, in_row, v, 0.0, lds);
+    else if (r.d.from == kRest) token = token_of_part(a, r.d, border_of(share, a.parts, v, lane), 0.0, lds);
+    if (token.id < 0) {                                         // from p, or nothing is left but that
+        r.d.from = kRow;
+        token = token_of_part(a, r.d, border_of(in_row, a.parts, v, lane), 0.0, lds);
+    }
+    finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], r.d, token);
+}
+
+// Few open draws, from p: its sums anew, in binary64; the last workgroup to add up its part draws.
+__global__ __launch_bounds__(kDrawThreads) void verify_again_kernel(VerifyLaunch a)
+{
+    __shared__ DrawLds lds;
+    const int lane = threadIdx.x & 63;
+    every_item(a, [&](const OpenDraw &o, OpenDraw &there, int k) {
+        Draw d = {};
+        d.from = o.from, d.row = o.row, d.x = o.x, d.t = temper_from(o.T), d.p = row_at(a.logits, a.stride, a.fp32, o.row), d.p_top = o.p_top, d.p_scale = o.p_scale;
+        const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, k * a.part_len, part_end(a, k), d.t);
+        double *const sums = a.rest + (int64_t)o.row * a.parts;
+        if (!last_to_publish(a, there, sums + k, share_of(p, d))) return;
+        const double v = number_of(a, o.b);
+        auto share = [&](int k) { return published(sums + k); };
+        Token token = {-1, 0.f};
+        if (d.from == kRowWithout) token = draw_without(a, d, share, v, 0.0, lds);
+        if (token.id < 0) {                                     // (or nothing is left without the draft)
+            d.from = kRow;
+            token = token_of_part(a, d, border_of(share, a.parts, v, lane), 0.0, lds);
+        }
+        finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, token);
+    });
+}
+// ... from p - q, whose sums are binary64: what is left of it, in the same way.
+__global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch a)
+{
+    __shared__ DrawLds lds;
+    every_item(a, [&](const OpenDraw &o, OpenDraw &there, int k) {
+        Opened r = open_draw(a, o, threadIdx.x & 63);
+        double w[kVec];
+        float x[kVec];
+        const double sum = block_sum(weights_of_part(w, x, a, r.d, k), lds);
+        double *const sums = a.rest + (int64_t)o.row * a.parts;
+        if (last_to_publish(a, there, sums + k, sum)) close_draw(a, o, r, [&](int k) { return published(sums + k); }, lds);
     });
 }
 
-// An open draw with what the sums of its rows say.
-__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, const OpenDraw &o, int lane)
+// Many open draws: the sums of p and of q anew, in binary64, a part to a workgroup of two waves;
+constexpr int kOpenThreads = 128;
+__global__ __launch_bounds__(kOpenThreads) void verify_resum_kernel(VerifyLaunch a)
 {
-    Draw d = {};
-    d.from = o.from, d.row = o.row, d.x = o.x, d.t = temper_from(o.T), d.p = row_at(a.logits, a.stride, a.fp32, o.row);
-    const Whole p = whole_row(a.row + (int64_t)o.row * a.parts, a.parts, d.t, lane);
-    d.p_top = p.top, d.p_scale = 1.0 / p.sum;
-    if (o.from == kRest) {
-        const Whole q = whole_row(a.draft_row + (int64_t)o.row * a.parts, a.parts, d.t, lane);
-        d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
-    }
-    return d;
-}
-
-// What is left of each part of p - q.
-__global__ __launch_bounds__(kVerifyThreads) void verify_rest_kernel(VerifyLaunch a)
-{
-    const int lane = threadIdx.x & 63;
-    every_item(a, [&](const OpenDraw &o, int k) {
+    every_item(a, [&](const OpenDraw &o, OpenDraw &, int k) {
+        const Temper t = temper_from(o.T);
+        const int begin = k * a.part_len, end = part_end(a, k);
+        const RowPart p = part_of<true, kOpenThreads>(row_at(a.logits, a.stride, a.fp32, o.row), a.fp32, begin, end, t);
+        if (threadIdx.x == 0) a.row[(int64_t)o.row * a.parts + k] = p;
         if (o.from != kRest) return;
-        const Draw d = open_draw(a, o, lane);
+        const RowPart q = part_of<true, kOpenThreads>(row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row), a.draft_fp32, begin, end, t);
+        if (threadIdx.x == 0) a.draft_row[(int64_t)o.row * a.parts + k] = q;
+    });
+}
+// what is left of each part of p - q;
+__global__ __launch_bounds__(kOpenThreads) void verify_left_kernel(VerifyLaunch a)
+{
+    __shared__ double sums[kOpenThreads / 64];
+    const int tid = threadIdx.x;
+    every_item(a, [&](const OpenDraw &o, OpenDraw &, int k) {
+        if (o.from != kRest) return;
+        const Opened r = open_draw(a, o, tid & 63);
         const int end = part_end(a, k);
         double sum = 0.0, w[kVec];
         float x[kVec];
-        for (int i = k * a.part_len + lane * kVec; i < end; i += 64 * kVec) {
-            weights_at(w, x, a, d, i, end);
+        for (int i = k * a.part_len + tid * kVec; i < end; i += kOpenThreads * kVec) {
+            weights_at(w, x, a, r.d, i, end);
 #pragma unroll
             for (int j = 0; j < kVec; j++) sum += w[j];
         }
         sum = wave_sum(sum);
-        if (lane == 0) a.rest[(int64_t)o.row * a.parts + k] = sum;
+        if ((tid & 63) == 0) sums[tid >> 6] = sum;
+        __syncthreads();
+        if (tid == 0) a.rest[(int64_t)o.row * a.parts + k] = sums[0] + sums[1];
     });
 }
-
-// The tokens of the open draws, a workgroup each.
+// and the tokens, a draw to a workgroup.
 __global__ __launch_bounds__(kDrawThreads) void verify_close_kernel(VerifyLaunch a)
 {
-    const int n = a.opened[0];
-    if ((int)blockIdx.x >= n) return;
+    __shared__ DrawLds lds;
     const OpenDraw o = a.open[blockIdx.x];
-    const Draw d = open_draw(a, o, threadIdx.x & 63);
-    finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, draw(a, d, number_of(a, o.b), 0.0));
+    if ((int)blockIdx.x >= a.opened[0]) return;
+    Opened r = open_draw(a, o, threadIdx.x & 63);
+    const double *const sums = a.rest + (int64_t)o.row * a.parts;
+    close_draw(a, o, r, [&](int k) { return sums[k]; }, lds);
 }
 
 // Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
@@ -761,8 +871,8 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, voi
     const size_t parts = (size_t)a.R * a.parts;
     a.row = (RowPart *)take(parts * sizeof(RowPart));
     if (drafted) a.draft_row = (RowPart *)take(parts * sizeof(RowPart));
-    if (drafted) a.rest = (double *)take(parts * sizeof(double));
     if (drafted || !a.exact) {
+        a.rest = (double *)take(parts * sizeof(double));
         a.opened = (int32_t *)take(sizeof(int32_t));
         a.open = (OpenDraw *)take((size_t)a.B * sizeof(OpenDraw));
     }
@@ -778,8 +888,8 @@ bool verify_fits(const VerifyLaunch &a, bool drafted)
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
 {
     const unsigned rows = (unsigned)a.R * (unsigned)a.parts * (a.draft ? 2u : 1u), each = kVerifyThreads / 64;
-    const int64_t items = ((int64_t)a.B * a.parts + each - 1) / each, most = 8 * a.num_cus;
-    const dim3 seqs((unsigned)a.B), threads(kDrawThreads), open((unsigned)(items < most ? items : most)), open_threads(kVerifyThreads);
+    const int64_t items = (int64_t)a.B * a.parts, most = 2 * a.num_cus, lots = 16 * a.num_cus;
+    const dim3 seqs((unsigned)a.B), threads(kDrawThreads), open((unsigned)(items < most ? items : most)), many((unsigned)(items < lots ? items : lots));
     if (a.R > 0) {
         const dim3 grid(a.alone ? (rows + each - 1) / each : rows);
         if (a.exact && a.alone) hipLaunchKernelGGL((verify_rows_kernel<true, true>), grid, dim3(kVerifyThreads), 0, s, a);
@@ -792,9 +902,13 @@ hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
     if (a.exact) hipLaunchKernelGGL(verify_draw_kernel<true>, seqs, threads, 0, s, a);
     else hipLaunchKernelGGL(verify_draw_kernel<false>, seqs, threads, 0, s, a);
     if (!a.opened || a.R == 0) return hipGetLastError();        // (nothing is left open)
-    if (!a.exact) hipLaunchKernelGGL(verify_resum_kernel, open, open_threads, 0, s, a);
-    if (a.draft) hipLaunchKernelGGL(verify_rest_kernel, open, open_threads, 0, s, a);
-    hipLaunchKernelGGL(verify_close_kernel, seqs, threads, 0, s, a);
+    if (!a.draft) hipLaunchKernelGGL(verify_again_kernel, open, threads, 0, s, a);
+    else if (a.exact) hipLaunchKernelGGL(verify_rest_kernel, open, threads, 0, s, a);
+    else {
+        hipLaunchKernelGGL(verify_resum_kernel, many, dim3(kOpenThreads), 0, s, a);
+        hipLaunchKernelGGL(verify_left_kernel, many, dim3(kOpenThreads), 0, s, a);
+        hipLaunchKernelGGL(verify_close_kernel, seqs, threads, 0, s, a);
+    }
     return hipGetLastError();
 }
 
