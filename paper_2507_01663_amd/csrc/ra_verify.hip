@@ -229,13 +229,12 @@ template <bool EXACT> __device__ __forceinline__ RowPart wave_part(const Met<EXA
 }
 
 // A part of a row by a workgroup.
-template <bool EXACT, int THREADS, bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int begin, int end, const Temper &t)
+template <bool EXACT, int THREADS> __device__ __forceinline__ RowPart block_part(const Met<EXACT> &met, const Temper &t)
 {
     constexpr int WAVES = THREADS / 64;
     __shared__ float tops[WAVES];
     __shared__ RowPart sums[WAVES];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const Met<EXACT> met = meet_all<EXACT, THREADS>(row, begin, end, t, tid);
     float all = wave_top(met.top);
     if (lane == 0) tops[wave] = all;
     __syncthreads();
@@ -250,6 +249,10 @@ template <bool EXACT, int THREADS, bool FP32> __device__ RowPart part_of_row(con
     for (int w = 1; w < WAVES; w++) r.sum += sums[w].sum, r.first = sums[w].first < r.first ? sums[w].first : r.first;
     __syncthreads();
     return r;
+}
+template <bool EXACT, int THREADS, bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int begin, int end, const Temper &t)
+{
+    return block_part<EXACT, THREADS>(meet_all<EXACT, THREADS>(row, begin, end, t, threadIdx.x), t);
 }
 
 // The sequence that row t belongs to: the number of those whose rows end at or before it, by 64 looks at a time.
@@ -289,16 +292,15 @@ template <bool EXACT> __device__ __forceinline__ RowPart part_by_wave(const uint
 }
 __device__ __forceinline__ int part_end(const VerifyLaunch &a, int k) { return k + 1 < a.parts ? (k + 1) * a.part_len : a.V; }
 
-// A part of a target row, or of the draft's row that belongs to it, for each workgroup, or for each of its waves (ALONE): the target's rows
-// come first.
-template <bool EXACT, bool ALONE> __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
+// A part of a target row, or of the draft's row that belongs to it, for each wave: the target's rows come first.
+template <bool EXACT> __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
 {
     const int lane = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.opened) a.opened[0] = 0;
-    const unsigned n = __builtin_amdgcn_readfirstlane(ALONE ? blockIdx.x * (kVerifyThreads / 64) + threadIdx.x / 64 : blockIdx.x);
+    const unsigned n = __builtin_amdgcn_readfirstlane(blockIdx.x * (kVerifyThreads / 64) + threadIdx.x / 64);
     const unsigned rows = n / (unsigned)a.parts, k = n % (unsigned)a.parts;
     const bool drafted = rows >= (unsigned)a.R;
-    if (ALONE && rows >= (unsigned)a.R * (a.draft ? 2u : 1u)) return;
+    if (rows >= (unsigned)a.R * (a.draft ? 2u : 1u)) return;
     const int t = (int)(drafted ? rows - a.R : rows);
     const int b = sequence_of_row(a, t, lane);
     if (b >= a.B || t < a.cu[b]) return;
@@ -309,10 +311,37 @@ template <bool EXACT, bool ALONE> __global__ __launch_bounds__(kVerifyThreads) v
         if (t + 1 >= a.cu[b + 1] || d < 0 || temper.c == 0.0) return;
         at = row_at(a.draft, a.draft_stride, a.draft_fp32, d);
     }
-    const int begin = k * a.part_len, end = part_end(a, k), fp32 = drafted ? a.draft_fp32 : a.fp32;
-    const RowPart r = ALONE ? part_by_wave<EXACT>(at, fp32, begin, end, temper) : part_of<EXACT, kVerifyThreads>(at, fp32, begin, end, temper);
-    if (ALONE ? lane : threadIdx.x) return;
-    (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
+    const RowPart r = part_by_wave<EXACT>(at, drafted ? a.draft_fp32 : a.fp32, k * a.part_len, part_end(a, k), temper);
+    if (lane == 0) (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
+}
+
+// The same for each workgroup, where there are few: a thread has two loads of a part at most, and a target's are asked for before it is
+// known whose row it is.
+__global__ __launch_bounds__(kVerifyThreads) void verify_few_rows_kernel(VerifyLaunch a)
+{
+    const int tid = threadIdx.x, lane = tid & 63;
+    if (blockIdx.x == 0 && tid == 0 && a.opened) a.opened[0] = 0;
+    const unsigned rows = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
+    const bool drafted = rows >= (unsigned)a.R;
+    const int t = (int)(drafted ? rows - a.R : rows), end = part_end(a, k), i = k * a.part_len + tid * kVec, j = i + kVerifyThreads * kVec;
+    float x[kVec], y[kVec];
+    auto load = [&](const uint8_t *at, int fp32) {
+        if (fp32) Row<true>{at}.load_some(x, i, end), Row<true>{at}.load_some(y, j, end);
+        else Row<false>{at}.load_some(x, i, end), Row<false>{at}.load_some(y, j, end);
+    };
+    if (!drafted) load(row_at(a.logits, a.stride, a.fp32, t), a.fp32);
+    const int b = sequence_of_row(a, t, lane);
+    if (b >= a.B || t < a.cu[b]) return;
+    const Temper temper = temper_of(a, b);
+    if (drafted) {
+        const int64_t d = draft_row_of(a, b, t);
+        if (t + 1 >= a.cu[b + 1] || d < 0 || temper.c == 0.0) return;
+        load(row_at(a.draft, a.draft_stride, a.draft_fp32, d), a.draft_fp32);
+    }
+    Met<true> met;
+    met.meet(x, i, temper, temper.c == 0.0), met.meet(y, j, temper, temper.c == 0.0);
+    const RowPart r = block_part<true, kVerifyThreads>(met, temper);
+    if (tid == 0) (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
 }
 
 // ---- decisions ----------------------------------------------------------------------------------------
@@ -891,11 +920,10 @@ hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
     const int64_t items = (int64_t)a.B * a.parts, most = 2 * a.num_cus, lots = 16 * a.num_cus;
     const dim3 seqs((unsigned)a.B), threads(kDrawThreads), open((unsigned)(items < most ? items : most)), many((unsigned)(items < lots ? items : lots));
     if (a.R > 0) {
-        const dim3 grid(a.alone ? (rows + each - 1) / each : rows);
-        if (a.exact && a.alone) hipLaunchKernelGGL((verify_rows_kernel<true, true>), grid, dim3(kVerifyThreads), 0, s, a);
-        else if (a.exact) hipLaunchKernelGGL((verify_rows_kernel<true, false>), grid, dim3(kVerifyThreads), 0, s, a);
-        else if (a.alone) hipLaunchKernelGGL((verify_rows_kernel<false, true>), grid, dim3(kVerifyThreads), 0, s, a);
-        else hipLaunchKernelGGL((verify_rows_kernel<false, false>), grid, dim3(kVerifyThreads), 0, s, a);
+        const dim3 grid((rows + each - 1) / each);
+        if (!a.exact) hipLaunchKernelGGL(verify_rows_kernel<false>, grid, dim3(kVerifyThreads), 0, s, a);
+        else if (a.alone) hipLaunchKernelGGL(verify_rows_kernel<true>, grid, dim3(kVerifyThreads), 0, s, a);
+        else hipLaunchKernelGGL(verify_few_rows_kernel, dim3(rows), dim3(kVerifyThreads), 0, s, a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
