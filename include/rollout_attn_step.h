@@ -178,13 +178,13 @@ typedef struct {
 
 ra_status rollout_attn_check_verify(const ra_verify *verify, char *msg, size_t msg_len);
 
-/* Bytes of device workspace rollout_attn_verify needs for this shape (only num_seqs, total_rows, vocab, and whether draft_logits
- * is NULL are read).  ctx may be NULL: the size for a 256-compute-unit device is returned. */
+/* Bytes of device workspace rollout_attn_verify needs for this shape (only num_seqs, total_rows, vocab, logits_dtype, and whether
+ * draft_logits is NULL are read).  ctx may be NULL: the size for a 256-compute-unit device is returned. */
 ra_status rollout_attn_verify_workspace_size(const ra_ctx *ctx, const ra_verify *shape_only, size_t *bytes);
 
 /* Enqueues the verification on hip_stream: two kernels, in large batches three or four.  The environment's
- * ROLLOUT_ATTN_VERIFY_FEW=n, read by rollout_attn_create, is the number of logits (target's and draft model's) up to which all sums
- * are binary64 from the start.  workspace as for rollout_attn_decode: dev memory of at least
+ * ROLLOUT_ATTN_VERIFY_FEW=n, read by rollout_attn_create, is the number of bf16 logits up to which all sums are binary64 from the
+ * start; of binary32 logits, and of logits with a draft model's (both counted), three times as many, of both together five times.  workspace as for rollout_attn_decode: dev memory of at least
  * rollout_attn_verify_workspace_size() bytes, 256-byte aligned, contents irrelevant on entry and undefined afterwards; calls
  * that overlap in time need distinct workspaces. */
 ra_status rollout_attn_verify(ra_ctx *ctx, const ra_verify *verify, void *workspace, size_t workspace_bytes, void *hip_stream);

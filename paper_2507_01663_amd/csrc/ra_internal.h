@@ -17,7 +17,7 @@ constexpr int kCostPrefixFp8 = 5;   // ... of an e4m3 pool (32 query rows)
 constexpr int kCostItem = 16;       // ... of a segment, on top of its pages
 constexpr int kCostItemPrefix = 16;    // ... of a shared-prefix row's segment (bf16 pools)
 constexpr int kCostItemPrefixFp8 = 48; // ... (e4m3 pools)
-constexpr int64_t kVerifyFew = 8 << 20; // logits of a verification up to which all its sums are binary64 (see verify_shape)
+constexpr int64_t kVerifyFew = 16 << 20; // bf16 logits of a verification up to which all its sums are binary64 (see verify_shape)
 
 // Device pointers into the caller's workspace.  All offsets are fixed by the shape alone.
 struct Workspace {

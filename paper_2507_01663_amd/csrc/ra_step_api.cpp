@@ -99,7 +99,7 @@ ra_status check_verify(const ra_verify *p, char *msg, size_t n)
 void fill_shape(ra::VerifyLaunch &a, const ra_verify *p)
 {
     memset(&a, 0, sizeof a);
-    a.B = p->num_seqs, a.R = p->total_rows, a.V = p->vocab;
+    a.B = p->num_seqs, a.R = p->total_rows, a.V = p->vocab, a.fp32 = p->logits_dtype == RA_LOGITS_FP32;
 }
 
 template <typename P> void fill_pages(ra::PagesLaunch &a, const P *p)
@@ -170,7 +170,7 @@ ra_status rollout_attn_verify(ra_ctx *c, const ra_verify *p, void *workspace, si
         set_err(c, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);
         return RA_ERR_WORKSPACE_TOO_SMALL;
     }
-    a.fp32 = p->logits_dtype == RA_LOGITS_FP32, a.logits = p->logits, a.stride = p->logits_stride;
+    a.logits = p->logits, a.stride = p->logits_stride;
     if (p->draft_logits) {
         a.draft_fp32 = p->draft_dtype == RA_LOGITS_FP32, a.draft = p->draft_logits, a.draft_stride = p->draft_stride;
         a.total_draft_rows = p->total_draft_rows, a.draft_rows = p->draft_rows;

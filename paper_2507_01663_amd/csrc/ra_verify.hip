@@ -870,15 +870,21 @@ __global__ __launch_bounds__(kDrawThreads) void verify_close_kernel(VerifyLaunch
 }
 
 // Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
-// Whether all sums are binary64 from the start: where that costs less than the two kernels for the draws that binary32 leaves open.
+// A row's parts go to a wave each where those are six for every compute unit, to a workgroup each where there are fewer.  (us of a
+// call, waves and workgroups: 1 216 parts 14.1, 13.1; 1 824 parts 14.5, 15.4; 3 840 24.3, 26.7.)
+// Whether all sums are binary64 from the start: binary32 sums are three times as fast, but leave draws open, which take another kernel (9
+// us), or three (35 us) with a draft model; and they wait for memory, twice as long where logits are binary32.  (us of a call, binary64
+// and binary32 first.  One row of 152 064 for a sequence: bf16, 9.7 million values 16.8 and 21.4, 14.6 20.6 and 16.4, 38.9 36.7 and
+// 31.5; binary32, 19.5 24.1 and 30.1, 38.9 40.5 and 41.7.  Five rows and a draft model's: bf16, 36.5 47.1 and 47.6, 48.7 58.0 and 53.2;
+// binary32, 73.0 75.5 and 77.3, 97.3 115 and 98.)
 static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted)
 {
     const int64_t rows = (int64_t)a.R * (drafted ? 2 : 1);
     a.num_cus = num_cus;
     a.part_len = kDrawThreads * kVec;
     a.parts = (a.V + a.part_len - 1) / a.part_len;
-    a.alone = rows * a.parts >= (int64_t)num_cus * 16;
-    a.exact = rows * a.V <= few;
+    a.alone = rows * a.parts >= (int64_t)num_cus * 6;
+    a.exact = rows * a.V <= few * (drafted && a.fp32 ? 5 : drafted || a.fp32 ? 3 : 1);
     // The error of a sum of weights as weight32 gives them, in parts of the row's whole sum W: a weight w is off by (3 ln 2 |y| + 2) 2^-24
     // of it and a sum of eight by 3 2^-24; y is against the thread's value, which is at most 8 / c below one it met: |y| is at most 8
     // more than against the row's largest.  Against that, log2(W) + sum(w |y|) / W is the entropy of the row in bits, at most log2(V),
