@@ -7,41 +7,34 @@
 // new tokens, so the token that begins a page also writes it into the table.
 #include "ra_device.h"
 #include "ra_step.h"
+#include "ra_wave.h"
 
 namespace ra {
 
 constexpr int kTileSeqs = 1024, kTileWaves = kTileSeqs / 64;
 
-// Inclusive sums over the 1024 threads of a workgroup, on top of what was carried in; the new totals are carried out.
+// Inclusive sums over the 1024 threads of a workgroup, on top of what was carried in; the new totals are carried out.  (Tokens of sequences
+// that a table has room for are fewer than 2^35: whole numbers of binary64.)
 struct TwoSums {
     int32_t pages;
-    int64_t tokens;
+    double tokens;
 };
 struct ScanLds {
     int32_t pages[kTileWaves];
-    int64_t tokens[kTileWaves];
+    double tokens[kTileWaves];
 };
 __device__ __forceinline__ TwoSums scan(TwoSums x, TwoSums &carry, ScanLds &lds)
 {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int32_t p = __shfl_up(x.pages, d);
-        const int64_t t = __shfl_up((long long)x.tokens, d);
-        if (lane >= d) x.pages += p, x.tokens += t;
-    }
+    x.pages = wave_scan(x.pages), x.tokens = wave_scan(x.tokens);
     if (lane == 63) lds.pages[wave] = x.pages, lds.tokens[wave] = x.tokens;
     __syncthreads();
-    TwoSums before = carry, all = carry;
+    TwoSums all = carry;
 #pragma unroll
     for (int w = 0; w < kTileWaves; w++) {
-        const int32_t p = lds.pages[w];
-        const int64_t t = lds.tokens[w];
-        if (w < wave) before.pages += p, before.tokens += t;
-        all.pages += p, all.tokens += t;
+        if (w == wave) x.pages += all.pages, x.tokens += all.tokens;
+        all.pages += lds.pages[w], all.tokens += lds.tokens[w];
     }
-    __syncthreads();
-    x.pages += before.pages, x.tokens += before.tokens;
     carry = all;
     return x;
 }
@@ -81,16 +74,32 @@ __device__ __forceinline__ int64_t first_block(int x)
     return (int64_t)b + (blockIdx.x >= mine ? blockIdx.x - mine : blockIdx.x + n - mine);
 }
 
+constexpr int kOwn = 4; // a sequence with so few new tokens places them itself, where all of a tile have no more
+
 // TOKENS: the tokens are placed, by workgroups that share the tokens in blocks of 1024; STATE: the new lengths, counts and
 // offsets are written.  Both at once only with one workgroup: lengths and counts may be written where they are read.
 template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void place_kernel(PagesLaunch a)
 {
-    __shared__ ScanLds sums;
+    __shared__ ScanLds sums[2];
     __shared__ int32_t first[kTileSeqs];                        // tokens before the sequence
     __shared__ int4 row[kTileSeqs];                             // {tokens held, pages held, pages with the group's, stack's entry of the first taken}
     __shared__ int32_t listed[kTileSeqs];                       // where its group's pages are
     const int tid = threadIdx.x, free = stack_height(a);
-    TwoSums wanted = {0, 0}, given = {0, 0};
+    TwoSums wanted = {0, 0.0}, given = {0, 0.0};
+    auto put = [&](int64_t b, int place, const int4 &r, int at, int t) {
+        const int i = place / kPage;
+        int32_t *const entries = a.table + b * a.max_pages;
+        int page;
+        if (i < r.y) page = entries[i];
+        else if (i < r.z) page = a.pfx_pages[at + i];
+        else {
+            page = a.stack[r.w - (i - r.z)];
+            if (place % kPage == 0) entries[i] = page;
+        }
+        if (a.positions) a.positions[t] = place;
+        if (a.slots) a.slots[t] = (int64_t)page * kPage + place % kPage;
+        if (a.seqs) a.seqs[t] = (int32_t)b;
+    };
     for (int base = 0; base < a.B; base += kTileSeqs) {
         const int b = base + tid;
         int L = 0, n = 0, H = 0, F = 0, at = 0;
@@ -99,49 +108,44 @@ template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void 
         const int64_t end = (int64_t)L + n;
         const int64_t P = (end + kPage - 1) / kPage;
         const bool fine = n > 0 && L >= 0 && H >= 0 && S <= a.max_pages && P <= a.max_pages && L <= (int64_t)kPage * S;
-        TwoSums mine = {0, 0};
-        if (fine) mine = {P > S ? (int32_t)P - S : 0, n};
-        const TwoSums upto = scan(mine, wanted, sums);
+        const TwoSums was = given;
+        TwoSums mine = {0, 0.0};
+        if (fine) mine = {P > S ? (int32_t)P - S : 0, (double)n};
+        const TwoSums upto = scan(mine, wanted, sums[0]);
         const bool served = fine && (mine.pages == 0 || upto.pages <= free) && upto.tokens <= a.T;
-        if (!served) mine = {0, 0};
-        const TwoSums incl = scan(mine, given, sums);
+        TwoSums incl = upto;
+        if (wanted.pages > free || wanted.tokens > a.T) {       // (else all are served, so far, and these are the sums)
+            if (!served) mine = {0, 0.0};
+            incl = scan(mine, given, sums[1]);
+        } else given = wanted;
         const int32_t cu = (int32_t)(incl.tokens - mine.tokens);
         if (STATE && b < a.B) {
             a.cu[b] = cu;
-            a.lens_out[b] = L + (int32_t)mine.tokens;
+            a.lens_out[b] = served ? L + n : L;
             a.held_out[b] = served && P > S ? (int32_t)P : served ? S : H;
         }
         if (TOKENS) {
-            const int top = free - 1 - (incl.pages - mine.pages);
-            first[tid] = cu, row[tid] = make_int4(L, H, S, top), listed[tid] = at;
-            __syncthreads();
-            const int t0 = first[0], t1 = (int)given.tokens;
+            const int4 r = make_int4(L, H, S, free - 1 - (incl.pages - mine.pages));
+            const int t0 = (int)was.tokens, t1 = (int)given.tokens;
             if (served && F > H && (cu / kTileSeqs) % gridDim.x == blockIdx.x)
                 for (int i = H; i < F; i++) a.table[(int64_t)b * a.max_pages + i] = a.pfx_pages[at + i];
-            for (int64_t blk = first_block(t0); blk * kTileSeqs < t1; blk += gridDim.x) {
-                const int64_t at64 = blk * kTileSeqs + tid;
-                if (at64 < t0 || at64 >= t1) continue;
-                const int t = (int)at64;
-                const int s = owner(first, t);
-                const int4 r = row[s];
-                const int place = r.x + t - first[s], i = place / kPage;
-                int32_t *const entries = a.table + (int64_t)(base + s) * a.max_pages;
-                int page;
-                if (i < r.y) page = entries[i];
-                else if (i < r.z) page = a.pfx_pages[listed[s] + i];
-                else {
-                    page = a.stack[r.w - (i - r.z)];
-                    if (place % kPage == 0) entries[i] = page;
-                }
-                if (a.positions) a.positions[t] = place;
-                if (a.slots) a.slots[t] = (int64_t)page * kPage + place % kPage;
-                if (a.seqs) a.seqs[t] = base + s;
+            if (t1 - t0 <= kTileSeqs && gridDim.x == 1 && __syncthreads_and(n <= kOwn || !served)) {
+                for (int i = 0; served && i < n; i++) put(b, L + i, r, at, cu + i);
+                continue;
             }
+            first[tid] = cu, row[tid] = r, listed[tid] = at;
             __syncthreads();
+            for (int64_t blk = first_block(t0); blk * kTileSeqs < t1; blk += gridDim.x) {
+                const int64_t t = blk * kTileSeqs + tid;
+                if (t < t0 || t >= t1) continue;
+                const int s = owner(first, (int)t);
+                put(base + s, row[s].x + (int)t - first[s], row[s], listed[s], (int)t);
+            }
         }
+        if (base + kTileSeqs < a.B) __syncthreads();
     }
     if (TOKENS)
-        for (int64_t t = given.tokens + (int64_t)blockIdx.x * kTileSeqs + tid; t < a.T; t += (int64_t)gridDim.x * kTileSeqs) {
+        for (int64_t t = (int64_t)given.tokens + (int64_t)blockIdx.x * kTileSeqs + tid; t < a.T; t += (int64_t)gridDim.x * kTileSeqs) {
             if (a.positions) a.positions[t] = -1;
             if (a.slots) a.slots[t] = -1;
             if (a.seqs) a.seqs[t] = -1;
@@ -154,7 +158,7 @@ template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void r
     __shared__ ScanLds sums;
     __shared__ int32_t first[kTileSeqs], begin[kTileSeqs];      // pages before the sequence's, and its first that goes back
     const int tid = threadIdx.x, free = stack_height(a);
-    TwoSums back = {0, 0};
+    TwoSums back = {0, 0.0};
     for (int base = 0; base < a.B; base += kTileSeqs) {
         const int b = base + tid, before = back.pages;
         int keep = 0, H = 0, F = 0, at;
@@ -162,7 +166,7 @@ template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void r
         const int kept = keep > 0 ? (int)(((int64_t)keep + kPage - 1) / kPage) : 0, K = kept < H ? kept : H;
         const bool fine = H >= 0 && H <= a.max_pages;
         const int from = K > F ? K : F;
-        const TwoSums mine = {fine && from < H ? H - from : 0, 0};
+        const TwoSums mine = {fine && from < H ? H - from : 0, 0.0};
         const TwoSums incl = scan(mine, back, sums);
         if (STATE && b < a.B) a.held_out[b] = fine ? K : H;
         if (PAGES) {
@@ -176,8 +180,8 @@ template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void r
                 const int64_t to = (int64_t)free + e;
                 if (to < a.num_pages) a.stack[to] = a.table[(int64_t)(base + s) * a.max_pages + begin[s] + e - first[s]];
             }
-            __syncthreads();
         }
+        if (base + kTileSeqs < a.B) __syncthreads();
     }
     if (STATE && tid == 0) a.free_out[0] = (int64_t)free + back.pages < a.num_pages ? free + back.pages : a.num_pages;
 }

@@ -5,6 +5,7 @@
 // changes one token in a few hundred; so weights, sums and comparisons are binary64, at the same rate as binary32 on this machine.
 #include "ra_device.h"
 #include "ra_step.h"
+#include "ra_wave.h"
 
 namespace ra {
 
@@ -69,24 +70,6 @@ __device__ __forceinline__ double rescale(float from, float to, const Temper &t)
     return power(__builtin_fmax((double)from - (double)to, t.low), t.c);
 }
 
-// Over the lanes of a wave by steps inside the vector unit: rows of sixteen lanes, then the last lane of a row to the next, then of the
-// lower half to the upper.
-template <int CTRL, int ROWS> __device__ __forceinline__ int from_lane(int x, int none) { return __builtin_amdgcn_update_dpp(none, x, CTRL, ROWS, 0xf, false); }
-template <int CTRL, int ROWS> __device__ __forceinline__ double from_lane(double x)
-{
-    const int2 w = {__double2loint(x), __double2hiint(x)};
-    return __hiloint2double(from_lane<CTRL, ROWS>(w.y, 0), from_lane<CTRL, ROWS>(w.x, 0));
-}
-__device__ __forceinline__ double wave_scan(double x)           // the sum up to this lane, itself included
-{
-    x += from_lane<0x111, 0xf>(x);
-    x += from_lane<0x112, 0xf>(x);
-    x += from_lane<0x114, 0xf>(x);
-    x += from_lane<0x118, 0xf>(x);
-    x += from_lane<0x142, 0xa>(x);
-    x += from_lane<0x143, 0xc>(x);
-    return x;
-}
 __device__ __forceinline__ double last_lane(double x)
 {
     return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(x), 63), __builtin_amdgcn_readlane(__double2loint(x), 63));
