@@ -86,7 +86,7 @@ typedef struct {
  * before touching the device.  msg (may be NULL) receives a NUL-terminated explanation. */
 ra_status rollout_attn_check_place(const ra_place *place, char *msg, size_t msg_len);
 
-/* Enqueues the placing: one kernel, two where many tokens may come. */
+/* Enqueues the placing: one kernel; two where many tokens may come and lengths or counts are written where they are read. */
 ra_status rollout_attn_place(ra_ctx *ctx, const ra_place *place, void *hip_stream);
 
 /*
@@ -115,7 +115,7 @@ typedef struct {
 
 ra_status rollout_attn_check_release(const ra_release *release, char *msg, size_t msg_len);
 
-/* Enqueues the release: one kernel, two where many pages may come back. */
+/* Enqueues the release: one kernel; two where many pages may come back and counts are written where they are read. */
 ra_status rollout_attn_release(ra_ctx *ctx, const ra_release *release, void *hip_stream);
 
 typedef enum { RA_LOGITS_BF16 = 0, RA_LOGITS_FP32 = 1 } ra_logits_dtype;

@@ -76,8 +76,8 @@ __device__ __forceinline__ int64_t first_block(int x)
 
 constexpr int kOwn = 4; // a sequence with so few new tokens places them itself, where all of a tile have no more
 
-// TOKENS: the tokens are placed, by workgroups that share the tokens in blocks of 1024; STATE: the new lengths, counts and
-// offsets are written.  Both at once only with one workgroup: lengths and counts may be written where they are read.
+// TOKENS: the tokens are placed, by workgroups that share the tokens in blocks of 1024; STATE: the first workgroup writes the
+// new lengths, counts and offsets.  Both at once with one workgroup alone, or where no other reads what that writes.
 template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void place_kernel(PagesLaunch a)
 {
     __shared__ ScanLds sums[2];
@@ -119,7 +119,7 @@ template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void 
             incl = scan(mine, given, sums[1]);
         } else given = wanted;
         const int32_t cu = (int32_t)(incl.tokens - mine.tokens);
-        if (STATE && b < a.B) {
+        if (STATE && b < a.B && blockIdx.x == 0) {
             a.cu[b] = cu;
             a.lens_out[b] = served ? L + n : L;
             a.held_out[b] = served && P > S ? (int32_t)P : served ? S : H;
@@ -150,7 +150,7 @@ template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void 
             if (a.slots) a.slots[t] = -1;
             if (a.seqs) a.seqs[t] = -1;
         }
-    if (STATE && tid == 0) a.cu[a.B] = (int32_t)given.tokens, a.free_out[0] = free - given.pages;
+    if (STATE && tid == 0 && blockIdx.x == 0) a.cu[a.B] = (int32_t)given.tokens, a.free_out[0] = free - given.pages;
 }
 
 template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void release_kernel(PagesLaunch a)
@@ -168,7 +168,7 @@ template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void r
         const int from = K > F ? K : F;
         const TwoSums mine = {fine && from < H ? H - from : 0, 0.0};
         const TwoSums incl = scan(mine, back, sums);
-        if (STATE && b < a.B) a.held_out[b] = fine ? K : H;
+        if (STATE && b < a.B && blockIdx.x == 0) a.held_out[b] = fine ? K : H;
         if (PAGES) {
             first[tid] = incl.pages - mine.pages, begin[tid] = from;
             __syncthreads();
@@ -183,43 +183,43 @@ template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void r
         }
         if (base + kTileSeqs < a.B) __syncthreads();
     }
-    if (STATE && tid == 0) a.free_out[0] = (int64_t)free + back.pages < a.num_pages ? free + back.pages : a.num_pages;
+    if (STATE && tid == 0 && blockIdx.x == 0) a.free_out[0] = (int64_t)free + back.pages < a.num_pages ? free + back.pages : a.num_pages;
 }
 
-// Workgroups that share n tokens (or pages): one up to kAlone of them, which then writes the state too; else one for each kEach and a
-// kernel for the state, since lengths and counts may be written where the others still read them.
-constexpr int kAlone = 4096, kEach = 2048;
+// Workgroups that share n tokens (or pages): one up to kAlone of them, else one for each 1024.  The first writes the state too, unless it is
+// written where the others still read it: then a kernel of its own does.
+constexpr int kAlone = 4096;
 static unsigned workgroups(int64_t n, int num_cus)
 {
-    const int64_t w = (n + kEach - 1) / kEach;
+    const int64_t w = (n + kTileSeqs - 1) / kTileSeqs;
     return n <= kAlone ? 1u : w < num_cus ? (unsigned)w : (unsigned)num_cus;
 }
 
 hipError_t launch_place(const PagesLaunch &a, int num_cus, hipStream_t s)
 {
-    const unsigned n = workgroups(a.T, num_cus);
-    if (n == 1) {
-        hipLaunchKernelGGL((place_kernel<true, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+    const dim3 n(workgroups(a.T, num_cus)), threads(kTileSeqs);
+    if (n.x == 1 || (a.lens_out != a.lens && a.held_out != a.held && a.free_out != a.free_count)) {
+        hipLaunchKernelGGL((place_kernel<true, true>), n, threads, 0, s, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((place_kernel<true, false>), dim3(n), dim3(kTileSeqs), 0, s, a);
+    hipLaunchKernelGGL((place_kernel<true, false>), n, threads, 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((place_kernel<false, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+    hipLaunchKernelGGL((place_kernel<false, true>), dim3(1), threads, 0, s, a);
     return hipGetLastError();
 }
 
 hipError_t launch_release(const PagesLaunch &a, int num_cus, hipStream_t s)
 {
-    const unsigned n = workgroups((int64_t)a.B * a.max_pages, num_cus);
-    if (n == 1) {
-        hipLaunchKernelGGL((release_kernel<true, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+    const dim3 n(workgroups((int64_t)a.B * a.max_pages, num_cus)), threads(kTileSeqs);
+    if (n.x == 1 || (a.held_out != a.held && a.free_out != a.free_count)) {
+        hipLaunchKernelGGL((release_kernel<true, true>), n, threads, 0, s, a);
         return hipGetLastError();
     }
-    hipLaunchKernelGGL((release_kernel<true, false>), dim3(n), dim3(kTileSeqs), 0, s, a);
+    hipLaunchKernelGGL((release_kernel<true, false>), n, threads, 0, s, a);
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    hipLaunchKernelGGL((release_kernel<false, true>), dim3(1), dim3(kTileSeqs), 0, s, a);
+    hipLaunchKernelGGL((release_kernel<false, true>), dim3(1), threads, 0, s, a);
     return hipGetLastError();
 }
 
