@@ -583,7 +583,8 @@ def place_from_tensors(seq_lens, new_tokens, held, block_table, free_pages, free
     """Fills a ra_place from device tensors, int32 but for slots (int64): seq_lens, new_tokens, held, lens_out, held_out [n];
     block_table [n,max_pages]; free_pages [num_pages]; free_count, free_count_out [1]; cu_seqlens [n+1]; positions, slots and seqs
     [total_tokens] (each may be None); total_tokens: the bound on the new tokens (None: the length of positions, slots or seqs, or what
-    the table has room for); the group hint as for problem_from_tensors."""
+    the table has room for); the group hint as for problem_from_tensors.  The descriptor keeps the tensors: one that was made for the
+    call alone lives until it is enqueued (a workspace made on the way could lie where it was)."""
     import torch
     p = ra_place()
     p.num_seqs, p.page_size, p.num_pages = seq_lens.numel(), page_size, free_pages.numel()
@@ -606,12 +607,15 @@ def place_from_tensors(seq_lens, new_tokens, held, block_table, free_pages, free
     _fill_groups(p, seq_group, prefix_page_offsets)
     if seq_group is not None:
         p.prefix_pages = _int32(prefix_pages, prefix_pages.numel(), "prefix_pages")
+    p.tensors = (seq_lens, new_tokens, held, block_table, free_pages, free_count, cu_seqlens, lens_out, held_out, free_count_out, positions, slots, seqs,
+                 seq_group, prefix_page_offsets, prefix_pages)
     return p
 
 
 def release_from_tensors(keep_lens, held, block_table, free_pages, free_count, held_out, free_count_out, seq_group=None, prefix_page_offsets=None,
                          page_size=16):
-    """Fills a ra_release from device tensors (int32): keep_lens, held, held_out [n]; the rest as for place_from_tensors."""
+    """Fills a ra_release from device tensors (int32): keep_lens, held, held_out [n]; the rest as for place_from_tensors.
+    It keeps the tensors, too."""
     p = ra_release()
     p.num_seqs, p.page_size, p.num_pages = keep_lens.numel(), page_size, free_pages.numel()
     assert block_table.dim() == 2 and block_table.shape[0] == p.num_seqs
@@ -621,6 +625,7 @@ def release_from_tensors(keep_lens, held, block_table, free_pages, free_count, h
     p.block_table = _int32(block_table, block_table.numel(), "block_table")
     p.free_pages, p.free_count, p.free_count_out = _int32(free_pages, p.num_pages, "free_pages"), _int32(free_count, 1, "free_count"), _int32(free_count_out, 1, "free_count_out")
     _fill_groups(p, seq_group, prefix_page_offsets)
+    p.tensors = (keep_lens, held, block_table, free_pages, free_count, held_out, free_count_out, seq_group, prefix_page_offsets)
     return p
 
 
@@ -638,7 +643,7 @@ def verify_from_tensors(logits, cu_rows, tokens, accept_uniform, draw_uniform, a
     """Fills a ra_verify from device tensors: logits bf16 or float32 [R,vocab] (rows any stride apart); cu_rows int32 [n+1]; tokens int32
     [R]; accept_uniform float32 [R]; draw_uniform float32 [n]; accepted, next_tokens int32 [n]; out_tokens int32 [R]; out_logprobs
     float32 [R]; temperature float32 [n] (None: 1); draft_logits like logits (either type) with draft_rows int32 [n], the first row
-    of each sequence there (None: drafts are plain guesses)."""
+    of each sequence there (None: drafts are plain guesses).  The descriptor keeps the tensors, as place_from_tensors' does."""
     import torch
     p = ra_verify()
     p.num_seqs = cu_rows.numel() - 1
@@ -659,6 +664,7 @@ def verify_from_tensors(logits, cu_rows, tokens, accept_uniform, draw_uniform, a
         if not p.total_draft_rows:                           # (torch gives an empty tensor no address, which would say that there are none)
             p.draft_logits, p.draft_stride, p.draft_dtype = p.logits, p.logits_stride, p.logits_dtype
         p.draft_rows = _int32(draft_rows, p.num_seqs, "draft_rows")
+    p.tensors = (logits, cu_rows, tokens, accept_uniform, draw_uniform, accepted, out_tokens, out_logprobs, next_tokens, temperature, draft_logits, draft_rows)
     return p
 
 

@@ -154,3 +154,28 @@ def test_descriptors_refuse_tensors_of_other_shapes():
                 dict(positions=i(4), seqs=i(5)), dict(seq_group=i(1), prefix_page_offsets=i(2), prefix_pages=i(3))):
         with pytest.raises(AssertionError):
             ra.place_from_tensors(**{**good(), **bad})
+
+
+def test_descriptors_keep_their_tensors():
+    """A tensor that is made in the call's arguments must not give its memory back before the call is enqueued: a workspace that the
+    Decoder makes on the way could get it."""
+    import gc
+    import weakref
+    import torch
+    gone = []
+
+    def new(*shape, kind=torch.int32):
+        t = torch.zeros(shape, dtype=kind)
+        weakref.finalize(t, gone.append, 1)
+        return t
+
+    f = lambda *s: new(*s, kind=torch.float32)
+    made = [ra.verify_from_tensors(f(4, 10), new(3), new(4), f(4), f(2), new(2), new(4), f(4), new(2), f(2), f(2, 10), new(2)),
+            ra.place_from_tensors(new(2), new(2), new(2), new(2, 5), new(9), new(1), new(3), new(2), new(2), new(1), new(4), new(4, kind=torch.int64), new(4),
+                                  None, new(2), new(2), new(1)),
+            ra.release_from_tensors(new(2), new(2), new(2, 5), new(9), new(1), new(2), new(1), new(2), new(2))]
+    gc.collect()
+    assert not gone
+    del made
+    gc.collect()
+    assert len(gone) == 12 + 16 + 9
