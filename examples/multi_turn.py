@@ -128,12 +128,12 @@ class Rollout:
         return accepted, following
 
     def draft(self, tokens, count):
-        """`count` tokens behind each of tokens, by the model without attention, and badly (its logits are off by three or so): ([seqs,
+        """`count` tokens behind each of tokens, by the model without attention, and badly (its logits are off by one or two): ([seqs,
         count], the logits they are from)."""
         drafts, logits = [], []
         for _ in range(count):
             sure = self.m.logits(self.m.embedding[tokens.long()])
-            logits.append(sure + 3 * torch.randn(sure.shape, generator=self.g, device=DEV).to(sure.dtype))
+            logits.append(sure + 1.5 * torch.randn(sure.shape, generator=self.g, device=DEV).to(sure.dtype))
             tokens = self.verify(logits[-1])[1]
             drafts.append(tokens)
         return torch.stack(drafts, 1), torch.stack(logits, 1).flatten(0, 1)

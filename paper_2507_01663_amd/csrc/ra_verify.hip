@@ -109,6 +109,14 @@ __device__ __forceinline__ int wave_least(int x)
     return __builtin_amdgcn_readlane(x, 63);
 }
 
+// Sixteen bytes from anywhere an element may lie.
+template <bool FP32> struct Words {
+    typedef uint32_t type __attribute__((ext_vector_type(4), aligned(4)));
+};
+template <> struct Words<false> {
+    typedef uint32_t type __attribute__((ext_vector_type(4), aligned(2)));
+};
+
 template <bool FP32> struct Row {
     const uint8_t *at;
     static constexpr int kBytes = FP32 ? 4 : 2;
@@ -118,13 +126,17 @@ template <bool FP32> struct Row {
         else return __uint_as_float((uint32_t)((const uint16_t *)at)[i] << 16);
     }
     // Values i .. i + 7.  (A row begins at any element: the load is of no alignment but that.)
-    __device__ __forceinline__ void load(float (&x)[kVec], int i) const
+    // STREAM: with the hint that they are read once.
+    template <bool STREAM = false> __device__ __forceinline__ void load(float (&x)[kVec], int i) const
     {
+        typedef typename Words<FP32>::type words;
+        const words *const from = (const words *)(at + (size_t)i * kBytes);
         if constexpr (FP32) {
-            __builtin_memcpy(x, at + (size_t)i * 4, 32);
+            const words w = STREAM ? __builtin_nontemporal_load(from) : *from, v = STREAM ? __builtin_nontemporal_load(from + 1) : from[1];
+#pragma unroll
+            for (int j = 0; j < 4; j++) x[j] = __uint_as_float(w[j]), x[4 + j] = __uint_as_float(v[j]);
         } else {
-            uint32_t w[4];
-            __builtin_memcpy(w, at + (size_t)i * 2, 16);
+            const words w = STREAM ? __builtin_nontemporal_load(from) : *from;
 #pragma unroll
             for (int j = 0; j < 4; j++) x[2 * j] = __uint_as_float(w[j] << 16), x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
         }
@@ -186,7 +198,7 @@ template <bool EXACT, int THREADS, bool FP32> __device__ __forceinline__ Met<EXA
     float x[kVec], y[kVec];
     int i = begin + tid * kVec;
     for (; i + THREADS * kVec < whole; i += 2 * THREADS * kVec) {
-        row.load(x, i), row.load(y, i + THREADS * kVec);
+        row.template load<!EXACT>(x, i), row.template load<!EXACT>(y, i + THREADS * kVec);
         met.meet(x, i, t, greedy), met.meet(y, i + THREADS * kVec, t, greedy);
     }
     if (i < whole) {
