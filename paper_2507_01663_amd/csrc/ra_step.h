@@ -32,8 +32,12 @@ struct RowPart {
 struct OpenDraw {
     int32_t b, from, row, x;     // from: see DrawFrom; x: the draft that was turned down
     int32_t q_row, arrived;      // row of the draft model's logits; workgroups that have added up their part
-    float T, p_top;
-    double p_scale;
+    float T, p_top, q_top;       // the rows' largest, and 1 / their sums as they are known
+    double p_scale, q_scale;
+};
+// Sums over a part of its rows, in binary64 (see verify_left_kernel).
+struct OpenPart {
+    double p, q, more, under, near;
 };
 struct VerifyLaunch {
     int32_t B, R, V, parts, part_len; // a row's parts, and the values of a part
@@ -48,6 +52,7 @@ struct VerifyLaunch {
     double *rest;                // [R][parts]  sums of what open draws are from
     int32_t *opened;             // [1]         open draws
     OpenDraw *open;              // [B]
+    OpenPart *left;              // [B][parts]
     int32_t num_cus;
     int32_t alone;               // a part to a wave, not to a workgroup
     int32_t exact;               // all sums in binary64 from the start

@@ -245,7 +245,7 @@ template <bool EXACT, int THREADS> __device__ __forceinline__ RowPart block_part
     __syncthreads();
     return r;
 }
-template <bool EXACT, int THREADS, bool FP32> __device__ RowPart part_of_row(const Row<FP32> row, int begin, int end, const Temper &t)
+template <bool EXACT, int THREADS, bool FP32> __device__ __forceinline__ RowPart part_of_row(const Row<FP32> row, int begin, int end, const Temper &t)
 {
     return block_part<EXACT, THREADS>(meet_all<EXACT, THREADS>(row, begin, end, t, threadIdx.x), t);
 }
@@ -476,7 +476,7 @@ __device__ __forceinline__ Draw judge_row(const VerifyLaunch &a, int b, int row,
 }
 
 // A whole row, all over again in binary64, by a workgroup of the draws.
-__device__ Whole exact_row(const VerifyLaunch &a, const uint8_t *at, int fp32, const Temper &t)
+__device__ __forceinline__ Whole exact_row(const VerifyLaunch &a, const uint8_t *at, int fp32, const Temper &t)
 {
     const RowPart r = part_of<true, kDrawThreads>(at, fp32, 0, a.V, t);
     return {r.sum, r.top, r.first};
@@ -614,7 +614,7 @@ struct Token {
 };
 // The first value of the border's part at which the running sum of the part's weights passes the border; none where the sum is within `unsure` of
 // the border at it or before it.
-__device__ Token token_of_part(const VerifyLaunch &a, const Draw &d, Border at, double unsure, DrawLds &lds)
+__device__ __forceinline__ Token token_of_part(const VerifyLaunch &a, const Draw &d, Border at, double unsure, DrawLds &lds)
 {
     __shared__ Token token;
     const int tid = threadIdx.x, k = at.part;
@@ -709,7 +709,7 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_dra
     }
     if (d.from == kRest || (!EXACT && token.id < 0 && d.from != kNothing)) {
         // (in any order: draws do not look at each other)
-        if (tid == 0) a.open[atomicAdd(a.opened, 1)] = {b, d.from, d.row, d.x, d.q_row, 0, T, d.p_top, d.p_scale};
+        if (tid == 0) a.open[atomicAdd(a.opened, 1)] = {b, d.from, d.row, d.x, d.q_row, 0, T, d.p_top, d.q_top, d.p_scale, d.q_scale};
     } else finish(a, b, begin, end, d, token);
 }
 
@@ -736,70 +736,44 @@ template <typename F> __device__ __forceinline__ void every_item(const VerifyLau
     OpenDraw o = a.open[at];                                    // (there is one, if of nothing: asked for beside their number)
     const unsigned n = (unsigned)a.opened[0] * (unsigned)a.parts;
     for (unsigned j = blockIdx.x; j < n;) {
-        f(o, a.open[at], (int)k);
+        f(o, (int)at, (int)k);
         j += gridDim.x, at = j / (unsigned)a.parts, k = j % (unsigned)a.parts;
         if (j < n) o = a.open[at];
         __syncthreads();
     }
 }
 
-// The rows of an open draw and their sums; its shares are known by `share`, or by the row's sums where it is from p.  The whole workgroup, and
-// all of it knows the same.
-struct Opened {
-    Draw d;
-    const RowPart *parts;
-    RowPart mine;                // parts[lane]
-};
-__device__ __forceinline__ Opened open_draw(const VerifyLaunch &a, const OpenDraw &o, int lane)
+// An open draw by what the draws' kernel knew of its rows.
+__device__ __forceinline__ Draw open_draw(const VerifyLaunch &a, const OpenDraw &o)
 {
-    const RowPart none = {0.0, -INFINITY, INT32_MAX};
-    Opened r;
-    r.parts = a.row + (int64_t)o.row * a.parts, r.mine = lane < a.parts ? r.parts[lane] : none;
-    r.d = {};
-    r.d.from = o.from, r.d.row = o.row, r.d.x = o.x, r.d.t = temper_from(o.T), r.d.p = row_at(a.logits, a.stride, a.fp32, o.row);
-    if (o.from == kRest) {
-        const RowPart *const qs = a.draft_row + (int64_t)o.row * a.parts;
-        const Whole q = whole_row(qs, lane < a.parts ? qs[lane] : none, a.parts, r.d.t, lane);
-        r.d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row), r.d.q_top = q.top, r.d.q_scale = 1.0 / q.sum;
-    }
-    const Whole p = whole_row(r.parts, r.mine, a.parts, r.d.t, lane);
-    r.d.p_top = p.top, r.d.p_scale = 1.0 / p.sum;
-    return r;
+    Draw d = {};
+    d.from = o.from, d.row = o.row, d.x = o.x, d.q_row = o.q_row, d.t = temper_from(o.T), d.p = row_at(a.logits, a.stride, a.fp32, o.row);
+    d.p_top = o.p_top, d.p_scale = o.p_scale, d.q_top = o.q_top, d.q_scale = o.q_scale;
+    if (o.from == kRest) d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row);
+    return d;
 }
-template <typename F> __device__ __forceinline__ void close_draw(const VerifyLaunch &a, const OpenDraw &o, Opened &r, F share, DrawLds &lds)
+// Its token, by the shares of its row's parts (and of p's parts, where nothing is left of p - q, or without the draft).  The whole workgroup.
+template <typename F, typename G> __device__ __forceinline__ Token close_draw(const VerifyLaunch &a, Draw &d, F share, G share_in_p, double v, DrawLds &lds)
 {
-    const int lane = threadIdx.x & 63;
-    const double v = number_of(a, o.b);
-    auto in_row = [&](int k) { return share_of(k == lane ? r.mine : r.parts[k], r.d); };
     Token token = {-1, 0.f};
-    if (r.d.from == kRowWithout) token = draw_without(a, r.d, in_row, v, 0.0, lds);
-    else if (r.d.from == kRest) token = token_of_part(a, r.d, border_of(share, a.parts, v, lane), 0.0, lds);
-    if (token.id < 0) {                                         // from p, or nothing is left but that
-        r.d.from = kRow;
-        token = token_of_part(a, r.d, border_of(in_row, a.parts, v, lane), 0.0, lds);
-    }
-    finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], r.d, token);
+    if (d.from == kRowWithout) token = draw_without(a, d, share, v, 0.0, lds);
+    else if (d.from == kRest) token = token_of_part(a, d, border_of(share, a.parts, v, threadIdx.x & 63), 0.0, lds);
+    if (token.id >= 0) return token;
+    d.from = kRow;
+    return token_of_part(a, d, border_of(share_in_p, a.parts, v, threadIdx.x & 63), 0.0, lds);
 }
 
 // Few open draws, from p: its sums anew, in binary64; the last workgroup to add up its part draws.
 __global__ __launch_bounds__(kDrawThreads) void verify_again_kernel(VerifyLaunch a)
 {
     __shared__ DrawLds lds;
-    const int lane = threadIdx.x & 63;
-    every_item(a, [&](const OpenDraw &o, OpenDraw &there, int k) {
-        Draw d = {};
-        d.from = o.from, d.row = o.row, d.x = o.x, d.t = temper_from(o.T), d.p = row_at(a.logits, a.stride, a.fp32, o.row), d.p_top = o.p_top, d.p_scale = o.p_scale;
+    every_item(a, [&](const OpenDraw &o, int at, int k) {
+        Draw d = open_draw(a, o);
         const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, k * a.part_len, part_end(a, k), d.t);
         double *const sums = a.rest + (int64_t)o.row * a.parts;
-        if (!last_to_publish(a, there, sums + k, share_of(p, d))) return;
-        const double v = number_of(a, o.b);
+        if (!last_to_publish(a, a.open[at], sums + k, share_of(p, d))) return;
         auto share = [&](int k) { return published(sums + k); };
-        Token token = {-1, 0.f};
-        if (d.from == kRowWithout) token = draw_without(a, d, share, v, 0.0, lds);
-        if (token.id < 0) {                                     // (or nothing is left without the draft)
-            d.from = kRow;
-            token = token_of_part(a, d, border_of(share, a.parts, v, lane), 0.0, lds);
-        }
+        const Token token = close_draw(a, d, share, share, number_of(a, o.b), lds);
         finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, token);
     });
 }
@@ -807,61 +781,106 @@ __global__ __launch_bounds__(kDrawThreads) void verify_again_kernel(VerifyLaunch
 __global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch a)
 {
     __shared__ DrawLds lds;
-    every_item(a, [&](const OpenDraw &o, OpenDraw &there, int k) {
-        Opened r = open_draw(a, o, threadIdx.x & 63);
+    every_item(a, [&](const OpenDraw &o, int at, int k) {
+        Draw d = open_draw(a, o);
         double w[kVec];
         float x[kVec];
-        const double sum = block_sum(weights_of_part(w, x, a, r.d, k), lds);
+        const double sum = block_sum(weights_of_part(w, x, a, d, k), lds);
         double *const sums = a.rest + (int64_t)o.row * a.parts;
-        if (last_to_publish(a, there, sums + k, sum)) close_draw(a, o, r, [&](int k) { return published(sums + k); }, lds);
+        if (!last_to_publish(a, a.open[at], sums + k, sum)) return;
+        const RowPart *const parts = a.row + (int64_t)o.row * a.parts;
+        const Token token = close_draw(a, d, [&](int k) { return published(sums + k); }, [&](int k) { return share_of(parts[k], d); }, number_of(a, o.b), lds);
+        finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, token);
     });
 }
 
-// Many open draws: the sums of p and of q anew, in binary64, a part to a workgroup of two waves;
+// Many open draws, whose sums are binary32: all of it anew, in binary64, and in one pass over p and q, though their scales are only known
+// when it is over.  With a and b the weights of a value by the scales at hand, p = alpha a and q = beta b, alpha and beta within eps of 1:
+//   sum max(p - q, 0) = alpha sum max(a - b, 0) + (alpha - beta) sum_{a > b} b,
+// but for values where p and q are so near each other that the scales decide which is larger, |a - b| < 4 eps b: each is off by 6 eps b
+// at most.  The sum of those b says how much all may be off, which is next to nothing, or where models agree over much of a row, a doubt
+// that verify_close_kernel settles.  A workgroup of two waves has a part.
 constexpr int kOpenThreads = 128;
-__global__ __launch_bounds__(kOpenThreads) void verify_resum_kernel(VerifyLaunch a)
+template <bool FP32, bool QFP32> __device__ __forceinline__ void add_up(OpenPart &s, const Draw &d, double near, int i, int end)
 {
-    every_item(a, [&](const OpenDraw &o, OpenDraw &, int k) {
-        const Temper t = temper_from(o.T);
-        const int begin = k * a.part_len, end = part_end(a, k);
-        const RowPart p = part_of<true, kOpenThreads>(row_at(a.logits, a.stride, a.fp32, o.row), a.fp32, begin, end, t);
-        if (threadIdx.x == 0) a.row[(int64_t)o.row * a.parts + k] = p;
-        if (o.from != kRest) return;
-        const RowPart q = part_of<true, kOpenThreads>(row_at(a.draft, a.draft_stride, a.draft_fp32, o.q_row), a.draft_fp32, begin, end, t);
-        if (threadIdx.x == 0) a.draft_row[(int64_t)o.row * a.parts + k] = q;
-    });
+    float x[kVec], y[kVec];
+    Row<FP32>{d.p}.load_some(x, i, end), Row<QFP32>{d.q}.load_some(y, i, end);
+    bool any = false;
+    double a[kVec], b[kVec];
+#pragma unroll
+    for (int j = 0; j < kVec; j++) {
+#pragma clang fp contract(off)
+        const double p = weight(x[j], d.p_top, d.t), q = weight(y[j], d.q_top, d.t);
+        s.p += p, s.q += q;
+        a[j] = p * d.p_scale, b[j] = q * d.q_scale;
+        const double more = a[j] - b[j];
+        s.more += __builtin_fmax(more, 0.0);
+        s.under += more > 0.0 ? b[j] : 0.0;
+        any |= __builtin_fabs(more) < near * b[j];
+    }
+    if (!__any(any)) return;
+#pragma unroll
+    for (int j = 0; j < kVec; j++) s.near += __builtin_fabs(a[j] - b[j]) < near * b[j] ? b[j] : 0.0;
 }
-// what is left of each part of p - q;
 __global__ __launch_bounds__(kOpenThreads) void verify_left_kernel(VerifyLaunch a)
 {
-    __shared__ double sums[kOpenThreads / 64];
+    __shared__ OpenPart other;
     const int tid = threadIdx.x;
-    every_item(a, [&](const OpenDraw &o, OpenDraw &, int k) {
-        if (o.from != kRest) return;
-        const Opened r = open_draw(a, o, tid & 63);
+    every_item(a, [&](const OpenDraw &o, int at, int k) {
+        const Draw d = open_draw(a, o);
         const int end = part_end(a, k);
-        double sum = 0.0, w[kVec];
-        float x[kVec];
+        const double near = 4.0 * a.eps;
+        OpenPart s = {};
         for (int i = k * a.part_len + tid * kVec; i < end; i += kOpenThreads * kVec) {
-            weights_at(w, x, a, r.d, i, end);
+            if (d.from != kRest) {
+                float x[kVec];
+                if (a.fp32) Row<true>{d.p}.load_some(x, i, end);
+                else Row<false>{d.p}.load_some(x, i, end);
 #pragma unroll
-            for (int j = 0; j < kVec; j++) sum += w[j];
+                for (int j = 0; j < kVec; j++) s.p += weight(x[j], d.p_top, d.t);
+            } else if (a.fp32) a.draft_fp32 ? add_up<true, true>(s, d, near, i, end) : add_up<true, false>(s, d, near, i, end);
+            else a.draft_fp32 ? add_up<false, true>(s, d, near, i, end) : add_up<false, false>(s, d, near, i, end);
         }
-        sum = wave_sum(sum);
-        if ((tid & 63) == 0) sums[tid >> 6] = sum;
+        s = {wave_sum(s.p), wave_sum(s.q), wave_sum(s.more), wave_sum(s.under), wave_sum(s.near)};
+        if (tid == 64) other = s;
         __syncthreads();
-        if (tid == 0) a.rest[(int64_t)o.row * a.parts + k] = sums[0] + sums[1];
+        if (tid == 0) a.left[(int64_t)at * a.parts + k] = {s.p + other.p, s.q + other.q, s.more + other.more, s.under + other.under, s.near + other.near};
     });
 }
-// and the tokens, a draw to a workgroup.
+// The tokens, a draw to a workgroup.
 __global__ __launch_bounds__(kDrawThreads) void verify_close_kernel(VerifyLaunch a)
 {
     __shared__ DrawLds lds;
+    const int lane = threadIdx.x & 63;
     const OpenDraw o = a.open[blockIdx.x];
+    const OpenPart *const parts = a.left + (int64_t)blockIdx.x * a.parts;
+    const OpenPart mine = lane < a.parts ? parts[lane] : OpenPart{}; // (before it is known that there is such a draw)
     if ((int)blockIdx.x >= a.opened[0]) return;
-    Opened r = open_draw(a, o, threadIdx.x & 63);
-    const double *const sums = a.rest + (int64_t)o.row * a.parts;
-    close_draw(a, o, r, [&](int k) { return sums[k]; }, lds);
+    Draw d = open_draw(a, o);
+    OpenPart all = mine;
+    for (int k = lane + 64; k < a.parts; k += 64) all.p += parts[k].p, all.q += parts[k].q, all.near += parts[k].near;
+    const double p_scale = 1.0 / wave_sum(all.p), q_scale = 1.0 / wave_sum(all.q), v = number_of(a, o.b);
+    const double alpha = p_scale / d.p_scale, skew = alpha - q_scale / d.q_scale, unsure = 12.0 * a.eps * wave_sum(all.near);
+    d.p_scale = p_scale, d.q_scale = q_scale;
+    auto part = [&](int k) { return k == lane ? mine : parts[k]; };
+    auto share_in_p = [&](int k) { return part(k).p * p_scale; };
+    Token token = {-1, 0.f};
+    if (d.from == kRest) {
+        const Border at = border_of([&](int k) { const OpenPart s = part(k); return alpha * s.more + skew * s.under; }, a.parts, v, lane);
+        token = token_of_part(a, d, at, unsure, lds);
+        if (token.id < 0) {                                     // in doubt, or nothing is left: part by part
+            double *const sums = a.rest + (int64_t)o.row * a.parts;
+            for (int k = 0; k < a.parts; k++) {
+                double w[kVec];
+                float x[kVec];
+                const double sum = block_sum(weights_of_part(w, x, a, d, k), lds);
+                if (threadIdx.x == 0) sums[k] = sum;
+            }
+            __syncthreads();
+            token = close_draw(a, d, [&](int k) { return sums[k]; }, share_in_p, v, lds);
+        }
+    } else token = close_draw(a, d, share_in_p, share_in_p, v, lds);
+    finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, token);
 }
 
 // Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
@@ -905,6 +924,7 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, voi
         a.rest = (double *)take(parts * sizeof(double));
         a.opened = (int32_t *)take(sizeof(int32_t));
         a.open = (OpenDraw *)take((size_t)a.B * sizeof(OpenDraw));
+        if (drafted && !a.exact) a.left = (OpenPart *)take((size_t)a.B * a.parts * sizeof(OpenPart));
     }
     return at;
 }
@@ -934,7 +954,6 @@ hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)
     if (!a.draft) hipLaunchKernelGGL(verify_again_kernel, open, threads, 0, s, a);
     else if (a.exact) hipLaunchKernelGGL(verify_rest_kernel, open, threads, 0, s, a);
     else {
-        hipLaunchKernelGGL(verify_resum_kernel, many, dim3(kOpenThreads), 0, s, a);
         hipLaunchKernelGGL(verify_left_kernel, many, dim3(kOpenThreads), 0, s, a);
         hipLaunchKernelGGL(verify_close_kernel, seqs, threads, 0, s, a);
     }
