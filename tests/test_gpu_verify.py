@@ -65,6 +65,19 @@ def test_few_long_rows(dec, rows, V):
         run(dec, drafting(rows, [rows, 1], V, "bf16", drafts))
 
 
+@pytest.mark.parametrize("drafts", ["logits", "guess"])
+def test_rows_of_more_parts_than_a_wave_has_lanes(dec, drafts):
+    """More than 64 parts of 4096 values to a row; of the flat ones no binary32 sum settles anything."""
+    x = drafting(5, [2, 3, 1], 300001, "bf16", drafts, [1.0, 0.0, 2.5])
+    run(dec, x)
+    flat = rows_of(6, 60, 300001, "fp32", 0.1) if drafts == "guess" else rows_of(6, 4, 540000, "fp32", 0.1)
+    n = len(flat) // 2
+    r = np.random.default_rng(7)
+    x = Verifying([2] * n, flat, r.integers(0, flat.shape[1], 2 * n), np.full(2 * n, 0.5), r.random(n), draft=None if drafts == "guess" else flat[::-1][:n].copy(),
+                  draft_rows=None if drafts == "guess" else list(range(n)), dtype="fp32")
+    run(dec, x)
+
+
 @pytest.mark.parametrize("rows", [20, 70, 200])
 def test_long_drafts(dec, rows):
     """More rows than a workgroup looks at together; drafts that all stay."""
@@ -88,6 +101,30 @@ def test_a_draft_model_like_the_target(dec):
         assert x.accepted.tolist() == [4]
     x = run(dec, Verifying([5], logits, tokens, [0.5, 1.0, 0, 0, 0], [0.4], draft=logits[:4], draft_rows=[0], dtype="fp32"))
     assert x.accepted.tolist() == [1]
+
+
+@pytest.mark.parametrize("V", [40, 5000, 30000])
+@pytest.mark.parametrize("pairs", [1, 7])
+def test_models_that_agree_but_for_a_few_tokens(dec, V, pairs):
+    """The draft's logits are the target's with a few pairs of tokens changed about: p and q are the same everywhere else, to the last
+    bits, and all that is left of p - q lies in those tokens, also for numbers next to their borders (by much more than what 64-bit sums of
+    one row in two orders may differ by, 1e-13 of what is left)."""
+    r = np.random.default_rng(V + pairs)
+    v = [0.5, 1e-6, 1 - 2.0 ** -20, 0.25, 0.75, 1e-9, float(np.float32(1 - 2.0 ** -24)), 0.01]
+    n = len(v)
+    logits = rows_of(V, 2 * n, V, "fp32", 1.0)
+    draft = logits[::2].copy()
+    tokens, starts = np.zeros(2 * n, dtype=np.int64), np.arange(n)
+    for b in range(n):
+        at = r.permutation(V)[:2 * pairs].reshape(pairs, 2)
+        for i, j in at:
+            logits[2 * b, i], logits[2 * b, j] = 4.0, 1.0
+            draft[b, i], draft[b, j] = 1.0, 4.0
+        tokens[2 * b + 1] = at[0, 1]                         # of the draft's liking: turned down at 0.5 of 1 / e^3
+    x = run(dec, Verifying([2] * n, logits, tokens, [0.5] * (2 * n), v, draft=draft, draft_rows=starts, dtype="fp32"))
+    assert x.accepted.tolist() == [0] * n
+    T = [0.7, 1.3, 2.0, 0.5, 1.0, 1.0, 3.0, 0.9]
+    run(dec, Verifying([2] * n, logits, tokens, [0.9] * (2 * n), v, T, draft=draft, draft_rows=starts, dtype="fp32"))
 
 
 @pytest.mark.parametrize("V", [1, 4, 256, 4096, 65536])
@@ -263,6 +300,17 @@ def test_refusals_enqueue_nothing(dec):
     assert e.value.status == ra.RA_ERR_INVALID_ARG and "dtype" in str(e.value)
     torch.cuda.synchronize()
     assert (x.out == -77).all() and (x.accepted == -77).all()
+
+
+@pytest.mark.parametrize("drafts,V,rows", [("logits", 4097, 5), ("guess", 4097, 4), ("guess", 12289, 1)])
+def test_flat_rows(dec, drafts, V, rows):
+    """Logits all but equal: every token is about as likely, thousands of borders lie close together, and no binary32 sum tells them
+    apart."""
+    n = 60
+    x = drafting(V, [rows] * n, V, "fp32", drafts, near=0.01)
+    x = Verifying(x.rows, rounded(0.01 * x.host[0], "fp32"), x.host[2], x.host[3], x.host[4], None, None if x.host[6] is None else rounded(0.01 * x.host[6], "fp32"),
+                  x.host[7], dtype="fp32")
+    run(dec, x)
 
 
 def test_first_tokens_are_distributed_as_the_target_s(dec):
