@@ -125,22 +125,29 @@ template <bool FP32> struct Row {
         if constexpr (FP32) return ((const float *)at)[i];
         else return __uint_as_float((uint32_t)((const uint16_t *)at)[i] << 16);
     }
-    // Values i .. i + 7.  (A row begins at any element: the load is of no alignment but that.)
-    // STREAM: with the hint that they are read once.
-    template <bool STREAM = false> __device__ __forceinline__ void load(float (&x)[kVec], int i) const
+    // Values i .. i + 7 as they lie there (a row begins at any element: the load is of no alignment but that), and as they are.  STREAM:
+    // with the hint that they are read once.
+    typedef typename Words<FP32>::type words;
+    struct Raw {
+        words w[FP32 ? 2 : 1];
+    };
+    template <bool STREAM = false> __device__ __forceinline__ Raw ask(int i) const
     {
-        typedef typename Words<FP32>::type words;
         const words *const from = (const words *)(at + (size_t)i * kBytes);
-        if constexpr (FP32) {
-            const words w = STREAM ? __builtin_nontemporal_load(from) : *from, v = STREAM ? __builtin_nontemporal_load(from + 1) : from[1];
+        Raw r;
 #pragma unroll
-            for (int j = 0; j < 4; j++) x[j] = __uint_as_float(w[j]), x[4 + j] = __uint_as_float(v[j]);
-        } else {
-            const words w = STREAM ? __builtin_nontemporal_load(from) : *from;
+        for (int j = 0; j < (FP32 ? 2 : 1); j++) r.w[j] = STREAM ? __builtin_nontemporal_load(from + j) : from[j];
+        return r;
+    }
+    static __device__ __forceinline__ void take(float (&x)[kVec], const Raw &r)
+    {
 #pragma unroll
-            for (int j = 0; j < 4; j++) x[2 * j] = __uint_as_float(w[j] << 16), x[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+        for (int j = 0; j < 4; j++) {
+            if constexpr (FP32) x[j] = __uint_as_float(r.w[0][j]), x[4 + j] = __uint_as_float(r.w[1][j]);
+            else x[2 * j] = __uint_as_float(r.w[0][j] << 16), x[2 * j + 1] = __uint_as_float(r.w[0][j] & 0xffff0000u);
         }
     }
+    __device__ __forceinline__ void load(float (&x)[kVec], int i) const { take(x, ask(i)); }
     // ... of which those at or past end are -inf.
     __device__ __forceinline__ void load_some(float (&x)[kVec], int i, int end) const
     {
@@ -188,20 +195,27 @@ template <bool EXACT> struct Met {
     }
 };
 
-// Values [begin, end) of a row, by THREADS threads of which this is number tid: two loads of eight values at a time, then one, then what is
-// left of a load, a value to a thread.
+// Values [begin, end) of a row, by THREADS threads of which this is number tid: four loads of eight values are on their way at a time, then
+// one, then what is left of a load, a value to a thread.
 template <bool EXACT, int THREADS, bool FP32> __device__ __forceinline__ Met<EXACT> meet_all(const Row<FP32> row, int begin, int end, const Temper &t, int tid)
 {
+    constexpr int kAhead = 2, kStep = THREADS * kVec;
     const bool greedy = t.c == 0.0;
     const int whole = begin + ((end - begin) & ~(kVec - 1));
     Met<EXACT> met;
-    float x[kVec], y[kVec];
+    float x[kVec];
     int i = begin + tid * kVec;
-    for (; i + THREADS * kVec < whole; i += 2 * THREADS * kVec) {
-        row.template load<!EXACT>(x, i), row.template load<!EXACT>(y, i + THREADS * kVec);
-        met.meet(x, i, t, greedy), met.meet(y, i + THREADS * kVec, t, greedy);
+    for (; i + (kAhead - 1) * kStep < whole; i += kAhead * kStep) {
+        typename Row<FP32>::Raw r[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; j++) r[j] = row.template ask<!EXACT>(i + j * kStep);
+#pragma unroll
+        for (int j = 0; j < kAhead; j++) {
+            row.take(x, r[j]);
+            met.meet(x, i + j * kStep, t, greedy);
+        }
     }
-    if (i < whole) {
+    for (; i < whole; i += kStep) {
         row.load(x, i);
         met.meet(x, i, t, greedy);
     }
@@ -860,7 +874,7 @@ __global__ __launch_bounds__(kDrawThreads) void verify_close_kernel(VerifyLaunch
     OpenPart all = mine;
     for (int k = lane + 64; k < a.parts; k += 64) all.p += parts[k].p, all.q += parts[k].q, all.near += parts[k].near;
     const double p_scale = 1.0 / wave_sum(all.p), q_scale = 1.0 / wave_sum(all.q), v = number_of(a, o.b);
-    const double alpha = p_scale / d.p_scale, skew = alpha - q_scale / d.q_scale, unsure = 12.0 * a.eps * wave_sum(all.near);
+    const double alpha = p_scale / d.p_scale, skew = alpha - q_scale / d.q_scale, unsure = 13.0 * a.eps * wave_sum(all.near);
     d.p_scale = p_scale, d.q_scale = q_scale;
     auto part = [&](int k) { return k == lane ? mine : parts[k]; };
     auto share_in_p = [&](int k) { return part(k).p * p_scale; };
