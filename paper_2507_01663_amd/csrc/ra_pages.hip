@@ -80,6 +80,7 @@ constexpr int kOwn = 4; // a sequence with so few new tokens places them itself,
 // new lengths, counts and offsets.  Both at once with one workgroup alone, or where no other reads what that writes.
 template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void place_kernel(PagesLaunch a)
 {
+    touch_lines(a);
     __shared__ ScanLds sums[2];
     __shared__ int32_t first[kTileSeqs];                        // tokens before the sequence
     __shared__ int4 row[kTileSeqs];                             // {tokens held, pages held, pages with the group's, stack's entry of the first taken}
@@ -155,6 +156,7 @@ template <bool TOKENS, bool STATE> __global__ __launch_bounds__(kTileSeqs) void 
 
 template <bool PAGES, bool STATE> __global__ __launch_bounds__(kTileSeqs) void release_kernel(PagesLaunch a)
 {
+    touch_lines(a);
     __shared__ ScanLds sums;
     __shared__ int32_t first[kTileSeqs], begin[kTileSeqs];      // pages before the sequence's, and its first that goes back
     const int tid = threadIdx.x, free = stack_height(a);

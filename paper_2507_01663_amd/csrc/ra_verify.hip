@@ -304,6 +304,7 @@ __device__ __forceinline__ int part_end(const VerifyLaunch &a, int k) { return k
 // A part of a target row, or of the draft's row that belongs to it, for each wave: the target's rows come first.
 template <bool EXACT> __global__ __launch_bounds__(kVerifyThreads) void verify_rows_kernel(VerifyLaunch a)
 {
+    touch_lines(a);
     const int lane = threadIdx.x & 63;
     if (blockIdx.x == 0 && threadIdx.x == 0 && a.opened) a.opened[0] = 0;
     const unsigned n = __builtin_amdgcn_readfirstlane(blockIdx.x * (kVerifyThreads / 64) + threadIdx.x / 64);
@@ -328,6 +329,7 @@ template <bool EXACT> __global__ __launch_bounds__(kVerifyThreads) void verify_r
 // known whose row it is.
 __global__ __launch_bounds__(kVerifyThreads) void verify_few_rows_kernel(VerifyLaunch a)
 {
+    touch_lines(a);
     const int tid = threadIdx.x, lane = tid & 63;
     if (blockIdx.x == 0 && tid == 0 && a.opened) a.opened[0] = 0;
     const unsigned rows = blockIdx.x / (unsigned)a.parts, k = blockIdx.x % (unsigned)a.parts;
@@ -397,35 +399,48 @@ struct Draw {
     Temper t;
 };
 
-// What row `row` of sequence b says to its draft, and how a token is drawn from it if that does not stay.  All lanes of a wave.
+// What row `row` says to its draft, and how a token is drawn from it if that does not stay: by the row's sums, what its draft is (x, no
+// token: -1), the logits of that in the target's row and in the draft model's, and the draft model's row (-1: none).  All lanes of a wave.
 enum Verdict { kGoes, kStays, kUnsure };
-__device__ __forceinline__ Draw judge(const VerifyLaunch &a, int b, int row, int end, const Temper &t, const Whole &p, const Whole &q, double unsure, Verdict &says, double &lp)
+struct Asked {
+    int row, x;
+    int64_t q_row;
+    float l, m, u;
+};
+__device__ __forceinline__ Asked ask_row(const VerifyLaunch &a, int b, int row, int end)
 {
-    const int x = row + 1 == end ? -1 : a.tokens[row + 1];
-    const bool token = x >= 0 && x < a.V;
+    Asked r = {row, -1, -1, 0.f, 0.f, a.u[row]};
+    if (row + 1 < end) r.x = a.tokens[row + 1];
+    if (r.x < 0 || r.x >= a.V) r.x = -1;
+    if (r.x < 0) return r;
+    r.l = logit_at(a.logits, a.stride, a.fp32, row, r.x);
+    if (a.draft) r.q_row = draft_row_of(a, b, row);
+    if (r.q_row >= 0) r.m = logit_at(a.draft, a.draft_stride, a.draft_fp32, r.q_row, r.x);
+    return r;
+}
+__device__ __forceinline__ Draw judge(const VerifyLaunch &a, const Asked &r, const Temper &t, const Whole &p, const Whole &q, double unsure, Verdict &says, double &lp)
+{
     Draw d = {};
-    d.row = row, d.x = x, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, row), d.p_top = p.top, d.p_scale = 1.0 / p.sum;
+    d.row = r.row, d.x = r.x, d.t = t, d.p = row_at(a.logits, a.stride, a.fp32, r.row), d.p_top = p.top, d.p_scale = 1.0 / p.sum;
     says = kGoes, lp = 0.0;
     if (!is_finite(p.top)) {
         d.from = kNothing;
         return d;
     }
     if (t.c == 0.0) {
-        d.from = kTop, says = token && x == p.first ? kStays : kGoes, d.x = p.first;
+        d.from = kTop, says = r.x >= 0 && r.x == p.first ? kStays : kGoes, d.x = p.first;
         return d;
     }
     d.from = kRow;
-    if (!token) return d;
-    const float l = logit_at(a.logits, a.stride, a.fp32, row, x);
-    const double px = weight(l, p.top, t) / p.sum;
-    lp = ((double)l - (double)p.top) * t.c / kLog2e - log(p.sum);
-    double against = (double)a.u[row];
+    if (r.x < 0) return d;
+    const double px = weight(r.l, p.top, t) / p.sum;
+    lp = ((double)r.l - (double)p.top) * t.c / kLog2e - log(p.sum);
+    double against = (double)r.u;
     if (!a.draft) d.from = kRowWithout;
     else {
-        const int64_t r = draft_row_of(a, b, row);
-        if (r < 0 || !is_finite(q.top)) return d;
-        d.from = kRest, d.q_row = (int)r, d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, r), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
-        against *= weight(logit_at(a.draft, a.draft_stride, a.draft_fp32, r, x), q.top, t) / q.sum;
+        if (r.q_row < 0 || !is_finite(q.top)) return d;
+        d.from = kRest, d.q_row = (int)r.q_row, d.q = row_at(a.draft, a.draft_stride, a.draft_fp32, r.q_row), d.q_top = q.top, d.q_scale = 1.0 / q.sum;
+        against *= weight(r.m, q.top, t) / q.sum;
     }
     says = against < px ? kStays : kGoes;
     // (where px is 0 or the number is not positive, no error of the sums changes the answer)
@@ -474,17 +489,18 @@ __device__ __forceinline__ double share_of(const RowPart &r, const Draw &d)
 }
 
 // Row `row` of sequence b by the sums that the first kernel left: the draw from it, what it says to its draft, and where v lies in it.
+// (All that it reads is asked for before any of it is waited for.)
 __device__ __forceinline__ Draw judge_row(const VerifyLaunch &a, int b, int row, int end, const Temper &t, double v, int lane, double unsure, Verdict &says, double &lp, Border &border)
 {
-    const RowPart *const parts = a.row + (int64_t)row * a.parts;
-    const RowPart mine = lane < a.parts ? parts[lane] : RowPart{0.0, -INFINITY, INT32_MAX};
+    const RowPart none = {0.0, -INFINITY, INT32_MAX}, *const parts = a.row + (int64_t)row * a.parts, *const theirs = a.draft_row + (int64_t)row * a.parts;
+    RowPart mine = none, yours = none;
+    if (lane < a.parts) mine = parts[lane];
+    if (a.draft && lane < a.parts) yours = theirs[lane];        // (of whatever was there before, if the row has none; it is not used then)
+    const Asked asked = ask_row(a, b, row, end);
     const Whole p = whole_row(parts, mine, a.parts, t, lane);
     Whole q = {1.0, -INFINITY, 0};
-    if (a.draft && row + 1 < end && t.c != 0.0 && draft_row_of(a, b, row) >= 0) {
-        const RowPart *const theirs = a.draft_row + (int64_t)row * a.parts;
-        q = whole_row(theirs, lane < a.parts ? theirs[lane] : RowPart{0.0, -INFINITY, INT32_MAX}, a.parts, t, lane);
-    }
-    const Draw d = judge(a, b, row, end, t, p, q, unsure, says, lp);
+    if (asked.q_row >= 0 && t.c != 0.0) q = whole_row(theirs, yours, a.parts, t, lane);
+    const Draw d = judge(a, asked, t, p, q, unsure, says, lp);
     if (d.from == kRow) border = border_of([&](int k) { return share_of(k == lane ? mine : parts[k], d); }, a.parts, v, lane);
     return d;
 }
@@ -526,7 +542,7 @@ template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch 
             const Whole q = d.from == kRest ? exact_row(a, d.q, a.draft_fp32, t) : Whole{1.0, -INFINITY, 0};
             Verdict sure;
             double unused;
-            (void)judge(a, b, d.row, end, t, p, q, 0.0, sure, unused);
+            (void)judge(a, ask_row(a, b, d.row, end), t, p, q, 0.0, sure, unused);
             if (sure != kStays) break;
         }
         if (wave < n && lane == 0) {
@@ -695,6 +711,7 @@ __device__ __forceinline__ void finish(const VerifyLaunch &a, int b, int begin, 
 // from p - q, and those that binary32 sums do not settle.
 template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_draw_kernel(VerifyLaunch a)
 {
+    touch_lines(a);
     __shared__ DrawLds lds;
     const int tid = threadIdx.x, b = blockIdx.x;
     const int begin = a.cu[b], end = a.cu[b + 1];
@@ -780,6 +797,7 @@ template <typename F, typename G> __device__ __forceinline__ Token close_draw(co
 // Few open draws, from p: its sums anew, in binary64; the last workgroup to add up its part draws.
 __global__ __launch_bounds__(kDrawThreads) void verify_again_kernel(VerifyLaunch a)
 {
+    touch_lines(a);
     __shared__ DrawLds lds;
     every_item(a, [&](const OpenDraw &o, int at, int k) {
         Draw d = open_draw(a, o);
@@ -794,6 +812,7 @@ __global__ __launch_bounds__(kDrawThreads) void verify_again_kernel(VerifyLaunch
 // ... from p - q, whose sums are binary64: what is left of it, in the same way.
 __global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch a)
 {
+    touch_lines(a);
     __shared__ DrawLds lds;
     every_item(a, [&](const OpenDraw &o, int at, int k) {
         Draw d = open_draw(a, o);
@@ -838,6 +857,7 @@ template <bool FP32, bool QFP32> __device__ __forceinline__ void add_up(OpenPart
 }
 __global__ __launch_bounds__(kOpenThreads) void verify_left_kernel(VerifyLaunch a)
 {
+    touch_lines(a);
     __shared__ OpenPart other;
     const int tid = threadIdx.x;
     every_item(a, [&](const OpenDraw &o, int at, int k) {
@@ -864,6 +884,7 @@ __global__ __launch_bounds__(kOpenThreads) void verify_left_kernel(VerifyLaunch 
 // The tokens, a draw to a workgroup.
 __global__ __launch_bounds__(kDrawThreads) void verify_close_kernel(VerifyLaunch a)
 {
+    touch_lines(a);
     __shared__ DrawLds lds;
     const int lane = threadIdx.x & 63;
     const OpenDraw o = a.open[blockIdx.x];
