@@ -153,7 +153,7 @@ typedef enum { RA_LOGITS_BF16 = 0, RA_LOGITS_FP32 = 1 } ra_logits_dtype;
  * 16-byte aligned rows are read fastest.  Inputs and outputs overlap nothing.
  * A probability below 2^-990 counts as 0.
  * Supported: vocab <= 2^24; num_seqs and total_rows <= 2^22; a batch whose parts of 4096 values (num_seqs, or twice total_rows,
- * times those of a row) are fewer than 2^23.
+ * times those of a row) are fewer than 2^26.
  */
 typedef struct {
     int32_t num_seqs, total_rows, vocab;
@@ -182,7 +182,7 @@ ra_status rollout_attn_check_verify(const ra_verify *verify, char *msg, size_t m
  * draft_logits is NULL are read).  ctx may be NULL: the size for a 256-compute-unit device is returned. */
 ra_status rollout_attn_verify_workspace_size(const ra_ctx *ctx, const ra_verify *shape_only, size_t *bytes);
 
-/* Enqueues the verification on hip_stream: two kernels, in large batches three or four.  The environment's
+/* Enqueues the verification on hip_stream: two kernels, one more with draft_logits and one more in large batches.  The environment's
  * ROLLOUT_ATTN_VERIFY_FEW=n, read by rollout_attn_create, is the number of bf16 logits up to which all sums are binary64 from the
  * start; of binary32 logits, and of logits with a draft model's (both counted), three times as many, of both together five times.  workspace as for rollout_attn_decode: dev memory of at least
  * rollout_attn_verify_workspace_size() bytes, 256-byte aligned, contents irrelevant on entry and undefined afterwards; calls

@@ -48,7 +48,7 @@ __device__ __forceinline__ int shared_pages(const PagesLaunch &a, int b, int &at
     if (g < 0 || g >= a.num_groups) return 0;
     at = a.pfx_off[g];
     const int n = a.pfx_off[g + 1] - at;
-    return n > 0 ? n : 0;
+    return n > 0 && at >= 0 ? n : 0;
 }
 
 __device__ __forceinline__ int stack_height(const PagesLaunch &a)
