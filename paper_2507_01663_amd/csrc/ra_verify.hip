@@ -832,8 +832,9 @@ __global__ __launch_bounds__(kDrawThreads) void verify_rest_kernel(VerifyLaunch 
 //   sum max(p - q, 0) = alpha sum max(a - b, 0) + (alpha - beta) sum_{a > b} b,
 // but for values where p and q are so near each other that the scales decide which is larger, |a - b| < 4 eps b: each is off by 6 eps b
 // at most.  The sum of those b says how much all may be off, which is next to nothing, or where models agree over much of a row, a doubt
-// that verify_close_kernel settles.  A workgroup of two waves has a part.
-constexpr int kOpenThreads = 128;
+// that verify_close_kernel settles.  A workgroup has a part.  (128, 256, 512 threads: 97.5, 96.0, 99.2 us of 128 x 5 rows of 152 064 bf16 values with a
+// draft model's.)
+constexpr int kOpenThreads = 256;
 template <bool FP32, bool QFP32> __device__ __forceinline__ void add_up(OpenPart &s, const Draw &d, double near, int i, int end)
 {
     float x[kVec], y[kVec];
@@ -858,7 +859,7 @@ template <bool FP32, bool QFP32> __device__ __forceinline__ void add_up(OpenPart
 __global__ __launch_bounds__(kOpenThreads) void verify_left_kernel(VerifyLaunch a)
 {
     touch_lines(a);
-    __shared__ OpenPart other;
+    __shared__ OpenPart waves[kOpenThreads / 64];
     const int tid = threadIdx.x;
     every_item(a, [&](const OpenDraw &o, int at, int k) {
         const Draw d = open_draw(a, o);
@@ -876,9 +877,12 @@ __global__ __launch_bounds__(kOpenThreads) void verify_left_kernel(VerifyLaunch 
             else a.draft_fp32 ? add_up<false, true>(s, d, near, i, end) : add_up<false, false>(s, d, near, i, end);
         }
         s = {wave_sum(s.p), wave_sum(s.q), wave_sum(s.more), wave_sum(s.under), wave_sum(s.near)};
-        if (tid == 64) other = s;
+        if ((tid & 63) == 0) waves[tid >> 6] = s;
         __syncthreads();
-        if (tid == 0) a.left[(int64_t)at * a.parts + k] = {s.p + other.p, s.q + other.q, s.more + other.more, s.under + other.under, s.near + other.near};
+        if (tid) return;
+#pragma unroll
+        for (int w = 1; w < kOpenThreads / 64; w++) s.p += waves[w].p, s.q += waves[w].q, s.more += waves[w].more, s.under += waves[w].under, s.near += waves[w].near;
+        a.left[(int64_t)at * a.parts + k] = s;
     });
 }
 // The tokens, a draw to a workgroup.
