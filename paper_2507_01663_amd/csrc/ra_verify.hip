@@ -38,7 +38,6 @@ __device__ __forceinline__ Temper temper_from(float T)
     const double c = kLog2e / (double)T;
     return {c, -1100.0 / kLog2e * (double)T, (float)c};
 }
-__device__ __forceinline__ Temper temper_of(const VerifyLaunch &a, int b) { return temper_from(a.temperature ? a.temperature[b] : 1.f); }
 
 // 2^x for x = d * c >= -1100, right to 2^-39: to the nearest whole number (by an addition that leaves it in the low bits), and for the
 // rest the polynomial of degree eight through 2^x at nine Chebyshev nodes of [-1/2, 1/2], with the constant term at 1.
@@ -288,6 +287,38 @@ __device__ __forceinline__ int sequence_of_row(const VerifyLaunch &a, int t, int
     return b;
 }
 
+// The sequence that row t belongs to, its rows and what else of it a row needs; b is not below the number of sequences where there is none.
+// Of up to 64 sequences, a wave's lanes, all is asked for at once: one trip to memory instead of three.  (With what the draws ask for early,
+// see verify_draw_kernel: one sequence with four drafts 14.6 and 13.8 us, four without 10.2 and 9.7, 128 with four 95.7 and 92.3.)
+struct Owner {
+    int b, begin, end;
+    float T;
+    int64_t draft_row;           // of row t: its place in draft_logits, or -1
+};
+__device__ __forceinline__ Owner owner_of_row(const VerifyLaunch &a, int t, int lane)
+{
+    Owner o = {0, 0, 0, 1.f, -1};
+    int first = 0;
+    if (a.B <= 64) {
+        const bool in = lane < a.B;
+        const int next = in ? a.cu[lane + 1] : INT32_MAX, drafts = in && a.draft ? a.draft_rows[lane] : 0, none = a.cu[0];
+        const float T = in && a.temperature ? a.temperature[lane] : 1.f;
+        o.b = __popcll(__ballot(next <= t));
+        if (o.b >= a.B) return o;
+        o.begin = o.b ? __builtin_amdgcn_readlane(next, o.b - 1) : none, o.end = __builtin_amdgcn_readlane(next, o.b);
+        o.T = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(T), o.b)), first = __builtin_amdgcn_readlane(drafts, o.b);
+    } else {
+        o.b = sequence_of_row(a, t, lane);
+        if (o.b >= a.B) return o;
+        o.begin = a.cu[o.b], o.end = a.cu[o.b + 1];
+        if (a.temperature) o.T = a.temperature[o.b];
+        if (a.draft) first = a.draft_rows[o.b];
+    }
+    const int64_t r = (int64_t)first + t - o.begin;
+    o.draft_row = a.draft && r >= 0 && r < a.total_draft_rows ? r : -1;
+    return o;
+}
+
 __device__ __forceinline__ const uint8_t *row_at(const void *logits, int64_t stride, int fp32, int64_t t)
 {
     return (const uint8_t *)logits + t * stride * (fp32 ? 4 : 2);
@@ -323,14 +354,13 @@ template <bool EXACT> __global__ __launch_bounds__(kVerifyThreads) void verify_r
     const bool drafted = rows >= (unsigned)a.R;
     if (rows >= (unsigned)a.R * (a.draft ? 2u : 1u)) return;
     const int t = (int)(drafted ? rows - a.R : rows);
-    const int b = sequence_of_row(a, t, lane);
-    if (b >= a.B || t < a.cu[b]) return;
-    const Temper temper = temper_of(a, b);
+    const Owner of = owner_of_row(a, t, lane);
+    if (of.b >= a.B || t < of.begin) return;
+    const Temper temper = temper_from(of.T);
     const uint8_t *at = row_at(a.logits, a.stride, a.fp32, t);
     if (drafted) {
-        const int64_t d = draft_row_of(a, b, t);
-        if (t + 1 >= a.cu[b + 1] || d < 0 || temper.c == 0.0) return;
-        at = row_at(a.draft, a.draft_stride, a.draft_fp32, d);
+        if (t + 1 >= of.end || of.draft_row < 0 || temper.c == 0.0) return;
+        at = row_at(a.draft, a.draft_stride, a.draft_fp32, of.draft_row);
     }
     const RowPart r = part_by_wave<EXACT>(at, drafted ? a.draft_fp32 : a.fp32, k * a.part_len, part_end(a, k), temper);
     if (lane == 0) (drafted ? a.draft_row : a.row)[(int64_t)t * a.parts + k] = r;
@@ -352,13 +382,12 @@ __global__ __launch_bounds__(kVerifyThreads) void verify_few_rows_kernel(VerifyL
         else Row<false>{at}.load_some(x, i, end), Row<false>{at}.load_some(y, j, end);
     };
     if (!drafted) load(row_at(a.logits, a.stride, a.fp32, t), a.fp32);
-    const int b = sequence_of_row(a, t, lane);
-    if (b >= a.B || t < a.cu[b]) return;
-    const Temper temper = temper_of(a, b);
+    const Owner of = owner_of_row(a, t, lane);
+    if (of.b >= a.B || t < of.begin) return;
+    const Temper temper = temper_from(of.T);
     if (drafted) {
-        const int64_t d = draft_row_of(a, b, t);
-        if (t + 1 >= a.cu[b + 1] || d < 0 || temper.c == 0.0) return;
-        load(row_at(a.draft, a.draft_stride, a.draft_fp32, d), a.draft_fp32);
+        if (t + 1 >= of.end || of.draft_row < 0 || temper.c == 0.0) return;
+        load(row_at(a.draft, a.draft_stride, a.draft_fp32, of.draft_row), a.draft_fp32);
     }
     Met<true> met;
     met.meet(x, i, temper, temper.c == 0.0), met.meet(y, j, temper, temper.c == 0.0);
@@ -418,14 +447,27 @@ struct Asked {
     int64_t q_row;
     float l, m, u;
 };
-__device__ __forceinline__ Asked ask_row(const VerifyLaunch &a, int b, int row, int end)
+// What a row reads whose place is known, though not yet whose it is: its parts' sums, the draft model's, its draft and number.
+struct Early {
+    int row, x;
+    float u;
+    RowPart mine, yours;         // (yours: of whatever was there before, if the row has none; it is not used then)
+};
+__device__ __forceinline__ Early ask_early(const VerifyLaunch &a, int row, int lane)
 {
-    Asked r = {row, -1, -1, 0.f, 0.f, a.u[row]};
-    if (row + 1 < end) r.x = a.tokens[row + 1];
+    const RowPart none = {0.0, -INFINITY, INT32_MAX};
+    Early e = {row, row + 1 < a.R ? a.tokens[row + 1] : -1, a.u[row], none, none};
+    if (lane < a.parts) e.mine = a.row[(int64_t)row * a.parts + lane];
+    if (a.draft && lane < a.parts) e.yours = a.draft_row[(int64_t)row * a.parts + lane];
+    return e;
+}
+__device__ __forceinline__ Asked ask_row(const VerifyLaunch &a, int b, const Early &e, int end)
+{
+    Asked r = {e.row, e.row + 1 < end ? e.x : -1, -1, 0.f, 0.f, e.u};
     if (r.x < 0 || r.x >= a.V) r.x = -1;
     if (r.x < 0) return r;
-    r.l = logit_at(a.logits, a.stride, a.fp32, row, r.x);
-    if (a.draft) r.q_row = draft_row_of(a, b, row);
+    r.l = logit_at(a.logits, a.stride, a.fp32, r.row, r.x);
+    if (a.draft) r.q_row = draft_row_of(a, b, r.row);
     if (r.q_row >= 0) r.m = logit_at(a.draft, a.draft_stride, a.draft_fp32, r.q_row, r.x);
     return r;
 }
@@ -499,20 +541,16 @@ __device__ __forceinline__ double share_of(const RowPart &r, const Draw &d)
     return is_finite(r.top) ? r.sum * rescale(r.top, d.p_top, d.t) * d.p_scale : 0.0;
 }
 
-// Row `row` of sequence b by the sums that the first kernel left: the draw from it, what it says to its draft, and where v lies in it.
-// (All that it reads is asked for before any of it is waited for.)
-__device__ __forceinline__ Draw judge_row(const VerifyLaunch &a, int b, int row, int end, const Temper &t, double v, int lane, double unsure, Verdict &says, double &lp, Border &border)
+// A row of sequence b by the sums that the first kernel left: the draw from it, what it says to its draft, and where v lies in it.
+__device__ __forceinline__ Draw judge_row(const VerifyLaunch &a, int b, const Early &e, int end, const Temper &t, double v, int lane, double unsure, Verdict &says, double &lp, Border &border)
 {
-    const RowPart none = {0.0, -INFINITY, INT32_MAX}, *const parts = a.row + (int64_t)row * a.parts, *const theirs = a.draft_row + (int64_t)row * a.parts;
-    RowPart mine = none, yours = none;
-    if (lane < a.parts) mine = parts[lane];
-    if (a.draft && lane < a.parts) yours = theirs[lane];        // (of whatever was there before, if the row has none; it is not used then)
-    const Asked asked = ask_row(a, b, row, end);
-    const Whole p = whole_row(parts, mine, a.parts, t, lane);
+    const RowPart *const parts = a.row + (int64_t)e.row * a.parts, *const theirs = a.draft_row + (int64_t)e.row * a.parts;
+    const Asked asked = ask_row(a, b, e, end);
+    const Whole p = whole_row(parts, e.mine, a.parts, t, lane);
     Whole q = {1.0, -INFINITY, 0};
-    if (asked.q_row >= 0 && t.c != 0.0) q = whole_row(theirs, yours, a.parts, t, lane);
+    if (asked.q_row >= 0 && t.c != 0.0) q = whole_row(theirs, e.yours, a.parts, t, lane);
     const Draw d = judge(a, asked, t, p, q, unsure, says, lp);
-    if (d.from == kRow) border = border_of([&](int k) { return share_of(k == lane ? mine : parts[k], d); }, a.parts, v, lane);
+    if (d.from == kRow) border = border_of([&](int k) { return share_of(k == lane ? e.mine : parts[k], d); }, a.parts, v, lane);
     return d;
 }
 
@@ -524,8 +562,8 @@ __device__ __forceinline__ Whole exact_row(const VerifyLaunch &a, const uint8_t 
 }
 
 // The rows of sequence b, as many at a time as there are waves, up to the first that keeps no draft: that one's draw.  The drafts that stay
-// are written.  The whole workgroup.
-template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch &a, int b, int begin, int end, const Temper &t, double v, Border &border)
+// are written.  e: what was asked for before the rows were known.  The whole workgroup.
+template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch &a, int b, int begin, int end, const Temper &t, double v, Early e, Border &border)
 {
     __shared__ Draw draws[kDrawWaves];
     __shared__ Verdict verdict[kDrawWaves];
@@ -537,7 +575,8 @@ template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch 
         double lp = 0.0;
         if (row < end) {
             Border in_row = {-1, 0.0};
-            const Draw d = judge_row(a, b, row, end, t, v, lane, EXACT ? 0.0 : 4.0 * a.eps, says, lp, in_row);
+            if (e.row != row) e = ask_early(a, row, lane);
+            const Draw d = judge_row(a, b, e, end, t, v, lane, EXACT ? 0.0 : 4.0 * a.eps, says, lp, in_row);
             if (EXACT && says == kUnsure) says = kGoes;         // (equal: not less)
             if (lane == 0) draws[wave] = d, borders[wave] = in_row;
         }
@@ -553,7 +592,7 @@ template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch 
             const Whole q = d.from == kRest ? exact_row(a, d.q, a.draft_fp32, t) : Whole{1.0, -INFINITY, 0};
             Verdict sure;
             double unused;
-            (void)judge(a, ask_row(a, b, d.row, end), t, p, q, 0.0, sure, unused);
+            (void)judge(a, ask_row(a, b, ask_early(a, d.row, lane), end), t, p, q, 0.0, sure, unused);
             if (sure != kStays) break;
         }
         if (wave < n && lane == 0) {
@@ -725,6 +764,11 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_dra
     touch_lines(a);
     __shared__ DrawLds lds;
     const int tid = threadIdx.x, b = blockIdx.x;
+    // (where sequences have as many rows each, this wave's row is known before the offsets are)
+    const int64_t likely = (int64_t)b * (a.R / a.B) + (tid >> 6);
+    Early e = {};
+    e.row = -1;
+    if (likely < a.R) e = ask_early(a, (int)likely, tid & 63);
     const int begin = a.cu[b], end = a.cu[b + 1];
     if (begin < 0 || end > a.R || begin >= end) {
         if (tid == 0) {
@@ -737,7 +781,7 @@ template <bool EXACT> __global__ __launch_bounds__(kDrawThreads) void verify_dra
     const double v = number_of(a, b), unsure = EXACT ? 0.0 : 3.0 * a.eps; // (prefixes and totals are off by eps of the row each)
     const Temper t = temper_from(T);
     Border at;
-    const Draw d = decide<EXACT>(a, b, begin, end, t, v, at);
+    const Draw d = decide<EXACT>(a, b, begin, end, t, v, e, at);
     Token token = {d.from == kTop ? d.x : -1, 0.f};
     if (d.from == kRow) token = token_of_part(a, d, at, unsure, lds);
     else if (d.from == kRowWithout) {
