@@ -13,7 +13,7 @@
 //
 // Memory bounds the sums of large batches: 200 x 4 to 6 rows of 152 064 binary32 logits with a draft model's 180 us, 6.05 TB/s; 128 x 5 of
 // bf16 62 to 67, 5.2 to 5.6 TB/s; binary64 sums take 22 us for 24 million values, their instructions.  The draws are chains of
-// trips to memory, 6 to 10 us a kernel, and so is a small call: 4 rows of 32 000 in 9.5 us.
+// trips to memory, 6 to 10 us a kernel, and so is a small call: 4 rows of 32 000 in 9.4 us.
 #include "ra_device.h"
 #include "ra_step.h"
 #include "ra_wave.h"
