@@ -78,6 +78,17 @@ def test_rows_of_more_parts_than_a_wave_has_lanes(dec, drafts):
     run(dec, x)
 
 
+@pytest.mark.parametrize("n", [63, 64, 65, 130])
+@pytest.mark.parametrize("V", [40, 9000])
+def test_many_sequences(dec, n, V):
+    """As many sequences as a wave has lanes, and one more; as many rows each, ragged ones, none for the first and the last; rows of
+    nobody before and behind."""
+    T = np.where(np.arange(n) % 6 == 1, 0.0, 0.3 + np.arange(n) % 4 / 3)
+    for seed, rows in enumerate([[2] * n, [0] + [1 + b % 3 for b in range(n - 2)] + [0], [b % 2 * 3 for b in range(n)]]):
+        for drafts in ("logits", "guess"):
+            run(dec, drafting(n + seed, rows, V, "bf16", drafts, T if seed else None, lead=seed, behind=2 * seed), (n, V, seed, drafts))
+
+
 @pytest.mark.parametrize("rows", [20, 70, 200])
 def test_long_drafts(dec, rows):
     """More rows than a workgroup looks at together; drafts that all stay."""
