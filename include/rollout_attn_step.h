@@ -59,7 +59,7 @@ extern "C" {
  *   tokens of such positions, so a captured step may have room for more tokens than it has.
  * seq_lens and lens_out, held and held_out, free_count and free_count_out may be the same memory; otherwise outputs overlap
  * nothing.  *free_count counts as the nearest of 0 and num_pages outside them.  Page ids are not looked into.
- * Supported: page_size == 16; num_seqs * max_pages_per_seq < 2^31.
+ * Supported: page_size == 16; num_seqs * max_pages_per_seq < 2^31; num_seqs < 2^31 - 1024; max_pages_per_seq < 2^27.
  */
 typedef struct {
     int32_t num_seqs, total_tokens, page_size, num_pages, max_pages_per_seq;

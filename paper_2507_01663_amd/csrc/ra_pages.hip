@@ -17,7 +17,7 @@
 
 namespace ra {
 
-constexpr int kTileSeqs = 1024, kTileWaves = kTileSeqs / 64;
+constexpr int kTileWaves = kTileSeqs / 64;
 
 // Inclusive sums over the 1024 threads of a workgroup, on top of what was carried in; the new totals are carried out.  (Tokens of sequences
 // that a table has room for are fewer than 2^35: whole numbers of binary64.)

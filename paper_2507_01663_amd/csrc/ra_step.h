@@ -4,6 +4,9 @@
 
 namespace ra {
 
+// Sequences that the kernels of the pages go over at a time, by 32-bit numbers: the first behind the last tile is one, too.
+constexpr int32_t kTileSeqs = 1024, kMostPagedSeqs = INT32_MAX - kTileSeqs;
+
 // Pages of the sequences of a batch (ra_place, ra_release).
 struct PagesLaunch {
     int32_t B, T, num_pages, max_pages, num_groups;

@@ -18,7 +18,7 @@ template <typename P> ra_status check_pages(const P *p, const Fail &fail)
         return fail(RA_ERR_INVALID_ARG, "negative or zero dimension (num_seqs=%d page_size=%d num_pages=%d max_pages_per_seq=%d num_groups=%d)", p->num_seqs,
                     p->page_size, p->num_pages, p->max_pages_per_seq, p->num_groups);
     if (p->page_size != 16) return fail(RA_ERR_UNSUPPORTED, "page_size=%d (only 16 is supported)", p->page_size);
-    if ((int64_t)p->num_seqs * p->max_pages_per_seq >= (int64_t)1 << 31 || p->max_pages_per_seq > INT32_MAX / 16 || p->num_seqs == INT32_MAX)
+    if ((int64_t)p->num_seqs * p->max_pages_per_seq >= (int64_t)1 << 31 || p->max_pages_per_seq > INT32_MAX / 16 || p->num_seqs > ra::kMostPagedSeqs)
         return fail(RA_ERR_UNSUPPORTED, "batch too large");
     if (!p->free_count || !p->free_count_out) return fail(RA_ERR_INVALID_ARG, "a required pointer (free_count, free_count_out) is NULL");
     if (p->num_seqs == 0) return RA_OK;

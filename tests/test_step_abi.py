@@ -93,6 +93,27 @@ def test_check_release():
     refused(ra.rollout_attn_check_release, release, PAGES + [(dict(keep_lens=None), BAD, "pointer")])
 
 
+@pytest.mark.parametrize("max_pages", [0, 1])
+@pytest.mark.parametrize("check,make", [(ra.rollout_attn_check_place, place), (ra.rollout_attn_check_release, release)])
+def test_most_sequences(check, make, max_pages):
+    """Sequences are gone over 1024 at a time, and the 32-bit number of the first behind the last tile must not wrap: then a tile would
+    begin at a negative one."""
+    most = 2 ** 31 - 1 - 1024
+    for n, status in ((most, ra.RA_OK), (most + 1, NOT), (2 ** 31 - 2, NOT), (2 ** 31 - 1, NOT)):
+        p = make()
+        p.num_seqs, p.max_pages_per_seq = n, max_pages
+        st, msg = check(p)
+        assert st == status and (st == ra.RA_OK or "large" in msg), (n, st, msg)
+        if st == ra.RA_OK:
+            last = (n - 1) // 1024 * 1024                    # (the first of the last tile)
+            assert last + 1024 < 2 ** 31
+    p = make()
+    p.num_seqs, p.max_pages_per_seq = 1, (2 ** 31 - 1) // 16
+    assert check(p)[0] == ra.RA_OK
+    p.max_pages_per_seq += 1
+    assert check(p)[0] == NOT
+
+
 def test_check_verify():
     changes = [(dict(num_seqs=-1), BAD, "dimension"), (dict(total_rows=-1), BAD, "dimension"), (dict(vocab=0), BAD, "dimension"), (dict(vocab=2 ** 24 + 1), NOT, "vocab"),
                (dict(total_rows=2 ** 22 + 1), NOT, "large"), (dict(num_seqs=2 ** 22 + 1), NOT, "large"), (dict(logits_dtype=2), BAD, "dtype"), (dict(logits=None), BAD, "pointer"),
