@@ -124,7 +124,7 @@ typedef enum { RA_LOGITS_BF16 = 0, RA_LOGITS_FP32 = 1 } ra_logits_dtype;
  * Verification of drafted tokens, and the next token of every sequence.  Sequence b has the rows t = cu_rows[b] ..
  * cu_rows[b+1] - 1 of logits: row t is the target's at a token that the step took in, and tokens[t + 1] for t + 1 < cu_rows[b+1]
  * is the drafted token that row t judges (so tokens and cu_rows are what the step was called with: the last token of the
- * sequence and its drafts; tokens[cu_rows[b]] is not read).  The last row judges none.  With T = temperature[b],
+ * sequence and its drafts; tokens[cu_rows[b]] does not count).  The last row judges none.  With T = temperature[b],
  *   p_t = softmax(logits[t] / T),   q_t = softmax(draft_logits[draft_rows[b] + t - cu_rows[b]] / T)
  * where q_t is the distribution that tokens[t + 1] was drawn from; without draft_logits it is all on that token (a guess from
  * the text so far, a greedy draft).  In order, the draft x = tokens[t + 1] of row t is accepted if
@@ -168,7 +168,7 @@ typedef struct {
     int32_t total_draft_rows;
     const int32_t *draft_rows;     /* dev [num_seqs], or NULL without draft_logits: a sequence's first row of them */
     const float *temperature;      /* dev [num_seqs], or NULL: 1 */
-    const float *accept_uniform;   /* dev [total_rows]; a sequence's last is not read */
+    const float *accept_uniform;   /* dev [total_rows]; a sequence's last does not count, the array's last is not read */
     const float *draw_uniform;     /* dev [num_seqs] */
     int32_t *accepted;             /* dev [num_seqs] */
     int32_t *out_tokens;           /* dev [total_rows] */

@@ -440,7 +440,7 @@ struct Draw {
 };
 
 // What row `row` says to its draft, and how a token is drawn from it if that does not stay: by the row's sums, what its draft is (x, no
-// token: -1), the logits of that in the target's row and in the draft model's, and the draft model's row (-1: none).  All lanes of a wave.
+// token: -1), the logits of that in the target's row and in the draft model's, and the draft model's row (-1: none, or greedy).  All lanes of a wave.
 enum Verdict { kGoes, kStays, kUnsure };
 struct Asked {
     int row, x;
@@ -456,18 +456,19 @@ struct Early {
 __device__ __forceinline__ Early ask_early(const VerifyLaunch &a, int row, int lane)
 {
     const RowPart none = {0.0, -INFINITY, INT32_MAX};
-    Early e = {row, row + 1 < a.R ? a.tokens[row + 1] : -1, a.u[row], none, none};
+    Early e = {row, -1, 0.f, none, none};
+    if (row + 1 < a.R) e.x = a.tokens[row + 1], e.u = a.u[row]; // (the batch's last row judges none)
     if (lane < a.parts) e.mine = a.row[(int64_t)row * a.parts + lane];
     if (a.draft && lane < a.parts) e.yours = a.draft_row[(int64_t)row * a.parts + lane];
     return e;
 }
-__device__ __forceinline__ Asked ask_row(const VerifyLaunch &a, int b, const Early &e, int end)
+__device__ __forceinline__ Asked ask_row(const VerifyLaunch &a, int b, const Early &e, int end, const Temper &t)
 {
     Asked r = {e.row, e.row + 1 < end ? e.x : -1, -1, 0.f, 0.f, e.u};
     if (r.x < 0 || r.x >= a.V) r.x = -1;
     if (r.x < 0) return r;
     r.l = logit_at(a.logits, a.stride, a.fp32, r.row, r.x);
-    if (a.draft) r.q_row = draft_row_of(a, b, r.row);
+    if (a.draft && t.c != 0.0) r.q_row = draft_row_of(a, b, r.row);
     if (r.q_row >= 0) r.m = logit_at(a.draft, a.draft_stride, a.draft_fp32, r.q_row, r.x);
     return r;
 }
@@ -545,10 +546,10 @@ __device__ __forceinline__ double share_of(const RowPart &r, const Draw &d)
 __device__ __forceinline__ Draw judge_row(const VerifyLaunch &a, int b, const Early &e, int end, const Temper &t, double v, int lane, double unsure, Verdict &says, double &lp, Border &border)
 {
     const RowPart *const parts = a.row + (int64_t)e.row * a.parts, *const theirs = a.draft_row + (int64_t)e.row * a.parts;
-    const Asked asked = ask_row(a, b, e, end);
+    const Asked asked = ask_row(a, b, e, end, t);
     const Whole p = whole_row(parts, e.mine, a.parts, t, lane);
     Whole q = {1.0, -INFINITY, 0};
-    if (asked.q_row >= 0 && t.c != 0.0) q = whole_row(theirs, e.yours, a.parts, t, lane);
+    if (asked.q_row >= 0) q = whole_row(theirs, e.yours, a.parts, t, lane);
     const Draw d = judge(a, asked, t, p, q, unsure, says, lp);
     if (d.from == kRow) border = border_of([&](int k) { return share_of(k == lane ? e.mine : parts[k], d); }, a.parts, v, lane);
     return d;
@@ -592,7 +593,7 @@ template <bool EXACT> __device__ __forceinline__ Draw decide(const VerifyLaunch 
             const Whole q = d.from == kRest ? exact_row(a, d.q, a.draft_fp32, t) : Whole{1.0, -INFINITY, 0};
             Verdict sure;
             double unused;
-            (void)judge(a, ask_row(a, b, ask_early(a, d.row, lane), end), t, p, q, 0.0, sure, unused);
+            (void)judge(a, ask_row(a, b, ask_early(a, d.row, lane), end, t), t, p, q, 0.0, sure, unused);
             if (sure != kStays) break;
         }
         if (wave < n && lane == 0) {
