@@ -993,7 +993,8 @@ static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted
     a.part_len = kDrawThreads * kVec;
     a.parts = (a.V + a.part_len - 1) / a.part_len;
     a.alone = rows * a.parts >= (int64_t)num_cus * 6;
-    a.exact = rows * a.V <= few * (drafted && a.fp32 ? 5 : drafted || a.fp32 ? 3 : 1);
+    const int64_t times = drafted && a.fp32 ? 5 : drafted || a.fp32 ? 3 : 1;
+    a.exact = few > INT64_MAX / times || rows * a.V <= few * times;
     // The error of a sum of weights as weight32 gives them, in parts of the row's whole sum W: a weight w is off by (3 ln 2 |y| + 2) 2^-24
     // of it and a sum of eight by 3 2^-24; y is against the thread's value, which is at most 8 / c below one it met: |y| is at most 8
     // more than against the row's largest.  Against that, log2(W) + sum(w |y|) / W is the entropy of the row in bits, at most log2(V),

@@ -150,6 +150,23 @@ def test_verify_workspace_size():
     assert e.value.status == NOT
 
 
+@pytest.mark.parametrize("fp32,drafted", [(0, False), (0, True), (1, False), (1, True)])
+def test_any_number_of_logits_may_be_few(fp32, drafted):
+    """ROLLOUT_ATTN_VERIFY_FEW counts three or five times for some types; the largest numbers still mean that all sums are binary64.
+    (Which way a call goes shows in its workspace; the rule is called by the name the compiler gave it.)"""
+    carve = ra.load_library()._ZN2ra12carve_verifyERNS_12VerifyLaunchEilbPv
+    carve.restype, carve.argtypes = ctypes.c_size_t, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_bool, ctypes.c_void_p]
+
+    def size(few):
+        launch = (ctypes.c_int32 * 256)(40, 200, 50000, 0, 0, fp32)      # B, R, V, two that the rule sets, whether logits are binary32
+        return carve(launch, 256, few, drafted, None)
+
+    values = 200 * 50000 * (2 if drafted else 1)
+    assert size(0) > size(values)
+    for few in (2 ** 40, 2 ** 61, 2 ** 62, 2 ** 63 // 3 + 1, 2 ** 63 // 5 + 1, 2 ** 63 - 1):
+        assert size(few) == size(values), few
+
+
 def test_calls_without_a_context_are_rejected():
     for call, desc, more in ((ra.rollout_attn_place, place(), ()), (ra.rollout_attn_release, release(), ()), (ra.rollout_attn_verify, verify(), (None, 0))):
         with pytest.raises(ra.RolloutAttnError) as e:
