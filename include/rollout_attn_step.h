@@ -141,7 +141,8 @@ typedef enum { RA_LOGITS_BF16 = 0, RA_LOGITS_FP32 = 1 } ra_logits_dtype;
  *   accepted if it is that token.  T counts as the nearest of 1e-30 and 1e30 outside them.
  *   out_tokens[t]     for the sequence's rows: the accepted drafts, then the token drawn, then -1
  *   out_logprobs[t]   ln p_t(out_tokens[t]), 0 where out_tokens[t] is -1; rounded to binary32, and off by 2^-17 at most where sums
- *                     were of binary32 weights                                             (NULL: not written)
+ *                     were of binary32 weights.  Whether they were goes by the size of the batch: the same row's may differ by
+ *                     that much from one batch to another                                  (NULL: not written)
  *   next_tokens[b]    the token drawn                                                      (NULL: not written)
  * Logits of -inf have probability 0, whatever masks them; a row that has a NaN or +inf in it, or nothing but -inf, has no
  * distribution: p_t of such a row accepts no draft, and the token drawn from it is -1, with a log-probability of NaN; q_t of such a

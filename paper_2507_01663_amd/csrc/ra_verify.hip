@@ -857,11 +857,19 @@ __global__ __launch_bounds__(kDrawThreads) void verify_again_kernel(VerifyLaunch
     __shared__ DrawLds lds;
     every_item(a, [&](const OpenDraw &o, int at, int k) {
         Draw d = open_draw(a, o);
+        const double v = number_of(a, o.b);                     // (asked for before the sums are there)
         const RowPart p = part_of<true, kDrawThreads>(d.p, a.fp32, k * a.part_len, part_end(a, k), d.t);
         double *const sums = a.rest + (int64_t)o.row * a.parts;
         if (!last_to_publish(a, a.open[at], sums + k, share_of(p, d))) return;
-        auto share = [&](int k) { return published(sums + k); };
-        const Token token = close_draw(a, d, share, share, number_of(a, o.b), lds);
+        const int lane = threadIdx.x & 63;
+        const double mine = lane < a.parts ? published(sums + lane) : 0.0;
+        double all = mine;
+        for (int j = lane + 64; j < a.parts; j += 64) all += published(sums + j);
+        auto share = [&](int j) { return j == lane ? mine : published(sums + j); };
+        // the log-probability is of these sums, too, which come to 1 + more: 1 / (1 + more) to its third order, 10^-16
+        const double more = wave_sum(all) - 1.0, scale = d.p_scale * __builtin_fma(more, more - 1.0, 1.0);
+        const Token token = close_draw(a, d, share, share, v, lds);
+        d.p_scale = scale;
         finish(a, o.b, a.cu[o.b], a.cu[o.b + 1], d, token);
     });
 }

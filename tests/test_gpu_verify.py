@@ -343,3 +343,30 @@ def test_first_tokens_are_distributed_as_the_target_s(dec):
     counts = np.bincount(out.cpu().numpy()[::2], minlength=V)
     assert ((counts - n * p) ** 2 / (n * p)).sum() < 40
     assert abs(float(accepted.float().mean()) - np.minimum(p, q).sum()) < 5 * 0.5 / n ** 0.5
+
+
+@pytest.mark.parametrize("drafts", ["none", "guess"])
+@pytest.mark.parametrize("V", [4097, 300001])
+def test_open_draws_have_the_log_probability_of_binary64_sums(dec, V, drafts):
+    """Numbers so near a border (1e-6; binary32 sums leave open what is within 9e-6 or more) that the row's sums are made again in binary64,
+    at a temperature whose log2(e) / T is rounded by nearly half a step of binary32.  The log-probability is then rounded once, and off by
+    2^-37 beside that, as if all sums had been binary64 from the start."""
+    T = np.linspace(0.5, 2.0, 20001).astype(np.float32)
+    c = 1.0 / np.log(2.0) / T.astype(np.float64)
+    T = float(T[np.argmax(np.abs(c.astype(np.float32) / c - 1.0))])
+    r = np.random.default_rng(V)
+    small = np.log(0.4 / (V - 1)) * T
+    row = rounded(np.concatenate([[0.0], small + 0.2 * T * r.normal(0, 1, V - 1)]), "fp32")
+    p = distribution(row, float(np.float32(T)))
+    x = 7                                                    # the guess that is turned down
+    w = p.copy()
+    if drafts == "guess":
+        w[x] = 0.0
+    border = np.cumsum(w)[0] / w.sum()
+    at = [border - 1e-6, border - 3e-6, border + 1e-6]
+    n, rows = len(at), 1 if drafts == "none" else 2
+    v = Verifying([rows] * n, np.tile(row, (rows * n, 1)), [x] * (rows * n), [1.0] * (rows * n), at, [T] * n, dtype="fp32")
+    dec.verify(v.c)
+    v.exact = True
+    v.check()
+    assert v.next.tolist()[:2] == [0, 0] and v.next.tolist()[2] > 0
