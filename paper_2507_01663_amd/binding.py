@@ -679,7 +679,7 @@ class Decoder:
     may still use them.  A captured graph and a schedule that RA_FLAG_REUSE_SCHEDULE reuses are tied to the workspace
     they were made with: after the workspace has grown, capture or schedule again."""
 
-    _verify_ws_at = None             # the address and size of verify's workspace, as _chunk_ws_at is extend's
+    _verify_ws_at = None             # the address and size of verify's workspace, as _chunk_ws_at is extend's (all of them in _retired)
 
     def __init__(self, device_ordinal=0):
         self.device_ordinal = device_ordinal
@@ -687,7 +687,7 @@ class Decoder:
         self._ws = None
         self._ws_at = None           # its address and size, always those of one tensor
         self._chunk_ws_at = None     # extend's (a schedule that decode keeps in the other one outlives it)
-        self._retired = []           # tensors that enqueued work may use: every one of extend's, decode's former ones
+        self._retired = []           # tensors that enqueued work may use: every one of extend's and verify's, decode's former ones
         self._raw_stream = None
 
     def close(self):
@@ -805,8 +805,9 @@ class Decoder:
         _check(load_library().rollout_attn_release(self.ctx, release, self._hip_stream(stream)), self.ctx)
 
     def verify(self, verify, stream=None):
-        """Enqueues the verification of drafts and the choice of the next tokens.  Its workspace grows and is shared as extend's
-        is: put calls that overlap in time on one stream, or take a Decoder for each."""
+        """Enqueues the verification of drafts and the choice of the next tokens.  Its workspace is shared as extend's is (put calls
+        that overlap in time on one stream, or take a Decoder for each) and at least doubles when it grows, so that batches
+        that creep leave few outgrown ones behind."""
         s = self._hip_stream(stream)
         at = self._verify_ws_at      # (read once: another thread's call may put a larger one there)
         if at is not None:
@@ -815,11 +816,11 @@ class Decoder:
                 return
             if status != RA_ERR_WORKSPACE_TOO_SMALL:
                 _check(status, self.ctx)
-        need = max(256, rollout_attn_verify_workspace_size(self.ctx, verify))
-        ws = self._bytes(need, stream)
+        size = max(256, rollout_attn_verify_workspace_size(self.ctx, verify), 2 * at[1] if at is not None else 0)
+        ws = self._bytes(size, stream)
         self._retired.append(ws)
-        mine, at = (ws.data_ptr(), need), self._verify_ws_at
-        if at is None or at[1] < need:
+        mine, at = (ws.data_ptr(), size), self._verify_ws_at
+        if at is None or at[1] < size:
             self._verify_ws_at = mine
         rollout_attn_verify(self.ctx, verify, ctypes.c_void_p(mine[0]), mine[1], ctypes.c_void_p(s))
 
