@@ -36,6 +36,30 @@ def test_batches(dec, n, slack):
         run(dec, back)
 
 
+@pytest.mark.parametrize("n", [64, 1023, 1024, 1025, 2048, 2500])
+@pytest.mark.parametrize("slack", [1.0, 0.7])
+def test_steps_of_few_tokens(dec, n, slack):
+    """At most four new tokens a sequence and 1024 in a tile of 1024 sequences, which sequences place themselves: one for all, one for some, up to
+    four for some; and tiles of that kind before and behind one with a turn in it, or with more tokens than threads, or with a turn that
+    is not served.  With groups, too few pages, room for all, more or fewer tokens, in place or not."""
+    r = np.random.default_rng(n)
+    one, few = np.ones(n, dtype=np.int64), np.where(r.random(n) < 0.35, r.integers(1, 5, n), 0)
+    first, last, many, huge = few.copy(), few.copy(), few.copy(), few.copy()
+    first[min(5, n - 1)], last[n - 1], many[-(n // 5):] = 60, 61, 4
+    huge[[0, n // 2, n - 1]] = 100000                        # (more than a row has room for)
+    for seed, (group, prefix) in enumerate([(0, 0), (8, 2)]):
+        for name, asked in (("one", one), ("few", few), ("first", first), ("last", last), ("many", many), ("huge", huge)):
+            lens, _, held, table, stack, _, groups = batch(10 * n + seed, n, new=64, group=group, prefix=prefix, slack=1.0)
+            shared = [prefix if group and groups[0][b] >= 0 else 0 for b in range(n)]
+            need = sum(max(0, pages_of(int(a + k)) - max(int(h), s)) for a, k, h, s in zip(lens, asked, held, shared) if 0 < k < 100)
+            total = int(asked[asked < 100].sum())
+            for room in (total, min(4096, total + 700), total // 2):
+                for alias in (False, True):
+                    print("case", n, slack, group, name, room, alias, flush=True)
+                    assert room <= 4096
+                    run(dec, Placing(lens, asked, held, table, stack, int(need * slack), room, groups, alias), (name, group, room, alias))
+
+
 @pytest.mark.parametrize("tokens", [1, 15, 16, 17, 4095, 4096, 5000, 70000])
 def test_one_sequence(dec, tokens):
     for held_tokens in (0, 1, 15, 16, 31):
