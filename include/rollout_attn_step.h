@@ -185,7 +185,8 @@ ra_status rollout_attn_verify_workspace_size(const ra_ctx *ctx, const ra_verify 
 
 /* Enqueues the verification on hip_stream: two kernels, one more with draft_logits and one more in large batches.  The environment's
  * ROLLOUT_ATTN_VERIFY_FEW=n, read by rollout_attn_create, is the number of bf16 logits up to which all sums are binary64 from the
- * start; of binary32 logits, and of logits with a draft model's (both counted), three times as many, of both together five times.  workspace as for rollout_attn_decode: dev memory of at least
+ * start, of binary32 logits five times as many, and n / 680 more for every sequence; with a draft model's logits (both counted) n / 2 and
+ * 5 n / 4.  The default is 2^24.  workspace as for rollout_attn_decode: dev memory of at least
  * rollout_attn_verify_workspace_size() bytes, 256-byte aligned, contents irrelevant on entry and undefined afterwards; calls
  * that overlap in time need distinct workspaces. */
 ra_status rollout_attn_verify(ra_ctx *ctx, const ra_verify *verify, void *workspace, size_t workspace_bytes, void *hip_stream);

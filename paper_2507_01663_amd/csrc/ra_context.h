@@ -18,7 +18,7 @@ struct ra_ctx {
     int prefill_stay;          // -1: the prefill launch chooses by the batch; else ROLLOUT_ATTN_PREFILL_WGS_PER_DIE
     void *zeros;  // 256 bytes of zeros on the device
     int self_plan; // attention waves may plan their spans themselves (no schedule kernel)
-    int64_t verify_few; // logits of a verification up to which all sums are binary64 (ROLLOUT_ATTN_VERIFY_FEW)
+    int64_t verify_few; // bf16 logits of a verification up to which all sums are binary64 (ROLLOUT_ATTN_VERIFY_FEW)
     int direct;    // batches that direct_plan says so may go without a schedule
     int32_t *host_flags; // pinned, for RA_FLAG_VALIDATE
     int timing;          // record events around the phases

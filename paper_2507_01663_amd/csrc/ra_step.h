@@ -61,7 +61,7 @@ struct VerifyLaunch {
     int32_t exact;               // all sums in binary64 from the start
     double eps;                  // else: what a sum may be off by, in parts of the row's
 };
-// How a call is divided (from B, R, V), and its workspace: the bytes; places the pointers when base is not null.
+// How a call is divided (from B, R, V, fp32), and its workspace: the bytes; places the pointers when base is not null.
 size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, void *base);
 bool verify_fits(const VerifyLaunch &a, bool drafted); // in one launch each
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s);

@@ -989,11 +989,19 @@ __global__ __launch_bounds__(kDrawThreads) void verify_close_kernel(VerifyLaunch
 // Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
 // A row's parts go to a wave each where those are six for every compute unit, to a workgroup each where there are fewer.  (us of a
 // call, waves and workgroups: 1 216 parts 14.1, 13.1; 1 824 parts 14.5, 15.4; 3 840 24.3, 26.7.)
-// Whether all sums are binary64 from the start: binary32 sums are three times as fast, but leave draws open, which take another kernel (9
-// us), or three (35 us) with a draft model; and they wait for memory, twice as long where logits are binary32.  (us of a call, binary64
-// and binary32 first.  One row of 152 064 for a sequence: bf16, 9.7 million values 16.8 and 21.4, 14.6 20.6 and 16.4, 38.9 36.7 and
-// 31.5; binary32, 19.5 24.1 and 30.1, 38.9 40.5 and 41.7.  Five rows and a draft model's: bf16, 36.5 47.1 and 47.6, 48.7 58.0 and 53.2;
-// binary32, 73.0 75.5 and 77.3, 97.3 115 and 98.)
+// Whether all sums are binary64 from the start: binary32 sums are up to twice as fast, but leave draws open, which take another kernel or
+// two; and their draws' kernel needs 154 registers, so that a compute unit holds one workgroup of it, not two, which tells where there is
+// one for few logits (8 750 rows of 8 000: 185 us against 100).  With a draft model draws from p - q are open either way, and cost less after
+// binary32 sums.  Binary32 logits are twice the bytes: there is less to gain.
+// So: few logits for bf16, five times as many for binary32, and as many again for every kSeqsOfFew sequences; with a draft model's logits,
+// both counted, half as many and five quarters.  (us of a call, binary64 and binary32 first, and draws then open.  A row a sequence, bf16: 92 of
+// 152 064 values 21.1, 22.0, 0 to 3; 145 26.5, 26.7, 1 to 5; 329 50.4, 42.5, 3 to 6; 280 of 100 000 31.1, 32.9, 3 to 7; 360 38.2, 37.4, 4 to 10;
+// 557 of 50 257 38.0, 41.2, 6 or 7; 995 57.8, 55.7, 10 to 12; 1 125 of 32 000 47.0, 52.9, 3 to 6; 3 125 118.6, 114.6, 13 to 28; 8 750 of 8 000 162, 222, 11
+// to 14.  Five rows: 18 sequences of 152 064 23.9, 21.6, 0 or 1; 24 27.3, 27.7, 0 to 2; 37 33.2, 31.1, 0 to 3.  Binary32, a row: 395 of 152 064 61.3, 66.9, 7
+// to 12; 592 90.6, 92.4, 10 to 16; 723 108.8, 106.3, 13 to 16; five of 50 257, 298 sequences 82.5, 86.3, 3 to 5; 438 112.3, 110.2, 4 to 7.  Five
+// rows and a draft model's, bf16: 4 of 152 064 24.8, 25.3, 1 or 2; 6 24.5, 22.2, 0 to 3; 29 53.8, 41.6, 7 to 9; 55 83.7, 54.6, 12 to 15; 28 of 32 000
+// 28.7, 27.0, 4 to 12; binary32: 12 of 152 064 33.2, 35.6, 0 to 6; 15 41.2, 40.8, 3 to 6; 55 90.0, 78.9, 11 to 16.)
+constexpr double kSeqsOfFew = 680.0;
 static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted)
 {
     const int64_t rows = (int64_t)a.R * (drafted ? 2 : 1);
@@ -1001,8 +1009,8 @@ static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted
     a.part_len = kDrawThreads * kVec;
     a.parts = (a.V + a.part_len - 1) / a.part_len;
     a.alone = rows * a.parts >= (int64_t)num_cus * 6;
-    const int64_t times = drafted && a.fp32 ? 5 : drafted || a.fp32 ? 3 : 1;
-    a.exact = few > INT64_MAX / times || rows * a.V <= few * times;
+    const double times = drafted ? a.fp32 ? 1.25 : 0.5 : (a.fp32 ? 5.0 : 1.0) + a.B / kSeqsOfFew;
+    a.exact = (double)(rows * a.V) <= (double)few * times;
     // The error of a sum of weights as weight32 gives them, in parts of the row's whole sum W: a weight w is off by (3 ln 2 |y| + 2) 2^-24
     // of it and a sum of eight by 3 2^-24; y is against the thread's value, which is at most 8 / c below one it met: |y| is at most 8
     // more than against the row's largest.  Against that, log2(W) + sum(w |y|) / W is the entropy of the row in bits, at most log2(V),

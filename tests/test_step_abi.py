@@ -150,21 +150,37 @@ def test_verify_workspace_size():
     assert e.value.status == NOT
 
 
-@pytest.mark.parametrize("fp32,drafted", [(0, False), (0, True), (1, False), (1, True)])
-def test_any_number_of_logits_may_be_few(fp32, drafted):
-    """ROLLOUT_ATTN_VERIFY_FEW counts three or five times for some types; the largest numbers still mean that all sums are binary64.
-    (Which way a call goes shows in its workspace; the rule is called by the name the compiler gave it.)"""
+def workspace_of(seqs, rows, vocab, fp32, drafted, few):
+    """Bytes of a verification's workspace, which show which way it goes.  (The rule is called by the name the compiler gave it.)"""
     carve = ra.load_library()._ZN2ra12carve_verifyERNS_12VerifyLaunchEilbPv
     carve.restype, carve.argtypes = ctypes.c_size_t, [ctypes.c_void_p, ctypes.c_int, ctypes.c_int64, ctypes.c_bool, ctypes.c_void_p]
+    launch = (ctypes.c_int32 * 256)(seqs, rows, vocab, 0, 0, fp32)       # B, R, V, two that the rule sets, whether logits are binary32
+    return carve(launch, 256, few, drafted, None)
 
-    def size(few):
-        launch = (ctypes.c_int32 * 256)(40, 200, 50000, 0, 0, fp32)      # B, R, V, two that the rule sets, whether logits are binary32
-        return carve(launch, 256, few, drafted, None)
 
-    values = 200 * 50000 * (2 if drafted else 1)
-    assert size(0) > size(values)
+@pytest.mark.parametrize("fp32,drafted", [(0, False), (0, True), (1, False), (1, True)])
+def test_any_number_of_logits_may_be_few(fp32, drafted):
+    """ROLLOUT_ATTN_VERIFY_FEW counts several times for some types; the largest numbers still mean that all sums are binary64."""
+    size = lambda few: workspace_of(40, 200, 50000, fp32, drafted, few)
+    every = size(10 * 200 * 50000)
+    assert size(0) > every
     for few in (2 ** 40, 2 ** 61, 2 ** 62, 2 ** 63 // 3 + 1, 2 ** 63 // 5 + 1, 2 ** 63 - 1):
-        assert size(few) == size(values), few
+        assert size(few) == every, few
+
+
+@pytest.mark.parametrize("seqs,rows,vocab,fp32,drafted,us64,us32", [
+    (92, 92, 152064, 0, False, 21.1, 22.0), (329, 329, 152064, 0, False, 50.4, 42.5), (395, 395, 152064, 1, False, 61.3, 66.9), (1125, 1125, 32000, 0, False, 47.0, 52.9),
+    (8750, 8750, 8000, 0, False, 162.1, 221.5), (3750, 3750, 32000, 1, False, 149.5, 173.0), (66, 330, 152064, 0, False, 52.8, 42.3), (438, 2190, 32000, 1, False, 77.5, 81.7),
+    (3, 15, 152064, 0, True, 17.9, 19.2), (29, 145, 152064, 0, True, 53.8, 41.6), (139, 695, 32000, 0, True, 54.8, 42.6), (12, 60, 152064, 1, True, 33.2, 35.6),
+    (55, 275, 152064, 1, True, 90.0, 78.9), (260, 1300, 32000, 1, True, 93.0, 84.2)])
+def test_sums_are_binary64_where_that_is_faster(seqs, rows, vocab, fp32, drafted, us64, us32):
+    """Batches at which one way is faster by a twentieth or so, and what both measured (us a call)."""
+    p = verify(drafted)
+    p.num_seqs, p.total_rows, p.vocab, p.logits_dtype = seqs, rows, vocab, fp32
+    of = lambda few: workspace_of(seqs, rows, vocab, fp32, drafted, few)
+    binary64, binary32 = of(2 ** 40), of(0)
+    assert binary64 != binary32
+    assert ra.rollout_attn_verify_workspace_size(None, p) == (binary64 if us64 < us32 else binary32)
 
 
 def test_calls_without_a_context_are_rejected():
