@@ -153,8 +153,8 @@ typedef enum { RA_LOGITS_BF16 = 0, RA_LOGITS_FP32 = 1 } ra_logits_dtype;
  * Layout: element (t, i) of logits at t * logits_stride + i, V = vocab values in a row, aligned to an element; draft_logits alike.
  * 16-byte aligned rows are read fastest.  Inputs and outputs overlap nothing.
  * A probability below 2^-990 counts as 0.
- * Supported: vocab <= 2^24; num_seqs and total_rows <= 2^22; a batch whose parts of 4096 values (num_seqs, or twice total_rows,
- * times those of a row) are fewer than 2^26.
+ * Supported: vocab <= 2^24; num_seqs and total_rows <= 2^22; with a row's parts of 4096 values, total_rows (twice that with
+ * draft_logits) times those fewer than 2^26, and num_seqs times those fewer than 2^32.
  */
 typedef struct {
     int32_t num_seqs, total_rows, vocab;

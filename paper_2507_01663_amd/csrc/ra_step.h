@@ -63,7 +63,7 @@ struct VerifyLaunch {
 };
 // How a call is divided (from B, R, V, fp32), and its workspace: the bytes; places the pointers when base is not null.
 size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, void *base);
-bool verify_fits(const VerifyLaunch &a, bool drafted); // in one launch each
+bool verify_fits(int32_t B, int32_t R, int32_t V, bool drafted); // in one launch each
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s);
 
 } // namespace ra

@@ -64,7 +64,7 @@ ra_status check_shape(const ra_verify *p, const Fail &fail)
     if (p->num_seqs < 0 || p->total_rows < 0 || p->vocab <= 0)
         return fail(RA_ERR_INVALID_ARG, "negative or zero dimension (num_seqs=%d total_rows=%d vocab=%d)", p->num_seqs, p->total_rows, p->vocab);
     if (p->vocab > 1 << 24) return fail(RA_ERR_UNSUPPORTED, "vocab=%d (at most 2^24 is supported)", p->vocab);
-    if (p->num_seqs > 1 << 22 || p->total_rows > 1 << 22)
+    if (p->num_seqs > 1 << 22 || p->total_rows > 1 << 22 || !ra::verify_fits(p->num_seqs, p->total_rows, p->vocab, p->draft_logits != nullptr))
         return fail(RA_ERR_UNSUPPORTED, "batch too large");
     return RA_OK;
 }
@@ -152,7 +152,6 @@ ra_status rollout_attn_verify_workspace_size(const ra_ctx *c, const ra_verify *p
     ra::VerifyLaunch a;
     fill_shape(a, p);
     *bytes = ra::carve_verify(a, c ? c->num_cus : 256, c ? c->verify_few : ra::kVerifyFew, p->draft_logits != nullptr, nullptr);
-    if (!ra::verify_fits(a, p->draft_logits != nullptr)) { set_err(err, "batch too large"); return RA_ERR_UNSUPPORTED; }
     return RA_OK;
 }
 
@@ -164,7 +163,6 @@ ra_status rollout_attn_verify(ra_ctx *c, const ra_verify *p, void *workspace, si
     ra::VerifyLaunch a;
     fill_shape(a, p);
     const size_t need = ra::carve_verify(a, c->num_cus, c->verify_few, p->draft_logits != nullptr, workspace);
-    if (!ra::verify_fits(a, p->draft_logits != nullptr)) { set_err(c, "batch too large"); return RA_ERR_UNSUPPORTED; }
     if (need && (!workspace || ((uintptr_t)workspace & 255))) { set_err(c, "workspace is NULL or not 256-byte aligned"); return RA_ERR_INVALID_ARG; }
     if (workspace_bytes < need) {
         set_err(c, "workspace of %zu bytes given, %zu needed", workspace_bytes, need);

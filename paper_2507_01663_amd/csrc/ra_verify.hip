@@ -987,6 +987,9 @@ __global__ __launch_bounds__(kDrawThreads) void verify_close_kernel(VerifyLaunch
 }
 
 // Rows are cut into parts of 4096 values: a draw then looks at eight for each thread.
+constexpr int kPart = kDrawThreads * kVec;
+static int parts_of(int V) { return (V + kPart - 1) / kPart; }
+
 // A row's parts go to a wave each where those are six for every compute unit, to a workgroup each where there are fewer.  (us of a
 // call, waves and workgroups: 1 216 parts 14.1, 13.1; 1 824 parts 14.5, 15.4; 3 840 24.3, 26.7.)
 // Whether all sums are binary64 from the start: binary32 sums are up to twice as fast, but leave draws open, which take another kernel or
@@ -1006,8 +1009,8 @@ static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted
 {
     const int64_t rows = (int64_t)a.R * (drafted ? 2 : 1);
     a.num_cus = num_cus;
-    a.part_len = kDrawThreads * kVec;
-    a.parts = (a.V + a.part_len - 1) / a.part_len;
+    a.part_len = kPart;
+    a.parts = parts_of(a.V);
     a.alone = rows * a.parts >= (int64_t)num_cus * 6;
     const double times = drafted ? a.fp32 ? 1.25 : 0.5 : (a.fp32 ? 5.0 : 1.0) + a.B / kSeqsOfFew;
     a.exact = (double)(rows * a.V) <= (double)few * times;
@@ -1042,9 +1045,10 @@ size_t carve_verify(VerifyLaunch &a, int num_cus, int64_t few, bool drafted, voi
 }
 
 // (a launch has less than 2^32 threads)
-bool verify_fits(const VerifyLaunch &a, bool drafted)
+bool verify_fits(int32_t B, int32_t R, int32_t V, bool drafted)
 {
-    return (int64_t)a.R * a.parts * (drafted ? 2 : 1) * 64 < (int64_t)1 << 32 && (int64_t)a.B * a.parts < (int64_t)1 << 32;
+    const int64_t parts = parts_of(V);
+    return R * parts * (drafted ? 2 : 1) * 64 < (int64_t)1 << 32 && B * parts < (int64_t)1 << 32;
 }
 
 hipError_t launch_verify(const VerifyLaunch &a, hipStream_t s)

@@ -150,6 +150,29 @@ def test_verify_workspace_size():
     assert e.value.status == NOT
 
 
+@pytest.mark.parametrize("size,drafted,status", [
+    (dict(total_rows=2 ** 22, vocab=2 ** 16 - 4096), False, ra.RA_OK), (dict(total_rows=2 ** 22, vocab=2 ** 16 - 4095), False, NOT),
+    (dict(total_rows=2 ** 21, vocab=2 ** 16 - 4096), True, ra.RA_OK), (dict(total_rows=2 ** 21, vocab=2 ** 16 - 4095), True, NOT),
+    (dict(total_rows=2 ** 14 - 1, vocab=2 ** 24), False, ra.RA_OK), (dict(total_rows=2 ** 14, vocab=2 ** 24), False, NOT),
+    (dict(num_seqs=2 ** 22, vocab=2 ** 22 - 4096), False, ra.RA_OK), (dict(num_seqs=2 ** 22, vocab=2 ** 22 - 4095), False, NOT),
+    (dict(num_seqs=2 ** 20 - 1, vocab=2 ** 24), True, ra.RA_OK), (dict(num_seqs=2 ** 20, vocab=2 ** 24), True, NOT)])
+def test_parts_of_a_batch(size, drafted, status):
+    """Rows times their parts of 4096 values are fewer than 2^26 (a launch's threads), sequences times those fewer than 2^32; the check says
+    what the call would, and the workspace's size is that of a batch that is supported."""
+    p = verify(drafted)
+    for k, x in size.items():
+        setattr(p, k, x)
+    p.logits_stride = p.draft_stride = p.vocab
+    st, msg = ra.rollout_attn_check_verify(p)
+    assert st == status and (st == ra.RA_OK or "large" in msg), (st, msg)
+    if status == ra.RA_OK:
+        assert ra.rollout_attn_verify_workspace_size(None, p) > 0
+    else:
+        with pytest.raises(ra.RolloutAttnError) as e:
+            ra.rollout_attn_verify_workspace_size(None, p)
+        assert e.value.status == NOT
+
+
 def workspace_of(seqs, rows, vocab, fp32, drafted, few):
     """Bytes of a verification's workspace, which show which way it goes.  (The rule is called by the name the compiler gave it.)"""
     carve = ra.load_library()._ZN2ra12carve_verifyERNS_12VerifyLaunchEilbPv
