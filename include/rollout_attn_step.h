@@ -133,10 +133,10 @@ typedef enum { RA_LOGITS_BF16 = 0, RA_LOGITS_FP32 = 1 } ra_logits_dtype;
  * weights w of the row t that comes next, cu_rows[b] + accepted[b]:
  *   w = p_t                    if t is the last row,
  *   w = max(p_t - q_t, 0)      if its draft was turned down (without draft_logits: p_t without x); p_t if that is all zeros,
- * the token being the first one i with w_0 + .. + w_i > v * (w_0 + .. + w_{V-1}).  (With numbers that are independent and even on [0, 1) every
- * token is then distributed as if sampled from p alone.)  All of this is as in binary64, so that the sums of many small weights move
- * no border: with weights that are right to 2^-38; or, in large batches, with sums of binary32 weights where what they may be off by
- * settles the comparison, and in binary64 for the tests and draws that they leave open.
+ * the token being the first one i with w_0 + .. + w_i > v * (w_0 + .. + w_{V-1}).  (With numbers that are independent and even on
+ * [0, 1) every token is then distributed as if sampled from p alone.)  All of this is as in binary64, so that the sums of many small
+ * weights move no border: with weights that are right to 2^-38; or, in large batches, with sums of binary32 weights where what they
+ * may be off by settles the comparison, and in binary64 for the tests and draws that they leave open.
  *   T == 0 (or less, or NaN): greedy.  p_t is all on the largest logit, the first of equals; draft_logits are not read: a draft is
  *   accepted if it is that token.  T counts as the nearest of 1e-30 and 1e30 outside them.
  *   out_tokens[t]     for the sequence's rows: the accepted drafts, then the token drawn, then -1
@@ -148,8 +148,11 @@ typedef enum { RA_LOGITS_BF16 = 0, RA_LOGITS_FP32 = 1 } ra_logits_dtype;
  * distribution: p_t of such a row accepts no draft, and the token drawn from it is -1, with a log-probability of NaN; q_t of such a
  * row, a draft row outside [0, total_draft_rows) or a draft that is no token (not in [0, vocab)) has the draft turned down and
  * the token drawn from p_t.  v outside [0, 1] counts as the nearest of the two, NaN as 0.
- * A sequence without rows: accepted[b] = 0, next_tokens[b] = -1.  Rows behind cu_rows[num_seqs] are left as they were in the
- * outputs.  cu_rows starts at 0 or more and does not decrease; a sequence whose rows are not in [0, total_rows] counts as having none.
+ * A sequence without rows (one that asked for no tokens, or that rollout_attn_place did not serve): accepted[b] = 0,
+ * next_tokens[b] = -1.  Rows behind cu_rows[num_seqs] are left as they were in the outputs.  cu_rows starts at 0 or more and does not
+ * decrease; a sequence whose rows are not in [0, total_rows] counts as having none.
+ * Of what the step put into the cache, accepted[b] + 1 tokens stay, the one that it began with and the accepted drafts; but none of a
+ * sequence without rows: whoever keeps lengths adds that where cu_rows[b+1] > cu_rows[b] alone.
  * Layout: element (t, i) of logits at t * logits_stride + i, V = vocab values in a row, aligned to an element; draft_logits alike.
  * 16-byte aligned rows are read fastest.  Inputs and outputs overlap nothing.
  * A probability below 2^-990 counts as 0.
@@ -162,7 +165,7 @@ typedef struct {
     const void *logits;            /* dev */
     int64_t logits_stride;         /* in elements, at least vocab */
     const int32_t *cu_rows;        /* dev [num_seqs + 1] */
-    const int32_t *tokens;         /* dev [total_rows] */
+    const int32_t *tokens;         /* dev [total_rows]; needed, as accept_uniform is, also where no sequence has a draft */
     const void *draft_logits;      /* dev or NULL */
     int64_t draft_stride;
     int32_t draft_dtype;           /* ra_logits_dtype */

@@ -11,8 +11,8 @@
 // and one part again (verify_draw_kernel); and the draws that it leaves open, from p - q and those in doubt (verify_again_kernel,
 // verify_rest_kernel, or verify_left_kernel and verify_close_kernel).
 //
-// Memory bounds the sums of large batches: 200 x 4 to 6 rows of 152 064 binary32 logits with a draft model's 180 us, 6.05 TB/s; 128 x 5 of
-// bf16 62 to 67, 5.2 to 5.6 TB/s; binary64 sums take 22 us for 24 million values, their instructions.  The draws are chains of
+// Memory bounds the sums of large batches: 200 x 4 to 6 rows of 152 064 binary32 logits with a draft model's 179 us, 6.1 TB/s; 128 x 5 of
+// bf16 62 to 67, 5.2 to 5.6 TB/s; binary64 sums take 22 to 24 us for 24 million values, their instructions.  The draws are chains of
 // trips to memory, 6 to 10 us a kernel, and so is a small call: 4 rows of 32 000 in 9.4 us.
 #include "ra_device.h"
 #include "ra_step.h"
@@ -205,8 +205,9 @@ template <bool EXACT> struct Met {
     }
 };
 
-// Values [begin, end) of a row, by THREADS threads of which this is number tid: four loads of eight values are on their way at a time, then
-// one, then what is left of a load, a value to a thread.
+// Values [begin, end) of a row, by THREADS threads of which this is number tid: two loads of eight values are on their way at a time (the rows'
+// sums of 128 x 5 bf16 rows of 152 064 values and a draft model's 62 us; with four 69, with one 2 to 4 % more), then one, then what is left
+// of a load, a value to a thread.
 template <bool EXACT, int THREADS, bool FP32> __device__ __forceinline__ Met<EXACT> meet_all(const Row<FP32> row, int begin, int end, const Temper &t, int tid)
 {
     constexpr int kAhead = 2, kStep = THREADS * kVec;
@@ -997,13 +998,17 @@ static int parts_of(int V) { return (V + kPart - 1) / kPart; }
 // one for few logits (8 750 rows of 8 000: 185 us against 100).  With a draft model draws from p - q are open either way, and cost less after
 // binary32 sums.  Binary32 logits are twice the bytes: there is less to gain.
 // So: few logits for bf16, five times as many for binary32, and as many again for every kSeqsOfFew sequences; with a draft model's logits,
-// both counted, half as many and five quarters.  (us of a call, binary64 and binary32 first, and draws then open.  A row a sequence, bf16: 92 of
-// 152 064 values 21.1, 22.0, 0 to 3; 145 26.5, 26.7, 1 to 5; 329 50.4, 42.5, 3 to 6; 280 of 100 000 31.1, 32.9, 3 to 7; 360 38.2, 37.4, 4 to 10;
-// 557 of 50 257 38.0, 41.2, 6 or 7; 995 57.8, 55.7, 10 to 12; 1 125 of 32 000 47.0, 52.9, 3 to 6; 3 125 118.6, 114.6, 13 to 28; 8 750 of 8 000 162, 222, 11
-// to 14.  Five rows: 18 sequences of 152 064 23.9, 21.6, 0 or 1; 24 27.3, 27.7, 0 to 2; 37 33.2, 31.1, 0 to 3.  Binary32, a row: 395 of 152 064 61.3, 66.9, 7
-// to 12; 592 90.6, 92.4, 10 to 16; 723 108.8, 106.3, 13 to 16; five of 50 257, 298 sequences 82.5, 86.3, 3 to 5; 438 112.3, 110.2, 4 to 7.  Five
-// rows and a draft model's, bf16: 4 of 152 064 24.8, 25.3, 1 or 2; 6 24.5, 22.2, 0 to 3; 29 53.8, 41.6, 7 to 9; 55 83.7, 54.6, 12 to 15; 28 of 32 000
-// 28.7, 27.0, 4 to 12; binary32: 12 of 152 064 33.2, 35.6, 0 to 6; 15 41.2, 40.8, 3 to 6; 55 90.0, 78.9, 11 to 16.)
+// both counted, half as many and five quarters.  Measured, us of a call with binary64 and with binary32 sums first, and the draws then open:
+//   one row a sequence, bf16    92 x 152064   21.1   22.0  0-3     145 x 152064   26.5   26.7  1-5     329 x 152064   50.4   42.5   3-6
+//                              280 x 100000   31.1   32.9  3-7     360 x 100000   38.2   37.4  4-10    557 x 50257    38.0   41.2   6-7
+//                              995 x 50257    57.8   55.7  10-12  1125 x 32000    47.0   52.9  3-6    3125 x 32000   118.6  114.6  13-28
+//                             8750 x 8000    162.1  221.5  11-14
+//   ... binary32               395 x 152064   61.3   66.9  7-12    592 x 152064   90.6   92.4  10-16   723 x 152064  108.8  106.3  13-16
+//   five rows, bf16             18 x 152064   23.9   21.6  0-1      24 x 152064   27.3   27.7  0-2      37 x 152064   33.2   31.1   0-3
+//   ... binary32               298 x 50257    82.5   86.3  3-5     438 x 50257   112.3  110.2  4-7
+//   five rows, draft, bf16       4 x 152064   24.8   25.3  1-2       6 x 152064   24.5   22.2  0-3      29 x 152064   53.8   41.6   7-9
+//                               55 x 152064   83.7   54.6  12-15    28 x 32000    28.7   27.0  4-12
+//   ... binary32                12 x 152064   33.2   35.6  0-6      15 x 152064   41.2   40.8  3-6      55 x 152064   90.0   78.9  11-16
 constexpr double kSeqsOfFew = 680.0;
 static void verify_shape(VerifyLaunch &a, int num_cus, int64_t few, bool drafted)
 {
